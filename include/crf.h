@@ -277,6 +277,149 @@ CRF_API crf_status crf_kl(crf_ctx* ctx, const crf_model* model, const void* ref,
 CRF_API crf_status crf_kl_logits_noalloc(int device, const float* z_ref, const float* z_cur,
                                          int n_rows, int vocab, float* out_kl, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Extending a recovered cache with new tokens (a conversation's next turn, a
+ * run of drafted tokens, one generated token for each row of a batch): calls
+ * of one layer, and calls on the pages of the pool. They have no counterpart
+ * in the paper, whose recovered cache is consumed by an ordinary decoder. They
+ * keep the conventions above, with these differences:
+ *   - crf_rotary, crf_cache_append and crf_chunk_attention check every page id
+ *     where they use it: a write through an id outside [0, num_pages) is left
+ *     out, a read goes to page 0, and crf_check then returns CRF_EINVAL.
+ *   - crf_pages_* check their tables and counts in the call's first kernel; a
+ *     call that it rejects writes nothing outside its workspace.
+ *   - The current device is the same after the call as before it.
+ * They may be captured into a CUDA graph; lengths and positions, which the
+ * host passes, are then fixed, while the contents of tables, positions and
+ * counts are read at every replay. Calls whose kernels overlap on the GPU
+ * need workspaces of their own. */
+
+#define CRF_MAX_CHUNKS 128  /* requests of one append or attention call */
+#define CRF_MAX_TABLES 512  /* page tables of one crf_pages_* call */
+
+enum { CRF_BF16 = 0, CRF_FP16 = 1, CRF_FP32 = 2 };                  /* element types of crf_rotary */
+enum { CRF_ROPE_HALF = 0, CRF_ROPE_INTERLEAVED = 1 };               /* pairs (i, i + rot/2) or (2i, 2i + 1) */
+enum { CRF_ROPE_PLAIN = 0, CRF_ROPE_LINEAR = 1, CRF_ROPE_BASE = 2, CRF_ROPE_BANDS = 3 };
+
+/* Rotary positions. Pair i of the first rot_dim elements of a head (the rest
+ * pass through) turns by p f_i at position p:
+ *   (x, y) -> magnitude (x cos - y sin, y cos + x sin),  f_i = theta^(-2 i / rot_dim),
+ * and for contexts `factor` (>= 1) times as long as the trained ones
+ *   CRF_ROPE_LINEAR  f_i / factor (interpolated positions)
+ *   CRF_ROPE_BASE    theta factor^(rot_dim / (rot_dim - 2)) in theta's place (rot_dim > 2)
+ *   CRF_ROPE_BANDS   f_i (g + (1 - g) / factor), g = clamp((r - low) / (high - low), 0, 1) of the
+ *                    r = original f_i / (2 pi) turns that the pair makes over the `original` trained
+ *                    positions (0 <= low < high): fast pairs stay, slow ones are interpolated.
+ * head_dim 2..256; rot_dim even, 2..head_dim. `factor` is not read with
+ * CRF_ROPE_PLAIN; low, high and original are read with CRF_ROPE_BANDS alone. */
+typedef struct crf_rope {
+  int head_dim, rot_dim, layout, scaling;
+  double theta, factor, low, high, original, magnitude;
+} crf_rope;
+
+/* Heads of a batch of rows: element e of head h of row r of `x` is at
+ * x[r x_row + h x_head + e] (strides in elements, >= 0), `out` likewise. `out`
+ * may be `x` itself with the same strides; otherwise the two do not overlap. */
+typedef struct crf_heads {
+  const void* x;
+  void* out;
+  int heads;
+  int64_t x_row, x_head, out_row, out_head;
+} crf_heads;
+
+/* Rotates n_parts (1 or 2: queries, keys) sets of heads of n_rows rows (0: the
+ * call does nothing) at positions[r] (device int32, of any sign; angles are formed in 64-bit fixed
+ * point). `inverse` != 0 applies the transposed map (the rotation back,
+ * times magnitude): the gradient of the call without it. Arithmetic is fp32,
+ * rounded once to `type`. Elements are aligned to their size; rows of
+ * 16-byte aligned heads take the vector form. */
+CRF_API crf_status crf_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts, int n_parts,
+                              int type, int n_rows, const int32_t* positions, int inverse, void* stream);
+
+/* New rows of one request: n_new (>= 0) rows at positions pos .. pos + n_new - 1.
+ * The rows of a call's requests are packed in order. page_table: device int32,
+ * ceil((pos + n_new) / 16) entries to append, ceil(n_keys / 16) to attend.
+ * n_keys: cached positions that attention may see, the new rows' own (appended
+ * before) among them; usually pos + n_new. */
+typedef struct crf_chunk {
+  int n_new, pos, n_keys;
+  const int32_t* page_table;
+} crf_chunk;
+
+/* Writes the rows' keys and values (bf16) into the pages of `layer`, k rotated
+ * at the row's position first when `rope` is given; with `q` (which needs
+ * `rope`) the query heads are rotated into q->out in the same launch. The
+ * `out` members of k and v are not read; k->heads == v->heads == n_kv_heads.
+ * rope->head_dim == head_dim. head_dim 64 or 128. No two rows may share a
+ * slot. Every other slot of the pool is left as it was. */
+CRF_API crf_status crf_cache_append(crf_ctx* ctx, const crf_rope* rope, const crf_kv_pool* pool, int layer,
+                                    int n_kv_heads, int head_dim, const crf_chunk* chunks, int n_chunks,
+                                    const crf_heads* q, const crf_heads* k, const crf_heads* v, void* stream);
+
+/* Attention of the rows over their requests' cached keys of `layer`. Row r of a
+ * request (position p = pos + r) sees the keys
+ *   j < n_keys, and j <= p unless causal == 0, and j > p - window if window > 0,
+ * and o = softmax(scale q k) v over them, query head h reading kv head
+ * h / (heads / n_kv_heads). A row that sees no key gives o = 0 and lse = -inf.
+ *   q: x bf16 [rows] x heads, out the same shape (not overlapping x); heads a
+ *      multiple of n_kv_heads; head_dim 64 or 128; strides multiples of 8, 16-byte aligned.
+ *   lse: NULL, or device fp32 [rows][heads]: log of the sum of exp(scale q k).
+ *   scale: > 0, or 0 for 1 / sqrt(head_dim).
+ * Slots that a row does not see may hold anything, infinities and NaN
+ * included. Softmax weights enter the product with v in bf16; sums, maxima
+ * and o are fp32. `workspace` >= crf_chunk_attention_workspace_size bytes for
+ * these chunks, 256-byte aligned. Pages may be shared by requests. */
+CRF_API crf_status crf_chunk_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim,
+                                                      const crf_chunk* chunks, int n_chunks, int causal,
+                                                      int window, size_t* bytes);
+CRF_API crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer, int n_kv_heads,
+                                       int head_dim, const crf_chunk* chunks, int n_chunks,
+                                       const crf_heads* q, float* lse, float scale, int causal, int window,
+                                       void* workspace, size_t ws_bytes, void* stream);
+
+/* Pages are shared through a reference count a page (device int32 [num_pages];
+ * 0: free). One table of a request of n_tokens (>= 0) tokens: `table` device int32
+ * [ceil(n_tokens / 16)], `out` of the same length (see the calls). The counts go from refs_in to
+ * refs_out, which may be the same array; otherwise the two do not overlap. */
+typedef struct crf_pages {
+  int n_tokens;
+  const int32_t* table;
+  int32_t* out;
+} crf_pages;
+
+/* A second continuation of every request: `out` receives the child's table. Whole pages are
+ * shared (their count rises by one); a last page that is part filled, or with deep != 0 every
+ * page, gets a page of its own, count 1, into which the live slots of all n_layers layers are copied
+ * (the slots behind them are left as they were). New pages are the lowest free ones, dealt
+ * in order of tables and entries. A table id outside the pool or of count 0, or a
+ * negative count, rejects the call (CRF_EINVAL from crf_check), and so do too few free pages
+ * (CRF_ENOMEM from crf_check). `out` overlaps no table of the call. */
+CRF_API crf_status crf_pages_fork(crf_ctx* ctx, const crf_kv_pool* pool, int n_layers, int n_kv_heads,
+                                  int head_dim, const int32_t* refs_in, int32_t* refs_out,
+                                  const crf_pages* tables, int n_tables, int deep, void* workspace,
+                                  size_t ws_bytes, void* stream);
+
+/* Moves the live pages (count > 0) to the front of the pool: with L of them, the k-th lowest page at or
+ * above L moves into the k-th lowest free one below L, in all layers; `out` receives each
+ * table with the new ids (it may be `table` itself) and refs_out the moved counts, 0 from L on. The moved
+ * pages' old places keep their contents. Every reference must be in a table of the call: a
+ * page whose count is not the number of its entries rejects the call, as do ids outside the pool. */
+CRF_API crf_status crf_pages_compact(crf_ctx* ctx, const crf_kv_pool* pool, int n_layers, int n_kv_heads,
+                                     int head_dim, const int32_t* refs_in, int32_t* refs_out,
+                                     const crf_pages* tables, int n_tables, void* workspace,
+                                     size_t ws_bytes, void* stream);
+
+/* Gives back every entry of the tables: each lowers its page's count by one (a page several
+ * times if its entries are several). A count that would fall below zero, or an id outside the pool, rejects
+ * the call. `out` is not read. */
+CRF_API crf_status crf_pages_release(crf_ctx* ctx, int num_pages, const int32_t* refs_in, int32_t* refs_out,
+                                     const crf_pages* tables, int n_tables, void* workspace,
+                                     size_t ws_bytes, void* stream);
+
+/* Workspace bytes (256-byte aligned) of any crf_pages_* call on these tables. */
+CRF_API crf_status crf_pages_workspace_size(crf_ctx* ctx, int num_pages, const crf_pages* tables, int n_tables,
+                                            size_t* bytes);
+
 /* Per-kernel timing, for measurement: while enabled, every kernel launch and
  * device copy the library issues is bracketed by CUDA events recorded on the
  * caller's stream (the events are created here, up to `max_launches` launches

@@ -15,6 +15,14 @@ package computes any step of the path.
     ctx.recompute_window(model, cur, pool, [req], ws)
     ctx.drift(model.dims_c, cur, anchors, out_sq, ctx.drift_workspace(...))
     ctx.kl(model, ref_hidden, cur_hidden, out_kl, ...)
+
+A recovered cache is extended with new tokens by calls of one layer and of the pool's pages:
+
+    rope = Rope(head_dim, theta=1e6)
+    chunks = Chunks(page_tables, n_new, pos)         # one for all layers of a step
+    ctx.cache_append(pool, layer, chunks, k, v, q=q, q_out=q_rot, rope=rope)
+    ctx.chunk_attention(pool, layer, chunks, q_rot, o, ctx.chunk_attention_workspace(pool, chunks, n_heads))
+    ctx.pages_fork(pool, refs, PageTables(tables, n_tokens, child_tables), ctx.pages_workspace(...))
 """
 from __future__ import annotations
 
@@ -29,8 +37,8 @@ from .abi import CrfError
 
 MODULES = ("q", "k", "v", "o", "gate", "up", "down")
 
-__all__ = ["Context", "Model", "Adapter", "KVPool", "Request", "CrfError", "MODULES", "abi",
-           "kl_logits_noalloc"]
+__all__ = ["Context", "Model", "Adapter", "KVPool", "Request", "Rope", "Chunks", "PageTables", "CrfError",
+           "MODULES", "abi", "kl_logits_noalloc"]
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -118,6 +126,89 @@ class Request:
             self._hout = (c_void_p * max(1, len(hidden_out)))(*[t.data_ptr() for t in hidden_out])
         self.c = abi.Request(n_tokens, s, e, page_table.data_ptr(), _ptr(tokens), _ptr(hidden_in),
                              self._hout, _ptr(final_hidden_out))
+
+
+class Rope:
+    """Rotary positions (see crf_rope): the first ``rot_dim`` elements of a head turn in pairs of ``layout``
+    ("half" or "interleaved"); ``scaling`` "none", "linear", "base" or "bands" for contexts ``factor`` times
+    as long."""
+
+    def __init__(self, head_dim: int, rot_dim: Optional[int] = None, theta: float = 1e4, layout: str = "half",
+                 scaling: str = "none", factor: float = 1.0, low: float = 1.0, high: float = 32.0,
+                 original: float = 4096.0, magnitude: float = 1.0):
+        if layout not in abi.ROPE_LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(abi.ROPE_LAYOUTS)}")
+        if scaling not in abi.ROPE_SCALINGS:
+            raise ValueError(f"scaling must be one of {sorted(abi.ROPE_SCALINGS)}")
+        self.head_dim = head_dim
+        self.c = abi.Rope(head_dim, head_dim if rot_dim is None else rot_dim, abi.ROPE_LAYOUTS[layout],
+                          abi.ROPE_SCALINGS[scaling], theta, factor, low, high, original, magnitude)
+
+
+def _int32_on_device(name: str, t: torch.Tensor, n: int) -> torch.Tensor:
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name} must be a contiguous int32 tensor of at least {n} entries")
+    return t
+
+
+class Chunks:
+    """The new rows of a step's requests (see crf_chunk), packed in order: ``n_new[i]`` rows at positions
+    ``pos[i]`` on of the request cached on ``page_tables[i]``. ``n_keys[i]`` (default ``pos + n_new``)
+    cached positions are there for attention to see. One object serves every layer of a step."""
+
+    def __init__(self, page_tables: Sequence[torch.Tensor], n_new: Sequence[int], pos: Sequence[int],
+                 n_keys: Optional[Sequence[int]] = None):
+        n = len(page_tables)
+        if len(n_new) != n or len(pos) != n or (n_keys is not None and len(n_keys) != n):
+            raise ValueError("page_tables, n_new, pos and n_keys must have one entry a request")
+        self.page_tables = list(page_tables)
+        self.n, self.rows = n, sum(n_new)
+        self.append_entries, self.attend_entries = [], []
+        self.c = (abi.Chunk * max(1, n))()
+        for i, t in enumerate(self.page_tables):
+            m, p = int(n_new[i]), int(pos[i])
+            k = p + m if n_keys is None else int(n_keys[i])
+            if t.dtype != torch.int32 or not t.is_contiguous():
+                raise ValueError(f"page table {i} must be a contiguous int32 tensor")
+            self.append_entries.append((p + m + 15) // 16 if m else 0)
+            self.attend_entries.append((k + 15) // 16 if m else 0)
+            self.c[i] = abi.Chunk(m, p, k, t.data_ptr())
+        self.append_ok = all(t.numel() >= e for t, e in zip(self.page_tables, self.append_entries))
+        self.attend_ok = all(t.numel() >= e for t, e in zip(self.page_tables, self.attend_entries))
+
+
+class PageTables:
+    """Page tables of requests of ``n_tokens[i]`` tokens for the pages_* calls (see crf_pages); ``outs``
+    receives the new tables."""
+
+    def __init__(self, tables: Sequence[torch.Tensor], n_tokens: Sequence[int],
+                 outs: Optional[Sequence[torch.Tensor]] = None):
+        n = len(tables)
+        if len(n_tokens) != n or (outs is not None and len(outs) != n):
+            raise ValueError("tables, n_tokens and outs must have one entry a request")
+        self.tables, self.outs = list(tables), None if outs is None else list(outs)
+        self.n = n
+        self.c = (abi.Pages * max(1, n))()
+        for i, t in enumerate(self.tables):
+            need = (int(n_tokens[i]) + 15) // 16
+            _int32_on_device(f"table {i}", t, need)
+            if outs is not None:
+                _int32_on_device(f"outs[{i}]", outs[i], need)
+            self.c[i] = abi.Pages(int(n_tokens[i]), t.data_ptr(), None if outs is None else outs[i].data_ptr())
+
+
+_TYPES = {torch.bfloat16: abi.BF16, torch.float16: abi.FP16, torch.float32: abi.FP32}
+
+
+def _heads(name: str, x: torch.Tensor, out: Optional[torch.Tensor], dim: int) -> abi.Heads:
+    """crf_heads of x [rows, heads, dim] and out, of any row and head strides."""
+    if x.dim() != 3 or x.shape[2] != dim or (x.stride(2) != 1 and dim > 1):
+        raise ValueError(f"{name} must be [rows, heads, {dim}] with adjacent elements of a head")
+    if out is None:
+        return abi.Heads(x.data_ptr(), None, x.shape[1], x.stride(0), x.stride(1), 0, 0)
+    if out.shape != x.shape or out.dtype != x.dtype or (out.stride(2) != 1 and dim > 1):
+        raise ValueError(f"{name}: the output must have the input's shape and type and adjacent elements of a head")
+    return abi.Heads(x.data_ptr(), out.data_ptr(), x.shape[1], x.stride(0), x.stride(1), out.stride(0), out.stride(1))
 
 
 def _req_array(reqs: Sequence[Request]):
@@ -222,6 +313,129 @@ class Context:
                                   ref.data_ptr(), cur.data_ptr(), int(ref.shape[0]), vocab,
                                   out_kl.data_ptr(), _ptr(logits_out), workspace.data_ptr(),
                                   workspace.numel(), _stream(stream)))
+
+    # -------------------------------------------------------------- extension by new tokens
+    def _stream_here(self, stream) -> int:
+        return _stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+
+    def _here(self, **tensors) -> None:
+        for name, t in tensors.items():
+            if t is not None and (t.device.type != "cuda" or t.device.index != self.device):
+                raise ValueError(f"{name} must be on cuda:{self.device}")
+
+    def rotary(self, rope: Rope, positions: torch.Tensor, x: torch.Tensor, out: Optional[torch.Tensor] = None,
+               k: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False,
+               stream=None) -> None:
+        """x [rows, heads, head_dim] (bf16, fp16 or fp32, any row and head strides) rotated at
+        ``positions`` [rows] into ``out`` (default: in place), and ``k`` likewise into ``k_out``.
+        ``inverse``: the transposed map, the gradient of the call without it."""
+        self._here(positions=positions, x=x, out=out, k=k, k_out=k_out)
+        n = x.shape[0]
+        if x.dtype not in _TYPES:
+            raise ValueError("x must be bfloat16, float16 or float32")
+        _int32_on_device("positions", positions, n)
+        parts = (abi.Heads * 2)()
+        parts[0] = _heads("x", x, x if out is None else out, rope.head_dim)
+        if k is not None:
+            if k.dtype != x.dtype or k.shape[0] != n:
+                raise ValueError("k must have x's type and rows")
+            parts[1] = _heads("k", k, k if k_out is None else k_out, rope.head_dim)
+        abi.check(self.lib.crf_rotary(self.h, byref(rope.c), parts, 1 if k is None else 2, _TYPES[x.dtype], n,
+                                      positions.data_ptr(), int(inverse), self._stream_here(stream)))
+
+    def _pool_layer(self, pool: KVPool, layer: int) -> Tuple[int, int]:
+        if not 0 <= layer < len(pool.k_pages):
+            raise ValueError(f"layer {layer} is not in the pool")
+        k = pool.k_pages[layer]
+        return int(k.shape[1]), int(k.shape[3])
+
+    def cache_append(self, pool: KVPool, layer: int, chunks: Chunks, k: torch.Tensor, v: torch.Tensor,
+                     q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                     rope: Optional[Rope] = None, stream=None) -> None:
+        """Rows k, v [rows, kv heads, head_dim] into the requests' pages of ``layer``, k rotated at its
+        position when ``rope`` is given; and ``q`` rotated into ``q_out`` (default: in place)."""
+        hkv, dim = self._pool_layer(pool, layer)
+        self._here(k=k, v=v, q=q, q_out=q_out)
+        if not chunks.append_ok:
+            raise ValueError(f"page tables need {chunks.append_entries} entries to append")
+        for name, t in (("k", k), ("v", v), ("q", q)):
+            if t is not None and (t.dtype != torch.bfloat16 or t.shape[0] != chunks.rows):
+                raise ValueError(f"{name} must be bfloat16 with {chunks.rows} rows")
+        qh = None if q is None else byref(_heads("q", q, q if q_out is None else q_out, dim))
+        abi.check(self.lib.crf_cache_append(self.h, None if rope is None else byref(rope.c), byref(pool.c), layer,
+                                            hkv, dim, chunks.c, chunks.n, qh, byref(_heads("k", k, None, dim)),
+                                            byref(_heads("v", v, None, dim)), self._stream_here(stream)))
+
+    def chunk_attention_workspace(self, pool: KVPool, chunks: Chunks, n_q_heads: int, causal: bool = True,
+                                  window: int = 0) -> torch.Tensor:
+        """Workspace of a chunk_attention call; the same one serves every layer of the step."""
+        hkv, dim = self._pool_layer(pool, 0)
+        n = c_size_t()
+        abi.check(self.lib.crf_chunk_attention_workspace_size(self.h, n_q_heads, hkv, dim, chunks.c, chunks.n,
+                                                              int(causal), window, byref(n)))
+        return torch.empty(max(256, n.value), dtype=torch.uint8, device=f"cuda:{self.device}")
+
+    def chunk_attention(self, pool: KVPool, layer: int, chunks: Chunks, q: torch.Tensor, out: torch.Tensor,
+                        workspace: torch.Tensor, lse: Optional[torch.Tensor] = None, scale: float = 0.0,
+                        causal: bool = True, window: int = 0, stream=None) -> None:
+        """out = attention of the rows q [rows, heads, head_dim] (bf16) over their requests' cached keys of
+        ``layer`` (see crf_chunk_attention); ``lse`` fp32 [rows, heads]; ``scale`` 0: 1 / sqrt(head_dim)."""
+        hkv, dim = self._pool_layer(pool, layer)
+        self._here(q=q, out=out, workspace=workspace, lse=lse)
+        if not chunks.attend_ok:
+            raise ValueError(f"page tables need {chunks.attend_entries} entries to attend")
+        if q.dtype != torch.bfloat16 or q.shape[0] != chunks.rows:
+            raise ValueError(f"q must be bfloat16 with {chunks.rows} rows")
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
+            raise ValueError("lse must be a contiguous float32 [rows, heads]")
+        abi.check(self.lib.crf_chunk_attention(self.h, byref(pool.c), layer, hkv, dim, chunks.c, chunks.n,
+                                               byref(_heads("q", q, out, dim)), _ptr(lse), scale, int(causal),
+                                               window, workspace.data_ptr(), workspace.numel(),
+                                               self._stream_here(stream)))
+
+    # -------------------------------------------------------------- pages
+    def pages_workspace(self, num_pages: int, tables: PageTables) -> torch.Tensor:
+        n = c_size_t()
+        abi.check(self.lib.crf_pages_workspace_size(self.h, num_pages, tables.c, tables.n, byref(n)))
+        return torch.empty(max(256, n.value), dtype=torch.uint8, device=f"cuda:{self.device}")
+
+    def _refs(self, num_pages: int, refs: torch.Tensor, refs_out: Optional[torch.Tensor]) -> Tuple[int, int]:
+        self._here(refs=refs, refs_out=refs_out)
+        out = refs if refs_out is None else refs_out
+        for name, t in (("refs", refs), ("refs_out", out)):
+            if t.numel() != num_pages:
+                raise ValueError(f"{name} must have one count a page of the pool ({num_pages})")
+            _int32_on_device(name, t, num_pages)
+        return refs.data_ptr(), out.data_ptr()
+
+    def pages_fork(self, pool: KVPool, refs: torch.Tensor, tables: PageTables, workspace: torch.Tensor,
+                   refs_out: Optional[torch.Tensor] = None, deep: bool = False, stream=None) -> None:
+        """A second continuation of every request into ``tables.outs``: whole pages shared, a part-filled
+        last page (``deep``: every page) copied into the lowest free ones. ``refs`` is updated in place
+        unless ``refs_out`` is given."""
+        self._pages(self.lib.crf_pages_fork, pool, refs, refs_out, tables, workspace, stream, (int(deep),))
+
+    def pages_compact(self, pool: KVPool, refs: torch.Tensor, tables: PageTables, workspace: torch.Tensor,
+                      refs_out: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Live pages to the front of the pool; the tables with their new ids into ``tables.outs``."""
+        self._pages(self.lib.crf_pages_compact, pool, refs, refs_out, tables, workspace, stream, ())
+
+    def _pages(self, call, pool, refs, refs_out, tables, workspace, stream, flags) -> None:
+        hkv, dim = self._pool_layer(pool, 0)
+        if tables.outs is None:
+            raise ValueError("the tables need outs")
+        self._here(workspace=workspace)
+        a, b = self._refs(pool.num_pages, refs, refs_out)
+        abi.check(call(self.h, byref(pool.c), len(pool.k_pages), hkv, dim, a, b, tables.c, tables.n, *flags,
+                       workspace.data_ptr(), workspace.numel(), self._stream_here(stream)))
+
+    def pages_release(self, refs: torch.Tensor, tables: PageTables, workspace: torch.Tensor,
+                      refs_out: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Every table entry gives its reference back."""
+        self._here(workspace=workspace)
+        a, b = self._refs(refs.numel(), refs, refs_out)
+        abi.check(self.lib.crf_pages_release(self.h, refs.numel(), a, b, tables.c, tables.n, workspace.data_ptr(),
+                                             workspace.numel(), self._stream_here(stream)))
 
     def check(self, stream=None) -> None:
         abi.check(self.lib.crf_check(self.h, _stream(stream)))

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_float, c_int, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_float, c_int, c_int64, c_size_t, c_uint32, c_void_p
 
 LIB_DIR = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_lib")
 # CRF_LIB_VARIANT=debug selects the build with device-side page-id checks
@@ -22,13 +22,20 @@ STATUS_NAMES = ["CRF_OK", "CRF_EINVAL", "CRF_ESHAPE", "CRF_EUNSUPPORTED", "CRF_E
 NUM_MODULES = 7
 PAGE_SIZE = 16
 MAX_REQUESTS = 32
+MAX_CHUNKS = 128
+MAX_TABLES = 512
+BF16, FP16, FP32 = range(3)
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
 
 # Every symbol include/crf.h declares.
 EXPORTS = ("crf_create", "crf_destroy", "crf_last_error", "crf_check", "crf_workspace_size",
            "crf_recompute_window", "crf_drift_workspace_size", "crf_drift",
            "crf_kl_workspace_size", "crf_kl", "crf_kl_logits_noalloc", "crf_profile_enable",
            "crf_profile_read", "crf_decode_workspace_size", "crf_decode_step",
-           "crf_selftest_timeout")
+           "crf_selftest_timeout", "crf_rotary", "crf_cache_append",
+           "crf_chunk_attention_workspace_size", "crf_chunk_attention", "crf_pages_workspace_size",
+           "crf_pages_fork", "crf_pages_compact", "crf_pages_release")
 
 
 class ModelDims(ctypes.Structure):
@@ -70,6 +77,25 @@ class DecodeRow(ctypes.Structure):
     _fields_ = [("pos", c_int), ("page_table", c_void_p), ("token", c_void_p)]
 
 
+class Rope(ctypes.Structure):
+    _fields_ = [("head_dim", c_int), ("rot_dim", c_int), ("layout", c_int), ("scaling", c_int),
+                ("theta", c_double), ("factor", c_double), ("low", c_double), ("high", c_double),
+                ("original", c_double), ("magnitude", c_double)]
+
+
+class Heads(ctypes.Structure):
+    _fields_ = [("x", c_void_p), ("out", c_void_p), ("heads", c_int), ("x_row", c_int64),
+                ("x_head", c_int64), ("out_row", c_int64), ("out_head", c_int64)]
+
+
+class Chunk(ctypes.Structure):
+    _fields_ = [("n_new", c_int), ("pos", c_int), ("n_keys", c_int), ("page_table", c_void_p)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("n_tokens", c_int), ("table", c_void_p), ("out", c_void_p)]
+
+
 _lib = None
 
 
@@ -104,6 +130,16 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "crf_decode_step": ([P, POINTER(Model), POINTER(Adapter), POINTER(KVPool), POINTER(DecodeRow),
                              c_int, P, P, P, c_size_t, P], c_int),
         "crf_kl": ([P, POINTER(Model), P, P, c_int, c_int, P, P, P, c_size_t, P], c_int),
+        "crf_rotary": ([P, P, P, c_int, c_int, c_int, P, c_int, P], c_int),
+        "crf_cache_append": ([P, P, P, c_int, c_int, c_int, P, c_int, P, P, P, P], c_int),
+        "crf_chunk_attention_workspace_size": ([P, c_int, c_int, c_int, P, c_int, c_int, c_int,
+                                                POINTER(c_size_t)], c_int),
+        "crf_chunk_attention": ([P, P, c_int, c_int, c_int, P, c_int, P, P, c_float, c_int, c_int, P,
+                                 c_size_t, P], c_int),
+        "crf_pages_workspace_size": ([P, c_int, P, c_int, POINTER(c_size_t)], c_int),
+        "crf_pages_fork": ([P, P, c_int, c_int, c_int, P, P, P, c_int, c_int, P, c_size_t, P], c_int),
+        "crf_pages_compact": ([P, P, c_int, c_int, c_int, P, P, P, c_int, P, c_size_t, P], c_int),
+        "crf_pages_release": ([P, c_int, P, P, P, c_int, P, c_size_t, P], c_int),
         "crf_kl_logits_noalloc": ([c_int, P, P, c_int, c_int, P, P], c_int),
         "crf_profile_enable": ([P, c_int, c_int], c_int),
         "crf_profile_read": ([P, c_int, ctypes.c_char_p, POINTER(ctypes.c_double), POINTER(c_int),

@@ -10,9 +10,8 @@
 // where each GEMM launch computes its own unmerged adapter term (Eq. S3).
 // Then the last prefix row of each request that asks for it continues through
 // layers e..N-1 against the historical cache (first-step state, Section S2.1).
-#include "../../include/crf.h"
+#include "api.h"
 #include "common.cuh"
-#include "kernels.h"
 
 #include <algorithm>
 #include <cmath>
@@ -26,60 +25,19 @@
 
 using namespace crf;
 
-struct crf_ctx {
-  int device;
-  int num_sms;
-  int* status_dev;
-  // per-launch timing (crf_profile_enable)
-  bool prof_on = false;
-  std::vector<cudaEvent_t> ev;
-  int ev_used = 0;
-  struct Rec {
-    int kind, idx, kernels;
-  };
-  std::vector<Rec> rec;
-  int dropped = 0;
-};
-
 namespace {
 
-enum ProfKind : int {
-  kPQkv, kPO, kPGateUp, kPDown, kPAttn, kPNorm, kPEmbed, kPCopy,
-  kPDecode, kPLmHead, kPKl, kPDrift, kPCheck, kPNumKinds
-};
 const char* const kProfNames[kPNumKinds] = {
     "gemm_qkv_rope_paged", "gemm_o_resid", "gemm_gateup_swiglu", "gemm_down_resid",
     "attn_prefill_paged", "rmsnorm", "embed_gather", "row_copy",
-    "tail_decode", "lm_head", "kl_reduce", "drift_gram", "page_check"};
-
-// Brackets the launches issued in its lifetime with two events on `st` when
-// profiling is on; `kernels` is how many kernels those launches are.
-struct ProfScope {
-  crf_ctx* c;
-  int kind, kernels, idx;
-  cudaStream_t st;
-  ProfScope(crf_ctx* c_, int kind_, cudaStream_t st_, int kernels_ = 1)
-      : c(c_), kind(kind_), kernels(kernels_), idx(-1), st(st_) {
-    if (!c->prof_on) return;
-    if (c->ev_used + 2 > static_cast<int>(c->ev.size())) {
-      c->dropped += kernels;
-      return;
-    }
-    idx = c->ev_used;
-    c->ev_used += 2;
-    cudaEventRecord(c->ev[idx], st);
-  }
-  ~ProfScope() {
-    if (idx >= 0) {
-      cudaEventRecord(c->ev[idx + 1], st);
-      c->rec.push_back({kind, idx, kernels});
-    }
-  }
-};
+    "tail_decode", "lm_head", "kl_reduce", "drift_gram", "page_check", "rotary", "cache_append",
+    "chunk_attention", "page_plan", "page_copy"};
 
 thread_local std::string g_err;
 
-crf_status fail(crf_status st, const char* fmt, ...) {
+}  // namespace
+
+crf_status crf::fail(crf_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -89,15 +47,7 @@ crf_status fail(crf_status st, const char* fmt, ...) {
   return st;
 }
 
-#define CRF_CUDA(expr)                                                                  \
-  do {                                                                                  \
-    cudaError_t _e = (expr);                                                            \
-    if (_e != cudaSuccess)                                                              \
-      return fail(CRF_ECUDA, "%s failed: %s (%s:%d)", #expr, cudaGetErrorString(_e), __FILE__, \
-                  __LINE__);                                                            \
-  } while (0)
-
-inline size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
+namespace {
 
 struct Dims {
   int N, h, hq, hkv, d, f, V, qd, kvd;
@@ -158,8 +108,6 @@ crf_status check_lora(const crf_lora_dims& l) {
   if (l.module_mask & ~0x7Fu) return fail(CRF_EINVAL, "module_mask has bits beyond the 7 modules");
   return CRF_OK;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // ---------------------------------------------------------------- workspace plan
 struct Plan {
@@ -864,9 +812,16 @@ crf_status crf_check(crf_ctx* ctx, void* stream) {
     if (status & kStatusPages)
       return fail(CRF_EINVAL, "a page table held an id outside the pool or a page twice; that call wrote "
                   "nothing outside its workspace (status 0x%x)", status);
+    if (status & kStatusCounts)
+      return fail(CRF_EINVAL, "a page call's tables and reference counts contradict each other (an id outside the pool, "
+                  "a free or over-released page, a reference in no table); that call wrote nothing outside its "
+                  "workspace (status 0x%x)", status);
     if (status & kStatusBounds)
-      return fail(CRF_EINVAL, "a device-side bounds check failed: a token id outside the vocabulary%s "
-                  "(status 0x%x)", kDebugBuild ? " or a page id outside the pool" : "", status);
+      return fail(CRF_EINVAL, "a device-side bounds check failed: a token id outside the vocabulary or a page id "
+                  "outside the pool (status 0x%x)", status);
+    if (status & kStatusFull)
+      return fail(CRF_ENOMEM, "the pool has too few free pages for a fork; that call wrote nothing outside its "
+                  "workspace (status 0x%x)", status);
     return fail(CRF_ETIMEOUT, "a kernel abandoned a bounded wait (status 0x%x)", status);
   }
   return CRF_OK;

@@ -11,7 +11,7 @@
 namespace crf {
 
 // Status bits a kernel may set in the context's device status word.
-enum : int { kStatusTimeout = 1, kStatusBounds = 2, kStatusPages = 4 };
+enum : int { kStatusTimeout = 1, kStatusBounds = 2, kStatusPages = 4, kStatusCounts = 8, kStatusFull = 16 };
 
 // The per-call abort word: set by the page-table check that opens a call when a page id is out of
 // the pool or a page appears twice. Every later kernel of the call that writes memory outside the call's
