@@ -168,10 +168,12 @@ crf_status check_workspace(const void* ws, size_t have, size_t need) {
   return CRF_OK;
 }
 
-crf_status check_attention(int n_q_heads, int n_kv_heads, int window) {
+// rows: 0 where they are not known yet
+crf_status check_attention(int n_q_heads, int n_kv_heads, int window, int64_t rows) {
   if (n_q_heads < 1 || n_kv_heads < 1) return fail(CRF_EINVAL, "heads must be positive");
   if (n_q_heads % n_kv_heads) return fail(CRF_ESHAPE, "%d query heads are no multiple of %d kv heads", n_q_heads, n_kv_heads);
   if (window < 0) return fail(CRF_EINVAL, "window must be >= 0");
+  if (rows * n_q_heads > (1 << 30)) return fail(CRF_EUNSUPPORTED, "rows x query heads over 2^30");
   return CRF_OK;
 }
 
@@ -351,12 +353,13 @@ crf_status crf_chunk_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int n
                                               size_t* bytes) {
   return guarded([&]() -> crf_status {
     if (!ctx || !bytes) return fail(CRF_EINVAL, "null argument");
-    crf_status s = check_attention(n_q_heads, n_kv_heads, window);
+    crf_status s = check_attention(n_q_heads, n_kv_heads, window, 0);
     if (s != CRF_OK) return s;
     s = check_pool_shape(n_kv_heads, head_dim, 1);
     if (s != CRF_OK) return s;
     ChunkTable t;
     s = fill_chunks(chunks, n_chunks, true, 1, &t);
+    if (s == CRF_OK) s = check_attention(n_q_heads, n_kv_heads, window, t.row0[t.n]);
     if (s != CRF_OK) return s;
     *bytes = align256(chunk_attention_workspace(t, n_q_heads, n_kv_heads, head_dim, causal != 0, window, ctx->num_sms));
     return CRF_OK;
@@ -372,7 +375,7 @@ crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer,
     if (s != CRF_OK) return s;
     s = check_layer(pool, layer);
     if (s != CRF_OK) return s;
-    s = check_attention(q->heads, n_kv_heads, window);
+    s = check_attention(q->heads, n_kv_heads, window, 0);
     if (s != CRF_OK) return s;
     if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(CRF_EINVAL, "scale must be positive, or 0 for 1/sqrt(head_dim)");
     ChunkTable t;
@@ -380,6 +383,8 @@ crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer,
     if (s != CRF_OK) return s;
     const int rows = t.row0[t.n];
     if (rows == 0) return CRF_OK;
+    s = check_attention(q->heads, n_kv_heads, window, rows);
+    if (s != CRF_OK) return s;
     s = check_heads(*q, 16, true, "q");
     if (s != CRF_OK) return s;
     if ((q->x_row | q->x_head | q->out_row | q->out_head) % 8)

@@ -1,9 +1,29 @@
-// Attention of a chunk of new rows over their requests' cached keys. Row r of a request at position p sees the
-// keys lo <= j < hi with hi = min(n_keys, p + 1) (causal; n_keys otherwise) and lo = max(0, p - window + 1)
-// (0 without a window): o = softmax(scale q k) v, lse = log sum exp(scale q k). One warp per (row, query head)
-// walks the keys with a running maximum and sum.
+// Attention of a chunk of new rows over their requests' cached keys, on tcgen05. Row r of a request at position
+// p sees the keys lo <= j < hi with hi = min(n_keys, p + 1) (causal; n_keys otherwise) and lo = max(0, p - window + 1)
+// (0 without a window): o = softmax(scale q k) v, lse = log sum exp(scale q k).
+//
+// The query heads of one kv head read the same keys, so a request's rows and the group's heads are packed into
+// one axis (row r, head h of the group -> r group + h) and cut into tiles of 128 rows, the M of an MMA. Two chains
+// S -> softmax -> P V run side by side in a CTA, so that one's products fill the other's softmax:
+//   wide form    256 packed rows or a last part of them: chain t is query tile t, both read the same K/V tiles
+//   narrow form  requests of at most 128 packed rows (one token of 7 heads: 7): one query tile, chain t takes
+//                every other K/V tile, and the chains' (o, maximum, sum) meet in shared memory at the end
+// A step of the pair of chains is one K/V tile (wide) or two (narrow). Where the items (request, kv head,
+// query tiles) would leave SMs idle, each one's keys are cut into pieces of equally many steps; a piece writes its
+// unnormalised o, maximum and sum in fp32 to the workspace and chunk_attn_merge joins them in order of keys.
+//
+// Warp roles, TMEM and the ring follow the prefill attention (attention_tc.cu): warp 0 gathers the pages of K and V
+// tiles with TMA, warp 1 issues the MMAs, warps 4-7 and 8-11 are the chains' softmax (one packed row a thread,
+// P back into TMEM as bf16, o rescaled there when the maximum grows by more than 2^8). Here the softmax warps also
+// bring q into shared memory (rows of any strides, packed heads), and warps whose 32 rows are all padding do nothing.
+//
+// Unseen slots may hold anything: pages that no row of the CTA sees are not fetched; scores of unseen keys
+// become -inf whatever they were; v of keys that no row sees is zeroed, and in tiles that only some rows see an
+// infinite or NaN element of v is zeroed and given back, at the end, to the rows that see it (0 times infinity
+// would be NaN in the others; infinities absorb whatever they are added to, so when does not matter).
 #include "common.cuh"
 #include "extend.h"
+#include "tma_map.h"
 
 #include <algorithm>
 #include <cstring>
@@ -12,67 +32,818 @@ namespace crf {
 
 namespace {
 
-struct ChunkArgs {
-  ChunkAttnDesc d;
-  ChunkTable c;
+constexpr int kM = 128;  // packed rows per query tile
+constexpr int kN = 128;  // keys per K/V tile
+constexpr int kPagesPerTile = kN / kPage;
+constexpr int kThreads = 384;
+// setmaxnreg split: the first warpgroup (producer, issuer) keeps kRegsCtl, the softmax warpgroups take
+// kRegsSoftmax; the sum must fit what the CTA launched with.
+constexpr int kRegsCtl = 56;
+constexpr int kRegsSoftmax = 208;
+constexpr int kRegsNeeded = 128 * kRegsCtl + 256 * kRegsSoftmax;
+constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// How a call's work is cut. Items of request i: [item0[i], item0[i + 1]), longest first: query tile (or pair)
+// from the last down, kv head, piece of `piece_steps` steps.
+struct ChunkPlan {
+  int item0[kMaxChunks + 1];
+  int pieces[kMaxChunks];  // of each (query tile, head); 1: written straight to out
+  int piece_steps;
+  int split_rows[kMaxChunks + 1];  // packed rows x heads of split requests, prefix: the merge's blocks
 };
 
-template <int D>
-__global__ void __launch_bounds__(256) chunk_attn_simple(const __grid_constant__ ChunkArgs a) {
-  constexpr int E = D / 32;
-  const ChunkAttnDesc& d = a.d;
-  const int lane = threadIdx.x & 31;
-  const int64_t w = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  const int64_t r = w / d.n_q_heads;
-  const int h = static_cast<int>(w - r * d.n_q_heads), g = h / (d.n_q_heads / d.n_kv_heads);
-  if (r >= a.c.row0[a.c.n]) return;
-  int i = 0;
-  while (r >= a.c.row0[i + 1]) ++i;
-  const int p = a.c.pos[i] + static_cast<int>(r - a.c.row0[i]);
-  const int hi = d.causal ? min(a.c.n_keys[i], p + 1) : a.c.n_keys[i], lo = d.window ? max(0, p - d.window + 1) : 0;
-  float q[E], o[E], m = -INFINITY, l = 0.f;
+struct ChunkArgs {
+  CUtensorMap tmK, tmV;  // pages of the layer, box: one page of one kv head
+  ChunkAttnDesc d;
+  ChunkTable c;
+  ChunkPlan p;
+  float* part;  // split items: [item][rows of an item][D] o, then [item][rows][2] maximum and sum
+  float* part_ml;
+  int part_rows;
+};
+
+__host__ __device__ inline bool narrow_form(int packed_rows) { return packed_rows <= kM; }
+
+// Keys [lo, hi) that the rows a .. b (positions) of a request see in all; empty if hi <= lo.
+struct KeyRange {
+  int lo, hi;
+};
+__host__ __device__ inline KeyRange keys_of_rows(int first_pos, int last_pos, int n_keys, bool causal, int window) {
+  KeyRange k;
+  k.lo = window > 0 && first_pos + 1 > window ? first_pos + 1 - window : 0;
+  k.hi = causal && last_pos + 1 < n_keys ? last_pos + 1 : n_keys;
+  return k;
+}
+
+__device__ __forceinline__ void regs_dec_ctl() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsCtl)); }
+__device__ __forceinline__ void regs_inc_softmax() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+}
+__device__ __forceinline__ void softmax_groups_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+// One packed row's share of a K/V tile: 128 raw scores from TMEM, running maximum and sum, o rescaled in TMEM when
+// the maximum grows by more than 2^8, P (bf16, unnormalised) back over the scores. MASK: keys outside [lo, hi)
+// (relative to the tile) count as -inf. A row that has seen no key yet keeps a maximum of -inf.
+template <int D, bool MASK>
+__device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool first, int lo, int hi, float sl2,
+                                             float& m_run, float& l_run) {
+  uint32_t sr[4][32];
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    q[e] = __bfloat162float(d.q[r * d.q_row + h * d.q_head + lane * E + e]) * d.scale;
-    o[e] = 0.f;
-  }
-  for (int j = lo; j < hi; ++j) {
-    int page = a.c.pt[i][j / kPage];
-    if (page < 0 || page >= a.c.num_pages) {
-      if (lane == 0) atomicOr(d.status, kStatusBounds);
-      page = 0;
+  for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sr[c]);
+  tmem_ld_wait();
+  float mx[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) mx[k] = -INFINITY;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (MASK) {
+        const int k = c * 32 + 2 * i;
+        if (k < lo || k >= hi) sr[c][2 * i] = __float_as_uint(-INFINITY);
+        if (k + 1 < lo || k + 1 >= hi) sr[c][2 * i + 1] = __float_as_uint(-INFINITY);
+      }
+      mx[i & 7] = fmax3(mx[i & 7], __uint_as_float(sr[c][2 * i]), __uint_as_float(sr[c][2 * i + 1]));
     }
-    const size_t at = ((static_cast<size_t>(page) * d.n_kv_heads + g) * kPage + j % kPage) * D + lane * E;
-    float s = 0.f;
+  const float mt = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
+  const bool grow = (mt - m_run) * sl2 > kRescaleThreshold;  // false while both are -inf
+  const float alpha = grow ? ex2_approx((m_run - mt) * sl2) : 1.0f;
+  if (!first && __any_sync(0xffffffffu, grow)) {
+#pragma unroll 1
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t o[32];
+      tmem_ld32(tO + c * 32, o);
+      tmem_ld_wait();
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += q[e] * __bfloat162float(d.kpages[at + e]);
-    s = warp_sum(s);
-    const float mn = fmaxf(m, s), c = __expf(m - mn), w = __expf(s - mn);
-    l = l * c + w;
-    m = mn;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * c + w * __bfloat162float(d.vpages[at + e]);
+      for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+      tmem_st32(tO + c * 32, o);
+    }
+    tmem_st_wait();
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  if (grow) {
+    l_run *= alpha;
+    m_run = mt;
+  }
+  const float neg_m = m_run == -INFINITY ? 0.f : -m_run * sl2;
+  const uint64_t sl2x2 = f32x2(sl2, sl2), negm2 = f32x2(neg_m, neg_m);
+  uint64_t rs2[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
 #pragma unroll
-  for (int e = 0; e < E; ++e) d.out[r * d.out_row + h * d.out_head + lane * E + e] = __float2bfloat16_rn(o[e] * inv);
-  if (d.lse && lane == 0) d.lse[r * d.n_q_heads + h] = l > 0.f ? m + logf(l) : -INFINITY;
+  for (int c = 0; c < 4; ++c) {
+    uint32_t pk[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float x0, x1;
+      f32x2_split(fma_f32x2(f32x2(__uint_as_float(sr[c][2 * i]), __uint_as_float(sr[c][2 * i + 1])),
+                            sl2x2, negm2), x0, x1);
+      const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+      rs2[i & 1] = add_f32x2(rs2[i & 1], f32x2(p0, p1));
+      // the product with v is bf16 x bf16: a weight is off by 2^-8 of itself at most; the sum keeps the fp32 one
+      pk[i] = pack_bf16(p0, p1);
+    }
+    tmem_st16(tS + 16 * c, pk);
+  }
+  tmem_st_wait();
+  float r0, r1, r2, r3;
+  f32x2_split(rs2[0], r0, r1);
+  f32x2_split(rs2[1], r2, r3);
+  l_run += (r0 + r1) + (r2 + r3);
+}
+
+__device__ __forceinline__ bool not_finite_bf16(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
+
+template <int D>
+struct Tile {
+  static constexpr int HALVES = D / 64;
+  static constexpr int Q_BYTES = kM * D * 2;
+  static constexpr int KV_BYTES = kN * D * 2;
+  static constexpr int HALF_ROWS_BYTES = kN * 128;    // one 64-column half of a query tile
+  static constexpr int GROUP_BYTES = HALVES * 1024;   // 8 keys, all halves, in a K/V slot
+  static constexpr int kSmem = 2 * Q_BYTES + 5 * KV_BYTES + 1024;  // wide: 2 q tiles, 5 slots; narrow: 1 and 6
+};
+
+// Where an element of a K/V slot lies: key, 16-byte unit of the head.
+template <int D>
+__device__ __forceinline__ uint4* slot_unit(uint8_t* slot, int key, int unit) {
+  using T = Tile<D>;
+  return reinterpret_cast<uint4*>(slot + (key >> 3) * T::GROUP_BYTES + (unit >> 3) * 1024 + (key & 7) * 128 +
+                                  (((unit & 7) ^ (key & 7)) << 4));
+}
+
+struct Shared {
+  uint64_t q_full, o_full, drain;
+  uint64_t kv_full[6], kv_empty[6];
+  uint64_t s_full[2], p_full[2];
+  uint32_t tmem_base;
+  volatile int abort_flag;
+  volatile int dirty;  // an infinite or NaN element of v was zeroed
+};
+
+struct Item {
+  int req, g, q0, rows, piece;  // rows: packed rows of the request; q0: the item's first
+  int item;
+  bool narrow;
+};
+
+__device__ __forceinline__ Item item_of(const ChunkArgs& a, int idx) {
+  int lo = 0, hi = a.c.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.p.item0[mid] <= idx) lo = mid; else hi = mid - 1;
+  }
+  Item w;
+  w.req = lo;
+  w.item = idx;
+  w.rows = (a.c.row0[lo + 1] - a.c.row0[lo]) * (a.d.n_q_heads / a.d.n_kv_heads);
+  w.narrow = narrow_form(w.rows);
+  const int tile = w.narrow ? kM : 2 * kM, tiles = (w.rows + tile - 1) / tile;
+  idx -= a.p.item0[lo];
+  const int per_tile = a.d.n_kv_heads * a.p.pieces[lo], qt = idx / per_tile;
+  idx -= qt * per_tile;
+  w.g = idx / a.p.pieces[lo];
+  w.piece = idx - w.g * a.p.pieces[lo];
+  w.q0 = (tiles - 1 - qt) * tile;
+  return w;
+}
+
+template <int D, bool NARROW>
+__device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uint8_t* smem, Shared& sh) {
+  using T = Tile<D>;
+  constexpr int Q_BYTES = T::Q_BYTES, KV_BYTES = T::KV_BYTES, GROUP_BYTES = T::GROUP_BYTES;
+  constexpr int kSlots = NARROW ? 6 : 5;
+  constexpr int kTiles = NARROW ? 1 : 2;  // query tiles of the item
+  constexpr uint32_t TMEM_COLS = 512;
+  const ChunkAttnDesc& d = a.d;
+  uint8_t* sQ = smem;
+  uint8_t* sKV = sQ + kTiles * Q_BYTES;
+  const int grp = d.n_q_heads / d.n_kv_heads;
+  const int pos = a.c.pos[w.req], n_keys = a.c.n_keys[w.req], row0 = a.c.row0[w.req];
+  const int32_t* pt = a.c.pt[w.req];
+  const int last_row = w.rows - 1;
+  const bool split = a.p.pieces[w.req] > 1;
+
+  // Keys of each chain's query tile: [lo, hi) that some row sees, [flo, fhi) that all rows see
+  int lo[2], hi[2], flo[2], fhi[2], valid[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int r0 = w.q0 + (NARROW ? 0 : t * kM), r1 = min(r0 + kM - 1, last_row);
+    valid[t] = max(0, r1 - r0 + 1);
+    const int p0 = pos + r0 / grp, p1 = pos + max(r1, 0) / grp;
+    const KeyRange some = keys_of_rows(p0, p1, n_keys, d.causal, d.window);
+    const KeyRange all = keys_of_rows(p1, p0, n_keys, d.causal, d.window);
+    lo[t] = some.lo;
+    hi[t] = valid[t] ? some.hi : 0;
+    flo[t] = all.lo;
+    fhi[t] = all.hi;
+  }
+  // K/V tiles of the item, and of its piece: [jb, jb + J); chain t runs steps[t] of them
+  const int all_lo = lo[0], all_hi = max(hi[0], hi[1]);
+  const int jfirst = all_lo / kN, jend = max(jfirst, (all_hi + kN - 1) / kN);
+  const int per_piece = a.p.piece_steps * (NARROW ? 2 : 1);
+  const int jb = min(static_cast<int>(min(static_cast<int64_t>(jend), jfirst + static_cast<int64_t>(w.piece) * per_piece)), jend);
+  const int J = static_cast<int>(min(static_cast<int64_t>(jend - jb), static_cast<int64_t>(per_piece)));
+  int steps[2];
+  if (NARROW) {
+    steps[0] = (J + 1) / 2;
+    steps[1] = J / 2;
+  } else {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) steps[t] = min(J, max(0, (hi[t] + kN - 1) / kN - jb));
+  }
+  const int readers = NARROW ? 1 : (steps[0] > 0) + (steps[1] > 0);  // chains that release a ring slot
+  auto quarters = [&](int t) { return (valid[t] + 31) / 32; };       // warps of a chain with rows
+  auto tile_of = [&](int t, int s) { return NARROW ? 2 * s + t : s; };
+
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);  // uniform
+  const int lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    mbar_init(&sh.q_full, 8);
+    mbar_init(&sh.o_full, 1);
+    mbar_init(&sh.drain, 1);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&sh.s_full[t], 1);
+      mbar_init(&sh.p_full[t], max(1, quarters(t)));
+    }
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(&sh.kv_full[i], 1);
+      mbar_init(&sh.kv_empty[i], max(1, readers));
+    }
+    sh.abort_flag = 0;
+    sh.dirty = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&sh.tmem_base, TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem_base;
+
+  if (warp < 4) {
+    regs_dec_ctl();
+    if (warp == 0) {
+      // ---------------------------------------------------------------- producer
+      const bool issuer = elect_one();
+      bool ok = true;
+      int armed = 0, slot = 0;
+      uint32_t ph = 0;
+      const int n_pages = (all_hi + kPage - 1) / kPage;
+      auto page_id = [&](int j) {
+        const int i = (jb + j) * kPagesPerTile + (lane & (kPagesPerTile - 1));
+        int id = 0;
+        if (i < n_pages && i >= all_lo / kPage) {
+          id = pt[i];
+          if (id < 0 || id >= a.c.num_pages) {
+            if (d.status) atomicOr(d.status, kStatusBounds);
+            id = 0;
+          }
+        }
+        return id;
+      };
+      int ids = J > 0 ? page_id(0) : 0;
+      for (int j = 0; j < J && ok; ++j) {
+        const int next_ids = j + 1 < J ? page_id(j + 1) : 0;
+        // pages of the tile that some row sees
+        const int pg0 = max(0, all_lo / kPage - (jb + j) * kPagesPerTile);
+        const int pg1 = max(pg0, min(kPagesPerTile, n_pages - (jb + j) * kPagesPerTile));
+        for (int kv = 0; kv < 2; ++kv) {
+          ok = mbar_wait_warp(&sh.kv_empty[slot], ph ^ 1, &sh.abort_flag, d.status);
+          if (!ok) break;
+          if (issuer) mbar_arrive_expect_tx(&sh.kv_full[slot], (pg1 - pg0) * (kPage / 8) * GROUP_BYTES);
+          uint8_t* dst = sKV + slot * KV_BYTES;
+          const CUtensorMap* map = kv == 0 ? &a.tmK : &a.tmV;
+#pragma unroll
+          for (int p = 0; p < kPagesPerTile; ++p) {
+            const int group = (__shfl_sync(0xffffffffu, ids, p) * d.n_kv_heads + w.g) * (kPage / 8);
+            if (issuer && p >= pg0 && p < pg1)
+              tma_load_4d(dst + p * (kPage / 8) * GROUP_BYTES, map, &sh.kv_full[slot], 0, 0, 0, group);
+          }
+          ++armed;
+          if (++slot == kSlots) {
+            slot = 0;
+            ph ^= 1;
+          }
+        }
+        ids = next_ids;
+      }
+      if (!ok) {
+        // every copy issued lands before the CTA can exit: the last use of every slot
+        volatile int never = 0;
+        for (int i = 0; i < kSlots && i < armed; ++i) {
+          const int u = armed - 1 - i;
+          mbar_wait(&sh.kv_full[u % kSlots], static_cast<uint32_t>((u / kSlots) & 1), &never, nullptr);
+        }
+      }
+    } else if (warp == 1) {
+      // -------------------------------------------------------------- MMA issuer
+      // S of both chains' first tiles, then P V and the next S of each chain in turn. MMAs of one thread execute in
+      // issue order, so a chain's next S overwrites the score columns only after P V has read P from them.
+      const bool issuer = elect_one();
+      bool ok = J == 0 || mbar_wait_warp(&sh.q_full, 0, &sh.abort_flag, d.status);
+      bool issued = false;
+      const uint32_t idesc_s = idesc_bf16_f32(kM, kN);
+      const uint32_t idesc_o = idesc_bf16_f32(kM, D, false, true);
+      const uint64_t qd = smem_desc(smem_u32(sQ), 16, 1024, kSwizzle128B);
+      const uint64_t kd = smem_desc(smem_u32(sKV), 16, GROUP_BYTES, kSwizzle128B);
+      const uint64_t vd = smem_desc(smem_u32(sKV), 1024, GROUP_BYTES, kSwizzle128B);
+      auto issue_s = [&](int t, int slot) {
+        const uint64_t q = qd + static_cast<uint32_t>((NARROW ? 0 : t) * (Q_BYTES >> 4));
+        const uint64_t k = kd + static_cast<uint32_t>(slot * (KV_BYTES >> 4));
+        if (issuer) {
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            mma_bf16_ss(tmem + t * 128, q + (kk >> 2) * (T::HALF_ROWS_BYTES >> 4) + (kk & 3) * 2,
+                        k + (kk >> 2) * 64 + (kk & 3) * 2, idesc_s, kk > 0 ? 1u : 0u);
+          mma_commit(&sh.s_full[t]);
+        }
+      };
+      for (int t = 0; t < 2 && ok; ++t) {
+        if (steps[t] == 0) continue;
+        const int item = 2 * tile_of(t, 0);
+        ok = mbar_wait_warp(&sh.kv_full[item % kSlots], (item / kSlots) & 1, &sh.abort_flag, d.status);
+        if (!ok) break;
+        tc_fence_after();
+        issue_s(t, item % kSlots);
+        issued = true;
+      }
+      const int most = max(steps[0], steps[1]);
+      for (int s = 0; s < most && ok; ++s) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (s >= steps[t]) continue;
+          // P of this step is in TMEM, and its V and the chain's next K have landed
+          if (!mbar_wait_warp(&sh.p_full[t], s & 1, &sh.abort_flag, d.status)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint64_t v = vd + static_cast<uint32_t>(((2 * tile_of(t, s) + 1) % kSlots) * (KV_BYTES >> 4));
+          if (issuer) {
+#pragma unroll
+            for (int kk = 0; kk < kN / 16; ++kk)
+              mma_bf16_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, v + kk * (2 * GROUP_BYTES >> 4), idesc_o,
+                          (s > 0 || kk > 0) ? 1u : 0u);
+          }
+          if (s + 1 < steps[t]) issue_s(t, (2 * tile_of(t, s + 1)) % kSlots);
+        }
+      }
+      if (ok) {
+        if (issuer) mma_commit(&sh.o_full);
+      } else if (issued && issuer) {
+        mma_commit(&sh.drain);
+        volatile int never = 0;
+        mbar_wait(&sh.drain, 0, &never, nullptr);
+      }
+    }
+  } else {
+    regs_inc_softmax();
+    // ---------------------------------------------------------------- q, softmax, epilogue
+    const int t = (warp - 4) >> 2, tid = threadIdx.x - 128;
+    const int quarter = warp & 3;
+    const int r = quarter * 32 + lane;  // row of the query tile (= TMEM lane)
+    {
+      // q: 16-byte units of a row side by side in a warp; rows behind the request's last are zeros
+      constexpr int kUnits = D / 8, kStep = 256 / kUnits;
+      const int u = tid % kUnits;
+#pragma unroll 4
+      for (int i = tid / kUnits; i < kTiles * kM; i += kStep) {
+        const int R = w.q0 + i;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (R <= last_row) {
+          const int row = R / grp, h = w.g * grp + (R - row * grp);
+          v = *reinterpret_cast<const uint4*>(d.q + (row0 + row) * d.q_row + h * d.q_head + u * 8);
+        }
+        const int rr = i & (kM - 1);
+        *reinterpret_cast<uint4*>(sQ + (i / kM) * Q_BYTES + (u >> 3) * T::HALF_ROWS_BYTES + rr * 128 +
+                                  (((u & 7) ^ (rr & 7)) << 4)) = v;
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.q_full);
+    }
+    const uint32_t lane_off = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t tO = tmem + lane_off + 256 + t * 128;
+    const float sl2 = kLog2e * d.scale;
+    const int R = w.q0 + (NARROW ? 0 : t * kM) + r;  // packed row
+    const int row = min(R, last_row) / grp, p = pos + row;
+    const KeyRange mine = keys_of_rows(p, p, n_keys, d.causal, d.window);
+    float m_run = -INFINITY, l_run = 0.f;  // maximum in raw score units
+    bool ok = true;
+    // tiles that some row of the CTA does not see in full
+    auto masked_for = [&](int q, int k0) { return k0 < flo[q] || k0 + kN > fhi[q]; };
+    auto partial = [&](int k0) { return masked_for(0, k0) || (!NARROW && steps[1] > 0 && masked_for(1, k0)); };
+    if (quarter < quarters(t)) {
+      const uint32_t tS = tmem + lane_off + t * 128;
+      const int threads = 32 * quarters(t);
+      for (int s = 0; s < steps[t] && ok; ++s) {
+        const int j = tile_of(t, s), k0 = (jb + j) * kN;
+        ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[t], s & 1, &sh.abort_flag, d.status));
+        if (!ok) break;
+        tc_fence_after();
+        // S of this step complete: so is P V of the step before; this chain is done with that V and this K
+        if (quarter == 0 && lane == 0) {
+          mbar_arrive(&sh.kv_empty[(2 * j) % kSlots]);
+          if (s > 0) mbar_arrive(&sh.kv_empty[(2 * tile_of(t, s - 1) + 1) % kSlots]);
+        }
+        if (masked_for(NARROW ? 0 : t, k0))
+          softmax_tile<D, true>(tS, tO, s == 0, mine.lo - k0, mine.hi - k0, sl2, m_run, l_run);
+        else
+          softmax_tile<D, false>(tS, tO, s == 0, 0, 0, sl2, m_run, l_run);
+        const int vi = 2 * j + 1;
+        if (partial(k0)) {
+          ok = __all_sync(0xffffffffu, mbar_wait(&sh.kv_full[vi % kSlots], (vi / kSlots) & 1, &sh.abort_flag, d.status));
+          if (!ok) break;
+          uint8_t* vt = sKV + (vi % kSlots) * KV_BYTES;
+          constexpr int kUnits = D / 8;
+          // [some0, some1): keys that some row sees, [all0, all1) all rows
+          const int some0 = max(0, all_lo - k0), some1 = min(kN, all_hi - k0);
+          const int all0 = max(flo[0], NARROW || steps[1] == 0 ? flo[0] : flo[1]) - k0;
+          const int all1 = min(fhi[0], NARROW || steps[1] == 0 ? fhi[0] : fhi[1]) - k0;
+          for (int i = quarter * 32 + lane; i < kN * kUnits; i += threads) {
+            const int key = i / kUnits, unit = i % kUnits;
+            if (key >= all0 && key < all1) continue;
+            uint4* at = slot_unit<D>(vt, key, unit);
+            if (key < some0 || key >= some1) {
+              *at = make_uint4(0, 0, 0, 0);
+              continue;
+            }
+            uint4 v = *at;
+            uint32_t* e = reinterpret_cast<uint32_t*>(&v);
+            bool any = false;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if (not_finite_bf16(e[q])) {
+                e[q] &= 0xFFFF0000u;
+                any = true;
+              }
+              if (not_finite_bf16(e[q] >> 16)) {
+                e[q] &= 0x0000FFFFu;
+                any = true;
+              }
+            }
+            if (any) {
+              *at = v;
+              sh.dirty = 1;
+            }
+          }
+          fence_proxy_async_smem();
+        }
+        if (quarter == 0) {
+          // the products that read this P also need V and the chain's next K: hand over once they have landed
+          ok = __all_sync(0xffffffffu, mbar_wait(&sh.kv_full[vi % kSlots], (vi / kSlots) & 1, &sh.abort_flag, d.status));
+          if (ok && s + 1 < steps[t]) {
+            const int ki = 2 * tile_of(t, s + 1);
+            ok = __all_sync(0xffffffffu, mbar_wait(&sh.kv_full[ki % kSlots], (ki / kSlots) & 1, &sh.abort_flag, d.status));
+          }
+          if (!ok) break;
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_full[t]);
+      }
+    }
+    if (ok && J > 0) ok = __all_sync(0xffffffffu, mbar_wait(&sh.o_full, 0, &sh.abort_flag, d.status));
+    tc_fence_after();
+    float* xo = reinterpret_cast<float*>(sKV);  // narrow: chain 1's [D][128] of o, then 128 maxima and sums
+    const bool second = NARROW && steps[1] > 0;
+    if (second) {
+      // the ring is free: every product is done
+      if (t == 1 && ok && quarter < quarters(1)) {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld32(tO + c * 32, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) xo[(c * 32 + i) * kM + r] = __uint_as_float(o[i]);
+        }
+        xo[D * kM + r] = m_run;
+        xo[(D + 1) * kM + r] = l_run;
+      }
+      softmax_groups_sync();
+    }
+    if (ok && quarter < quarters(t) && !(NARROW && t == 1)) {
+      float own = 1.f, other = 0.f;
+      if (second) {
+        const float m1 = xo[D * kM + r], l1 = xo[(D + 1) * kM + r], m = fmaxf(m_run, m1);
+        own = m_run == -INFINITY ? 0.f : ex2_approx((m_run - m) * sl2);
+        other = m1 == -INFINITY ? 0.f : ex2_approx((m1 - m) * sl2);
+        l_run = l_run * own + l1 * other;
+        m_run = m;
+      }
+      const bool dirty = sh.dirty != 0;
+      const float inv = split ? 1.f : l_run != 0.f ? 1.0f / l_run : 0.f;
+      const bool store = R <= last_row;
+      const int h = w.g * grp + (min(R, last_row) - row * grp);
+      __nv_bfloat16* dst = d.out + (row0 + row) * d.out_row + h * d.out_head;
+      const size_t pr = static_cast<size_t>(w.item) * a.part_rows + (R - w.q0);
+      float* part = a.part + pr * D;
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t o[32];
+        if (steps[t] > 0) {
+          tmem_ld32(tO + c * 32, o);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) o[i] = 0;
+        }
+        if (second) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            o[i] = __float_as_uint(__uint_as_float(o[i]) * own + xo[(c * 32 + i) * kM + r] * other);
+        }
+        if (dirty) {
+          // the zeroed elements of v, to the rows that see them
+          for (int j = 0; j < J; ++j) {
+            const int k0 = (jb + j) * kN;
+            if (!partial(k0)) continue;
+            for (int key = max(k0, mine.lo); key < min(k0 + kN, mine.hi); ++key) {
+              const int page = pt[key / kPage];
+              if (page < 0 || page >= a.c.num_pages) continue;
+              const __nv_bfloat16* src =
+                  d.vpages + ((static_cast<size_t>(page) * d.n_kv_heads + w.g) * kPage + key % kPage) * D + c * 32;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) {
+                const float e = __bfloat162float(src[i]);
+                if (!isfinite(e)) o[i] = __float_as_uint(__uint_as_float(o[i]) + e);
+              }
+            }
+          }
+        }
+        if (!store) continue;
+        if (split) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            reinterpret_cast<uint4*>(part + c * 32)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint4 v;
+            v.x = pack_bf16(__uint_as_float(o[8 * i + 0]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
+            v.y = pack_bf16(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
+            v.z = pack_bf16(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
+            v.w = pack_bf16(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
+            reinterpret_cast<uint4*>(dst + c * 32)[i] = v;
+          }
+        }
+      }
+      if (store) {
+        if (split) {
+          // a sum of 0 marks a piece that the row sees nothing of
+          reinterpret_cast<float2*>(a.part_ml)[pr] = make_float2(m_run * sl2, l_run);
+        } else if (d.lse) {
+          d.lse[static_cast<size_t>(row0 + row) * d.n_q_heads + h] =
+              l_run == 0.f ? -INFINITY : (m_run * sl2 + log2f(l_run)) * kLn2;
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_constant__ ChunkArgs a) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) Shared sh;
+  griddep_launch_dependents();
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const Item w = item_of(a, blockIdx.x);
+  if (w.narrow)
+    attn_body<D, true>(a, w, smem, sh);
+  else
+    attn_body<D, false>(a, w, smem, sh);
+}
+
+// Joins the pieces of split items: one block per (packed row, kv head) of a split request; groups of lanes take
+// every kGroups-th piece, 16 bytes of o a lane.
+constexpr int kMergeThreads = 128;
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads) chunk_attn_merge(const __grid_constant__ ChunkArgs a) {
+  constexpr int kLanes = D / 4, kGroups = kMergeThreads / kLanes;
+  __shared__ float4 red_o[kGroups][kLanes];
+  __shared__ float red_m[kGroups], red_l[kGroups];
+  const ChunkAttnDesc& d = a.d;
+  int lo = 0, hi = a.c.n - 1;
+  const int b = blockIdx.x;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.p.split_rows[mid] <= b) lo = mid; else hi = mid - 1;
+  }
+  const int grp = d.n_q_heads / d.n_kv_heads;
+  const int rows = (a.c.row0[lo + 1] - a.c.row0[lo]) * grp;
+  const int at = b - a.p.split_rows[lo], g = at / rows, R = at - g * rows;
+  const int tile = narrow_form(rows) ? kM : 2 * kM, tiles = (rows + tile - 1) / tile, pieces = a.p.pieces[lo];
+  const int item = a.p.item0[lo] + ((tiles - 1 - R / tile) * d.n_kv_heads + g) * pieces;
+  const int q = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+  griddep_wait();
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  constexpr int kBatch = 4;
+  for (int k0 = q; k0 < pieces; k0 += kBatch * kGroups) {
+    float2 ml[kBatch];
+    float4 v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int k = k0 + i * kGroups;
+      ml[i] = make_float2(-INFINITY, 0.f);
+      if (k < pieces) {
+        const size_t pr = static_cast<size_t>(item + k) * a.part_rows + R % tile;
+        ml[i] = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + pr);
+        v[i] = __ldcg(reinterpret_cast<const float4*>(a.part + pr * D) + c);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (ml[i].y == 0.f) continue;  // nothing seen (its o holds no number)
+      const float mn = fmaxf(m, ml[i].x), keep = m == -INFINITY ? 0.f : ex2_approx(m - mn), add = ex2_approx(ml[i].x - mn);
+      o.x = o.x * keep + v[i].x * add;
+      o.y = o.y * keep + v[i].y * add;
+      o.z = o.z * keep + v[i].z * add;
+      o.w = o.w * keep + v[i].w * add;
+      l = l * keep + ml[i].y * add;
+      m = mn;
+    }
+  }
+  red_o[q][c] = o;
+  if (c == 0) {
+    red_m[q] = m;
+    red_l[q] = l;
+  }
+  __syncthreads();
+  if (q != 0) return;
+  float M = red_m[0], L = 0.f;
+#pragma unroll
+  for (int i = 1; i < kGroups; ++i) M = fmaxf(M, red_m[i]);
+  o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) {
+    if (red_l[i] == 0.f) continue;
+    const float e = ex2_approx(red_m[i] - M);
+    const float4 v = red_o[i][c];
+    o.x += v.x * e;
+    o.y += v.y * e;
+    o.z += v.z * e;
+    o.w += v.w * e;
+    L += red_l[i] * e;
+  }
+  const float inv = L != 0.f ? 1.0f / L : 0.f;
+  const int row = a.c.row0[lo] + R / grp, h = g * grp + R % grp;
+  *reinterpret_cast<uint2*>(d.out + row * d.out_row + h * d.out_head + c * 4) =
+      make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+  if (d.lse && c == 0) d.lse[static_cast<size_t>(row) * d.n_q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+}
+
+// ---------------------------------------------------------------- plan (host)
+struct Shape {
+  int tiles, steps;  // query tiles (or pairs) of a kv head, steps of the longest
+};
+Shape shape_of(const ChunkTable& c, int i, int grp, bool causal, int window) {
+  const int rows = (c.row0[i + 1] - c.row0[i]) * grp;
+  Shape s{0, 0};
+  if (rows == 0) return s;
+  const bool narrow = narrow_form(rows);
+  const int tile = narrow ? kM : 2 * kM;
+  s.tiles = (rows + tile - 1) / tile;
+  // K/V tiles of the longest query tile: at most those that the whole request sees, and with a causal window
+  // those that so many keys in a row can touch
+  const KeyRange all = keys_of_rows(c.pos[i], c.pos[i] + (rows - 1) / grp, c.n_keys[i], causal, window);
+  int64_t t = all.hi > all.lo ? (all.hi + kN - 1) / kN - all.lo / kN : 0;
+  if (causal && window > 0) {
+    const int64_t positions = (std::min(tile, rows) + grp - 2) / grp + 1, keys = window + positions - 1;
+    t = std::min(t, (keys + kN - 2) / kN + 1);
+  }
+  s.steps = static_cast<int>(narrow ? (t + 1) / 2 : t);
+  return s;
+}
+
+struct Planned {
+  ChunkPlan p;
+  int items, split_blocks, part_rows;
+};
+
+// A piece of s steps takes about s + kOverhead steps of time (a start, an end and its share of the merge), and
+// pieces run one to an SM in waves. Of the piece lengths that just fill 1, 2, ... waves the cheapest is taken; no piece
+// is cut where the items are many.
+constexpr int kOverhead = 2;
+constexpr int kMostWaves = 6;
+
+Planned make_plan(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms) {
+  Planned r;
+  std::memset(&r, 0, sizeof(r));
+  const int grp = n_q_heads / n_kv_heads;
+  Shape sh[kMaxChunks];
+  int longest = 1;
+  for (int i = 0; i < c.n; ++i) {
+    sh[i] = shape_of(c, i, grp, causal, window);
+    longest = std::max(longest, sh[i].steps);
+  }
+  auto items = [&](int piece) {
+    int64_t n = 0;
+    for (int i = 0; i < c.n; ++i) n += static_cast<int64_t>(sh[i].tiles) * n_kv_heads * std::max(1, (sh[i].steps + piece - 1) / piece);
+    return n;
+  };
+  const int64_t whole = items(longest);
+  int best = longest;
+  int64_t best_cost = (whole + num_sms - 1) / num_sms * (longest + kOverhead);
+  for (int w = 1; w <= kMostWaves && whole < static_cast<int64_t>(w) * num_sms; ++w) {
+    int a = 1, b = longest;  // the shortest piece whose items fit w waves
+    while (a < b) {
+      const int mid = (a + b) / 2;
+      if (items(mid) <= static_cast<int64_t>(w) * num_sms) b = mid; else a = mid + 1;
+    }
+    const int64_t cost = static_cast<int64_t>(w) * (a + kOverhead) + 1;
+    if (a < longest && cost < best_cost) {
+      best = a;
+      best_cost = cost;
+    }
+  }
+  r.p.piece_steps = best;
+  int64_t n = 0, blocks = 0;
+  for (int i = 0; i < c.n; ++i) {
+    r.p.item0[i] = static_cast<int>(n);
+    r.p.split_rows[i] = static_cast<int>(blocks);
+    r.p.pieces[i] = std::max(1, (sh[i].steps + best - 1) / best);
+    n += static_cast<int64_t>(sh[i].tiles) * n_kv_heads * r.p.pieces[i];
+    const int rows = (c.row0[i + 1] - c.row0[i]) * grp;
+    if (r.p.pieces[i] > 1) {
+      blocks += static_cast<int64_t>(rows) * n_kv_heads;
+      r.part_rows = std::max(r.part_rows, narrow_form(rows) ? std::min(rows, kM) : 2 * kM);
+    }
+  }
+  for (int i = c.n; i <= kMaxChunks; ++i) {
+    r.p.item0[i] = static_cast<int>(n);
+    r.p.split_rows[i] = static_cast<int>(blocks);
+  }
+  r.items = n > 0x7fffffff ? -1 : static_cast<int>(n);
+  r.split_blocks = static_cast<int>(blocks);
+  return r;
+}
+
+template <int D>
+cudaError_t launch_tc(const ChunkArgs& a, const Planned& p, cudaStream_t stream) {
+  static PerDevice once;
+  int dev = 0;
+  if (once.pending(&dev)) {
+    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tile<D>::kSmem);
+    if (e != cudaSuccess) return e;
+    // setmaxnreg.inc waits until the CTA's register pool can serve it: refuse to launch a build whose launch
+    // count leaves the split short
+    cudaFuncAttributes fa;
+    e = cudaFuncGetAttributes(&fa, chunk_attn_kernel<D>);
+    if (e != cudaSuccess) return e;
+    if (fa.numRegs * kThreads < kRegsNeeded) return cudaErrorInvalidConfiguration;
+    once.done(dev);
+  }
+  cudaError_t e = launch_kernel(chunk_attn_kernel<D>, dim3(p.items), dim3(kThreads), Tile<D>::kSmem, stream, a);
+  if (e != cudaSuccess || p.split_blocks == 0) return e;
+  PdlScope pdl;
+  return launch_kernel(chunk_attn_merge<D>, dim3(p.split_blocks), dim3(kMergeThreads), 0, stream, a);
+}
+
+size_t part_floats(const Planned& p, int head_dim, bool ml) {
+  if (p.split_blocks == 0) return 0;
+  return (static_cast<size_t>(p.items) * p.part_rows * (ml ? 2 : head_dim) + 63) & ~static_cast<size_t>(63);
 }
 
 }  // namespace
 
-size_t chunk_attention_workspace(const ChunkTable&, int, int, int, bool, int, int) { return 0; }
-int chunk_attention_launches(const ChunkTable&, int, int, int, bool, int, int) { return 1; }
+size_t chunk_attention_workspace(const ChunkTable& c, int n_q_heads, int n_kv_heads, int head_dim, bool causal,
+                                 int window, int num_sms) {
+  const Planned p = make_plan(c, n_q_heads, n_kv_heads, causal, window, num_sms);
+  return (part_floats(p, head_dim, false) + part_floats(p, head_dim, true)) * sizeof(float);
+}
 
-cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, void*, int, cudaStream_t stream) {
+int chunk_attention_launches(const ChunkTable& c, int n_q_heads, int n_kv_heads, int head_dim, bool causal, int window,
+                             int num_sms) {
+  return make_plan(c, n_q_heads, n_kv_heads, causal, window, num_sms).split_blocks ? 2 : 1;
+}
+
+cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, void* workspace, int num_sms,
+                                   cudaStream_t stream) {
+  const Planned p = make_plan(c, d.n_q_heads, d.n_kv_heads, d.causal, d.window, num_sms);
+  if (p.items == 0) return cudaSuccess;
+  if (p.items < 0) return cudaErrorInvalidValue;
   ChunkArgs a;
+  std::memset(&a, 0, sizeof(a));
+  const long pool_rows = static_cast<long>(c.num_pages) * d.n_kv_heads * kPage;
+  if (!tensor_map_pool(&a.tmK, d.kpages, pool_rows, d.head_dim) || !tensor_map_pool(&a.tmV, d.vpages, pool_rows, d.head_dim))
+    return cudaErrorInvalidValue;
   a.d = d;
   a.c = c;
-  const int64_t warps = static_cast<int64_t>(c.row0[c.n]) * d.n_q_heads;
-  if (warps == 0) return cudaSuccess;
-  const dim3 grid(static_cast<unsigned>((warps + 7) / 8));
-  return d.head_dim == 128 ? launch_kernel(chunk_attn_simple<128>, grid, dim3(256), 0, stream, a)
-                           : launch_kernel(chunk_attn_simple<64>, grid, dim3(256), 0, stream, a);
+  a.p = p.p;
+  a.part = static_cast<float*>(workspace);
+  a.part_ml = a.part + part_floats(p, d.head_dim, false);
+  a.part_rows = p.part_rows;
+  return d.head_dim == 128 ? launch_tc<128>(a, p, stream) : launch_tc<64>(a, p, stream);
 }
 
 }  // namespace crf
