@@ -202,13 +202,20 @@ _TYPES = {torch.bfloat16: abi.BF16, torch.float16: abi.FP16, torch.float32: abi.
 
 def _heads(name: str, x: torch.Tensor, out: Optional[torch.Tensor], dim: int) -> abi.Heads:
     """crf_heads of x [rows, heads, dim] and out, of any row and head strides."""
-    if x.dim() != 3 or x.shape[2] != dim or (x.stride(2) != 1 and dim > 1):
-        raise ValueError(f"{name} must be [rows, heads, {dim}] with adjacent elements of a head")
+    shape = x.shape
+    if len(shape) != 3 or shape[2] != dim:
+        raise ValueError(f"{name} must be [rows, heads, {dim}]")
+    row, head, one = x.stride()
     if out is None:
-        return abi.Heads(x.data_ptr(), None, x.shape[1], x.stride(0), x.stride(1), 0, 0)
-    if out.shape != x.shape or out.dtype != x.dtype or (out.stride(2) != 1 and dim > 1):
-        raise ValueError(f"{name}: the output must have the input's shape and type and adjacent elements of a head")
-    return abi.Heads(x.data_ptr(), out.data_ptr(), x.shape[1], x.stride(0), x.stride(1), out.stride(0), out.stride(1))
+        if one != 1:
+            raise ValueError(f"{name}: the elements of a head must be adjacent")
+        return abi.Heads(x.data_ptr(), None, shape[1], row, head, 0, 0)
+    if out is not x and (out.shape != shape or out.dtype != x.dtype):
+        raise ValueError(f"{name}: the output must have the input's shape and type")
+    out_row, out_head, out_one = out.stride()
+    if one != 1 or out_one != 1:
+        raise ValueError(f"{name}: the elements of a head must be adjacent")
+    return abi.Heads(x.data_ptr(), out.data_ptr(), shape[1], row, head, out_row, out_head)
 
 
 def _req_array(reqs: Sequence[Request]):
@@ -316,12 +323,13 @@ class Context:
 
     # -------------------------------------------------------------- extension by new tokens
     def _stream_here(self, stream) -> int:
-        return _stream(torch.cuda.current_stream(self.device) if stream is None else stream)
+        # the raw handle: a torch.cuda.Stream object costs a small call as much as its launch
+        return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else _stream(stream)
 
-    def _here(self, **tensors) -> None:
-        for name, t in tensors.items():
-            if t is not None and (t.device.type != "cuda" or t.device.index != self.device):
-                raise ValueError(f"{name} must be on cuda:{self.device}")
+    def _here(self, *tensors: Optional[torch.Tensor]) -> None:
+        for t in tensors:
+            if t is not None and t.get_device() != self.device:
+                raise ValueError(f"every tensor of the call must be on cuda:{self.device}")
 
     def rotary(self, rope: Rope, positions: torch.Tensor, x: torch.Tensor, out: Optional[torch.Tensor] = None,
                k: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False,
@@ -329,7 +337,7 @@ class Context:
         """x [rows, heads, head_dim] (bf16, fp16 or fp32, any row and head strides) rotated at
         ``positions`` [rows] into ``out`` (default: in place), and ``k`` likewise into ``k_out``.
         ``inverse``: the transposed map, the gradient of the call without it."""
-        self._here(positions=positions, x=x, out=out, k=k, k_out=k_out)
+        self._here(positions, x, out, k, k_out)
         n = x.shape[0]
         if x.dtype not in _TYPES:
             raise ValueError("x must be bfloat16, float16 or float32")
@@ -355,7 +363,7 @@ class Context:
         """Rows k, v [rows, kv heads, head_dim] into the requests' pages of ``layer``, k rotated at its
         position when ``rope`` is given; and ``q`` rotated into ``q_out`` (default: in place)."""
         hkv, dim = self._pool_layer(pool, layer)
-        self._here(k=k, v=v, q=q, q_out=q_out)
+        self._here(k, v, q, q_out)
         if not chunks.append_ok:
             raise ValueError(f"page tables need {chunks.append_entries} entries to append")
         for name, t in (("k", k), ("v", v), ("q", q)):
@@ -381,7 +389,7 @@ class Context:
         """out = attention of the rows q [rows, heads, head_dim] (bf16) over their requests' cached keys of
         ``layer`` (see crf_chunk_attention); ``lse`` fp32 [rows, heads]; ``scale`` 0: 1 / sqrt(head_dim)."""
         hkv, dim = self._pool_layer(pool, layer)
-        self._here(q=q, out=out, workspace=workspace, lse=lse)
+        self._here(q, out, workspace, lse)
         if not chunks.attend_ok:
             raise ValueError(f"page tables need {chunks.attend_entries} entries to attend")
         if q.dtype != torch.bfloat16 or q.shape[0] != chunks.rows:
@@ -400,7 +408,7 @@ class Context:
         return torch.empty(max(256, n.value), dtype=torch.uint8, device=f"cuda:{self.device}")
 
     def _refs(self, num_pages: int, refs: torch.Tensor, refs_out: Optional[torch.Tensor]) -> Tuple[int, int]:
-        self._here(refs=refs, refs_out=refs_out)
+        self._here(refs, refs_out)
         out = refs if refs_out is None else refs_out
         for name, t in (("refs", refs), ("refs_out", out)):
             if t.numel() != num_pages:
@@ -424,7 +432,7 @@ class Context:
         hkv, dim = self._pool_layer(pool, 0)
         if tables.outs is None:
             raise ValueError("the tables need outs")
-        self._here(workspace=workspace)
+        self._here(workspace)
         a, b = self._refs(pool.num_pages, refs, refs_out)
         abi.check(call(self.h, byref(pool.c), len(pool.k_pages), hkv, dim, a, b, tables.c, tables.n, *flags,
                        workspace.data_ptr(), workspace.numel(), self._stream_here(stream)))
@@ -432,7 +440,7 @@ class Context:
     def pages_release(self, refs: torch.Tensor, tables: PageTables, workspace: torch.Tensor,
                       refs_out: Optional[torch.Tensor] = None, stream=None) -> None:
         """Every table entry gives its reference back."""
-        self._here(workspace=workspace)
+        self._here(workspace)
         a, b = self._refs(refs.numel(), refs, refs_out)
         abi.check(self.lib.crf_pages_release(self.h, refs.numel(), a, b, tables.c, tables.n, workspace.data_ptr(),
                                              workspace.numel(), self._stream_here(stream)))

@@ -38,9 +38,10 @@ constexpr int kPagesPerTile = kN / kPage;
 constexpr int kThreads = 384;
 // setmaxnreg split: the first warpgroup (producer, issuer) keeps kRegsCtl, the softmax warpgroups take
 // kRegsSoftmax; the sum must fit what the CTA launched with.
-constexpr int kRegsCtl = 56;
+constexpr int kRegsCtl = 80;
 constexpr int kRegsSoftmax = 208;
 constexpr int kRegsNeeded = 128 * kRegsCtl + 256 * kRegsSoftmax;
+constexpr uint32_t kTmemCols = 512;  // S0 | S1 | O0 | O1, 128 each
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
@@ -50,7 +51,7 @@ struct ChunkPlan {
   int item0[kMaxChunks + 1];
   int pieces[kMaxChunks];  // of each (query tile, head); 1: written straight to out
   int piece_steps;
-  int split_rows[kMaxChunks + 1];  // packed rows x heads of split requests, prefix: the merge's blocks
+  int split_rows[kMaxChunks + 1];  // packed rows x kv heads of split requests, prefix: the merge's rows
 };
 
 struct ChunkArgs {
@@ -82,12 +83,33 @@ __device__ __forceinline__ void regs_inc_softmax() {
 }
 __device__ __forceinline__ void softmax_groups_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
 
+// Scores of keys outside [lo, hi) (relative to the tile) of the thread's row become -inf, 32 keys at a time; 32 keys
+// that every row of the warp sees are left alone. A pass of its own over TMEM, on the few tiles that need it, keeps the
+// softmax one short piece of code (with the mask in a second instance of it, a masked tile took 3300 cycles, and
+// 6600 where its instructions were not cached, against 1250 unmasked).
+__device__ __forceinline__ void mask_tile(uint32_t tS, int lo, int hi) {
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    if (!__any_sync(0xffffffffu, c * 32 < lo || c * 32 + 32 > hi)) continue;
+    const int h = min(32, max(0, hi - c * 32)), l = min(32, max(0, lo - c * 32));
+    const uint32_t below_h = h == 32 ? 0xffffffffu : (1u << h) - 1, below_l = l == 32 ? 0xffffffffu : (1u << l) - 1;
+    const uint32_t seen = below_h & ~below_l;
+    uint32_t x[32];
+    tmem_ld32(tS + c * 32, x);
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (!(seen & (1u << i))) x[i] = __float_as_uint(-INFINITY);
+    tmem_st32(tS + c * 32, x);
+  }
+  tmem_st_wait();
+}
+
 // One packed row's share of a K/V tile: 128 raw scores from TMEM, running maximum and sum, o rescaled in TMEM when
-// the maximum grows by more than 2^8, P (bf16, unnormalised) back over the scores. MASK: keys outside [lo, hi)
-// (relative to the tile) count as -inf. A row that has seen no key yet keeps a maximum of -inf.
-template <int D, bool MASK>
-__device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool first, int lo, int hi, float sl2,
-                                             float& m_run, float& l_run) {
+// the maximum grows by more than 2^8, P (bf16, unnormalised) back over the scores. A row that has seen no key yet
+// keeps a maximum of -inf.
+template <int D>
+__device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool first, float sl2, float& m_run, float& l_run) {
   uint32_t sr[4][32];
 #pragma unroll
   for (int c = 0; c < 4; ++c) tmem_ld32(tS + c * 32, sr[c]);
@@ -98,14 +120,8 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool firs
 #pragma unroll
   for (int c = 0; c < 4; ++c)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (MASK) {
-        const int k = c * 32 + 2 * i;
-        if (k < lo || k >= hi) sr[c][2 * i] = __float_as_uint(-INFINITY);
-        if (k + 1 < lo || k + 1 >= hi) sr[c][2 * i + 1] = __float_as_uint(-INFINITY);
-      }
+    for (int i = 0; i < 16; ++i)
       mx[i & 7] = fmax3(mx[i & 7], __uint_as_float(sr[c][2 * i]), __uint_as_float(sr[c][2 * i + 1]));
-    }
   const float mt = fmax3(fmax3(mx[0], mx[1], mx[2]), fmax3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7]));
   const bool grow = (mt - m_run) * sl2 > kRescaleThreshold;  // false while both are -inf
   const float alpha = grow ? ex2_approx((m_run - mt) * sl2) : 1.0f;
@@ -170,115 +186,130 @@ __device__ __forceinline__ uint4* slot_unit(uint8_t* slot, int key, int unit) {
                                   (((unit & 7) ^ (key & 7)) << 4));
 }
 
+// Keys [a0, a1) and [b0, b1) of a V tile, dealt to `threads`: those outside [lo, hi), which no row sees, become
+// zeros, and so do infinite and NaN elements of the others (*dirty is set).
+template <int D>
+__device__ __forceinline__ void clean_v(uint8_t* slot, int a0, int a1, int b0, int b1, int lo, int hi, int thread,
+                                        int threads, volatile int* dirty) {
+  constexpr int kUnits = D / 8;
+  const int unit = thread % kUnits, step = threads / kUnits, n = a1 - a0 + b1 - b0;
+#pragma unroll 1
+  for (int i = thread / kUnits; i < n; i += step) {
+    const int key = i < a1 - a0 ? a0 + i : b0 + i - (a1 - a0);
+    uint4* at = slot_unit<D>(slot, key, unit);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    bool write = key < lo || key >= hi;
+    if (!write) {
+      v = *at;
+      uint32_t* e = reinterpret_cast<uint32_t*>(&v);
+      uint32_t any = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t bad = (not_finite_bf16(e[q]) ? 0x0000FFFFu : 0u) | (not_finite_bf16(e[q] >> 16) ? 0xFFFF0000u : 0u);
+        e[q] &= ~bad;
+        any |= bad;
+      }
+      write = any != 0;
+      if (write) *dirty = 1;
+    }
+    if (write) *at = v;
+  }
+}
+
+// An item and the part of its keys that the CTA reads, found by one thread.
+struct Item {
+  int g, q0, rows;      // kv head; the item's first packed row; packed rows of the request
+  int pos, n_keys, row0;
+  const int32_t* pt;
+  bool narrow, split;
+  int all_lo, all_hi;   // keys that some row sees
+  KeyRange full0, full1;  // keys that all rows of a chain see
+  int jb, J;            // K/V tiles of the piece; every one holds a key that some row sees
+  int n0, n1;           // steps of the chains
+  int quarters0, quarters1;  // warps of a chain with rows
+};
+
 struct Shared {
   uint64_t q_full, o_full, drain;
   uint64_t kv_full[6], kv_empty[6];
   uint64_t s_full[2], p_full[2];
+  Item w;
   uint32_t tmem_base;
   volatile int abort_flag;
   volatile int dirty;  // an infinite or NaN element of v was zeroed
 };
 
-struct Item {
-  int req, g, q0, rows, piece;  // rows: packed rows of the request; q0: the item's first
-  int item;
-  bool narrow;
-};
-
-__device__ __forceinline__ Item item_of(const ChunkArgs& a, int idx) {
-  int lo = 0, hi = a.c.n - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.p.item0[mid] <= idx) lo = mid; else hi = mid - 1;
+__device__ __forceinline__ void find_item(const ChunkArgs& a, int idx, Item& w) {
+  int i = 0, top = a.c.n - 1;
+  while (i < top) {
+    const int mid = (i + top + 1) >> 1;
+    if (a.p.item0[mid] <= idx) i = mid; else top = mid - 1;
   }
-  Item w;
-  w.req = lo;
-  w.item = idx;
-  w.rows = (a.c.row0[lo + 1] - a.c.row0[lo]) * (a.d.n_q_heads / a.d.n_kv_heads);
-  w.narrow = narrow_form(w.rows);
-  const int tile = w.narrow ? kM : 2 * kM, tiles = (w.rows + tile - 1) / tile;
-  idx -= a.p.item0[lo];
-  const int per_tile = a.d.n_kv_heads * a.p.pieces[lo], qt = idx / per_tile;
-  idx -= qt * per_tile;
-  w.g = idx / a.p.pieces[lo];
-  w.piece = idx - w.g * a.p.pieces[lo];
-  w.q0 = (tiles - 1 - qt) * tile;
-  return w;
+  const int grp = a.d.n_q_heads / a.d.n_kv_heads, pieces = a.p.pieces[i];
+  const int rows = (a.c.row0[i + 1] - a.c.row0[i]) * grp;
+  const bool narrow = narrow_form(rows);
+  const int tile = narrow ? kM : 2 * kM, tiles = (rows + tile - 1) / tile;
+  idx -= a.p.item0[i];
+  const int qt = idx / (a.d.n_kv_heads * pieces);
+  idx -= qt * a.d.n_kv_heads * pieces;
+  const int g = idx / pieces, piece = idx - g * pieces;
+  const int q0 = (tiles - 1 - qt) * tile;
+  w.g = g;
+  w.q0 = q0;
+  w.rows = rows;
+  w.pos = a.c.pos[i];
+  w.n_keys = a.c.n_keys[i];
+  w.row0 = a.c.row0[i];
+  w.pt = a.c.pt[i];
+  w.narrow = narrow;
+  w.split = pieces > 1;
+  // keys of the chains' query tiles
+  KeyRange some[2], full[2];
+  int valid[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int r0 = q0 + (narrow ? 0 : t * kM), r1 = min(r0 + kM, rows) - 1;
+    valid[t] = max(0, r1 - r0 + 1);
+    const int p0 = w.pos + r0 / grp, p1 = w.pos + r1 / grp;
+    some[t] = keys_of_rows(p0, p1, w.n_keys, a.d.causal, a.d.window);
+    full[t] = keys_of_rows(p1, p0, w.n_keys, a.d.causal, a.d.window);
+    if (valid[t] == 0) some[t].hi = 0;
+  }
+  w.all_lo = some[0].lo;
+  w.all_hi = max(some[0].hi, some[1].hi);
+  w.full0 = full[0];
+  w.full1 = full[1];
+  const int jfirst = w.all_lo / kN, jend = w.all_hi > w.all_lo ? (w.all_hi + kN - 1) / kN : jfirst;
+  const int per_piece = a.p.piece_steps * (narrow ? 2 : 1);
+  w.jb = static_cast<int>(min(static_cast<int64_t>(jend), jfirst + static_cast<int64_t>(piece) * per_piece));
+  w.J = min(jend - w.jb, per_piece);
+  w.n0 = narrow ? (w.J + 1) / 2 : min(w.J, max(0, (some[0].hi + kN - 1) / kN - w.jb));
+  w.n1 = narrow ? w.J / 2 : min(w.J, max(0, (some[1].hi + kN - 1) / kN - w.jb));
+  w.quarters0 = (valid[0] + 31) / 32;
+  w.quarters1 = (valid[1] + 31) / 32;
 }
 
 template <int D, bool NARROW>
-__device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uint8_t* smem, Shared& sh) {
+__device__ __forceinline__ void attn_body(const ChunkArgs& a, uint8_t* smem, Shared& sh) {
   using T = Tile<D>;
   constexpr int Q_BYTES = T::Q_BYTES, KV_BYTES = T::KV_BYTES, GROUP_BYTES = T::GROUP_BYTES;
   constexpr int kSlots = NARROW ? 6 : 5;
   constexpr int kTiles = NARROW ? 1 : 2;  // query tiles of the item
-  constexpr uint32_t TMEM_COLS = 512;
   const ChunkAttnDesc& d = a.d;
+  const Item& w = sh.w;
   uint8_t* sQ = smem;
   uint8_t* sKV = sQ + kTiles * Q_BYTES;
-  const int grp = d.n_q_heads / d.n_kv_heads;
-  const int pos = a.c.pos[w.req], n_keys = a.c.n_keys[w.req], row0 = a.c.row0[w.req];
-  const int32_t* pt = a.c.pt[w.req];
-  const int last_row = w.rows - 1;
-  const bool split = a.p.pieces[w.req] > 1;
-
-  // Keys of each chain's query tile: [lo, hi) that some row sees, [flo, fhi) that all rows see
-  int lo[2], hi[2], flo[2], fhi[2], valid[2];
-#pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int r0 = w.q0 + (NARROW ? 0 : t * kM), r1 = min(r0 + kM - 1, last_row);
-    valid[t] = max(0, r1 - r0 + 1);
-    const int p0 = pos + r0 / grp, p1 = pos + max(r1, 0) / grp;
-    const KeyRange some = keys_of_rows(p0, p1, n_keys, d.causal, d.window);
-    const KeyRange all = keys_of_rows(p1, p0, n_keys, d.causal, d.window);
-    lo[t] = some.lo;
-    hi[t] = valid[t] ? some.hi : 0;
-    flo[t] = all.lo;
-    fhi[t] = all.hi;
-  }
-  // K/V tiles of the item, and of its piece: [jb, jb + J); chain t runs steps[t] of them
-  const int all_lo = lo[0], all_hi = max(hi[0], hi[1]);
-  const int jfirst = all_lo / kN, jend = max(jfirst, (all_hi + kN - 1) / kN);
-  const int per_piece = a.p.piece_steps * (NARROW ? 2 : 1);
-  const int jb = min(static_cast<int>(min(static_cast<int64_t>(jend), jfirst + static_cast<int64_t>(w.piece) * per_piece)), jend);
-  const int J = static_cast<int>(min(static_cast<int64_t>(jend - jb), static_cast<int64_t>(per_piece)));
-  int steps[2];
-  if (NARROW) {
-    steps[0] = (J + 1) / 2;
-    steps[1] = J / 2;
-  } else {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) steps[t] = min(J, max(0, (hi[t] + kN - 1) / kN - jb));
-  }
-  const int readers = NARROW ? 1 : (steps[0] > 0) + (steps[1] > 0);  // chains that release a ring slot
-  auto quarters = [&](int t) { return (valid[t] + 31) / 32; };       // warps of a chain with rows
+  const int J = w.J, jb = w.jb, n0 = w.n0, n1 = w.n1;
   auto tile_of = [&](int t, int s) { return NARROW ? 2 * s + t : s; };
-
+  // The ring's sequence: K0 V0 K1 V1 ... (wide), K0 K1 V0 V1 K2 K3 ... (narrow: both chains start early; a last
+  // odd tile alone)
+  auto item_k = [&](int j) { return NARROW ? 4 * (j >> 1) + (j & 1) : 2 * j; };
+  auto item_v = [&](int j) { return NARROW ? 4 * (j >> 1) + (j + 1 == J && (j & 1) == 0 ? 1 : 2 + (j & 1)) : 2 * j + 1; };
+  // pages [first, last) of tile j that some row sees
+  auto first_page = [&](int j) { return max(0, w.all_lo / kPage - (jb + j) * kPagesPerTile); };
+  auto last_page = [&](int j) { return min(kPagesPerTile, (w.all_hi + kPage - 1) / kPage - (jb + j) * kPagesPerTile); };
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);  // uniform
   const int lane = threadIdx.x & 31;
-  if (threadIdx.x == 0) {
-    mbar_init(&sh.q_full, 8);
-    mbar_init(&sh.o_full, 1);
-    mbar_init(&sh.drain, 1);
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(&sh.s_full[t], 1);
-      mbar_init(&sh.p_full[t], max(1, quarters(t)));
-    }
-    for (int i = 0; i < kSlots; ++i) {
-      mbar_init(&sh.kv_full[i], 1);
-      mbar_init(&sh.kv_empty[i], max(1, readers));
-    }
-    sh.abort_flag = 0;
-    sh.dirty = 0;
-    fence_barrier_init();
-  }
-  if (warp == 1) {
-    tmem_alloc(&sh.tmem_base, TMEM_COLS);
-    tmem_relinquish();
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
 
   if (warp < 4) {
@@ -289,12 +320,12 @@ __device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uin
       bool ok = true;
       int armed = 0, slot = 0;
       uint32_t ph = 0;
-      const int n_pages = (all_hi + kPage - 1) / kPage;
+      const int32_t* pt = w.pt;
       auto page_id = [&](int j) {
-        const int i = (jb + j) * kPagesPerTile + (lane & (kPagesPerTile - 1));
+        const int p = lane & (kPagesPerTile - 1);
         int id = 0;
-        if (i < n_pages && i >= all_lo / kPage) {
-          id = pt[i];
+        if (p >= first_page(j) && p < last_page(j)) {
+          id = pt[(jb + j) * kPagesPerTile + p];
           if (id < 0 || id >= a.c.num_pages) {
             if (d.status) atomicOr(d.status, kStatusBounds);
             id = 0;
@@ -302,21 +333,26 @@ __device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uin
         }
         return id;
       };
-      int ids = J > 0 ? page_id(0) : 0;
-      for (int j = 0; j < J && ok; ++j) {
-        const int next_ids = j + 1 < J ? page_id(j + 1) : 0;
-        // pages of the tile that some row sees
-        const int pg0 = max(0, all_lo / kPage - (jb + j) * kPagesPerTile);
-        const int pg1 = max(pg0, min(kPagesPerTile, n_pages - (jb + j) * kPagesPerTile));
-        for (int kv = 0; kv < 2; ++kv) {
+      constexpr int kGroup = NARROW ? 2 : 1;  // tiles whose K come before their V
+      int ids[kGroup], next_ids[kGroup];
+#pragma unroll
+      for (int i = 0; i < kGroup; ++i) ids[i] = i < J ? page_id(i) : 0;
+      for (int j0 = 0; j0 < J && ok; j0 += kGroup) {
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) next_ids[i] = j0 + kGroup + i < J ? page_id(j0 + kGroup + i) : 0;
+#pragma unroll
+        for (int x = 0; x < 2 * kGroup; ++x) {
+          const int i = x % kGroup, j = j0 + i, kv = x / kGroup;
+          if (!ok || j >= J) continue;
           ok = mbar_wait_warp(&sh.kv_empty[slot], ph ^ 1, &sh.abort_flag, d.status);
-          if (!ok) break;
+          if (!ok) continue;
+          const int pg0 = first_page(j), pg1 = last_page(j);
           if (issuer) mbar_arrive_expect_tx(&sh.kv_full[slot], (pg1 - pg0) * (kPage / 8) * GROUP_BYTES);
           uint8_t* dst = sKV + slot * KV_BYTES;
           const CUtensorMap* map = kv == 0 ? &a.tmK : &a.tmV;
 #pragma unroll
           for (int p = 0; p < kPagesPerTile; ++p) {
-            const int group = (__shfl_sync(0xffffffffu, ids, p) * d.n_kv_heads + w.g) * (kPage / 8);
+            const int group = (__shfl_sync(0xffffffffu, ids[i], p) * d.n_kv_heads + w.g) * (kPage / 8);
             if (issuer && p >= pg0 && p < pg1)
               tma_load_4d(dst + p * (kPage / 8) * GROUP_BYTES, map, &sh.kv_full[slot], 0, 0, 0, group);
           }
@@ -326,7 +362,8 @@ __device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uin
             ph ^= 1;
           }
         }
-        ids = next_ids;
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) ids[i] = next_ids[i];
       }
       if (!ok) {
         // every copy issued lands before the CTA can exit: the last use of every slot
@@ -359,34 +396,36 @@ __device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uin
           mma_commit(&sh.s_full[t]);
         }
       };
-      for (int t = 0; t < 2 && ok; ++t) {
-        if (steps[t] == 0) continue;
-        const int item = 2 * tile_of(t, 0);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (!ok || (t ? n1 : n0) == 0) continue;
+        const int item = item_k(tile_of(t, 0));
         ok = mbar_wait_warp(&sh.kv_full[item % kSlots], (item / kSlots) & 1, &sh.abort_flag, d.status);
-        if (!ok) break;
+        if (!ok) continue;
         tc_fence_after();
         issue_s(t, item % kSlots);
         issued = true;
       }
-      const int most = max(steps[0], steps[1]);
+      const int most = max(n0, n1);
       for (int s = 0; s < most && ok; ++s) {
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if (s >= steps[t]) continue;
+          if (!ok || s >= (t ? n1 : n0)) continue;
           // P of this step is in TMEM, and its V and the chain's next K have landed
-          if (!mbar_wait_warp(&sh.p_full[t], s & 1, &sh.abort_flag, d.status)) {
-            ok = false;
-            break;
-          }
+          ok = mbar_wait_warp(&sh.p_full[t], s & 1, &sh.abort_flag, d.status);
+          if (!ok) continue;
           tc_fence_after();
-          const uint64_t v = vd + static_cast<uint32_t>(((2 * tile_of(t, s) + 1) % kSlots) * (KV_BYTES >> 4));
+          const int j = tile_of(t, s), pg0 = first_page(j), pg1 = last_page(j);
+          const uint64_t v = vd + static_cast<uint32_t>((item_v(j) % kSlots) * (KV_BYTES >> 4));
           if (issuer) {
+            // 16 keys, one page, an MMA: pages that no row sees are left out
 #pragma unroll
             for (int kk = 0; kk < kN / 16; ++kk)
-              mma_bf16_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, v + kk * (2 * GROUP_BYTES >> 4), idesc_o,
-                          (s > 0 || kk > 0) ? 1u : 0u);
+              if (kk >= pg0 && kk < pg1)
+                mma_bf16_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, v + kk * (2 * GROUP_BYTES >> 4), idesc_o,
+                            (s > 0 || kk > pg0) ? 1u : 0u);
           }
-          if (s + 1 < steps[t]) issue_s(t, (2 * tile_of(t, s + 1)) % kSlots);
+          if (s + 1 < (t ? n1 : n0)) issue_s(t, item_k(tile_of(t, s + 1)) % kSlots);
         }
       }
       if (ok) {
@@ -402,22 +441,33 @@ __device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uin
     // ---------------------------------------------------------------- q, softmax, epilogue
     const int t = (warp - 4) >> 2, tid = threadIdx.x - 128;
     const int quarter = warp & 3;
+    const int steps = t ? n1 : n0, quarters = t ? w.quarters1 : w.quarters0;
+    const int grp = d.n_q_heads / d.n_kv_heads, last_row = w.rows - 1, row0 = w.row0;
     const int r = quarter * 32 + lane;  // row of the query tile (= TMEM lane)
     {
       // q: 16-byte units of a row side by side in a warp; rows behind the request's last are zeros
-      constexpr int kUnits = D / 8, kStep = 256 / kUnits;
+      constexpr int kUnits = D / 8, kStep = 256 / kUnits, kTurns = kTiles * kM / kStep;
       const int u = tid % kUnits;
-#pragma unroll 4
-      for (int i = tid / kUnits; i < kTiles * kM; i += kStep) {
-        const int R = w.q0 + i;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (R <= last_row) {
-          const int row = R / grp, h = w.g * grp + (R - row * grp);
-          v = *reinterpret_cast<const uint4*>(d.q + (row0 + row) * d.q_row + h * d.q_head + u * 8);
+      int row = (w.q0 + tid / kUnits) / grp, h = w.q0 + tid / kUnits - row * grp;
+      const int row_step = kStep / grp, h_step = kStep - row_step * grp;
+      uint4 v[kTurns];
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        v[i] = make_uint4(0, 0, 0, 0);
+        if (w.q0 + tid / kUnits + i * kStep <= last_row)
+          v[i] = *reinterpret_cast<const uint4*>(d.q + (row0 + row) * d.q_row + (w.g * grp + h) * d.q_head + u * 8);
+        row += row_step;
+        h += h_step;
+        if (h >= grp) {
+          h -= grp;
+          ++row;
         }
-        const int rr = i & (kM - 1);
-        *reinterpret_cast<uint4*>(sQ + (i / kM) * Q_BYTES + (u >> 3) * T::HALF_ROWS_BYTES + rr * 128 +
-                                  (((u & 7) ^ (rr & 7)) << 4)) = v;
+      }
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int at = tid / kUnits + i * kStep, rr = at & (kM - 1);
+        *reinterpret_cast<uint4*>(sQ + (at / kM) * Q_BYTES + (u >> 3) * T::HALF_ROWS_BYTES + rr * 128 +
+                                  (((u & 7) ^ (rr & 7)) << 4)) = v[i];
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -427,74 +477,44 @@ __device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uin
     const uint32_t tO = tmem + lane_off + 256 + t * 128;
     const float sl2 = kLog2e * d.scale;
     const int R = w.q0 + (NARROW ? 0 : t * kM) + r;  // packed row
-    const int row = min(R, last_row) / grp, p = pos + row;
-    const KeyRange mine = keys_of_rows(p, p, n_keys, d.causal, d.window);
+    const int row = min(R, last_row) / grp, p = w.pos + row;
+    const KeyRange mine = keys_of_rows(p, p, w.n_keys, d.causal, d.window);
     float m_run = -INFINITY, l_run = 0.f;  // maximum in raw score units
     bool ok = true;
-    // tiles that some row of the CTA does not see in full
-    auto masked_for = [&](int q, int k0) { return k0 < flo[q] || k0 + kN > fhi[q]; };
-    auto partial = [&](int k0) { return masked_for(0, k0) || (!NARROW && steps[1] > 0 && masked_for(1, k0)); };
-    if (quarter < quarters(t)) {
+    const KeyRange full = t ? w.full1 : w.full0;  // keys that all rows of the chain see, and of the CTA
+    const bool both = !NARROW && n1 > 0 && n0 > 0;
+    const int cta_lo = both ? max(w.full0.lo, w.full1.lo) : full.lo;
+    const int cta_hi = both ? min(w.full0.hi, w.full1.hi) : full.hi;
+    if (quarter < quarters) {
       const uint32_t tS = tmem + lane_off + t * 128;
-      const int threads = 32 * quarters(t);
-      for (int s = 0; s < steps[t] && ok; ++s) {
+      for (int s = 0; s < steps && ok; ++s) {
         const int j = tile_of(t, s), k0 = (jb + j) * kN;
         ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[t], s & 1, &sh.abort_flag, d.status));
         if (!ok) break;
         tc_fence_after();
         // S of this step complete: so is P V of the step before; this chain is done with that V and this K
         if (quarter == 0 && lane == 0) {
-          mbar_arrive(&sh.kv_empty[(2 * j) % kSlots]);
-          if (s > 0) mbar_arrive(&sh.kv_empty[(2 * tile_of(t, s - 1) + 1) % kSlots]);
+          mbar_arrive(&sh.kv_empty[item_k(j) % kSlots]);
+          if (s > 0) mbar_arrive(&sh.kv_empty[item_v(tile_of(t, s - 1)) % kSlots]);
         }
-        if (masked_for(NARROW ? 0 : t, k0))
-          softmax_tile<D, true>(tS, tO, s == 0, mine.lo - k0, mine.hi - k0, sl2, m_run, l_run);
-        else
-          softmax_tile<D, false>(tS, tO, s == 0, 0, 0, sl2, m_run, l_run);
-        const int vi = 2 * j + 1;
-        if (partial(k0)) {
+        if (k0 < full.lo || k0 + kN > full.hi) mask_tile(tS, mine.lo - k0, mine.hi - k0);
+        softmax_tile<D>(tS, tO, s == 0, sl2, m_run, l_run);
+        const int vi = item_v(j);
+        if (k0 < cta_lo || k0 + kN > cta_hi) {
           ok = __all_sync(0xffffffffu, mbar_wait(&sh.kv_full[vi % kSlots], (vi / kSlots) & 1, &sh.abort_flag, d.status));
           if (!ok) break;
-          uint8_t* vt = sKV + (vi % kSlots) * KV_BYTES;
-          constexpr int kUnits = D / 8;
-          // [some0, some1): keys that some row sees, [all0, all1) all rows
-          const int some0 = max(0, all_lo - k0), some1 = min(kN, all_hi - k0);
-          const int all0 = max(flo[0], NARROW || steps[1] == 0 ? flo[0] : flo[1]) - k0;
-          const int all1 = min(fhi[0], NARROW || steps[1] == 0 ? fhi[0] : fhi[1]) - k0;
-          for (int i = quarter * 32 + lane; i < kN * kUnits; i += threads) {
-            const int key = i / kUnits, unit = i % kUnits;
-            if (key >= all0 && key < all1) continue;
-            uint4* at = slot_unit<D>(vt, key, unit);
-            if (key < some0 || key >= some1) {
-              *at = make_uint4(0, 0, 0, 0);
-              continue;
-            }
-            uint4 v = *at;
-            uint32_t* e = reinterpret_cast<uint32_t*>(&v);
-            bool any = false;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              if (not_finite_bf16(e[q])) {
-                e[q] &= 0xFFFF0000u;
-                any = true;
-              }
-              if (not_finite_bf16(e[q] >> 16)) {
-                e[q] &= 0x0000FFFFu;
-                any = true;
-              }
-            }
-            if (any) {
-              *at = v;
-              sh.dirty = 1;
-            }
-          }
+          // the fetched pages' keys before those that all rows see, and behind them
+          const int a0 = first_page(j) * kPage, a1 = min(last_page(j) * kPage, max(a0, cta_lo - k0));
+          const int b1 = last_page(j) * kPage, b0 = min(b1, max(a1, cta_hi - k0));
+          clean_v<D>(sKV + (vi % kSlots) * KV_BYTES, a0, a1, b0, b1, w.all_lo - k0, w.all_hi - k0, quarter * 32 + lane,
+                     32 * quarters, &sh.dirty);
           fence_proxy_async_smem();
         }
         if (quarter == 0) {
           // the products that read this P also need V and the chain's next K: hand over once they have landed
           ok = __all_sync(0xffffffffu, mbar_wait(&sh.kv_full[vi % kSlots], (vi / kSlots) & 1, &sh.abort_flag, d.status));
-          if (ok && s + 1 < steps[t]) {
-            const int ki = 2 * tile_of(t, s + 1);
+          if (ok && s + 1 < steps) {
+            const int ki = item_k(tile_of(t, s + 1));
             ok = __all_sync(0xffffffffu, mbar_wait(&sh.kv_full[ki % kSlots], (ki / kSlots) & 1, &sh.abort_flag, d.status));
           }
           if (!ok) break;
@@ -506,92 +526,141 @@ __device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uin
     }
     if (ok && J > 0) ok = __all_sync(0xffffffffu, mbar_wait(&sh.o_full, 0, &sh.abort_flag, d.status));
     tc_fence_after();
-    float* xo = reinterpret_cast<float*>(sKV);  // narrow: chain 1's [D][128] of o, then 128 maxima and sums
-    const bool second = NARROW && steps[1] > 0;
-    if (second) {
-      // the ring is free: every product is done
-      if (t == 1 && ok && quarter < quarters(1)) {
+    const bool rows_here = ok && quarter < quarters;
+    if (rows_here && sh.dirty != 0) {
+      // the zeroed elements of v, to the rows that see them
+#pragma unroll 1
+      for (int s = 0; s < (NARROW ? steps : J) && steps > 0; ++s) {
+        const int k0 = (jb + tile_of(t, s)) * kN;
+        if (k0 >= cta_lo && k0 + kN <= cta_hi) continue;
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
           tmem_ld32(tO + c * 32, o);
           tmem_ld_wait();
+#pragma unroll 1
+          for (int key = max(k0, mine.lo); key < min(k0 + kN, mine.hi); ++key) {
+            const int page = w.pt[key / kPage];
+            if (page < 0 || page >= a.c.num_pages) continue;
+            const __nv_bfloat16* src =
+                d.vpages + ((static_cast<size_t>(page) * d.n_kv_heads + w.g) * kPage + key % kPage) * D + c * 32;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) xo[(c * 32 + i) * kM + r] = __uint_as_float(o[i]);
+            for (int i = 0; i < 32; ++i) {
+              const float e = __bfloat162float(src[i]);
+              if (!isfinite(e)) o[i] = __float_as_uint(__uint_as_float(o[i]) + e);
+            }
+          }
+          __syncwarp();
+          tmem_st32(tO + c * 32, o);
+          tmem_st_wait();
         }
-        xo[D * kM + r] = m_run;
-        xo[(D + 1) * kM + r] = l_run;
+      }
+    }
+    // The ring is free: every product is done. Rows of o pass through it, 16-byte units swizzled by the row.
+    constexpr int kRowUnits = D / 4;  // of an fp32 row
+    float4* xo = reinterpret_cast<float4*>(sKV);                  // narrow: chain 1's rows
+    float2* xml = reinterpret_cast<float2*>(xo + kM * kRowUnits);  // and maxima and sums
+    const bool second = NARROW && n1 > 0;
+    auto unit_of = [&](int rr, int u, int units) { return rr * units + (u ^ (rr & (units - 1))); };
+    // Loops of 32 columns, not unrolled: this code runs once a CTA, mostly out of the instruction cache (as straight
+    // code for 128 columns it took an item of few rows 1500 cycles longer).
+    if (second) {
+      if (t == 1 && rows_here) {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld32(tO + c * 32, o);
+          tmem_ld_wait();
+          if (R <= last_row) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              xo[unit_of(r, c * 8 + i, kRowUnits)] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
+                                                                 __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
+          }
+          __syncwarp();
+        }
+        xml[r] = make_float2(m_run, l_run);
       }
       softmax_groups_sync();
     }
-    if (ok && quarter < quarters(t) && !(NARROW && t == 1)) {
+    if (rows_here && !(NARROW && t == 1)) {
+      const bool store = R <= last_row;
       float own = 1.f, other = 0.f;
-      if (second) {
-        const float m1 = xo[D * kM + r], l1 = xo[(D + 1) * kM + r], m = fmaxf(m_run, m1);
+      if (second && store) {
+        const float m1 = xml[r].x, l1 = xml[r].y, m = fmaxf(m_run, m1);
         own = m_run == -INFINITY ? 0.f : ex2_approx((m_run - m) * sl2);
         other = m1 == -INFINITY ? 0.f : ex2_approx((m1 - m) * sl2);
         l_run = l_run * own + l1 * other;
         m_run = m;
       }
-      const bool dirty = sh.dirty != 0;
-      const float inv = split ? 1.f : l_run != 0.f ? 1.0f / l_run : 0.f;
-      const bool store = R <= last_row;
-      const int h = w.g * grp + (min(R, last_row) - row * grp);
-      __nv_bfloat16* dst = d.out + (row0 + row) * d.out_row + h * d.out_head;
-      const size_t pr = static_cast<size_t>(w.item) * a.part_rows + (R - w.q0);
-      float* part = a.part + pr * D;
+      if (!w.split) {
+        const float inv = l_run != 0.f ? 1.0f / l_run : 0.f;
+        own *= inv;
+        other *= inv;
+      }
+      // behind chain 1's rows; wide: one 128-row block a chain
+      uint8_t* stage = sKV + (NARROW ? kM * kRowUnits * 16 + kM * 8 : t * kM * kRowUnits * 16);
+      uint4* rows = reinterpret_cast<uint4*>(stage);
+      constexpr int kOutUnits = D / 8;  // of a bf16 row
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         uint32_t o[32];
-        if (steps[t] > 0) {
+        if (steps > 0) {
           tmem_ld32(tO + c * 32, o);
           tmem_ld_wait();
         } else {
 #pragma unroll
           for (int i = 0; i < 32; ++i) o[i] = 0;
         }
-        if (second) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            o[i] = __float_as_uint(__uint_as_float(o[i]) * own + xo[(c * 32 + i) * kM + r] * other);
+        for (int i = 0; i < 8; ++i) {
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (second && store) x = xo[unit_of(r, c * 8 + i, kRowUnits)];
+          uint32_t* e = &o[4 * i];
+          e[0] = __float_as_uint(__uint_as_float(e[0]) * own + x.x * other);
+          e[1] = __float_as_uint(__uint_as_float(e[1]) * own + x.y * other);
+          e[2] = __float_as_uint(__uint_as_float(e[2]) * own + x.z * other);
+          e[3] = __float_as_uint(__uint_as_float(e[3]) * own + x.w * other);
         }
-        if (dirty) {
-          // the zeroed elements of v, to the rows that see them
-          for (int j = 0; j < J; ++j) {
-            const int k0 = (jb + j) * kN;
-            if (!partial(k0)) continue;
-            for (int key = max(k0, mine.lo); key < min(k0 + kN, mine.hi); ++key) {
-              const int page = pt[key / kPage];
-              if (page < 0 || page >= a.c.num_pages) continue;
-              const __nv_bfloat16* src =
-                  d.vpages + ((static_cast<size_t>(page) * d.n_kv_heads + w.g) * kPage + key % kPage) * D + c * 32;
-#pragma unroll
-              for (int i = 0; i < 32; ++i) {
-                const float e = __bfloat162float(src[i]);
-                if (!isfinite(e)) o[i] = __float_as_uint(__uint_as_float(o[i]) + e);
-              }
-            }
-          }
-        }
-        if (!store) continue;
-        if (split) {
+        if (w.split) {
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            reinterpret_cast<uint4*>(part + c * 32)[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            rows[unit_of(r, c * 8 + i, kRowUnits)] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            uint4 v;
-            v.x = pack_bf16(__uint_as_float(o[8 * i + 0]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
-            v.y = pack_bf16(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
-            v.z = pack_bf16(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
-            v.w = pack_bf16(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
-            reinterpret_cast<uint4*>(dst + c * 32)[i] = v;
+            const uint32_t* e = &o[8 * i];
+            rows[unit_of(r, c * 4 + i, kOutUnits)] =
+                make_uint4(pack_bf16(__uint_as_float(e[0]), __uint_as_float(e[1])), pack_bf16(__uint_as_float(e[2]), __uint_as_float(e[3])),
+                           pack_bf16(__uint_as_float(e[4]), __uint_as_float(e[5])), pack_bf16(__uint_as_float(e[6]), __uint_as_float(e[7])));
           }
+        }
+        __syncwarp();
+      }
+      const int h = w.g * grp + (min(R, last_row) - row * grp);
+      const size_t pr = static_cast<size_t>(blockIdx.x) * a.part_rows + (R - w.q0);
+      const int first = quarter * 32, count = min(32, last_row - (R - lane) + 1);  // the warp's rows
+      if (w.split) {
+        // fp32 rows as they lie here, one bulk copy a warp: 512-byte rows a lane in 16-byte pieces took 13000 cycles a
+        // 256-row item
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          bulk_store(a.part + pr * D, smem_u32(rows + first * kRowUnits), count * kRowUnits * 16);
+          bulk_commit();
+        }
+      } else {
+        // whole rows side by side
+        const int64_t mine_at = (row0 + row) * d.out_row + h * d.out_head;
+#pragma unroll 1
+        for (int i0 = 0; i0 < count; i0 += 32 / kOutUnits) {
+          const int i = i0 + lane / kOutUnits, u = lane % kOutUnits;
+          const int64_t at = __shfl_sync(0xffffffffu, mine_at, i);
+          if (i < count) *reinterpret_cast<uint4*>(d.out + at + u * 8) = rows[unit_of(first + i, u, kOutUnits)];
         }
       }
       if (store) {
-        if (split) {
+        if (w.split) {
           // a sum of 0 marks a piece that the row sees nothing of
           reinterpret_cast<float2*>(a.part_ml)[pr] = make_float2(m_run * sl2, l_run);
         } else if (d.lse) {
@@ -599,6 +668,7 @@ __device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uin
               l_run == 0.f ? -INFINITY : (m_run * sl2 + log2f(l_run)) * kLn2;
         }
       }
+      if (w.split && lane == 0) bulk_wait_all();
     }
   }
 
@@ -606,7 +676,7 @@ __device__ __forceinline__ void attn_body(const ChunkArgs& a, const Item& w, uin
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, TMEM_COLS);
+    tmem_dealloc(tmem, kTmemCols);
   }
 }
 
@@ -616,24 +686,54 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
   __shared__ __align__(8) Shared sh;
   griddep_launch_dependents();
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  const Item w = item_of(a, blockIdx.x);
-  if (w.narrow)
-    attn_body<D, true>(a, w, smem, sh);
+  if (threadIdx.x / 32 == 1) {
+    tmem_alloc(&sh.tmem_base, kTmemCols);
+    tmem_relinquish();
+  } else if (threadIdx.x == 64) {
+    Item w;
+    find_item(a, blockIdx.x, w);
+    sh.w = w;
+    mbar_init(&sh.q_full, 8);
+    mbar_init(&sh.o_full, 1);
+    mbar_init(&sh.drain, 1);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&sh.s_full[t], 1);
+      mbar_init(&sh.p_full[t], max(1, t ? w.quarters1 : w.quarters0));
+    }
+    // a ring slot is free once every chain that reads it has released it
+    const int readers = w.narrow ? 1 : max(1, (w.n0 > 0) + (w.n1 > 0));
+    for (int i = 0; i < 6; ++i) {
+      mbar_init(&sh.kv_full[i], 1);
+      mbar_init(&sh.kv_empty[i], readers);
+    }
+    sh.abort_flag = 0;
+    sh.dirty = 0;
+    fence_barrier_init();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  griddep_wait();  // q, the pages and their tables may come from the kernel before
+  if (sh.w.narrow)
+    attn_body<D, true>(a, smem, sh);
   else
-    attn_body<D, false>(a, w, smem, sh);
+    attn_body<D, false>(a, smem, sh);
 }
 
-// Joins the pieces of split items: one block per (packed row, kv head) of a split request; groups of lanes take
-// every kGroups-th piece, 16 bytes of o a lane.
-constexpr int kMergeThreads = 128;
-template <int D>
-__global__ void __launch_bounds__(kMergeThreads) chunk_attn_merge(const __grid_constant__ ChunkArgs a) {
-  constexpr int kLanes = D / 4, kGroups = kMergeThreads / kLanes;
-  __shared__ float4 red_o[kGroups][kLanes];
-  __shared__ float red_m[kGroups], red_l[kGroups];
+// Joins the pieces of split items, in order of keys. A row of o (of a packed row and kv head of a split request) is
+// joined by GROUPS groups of D / 4 lanes, which take every GROUPS-th piece, 16 bytes of o a lane: one group where
+// the rows fill the SMs, eight where they are few and their pieces many.
+constexpr int kMergeThreads = 256;
+template <int D, int GROUPS>
+__global__ void __launch_bounds__(kMergeThreads) chunk_attn_merge(const __grid_constant__ ChunkArgs a, int total) {
+  constexpr int kLanes = D / 4, kRows = kMergeThreads / (kLanes * GROUPS);
+  __shared__ float4 red_o[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? kRows * kLanes : 1];
+  __shared__ float2 red_ml[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? kRows : 1];
+  griddep_launch_dependents();
   const ChunkAttnDesc& d = a.d;
+  const int c = threadIdx.x % kLanes, q = threadIdx.x / kLanes % GROUPS, rr = threadIdx.x / (kLanes * GROUPS);
+  const int b = min(static_cast<int>(blockIdx.x) * kRows + rr, total - 1);  // a last block's spare rows repeat the last
   int lo = 0, hi = a.c.n - 1;
-  const int b = blockIdx.x;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (a.p.split_rows[mid] <= b) lo = mid; else hi = mid - 1;
@@ -643,22 +743,21 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_attn_merge(const __grid_c
   const int at = b - a.p.split_rows[lo], g = at / rows, R = at - g * rows;
   const int tile = narrow_form(rows) ? kM : 2 * kM, tiles = (rows + tile - 1) / tile, pieces = a.p.pieces[lo];
   const int item = a.p.item0[lo] + ((tiles - 1 - R / tile) * d.n_kv_heads + g) * pieces;
-  const int q = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
   griddep_wait();
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   constexpr int kBatch = 4;
-  for (int k0 = q; k0 < pieces; k0 += kBatch * kGroups) {
+  for (int k0 = q; k0 < pieces; k0 += kBatch * GROUPS) {
     float2 ml[kBatch];
     float4 v[kBatch];
 #pragma unroll
     for (int i = 0; i < kBatch; ++i) {
-      const int k = k0 + i * kGroups;
+      const int k = k0 + i * GROUPS;
       ml[i] = make_float2(-INFINITY, 0.f);
       if (k < pieces) {
         const size_t pr = static_cast<size_t>(item + k) * a.part_rows + R % tile;
         ml[i] = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + pr);
-        v[i] = __ldcg(reinterpret_cast<const float4*>(a.part + pr * D) + c);
+        v[i] = __ldcg(reinterpret_cast<const float4*>(a.part + pr * D) + (c ^ (R % tile & (kLanes - 1))));
       }
     }
 #pragma unroll
@@ -673,33 +772,35 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_attn_merge(const __grid_c
       m = mn;
     }
   }
-  red_o[q][c] = o;
-  if (c == 0) {
-    red_m[q] = m;
-    red_l[q] = l;
-  }
-  __syncthreads();
-  if (q != 0) return;
-  float M = red_m[0], L = 0.f;
+  if (GROUPS > 1) {
+    red_o[q][rr * kLanes + c] = o;
+    if (c == 0) red_ml[q][rr] = make_float2(m, l);
+    __syncthreads();
+    if (q != 0) return;
+    float M = -INFINITY, L = 0.f;
 #pragma unroll
-  for (int i = 1; i < kGroups; ++i) M = fmaxf(M, red_m[i]);
-  o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < GROUPS; ++i) M = fmaxf(M, red_ml[i][rr].x);
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-  for (int i = 0; i < kGroups; ++i) {
-    if (red_l[i] == 0.f) continue;
-    const float e = ex2_approx(red_m[i] - M);
-    const float4 v = red_o[i][c];
-    o.x += v.x * e;
-    o.y += v.y * e;
-    o.z += v.z * e;
-    o.w += v.w * e;
-    L += red_l[i] * e;
+    for (int i = 0; i < GROUPS; ++i) {
+      const float2 ml = red_ml[i][rr];
+      if (ml.y == 0.f) continue;
+      const float e = ex2_approx(ml.x - M);
+      const float4 v = red_o[i][rr * kLanes + c];
+      o.x += v.x * e;
+      o.y += v.y * e;
+      o.z += v.z * e;
+      o.w += v.w * e;
+      L += ml.y * e;
+    }
+    m = M;
+    l = L;
   }
-  const float inv = L != 0.f ? 1.0f / L : 0.f;
+  const float inv = l != 0.f ? 1.0f / l : 0.f;
   const int row = a.c.row0[lo] + R / grp, h = g * grp + R % grp;
   *reinterpret_cast<uint2*>(d.out + row * d.out_row + h * d.out_head + c * 4) =
       make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
-  if (d.lse && c == 0) d.lse[static_cast<size_t>(row) * d.n_q_heads + h] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
+  if (d.lse && c == 0) d.lse[static_cast<size_t>(row) * d.n_q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // ---------------------------------------------------------------- plan (host)
@@ -727,7 +828,7 @@ Shape shape_of(const ChunkTable& c, int i, int grp, bool causal, int window) {
 
 struct Planned {
   ChunkPlan p;
-  int items, split_blocks, part_rows;
+  int items, merge_rows, part_rows;
 };
 
 // A piece of s steps takes about s + kOverhead steps of time (a start, an end and its share of the merge), and
@@ -784,12 +885,12 @@ Planned make_plan(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causa
     r.p.split_rows[i] = static_cast<int>(blocks);
   }
   r.items = n > 0x7fffffff ? -1 : static_cast<int>(n);
-  r.split_blocks = static_cast<int>(blocks);
+  r.merge_rows = static_cast<int>(blocks);
   return r;
 }
 
 template <int D>
-cudaError_t launch_tc(const ChunkArgs& a, const Planned& p, cudaStream_t stream) {
+cudaError_t launch_tc(const ChunkArgs& a, const Planned& p, int num_sms, cudaStream_t stream) {
   static PerDevice once;
   int dev = 0;
   if (once.pending(&dev)) {
@@ -803,14 +904,21 @@ cudaError_t launch_tc(const ChunkArgs& a, const Planned& p, cudaStream_t stream)
     if (fa.numRegs * kThreads < kRegsNeeded) return cudaErrorInvalidConfiguration;
     once.done(dev);
   }
-  cudaError_t e = launch_kernel(chunk_attn_kernel<D>, dim3(p.items), dim3(kThreads), Tile<D>::kSmem, stream, a);
-  if (e != cudaSuccess || p.split_blocks == 0) return e;
   PdlScope pdl;
-  return launch_kernel(chunk_attn_merge<D>, dim3(p.split_blocks), dim3(kMergeThreads), 0, stream, a);
+  cudaError_t e = launch_kernel(chunk_attn_kernel<D>, dim3(p.items), dim3(kThreads), Tile<D>::kSmem, stream, a);
+  if (e != cudaSuccess || p.merge_rows == 0) return e;
+  constexpr int kRow = kMergeThreads / (D / 4);  // rows a block with one group each
+  if (p.merge_rows < 4 * kRow * num_sms) {
+    constexpr int kRows8 = kRow / 8 > 0 ? kRow / 8 : 1;
+    return launch_kernel(chunk_attn_merge<D, 8>, dim3((p.merge_rows + kRows8 - 1) / kRows8), dim3(kMergeThreads), 0, stream, a,
+                         p.merge_rows);
+  }
+  return launch_kernel(chunk_attn_merge<D, 1>, dim3((p.merge_rows + kRow - 1) / kRow), dim3(kMergeThreads), 0, stream, a,
+                       p.merge_rows);
 }
 
 size_t part_floats(const Planned& p, int head_dim, bool ml) {
-  if (p.split_blocks == 0) return 0;
+  if (p.merge_rows == 0) return 0;
   return (static_cast<size_t>(p.items) * p.part_rows * (ml ? 2 : head_dim) + 63) & ~static_cast<size_t>(63);
 }
 
@@ -824,7 +932,7 @@ size_t chunk_attention_workspace(const ChunkTable& c, int n_q_heads, int n_kv_he
 
 int chunk_attention_launches(const ChunkTable& c, int n_q_heads, int n_kv_heads, int head_dim, bool causal, int window,
                              int num_sms) {
-  return make_plan(c, n_q_heads, n_kv_heads, causal, window, num_sms).split_blocks ? 2 : 1;
+  return make_plan(c, n_q_heads, n_kv_heads, causal, window, num_sms).merge_rows ? 2 : 1;
 }
 
 cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, void* workspace, int num_sms,
@@ -843,7 +951,7 @@ cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, 
   a.part = static_cast<float*>(workspace);
   a.part_ml = a.part + part_floats(p, d.head_dim, false);
   a.part_rows = p.part_rows;
-  return d.head_dim == 128 ? launch_tc<128>(a, p, stream) : launch_tc<64>(a, p, stream);
+  return d.head_dim == 128 ? launch_tc<128>(a, p, num_sms, stream) : launch_tc<64>(a, p, num_sms, stream);
 }
 
 }  // namespace crf

@@ -23,7 +23,6 @@ namespace {
 constexpr int kPlanCtas = 8;  // the largest portable cluster
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
-constexpr int kCopyThreads = 256;
 constexpr int kMaxCopyLayers = 64;  // of one copy launch
 
 // In the caller's workspace.
@@ -121,6 +120,7 @@ __global__ void __cluster_dims__(kPlanCtas, 1, 1) __launch_bounds__(kPlanThreads
   const int p0 = static_cast<int>(min(static_cast<int64_t>(P), static_cast<int64_t>(warp) * run));
   const int p1 = min(P, p0 + run);
   int bad = 0;
+  griddep_wait();
 
   // Entries of every page (release, compact); their ids are checked here, and a fork's counts too
   if (OP != kPageFork)
@@ -241,38 +241,108 @@ __global__ void __cluster_dims__(kPlanCtas, 1, 1) __launch_bounds__(kPlanThreads
   for (int p = max(p0, total) + lane; p < p1; p += 32) a.refs_out[p] = 0;
 }
 
-struct CopyArgs {
-  PageScratch s;
-  __nv_bfloat16* pool[2 * kMaxCopyLayers];  // K of the layers, then V
-  int pools;
-  int n_kv_heads, head_dim;
+// A copy unit: up to kCopyBytes of one listed page in one layer's K or V. One thread of a block moves units through
+// a ring of shared-memory stages with bulk copies (a stage is refilled once the bulk store that read it has), so no
+// registers stand between the load and the store and kCopyStages units a block are in flight.
+constexpr int kCopyBytes = 16384;
+constexpr int kCopyStages = 6;
+
+struct CopyUnit {
+  const uint8_t* src;
+  uint8_t* dst;
+  int heads, bytes;  // bytes of each head: its live slots
+  bool whole;
 };
 
-__global__ void __launch_bounds__(kCopyThreads) page_copy(const __grid_constant__ CopyArgs a) {
+struct CopyArgs {
+  PageScratch s;
+  uint8_t* pool[2 * kMaxCopyLayers];  // K of the layers, then V
+  int pools;
+  int heads, head_bytes, slot_bytes;  // of a page: kv heads, bytes of a head's 16 slots, of one slot
+  int unit_heads, subs;               // heads of a unit, units of a page
+  int* status;
+};
+
+__global__ void __launch_bounds__(32) page_copy(const __grid_constant__ CopyArgs a) {
+  extern __shared__ __align__(128) uint8_t stages[];
+  __shared__ __align__(8) uint64_t full[kCopyStages];
+  __shared__ CopyUnit ring[kCopyStages];
+  griddep_launch_dependents();
   griddep_wait();
-  if (a.s.abort[0]) return;
-  const int64_t units = static_cast<int64_t>(a.s.abort[1]) * a.pools;
-  const int head_vecs = kPage * a.head_dim / 8, page_vecs = a.n_kv_heads * head_vecs;  // 16 bytes each
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int k = static_cast<int>(u / a.pools), pool = static_cast<int>(u - static_cast<int64_t>(k) * a.pools);
-    const int live_vecs = a.s.live[k] * a.head_dim / 8;
-    const uint4* src = reinterpret_cast<const uint4*>(a.pool[pool]) + static_cast<int64_t>(a.s.src[k]) * page_vecs;
-    uint4* dst = reinterpret_cast<uint4*>(a.pool[pool]) + static_cast<int64_t>(a.s.dst[k]) * page_vecs;
-    constexpr int kBatch = 4;
-    for (int i = threadIdx.x; i < page_vecs; i += kBatch * kCopyThreads) {
-      uint4 v[kBatch];
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int j = i + b * kCopyThreads;
-        if (j < page_vecs && j % head_vecs < live_vecs) v[b] = __ldcs(src + j);
-      }
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        const int j = i + b * kCopyThreads;
-        if (j < page_vecs && j % head_vecs < live_vecs) __stcs(dst + j, v[b]);
-      }
+  if (threadIdx.x != 0 || a.s.abort[0]) return;
+  for (int i = 0; i < kCopyStages; ++i) mbar_init(&full[i], 1);
+  fence_barrier_init();
+  const int64_t units = static_cast<int64_t>(a.s.abort[1]) * a.pools * a.subs;
+  const int64_t page_bytes = static_cast<int64_t>(a.heads) * a.head_bytes;
+  auto unit_at = [&](int64_t u) {
+    CopyUnit x;
+    const int64_t kp = u / a.subs;
+    const int sub = static_cast<int>(u - kp * a.subs);
+    const int k = static_cast<int>(kp / a.pools);
+    uint8_t* pool = a.pool[kp - static_cast<int64_t>(k) * a.pools];
+    const int live = a.s.live[k];
+    const int64_t at = static_cast<int64_t>(sub) * a.unit_heads * a.head_bytes;
+    x.src = pool + a.s.src[k] * page_bytes + at;
+    x.dst = pool + a.s.dst[k] * page_bytes + at;
+    x.heads = min(a.unit_heads, a.heads - sub * a.unit_heads);
+    x.bytes = live * a.slot_bytes;
+    x.whole = live == kPage;
+    return x;
+  };
+  volatile int abort_flag = 0;
+  auto load = [&](int64_t u, int st) {
+    const CopyUnit x = unit_at(u);
+    ring[st] = x;
+    const uint32_t to = smem_u32(stages + st * kCopyBytes);
+    mbar_arrive_expect_tx(&full[st], x.heads * x.bytes);
+    if (x.whole) {
+      bulk_load(to, x.src, x.heads * x.bytes, &full[st]);
+    } else {
+      for (int h = 0; h < x.heads; ++h)
+        bulk_load(to + h * a.head_bytes, x.src + h * a.head_bytes, x.bytes, &full[st]);
+    }
+  };
+  auto store = [&](int st) {
+    const CopyUnit x = ring[st];
+    const uint32_t from = smem_u32(stages + st * kCopyBytes);
+    if (x.whole) {
+      bulk_store(x.dst, from, x.heads * x.bytes);
+    } else {
+      for (int h = 0; h < x.heads; ++h)
+        bulk_store(x.dst + h * a.head_bytes, from + h * a.head_bytes, x.bytes);
+    }
+    bulk_commit();
+  };
+  // unit i of the block is in stage i % kCopyStages; loads run kCopyStages - 1 units ahead of stores
+  const int64_t mine = units > blockIdx.x ? (units - blockIdx.x + gridDim.x - 1) / gridDim.x : 0;
+  auto at = [&](int64_t i) { return blockIdx.x + i * gridDim.x; };
+  constexpr int kAhead = kCopyStages - 1;
+  int64_t asked = 0;
+  for (; asked < kAhead && asked < mine; ++asked) load(at(asked), static_cast<int>(asked));
+  int st = 0;
+  uint32_t ph = 0;
+  for (int64_t i = 0; i < mine; ++i) {
+    if (!mbar_wait(&full[st], ph, &abort_flag, a.status)) break;
+    store(st);
+    if (asked < mine) {
+      // the stage of unit asked was read by the store of unit asked - kCopyStages = i - 1
+      bulk_wait_read<1>();
+      load(at(asked), static_cast<int>(asked % kCopyStages));
+      ++asked;
+    }
+    if (++st == kCopyStages) {
+      st = 0;
+      ph ^= 1;
     }
   }
+  if (abort_flag) {
+    // a load never came: the others land before the block's shared memory is released
+    for (int64_t i = asked > kCopyStages ? asked - kCopyStages : 0; i < asked; ++i) {
+      volatile int never = 0;
+      mbar_wait(&full[i % kCopyStages], static_cast<uint32_t>((i / kCopyStages) & 1), &never, nullptr);
+    }
+  }
+  bulk_wait_all();
 }
 
 size_t align256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
@@ -326,24 +396,37 @@ cudaError_t launch_pages(PageOp op, const PageTables& t, bool deep, const int32_
   a.deep = deep;
   a.status = status;
   auto* plan = op == kPageFork ? page_plan<kPageFork> : op == kPageCompact ? page_plan<kPageCompact> : page_plan<kPageRelease>;
+  PdlScope pdl;
   cudaError_t e = launch_kernel(plan, dim3(kPlanCtas), dim3(kPlanThreads), 0, stream, a);
   if (e != cudaSuccess || op == kPageRelease || (op == kPageFork && a.fresh == 0)) return e;
-  PdlScope pdl;
+  const int head_bytes = kPage * pool->head_dim * 2;
+  constexpr int smem = kCopyStages * kCopyBytes;
+  static PerDevice once;
+  int dev = 0;
+  if (once.pending(&dev)) {
+    e = cudaFuncSetAttribute(page_copy, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    once.done(dev);
+  }
   for (int l0 = 0; l0 < pool->n_layers; l0 += kMaxCopyLayers) {
     CopyArgs c;
     std::memset(&c, 0, sizeof(c));
     c.s = a.s;
     const int n = std::min(kMaxCopyLayers, pool->n_layers - l0);
     for (int l = 0; l < n; ++l) {
-      c.pool[l] = static_cast<__nv_bfloat16*>(pool->k[l0 + l]);
-      c.pool[n + l] = static_cast<__nv_bfloat16*>(pool->v[l0 + l]);
+      c.pool[l] = static_cast<uint8_t*>(pool->k[l0 + l]);
+      c.pool[n + l] = static_cast<uint8_t*>(pool->v[l0 + l]);
     }
     c.pools = 2 * n;
-    c.n_kv_heads = pool->n_kv_heads;
-    c.head_dim = pool->head_dim;
-    int64_t units = static_cast<int64_t>(num_sms) * 8;
-    if (op == kPageFork) units = std::min(units, static_cast<int64_t>(a.fresh) * c.pools);
-    e = launch_kernel(page_copy, dim3(static_cast<unsigned>(units)), dim3(kCopyThreads), 0, stream, c);
+    c.heads = pool->n_kv_heads;
+    c.head_bytes = head_bytes;
+    c.slot_bytes = pool->head_dim * 2;
+    c.unit_heads = std::min(pool->n_kv_heads, kCopyBytes / head_bytes);
+    c.subs = (pool->n_kv_heads + c.unit_heads - 1) / c.unit_heads;
+    c.status = status;
+    int64_t blocks = static_cast<int64_t>(num_sms) * 2;  // resident together
+    if (op == kPageFork) blocks = std::min(blocks, static_cast<int64_t>(a.fresh) * c.pools * c.subs);
+    e = launch_kernel(page_copy, dim3(static_cast<unsigned>(blocks)), dim3(32), smem, stream, c);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

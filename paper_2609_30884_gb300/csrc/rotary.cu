@@ -7,9 +7,9 @@
 // at p = 2^31 the angle is off by at most 2^-33 turns. Its top 32 bits are split into a quadrant and a
 // remainder of at most an eighth of a turn, whose sine and cosine are fp32 functions.
 //
-// Bound by memory: every element is read once and written once. A thread owns one 16-byte unit of a row's head
-// (for the half layout two, the pair's halves), forms its sines and cosines once and walks the heads with four
-// units in flight.
+// Bound by memory: every element is read once and written once. A thread owns one 16-byte unit of a row (for the
+// half layout two, the pair's halves) and every hg-th of its heads, the first kRotBatch of them asked for before the
+// angles are formed. The block's angles are formed once, in shared memory, for all heads of its rows.
 #include "../../include/crf.h"
 #include "common.cuh"
 #include "extend.h"
@@ -24,12 +24,14 @@ namespace crf {
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotBatch = 4;  // heads in flight
+constexpr int kRotBatch = 4;        // heads in flight
+constexpr int kRotMaxRows = 32;     // of a block
+constexpr int kRotMaxAngles = 2048; // of a block: at most 8 a thread
 
 struct RotaryArgs {
   RotaryDesc d;
   ChunkTable c;
-  int units, rot_units, rows_per_block, heads, heads_per_block;
+  int units, rot_units, rows_per_block, head_slots, heads;
 };
 
 // Request of packed row r.
@@ -73,26 +75,15 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
   using U = Unit<T, VEC>;
   constexpr bool kTwo = VEC == 1 || !INTER;  // a rotating unit is two pieces
   constexpr int kPairs = VEC == 1 ? 1 : (INTER ? VEC / 2 : VEC);
-  __shared__ uint64_t turns[kMaxPairs];
+  __shared__ int s_pos[kRotMaxRows], s_page[kRotMaxRows];
+  __shared__ float2 s_angle[kRotMaxAngles];  // [row][pair]
+  griddep_launch_dependents();
   const RotaryDesc& d = a.d;
-  for (int i = threadIdx.x; i < d.rot_dim / 2; i += kRotThreads) turns[i] = d.turns[i];
-  __syncthreads();
-  const int rb = threadIdx.x / a.units, u = threadIdx.x - rb * a.units;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * a.rows_per_block + rb;
-  if (rb >= a.rows_per_block || row >= d.n_rows) return;
-  int pos, page = 0, slot = 0;
-  if (d.positions) {
-    pos = d.positions[row];
-  } else {
-    const int i = chunk_of_row(a.c, static_cast<int>(row));
-    pos = a.c.pos[i] + (static_cast<int>(row) - a.c.row0[i]);
-    page = a.c.pt[i][pos / kPage];
-    slot = pos % kPage;
-    if (page < 0 || page >= a.c.num_pages) {
-      if (d.status) atomicOr(d.status, kStatusBounds);
-      page = -1;  // its writes are left out
-    }
-  }
+  const int R = a.rows_per_block;
+  const int u = threadIdx.x % a.units, rest = threadIdx.x / a.units;
+  const int rb = rest % R, h0 = rest / R;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * R, row = row0 + rb;
+  const bool active = h0 < a.head_slots && row < d.n_rows;
   const bool turning = u < a.rot_units;
   // first element of the unit's piece(s)
   int e0, e1 = 0;
@@ -105,59 +96,83 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
     e0 = u * VEC;
     e1 = e0 + d.rot_dim / 2;
   }
-  float cs[kPairs], sn[kPairs];
+  const bool two = kTwo && turning;
+  const int n0 = d.part[0].heads, n1 = n0 + d.part[1].heads;  // heads of parts that are not there: 0
+  auto part_of = [&](int h) { return h < n0 ? 0 : h < n1 ? 1 : 2; };
+  auto first_of = [&](int p) { return p == 0 ? 0 : p == 1 ? n0 : n1; };
+  U lo[kRotBatch], hi[kRotBatch];
+  auto load = [&](int h_base) {
+#pragma unroll
+    for (int b = 0; b < kRotBatch; ++b) {
+      const int h = h_base + b * a.head_slots;
+      if (!active || h >= a.heads) continue;
+      const int p = part_of(h);
+      const RotPart& t = d.part[p];
+      const T* src = static_cast<const T*>(t.x) + row * t.x_row + (h - first_of(p)) * t.x_head;
+      lo[b] = *reinterpret_cast<const U*>(src + e0);
+      if (two) hi[b] = *reinterpret_cast<const U*>(src + e1);
+    }
+  };
+  griddep_wait();
+  load(h0);
+  if (threadIdx.x < R && row0 + threadIdx.x < d.n_rows) {
+    const int r = static_cast<int>(row0) + threadIdx.x;
+    int pos, page = 0;
+    if (d.positions) {
+      pos = d.positions[r];
+    } else {
+      const int i = chunk_of_row(a.c, r);
+      pos = a.c.pos[i] + (r - a.c.row0[i]);
+      page = a.c.pt[i][pos / kPage];
+      if (page < 0 || page >= a.c.num_pages) {
+        if (d.status) atomicOr(d.status, kStatusBounds);
+        page = -1;  // its writes are left out
+      }
+    }
+    s_pos[threadIdx.x] = pos;
+    s_page[threadIdx.x] = page;
+  }
+  __syncthreads();
+  const int pairs = d.rot_dim / 2, here = static_cast<int>(min(static_cast<int64_t>(R), d.n_rows - row0));
+  for (int i = threadIdx.x; i < here * pairs; i += kRotThreads) {
+    const int k = i / here, r = i - k * here;  // lanes of a warp share few pairs
+    const float2 t = turn_cos_sin(static_cast<uint64_t>(static_cast<int64_t>(s_pos[r])) * d.turns[k]);
+    s_angle[r * pairs + k] = make_float2(t.x * d.magnitude, (d.inverse ? -t.y : t.y) * d.magnitude);
+  }
+  __syncthreads();
+  if (!active) return;
+  float2 cs[kPairs];
   if (turning) {
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) {
-      const float2 t = turn_cos_sin(static_cast<uint64_t>(static_cast<int64_t>(pos)) * turns[u * kPairs + i]);
-      cs[i] = t.x * d.magnitude;
-      sn[i] = (d.inverse ? -t.y : t.y) * d.magnitude;
-    }
+    for (int i = 0; i < kPairs; ++i) cs[i] = s_angle[rb * pairs + u * kPairs + i];
   }
-  const int h_begin = blockIdx.y * a.heads_per_block, h_end = min(a.heads, h_begin + a.heads_per_block);
-  int first = 0;  // heads of the parts before
-  for (int p = 0; p < d.n_parts; ++p) {
-    const RotPart& t = d.part[p];
-    const int last = min(h_end, first + t.heads);
-    const bool rotate = turning && t.rotate, two = kTwo && turning;
-    const T* x = static_cast<const T*>(t.x) + row * t.x_row;
-    T* out = static_cast<T*>(t.out);
-    int64_t out_head = t.out_head;
-    if (t.paged) {
-      out += (static_cast<int64_t>(page) * d.n_kv_heads * kPage + slot) * d.head_dim;
-      out_head = static_cast<int64_t>(kPage) * d.head_dim;
-    } else {
-      out += row * t.out_row;
-    }
-    for (int h0 = max(h_begin, first); h0 < last; h0 += kRotBatch) {
-      U lo[kRotBatch], hi[kRotBatch];
+  const int page = s_page[rb], slot = s_pos[rb] % kPage;
+  const int64_t page_at = (static_cast<int64_t>(page) * d.n_kv_heads * kPage + slot) * d.head_dim;
+  for (int h_base = h0; h_base < a.heads; h_base += kRotBatch * a.head_slots) {
+    if (h_base != h0) load(h_base);
 #pragma unroll
-      for (int b = 0; b < kRotBatch; ++b) {
-        if (h0 + b >= last) continue;
-        const T* src = x + (h0 + b - first) * t.x_head;
-        lo[b] = *reinterpret_cast<const U*>(src + e0);
-        if (two) hi[b] = *reinterpret_cast<const U*>(src + e1);
-      }
+    for (int b = 0; b < kRotBatch; ++b) {
+      const int h = h_base + b * a.head_slots;
+      if (h >= a.heads) continue;
+      const int p = part_of(h);
+      const RotPart& t = d.part[p];
+      if (turning && t.rotate) {
 #pragma unroll
-      for (int b = 0; b < kRotBatch; ++b) {
-        if (h0 + b >= last) continue;
-        if (rotate) {
-#pragma unroll
-          for (int i = 0; i < kPairs; ++i) {
-            T& xe = kTwo ? lo[b].e[i] : lo[b].e[(2 * i) % VEC];
-            T& ye = kTwo ? hi[b].e[i] : lo[b].e[(2 * i + 1) % VEC];
-            const float xf = to_f(xe), yf = to_f(ye);
-            xe = from_f<T>(xf * cs[i] - yf * sn[i]);
-            ye = from_f<T>(yf * cs[i] + xf * sn[i]);
-          }
+        for (int i = 0; i < kPairs; ++i) {
+          T& xe = kTwo ? lo[b].e[i] : lo[b].e[(2 * i) % VEC];
+          T& ye = kTwo ? hi[b].e[i] : lo[b].e[(2 * i + 1) % VEC];
+          const float xf = to_f(xe), yf = to_f(ye);
+          xe = from_f<T>(xf * cs[i].x - yf * cs[i].y);
+          ye = from_f<T>(yf * cs[i].x + xf * cs[i].y);
         }
-        if (t.paged && page < 0) continue;
-        T* dst = out + (h0 + b - first) * out_head;
-        *reinterpret_cast<U*>(dst + e0) = lo[b];
-        if (two) *reinterpret_cast<U*>(dst + e1) = hi[b];
       }
+      if (t.paged && page < 0) continue;
+      const int64_t at = t.paged ? page_at + static_cast<int64_t>(h - first_of(p)) * kPage * d.head_dim
+                                 : row * t.out_row + (h - first_of(p)) * t.out_head;
+      T* dst = static_cast<T*>(t.out) + at;
+      *reinterpret_cast<U*>(dst + e0) = lo[b];
+      if (two) *reinterpret_cast<U*>(dst + e1) = hi[b];
     }
-    first += t.heads;
   }
 }
 
@@ -166,15 +181,18 @@ cudaError_t launch_vec(RotaryArgs& a, int num_sms, cudaStream_t stream) {
   const RotaryDesc& d = a.d;
   a.rot_units = VEC == 1 ? d.rot_dim / 2 : d.interleaved ? d.rot_dim / VEC : d.rot_dim / 2 / VEC;
   a.units = a.rot_units + (d.head_dim - d.rot_dim) / VEC;
-  a.rows_per_block = kRotThreads / a.units;
   a.heads = 0;
   for (int p = 0; p < d.n_parts; ++p) a.heads += d.part[p].heads;
-  const int gx = static_cast<int>((static_cast<int64_t>(d.n_rows) + a.rows_per_block - 1) / a.rows_per_block);
-  // few rows: the heads are dealt to more blocks, down to one batch each
-  const int batches = (a.heads + kRotBatch - 1) / kRotBatch;
-  const int gy = std::min(batches, std::max(1, (8 * num_sms + gx - 1) / gx));
-  a.heads_per_block = (batches + gy - 1) / gy * kRotBatch;
-  const dim3 grid(gx, (a.heads + a.heads_per_block - 1) / a.heads_per_block);
+  // A block's threads: units x rows x head slots. Slots of a batch of heads each where the rows fill the SMs (few
+  // angles are formed twice); more slots and fewer rows where they do not.
+  const int room = kRotThreads / a.units;
+  a.head_slots = std::max(1, std::min(room, (a.heads + 2 * kRotBatch - 1) / (2 * kRotBatch)));
+  a.rows_per_block = std::max(1, std::min(kRotMaxRows, room / a.head_slots));
+  while (a.rows_per_block > 1 && (static_cast<int64_t>(d.n_rows) + a.rows_per_block - 1) / a.rows_per_block < 4 * num_sms)
+    a.rows_per_block /= 2;
+  a.head_slots = std::min(a.heads, room / a.rows_per_block);
+  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(d.n_rows) + a.rows_per_block - 1) / a.rows_per_block));
+  PdlScope pdl;
   return d.interleaved ? launch_kernel(rotary_kernel<T, VEC, true>, grid, dim3(kRotThreads), 0, stream, a)
                        : launch_kernel(rotary_kernel<T, VEC, false>, grid, dim3(kRotThreads), 0, stream, a);
 }
