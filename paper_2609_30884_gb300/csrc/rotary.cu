@@ -8,8 +8,10 @@
 // remainder of at most an eighth of a turn, whose sine and cosine are fp32 functions.
 //
 // Bound by memory: every element is read once and written once. A thread owns one 16-byte unit of a row (for the
-// half layout two, the pair's halves) and every hg-th of its heads, the first kRotBatch of them asked for before the
-// angles are formed. The block's angles are formed once, in shared memory, for all heads of its rows.
+// half layout two, the pair's halves) in up to four neighbouring heads and asks for all of them before the angles are
+// formed; a block's angles are formed once, in shared memory, for its rows' heads. A thread has one round of loads:
+// with its heads dealt in rounds (28 heads over 5 threads), 16384 bf16 rows of 32 heads took 66 us, so 44
+// (268 MB: 90% of the copy rate; fp32 82 us for 537 MB, 97%; interleaved 43).
 #include "../../include/crf.h"
 #include "common.cuh"
 #include "extend.h"
@@ -23,15 +25,19 @@ namespace crf {
 
 namespace {
 
-constexpr int kRotThreads = 256;
-constexpr int kRotBatch = 4;        // heads in flight
+constexpr int kRotThreads = 256;    // at most
+constexpr int kRotBatch = 4;        // heads of a thread, at most
 constexpr int kRotMaxRows = 32;     // of a block
 constexpr int kRotMaxAngles = 2048; // of a block: at most 8 a thread
 
 struct RotaryArgs {
   RotaryDesc d;
   ChunkTable c;
-  int units, rot_units, rows_per_block, head_slots, heads;
+  int units, rot_units;     // 16-byte units of a head, those that rotate
+  int rows;                 // of a block
+  int batch;                // heads of a slot
+  int slot0[3];             // each part's first slot
+  int slots, block_slots;   // of all parts; of a block
 };
 
 // Request of packed row r.
@@ -56,18 +62,48 @@ __device__ __forceinline__ float2 turn_cos_sin(uint64_t turn) {
   return make_float2((q == 1 || q == 2) ? -c : c, (q == 2 || q == 3) ? -n : n);
 }
 
-__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
-__device__ __forceinline__ float to_f(float v) { return v; }
-template <typename T> __device__ __forceinline__ T from_f(float v);
-template <> __device__ __forceinline__ __nv_bfloat16 from_f(float v) { return __float2bfloat16_rn(v); }
-template <> __device__ __forceinline__ __half from_f(float v) { return __float2half_rn(v); }
-template <> __device__ __forceinline__ float from_f(float v) { return v; }
-
+// A unit of VEC elements as fp32 and back, two elements a conversion where they are packed.
 template <typename T, int VEC>
 struct __align__(sizeof(T) * VEC) Unit {
   T e[VEC];
 };
+template <int VEC>
+__device__ __forceinline__ void unpack(const Unit<float, VEC>& u, float (&f)[VEC]) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) f[i] = u.e[i];
+}
+template <int VEC>
+__device__ __forceinline__ void pack(const float (&f)[VEC], Unit<float, VEC>& u) {
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) u.e[i] = f[i];
+}
+__device__ __forceinline__ float2 unpack2(__nv_bfloat16, uint32_t w) { return make_float2(bf16_lo(w), bf16_hi(w)); }
+__device__ __forceinline__ float2 unpack2(__half, uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ uint32_t pack2(__nv_bfloat16, float a, float b) { return pack_bf16(a, b); }
+__device__ __forceinline__ uint32_t pack2(__half, float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <typename T>
+__device__ __forceinline__ void unpack(const Unit<T, 8>& u, float (&f)[8]) {
+  const uint4 w = *reinterpret_cast<const uint4*>(&u);
+  const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 g = unpack2(T(), v[i]);
+    f[2 * i] = g.x;
+    f[2 * i + 1] = g.y;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void pack(const float (&f)[8], Unit<T, 8>& u) {
+  *reinterpret_cast<uint4*>(&u) =
+      make_uint4(pack2(T(), f[0], f[1]), pack2(T(), f[2], f[3]), pack2(T(), f[4], f[5]), pack2(T(), f[6], f[7]));
+}
+__device__ __forceinline__ void unpack(const Unit<__nv_bfloat16, 1>& u, float (&f)[1]) { f[0] = __bfloat162float(u.e[0]); }
+__device__ __forceinline__ void unpack(const Unit<__half, 1>& u, float (&f)[1]) { f[0] = __half2float(u.e[0]); }
+__device__ __forceinline__ void pack(const float (&f)[1], Unit<__nv_bfloat16, 1>& u) { u.e[0] = __float2bfloat16_rn(f[0]); }
+__device__ __forceinline__ void pack(const float (&f)[1], Unit<__half, 1>& u) { u.e[0] = __float2half_rn(f[0]); }
 
 // VEC elements a unit (16 bytes), or 1: a rotating unit is then one pair of elements.
 template <typename T, int VEC, bool INTER>
@@ -79,11 +115,16 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
   __shared__ float2 s_angle[kRotMaxAngles];  // [row][pair]
   griddep_launch_dependents();
   const RotaryDesc& d = a.d;
-  const int R = a.rows_per_block;
+  const int R = a.rows;
   const int u = threadIdx.x % a.units, rest = threadIdx.x / a.units;
-  const int rb = rest % R, h0 = rest / R;
+  const int rb = rest % R, slot = rest / R + blockIdx.y * a.block_slots;
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) * R, row = row0 + rb;
-  const bool active = h0 < a.head_slots && row < d.n_rows;
+  const bool active = rest / R < a.block_slots && slot < a.slots && row < d.n_rows;
+  // the slot's part and heads [head, head + heads)
+  const int p = slot >= a.slot0[2] ? 2 : slot >= a.slot0[1] ? 1 : 0;
+  const RotPart t = p == 0 ? d.part[0] : p == 1 ? d.part[1] : d.part[2];
+  const int head = (slot - (p == 0 ? 0 : p == 1 ? a.slot0[1] : a.slot0[2])) * a.batch;
+  const int heads = active ? min(a.batch, t.heads - head) : 0;
   const bool turning = u < a.rot_units;
   // first element of the unit's piece(s)
   int e0, e1 = 0;
@@ -97,24 +138,19 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
     e1 = e0 + d.rot_dim / 2;
   }
   const bool two = kTwo && turning;
-  const int n0 = d.part[0].heads, n1 = n0 + d.part[1].heads;  // heads of parts that are not there: 0
-  auto part_of = [&](int h) { return h < n0 ? 0 : h < n1 ? 1 : 2; };
-  auto first_of = [&](int p) { return p == 0 ? 0 : p == 1 ? n0 : n1; };
   U lo[kRotBatch], hi[kRotBatch];
-  auto load = [&](int h_base) {
+  griddep_wait();
+  {
+    const T* src = static_cast<const T*>(t.x) + row * t.x_row + head * t.x_head;
 #pragma unroll
     for (int b = 0; b < kRotBatch; ++b) {
-      const int h = h_base + b * a.head_slots;
-      if (!active || h >= a.heads) continue;
-      const int p = part_of(h);
-      const RotPart& t = d.part[p];
-      const T* src = static_cast<const T*>(t.x) + row * t.x_row + (h - first_of(p)) * t.x_head;
-      lo[b] = *reinterpret_cast<const U*>(src + e0);
-      if (two) hi[b] = *reinterpret_cast<const U*>(src + e1);
+      if (b < heads) {
+        lo[b] = *reinterpret_cast<const U*>(src + e0);
+        if (two) hi[b] = *reinterpret_cast<const U*>(src + e1);
+      }
+      src += t.x_head;
     }
-  };
-  griddep_wait();
-  load(h0);
+  }
   if (threadIdx.x < R && row0 + threadIdx.x < d.n_rows) {
     const int r = static_cast<int>(row0) + threadIdx.x;
     int pos, page = 0;
@@ -134,45 +170,45 @@ __global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_consta
   }
   __syncthreads();
   const int pairs = d.rot_dim / 2, here = static_cast<int>(min(static_cast<int64_t>(R), d.n_rows - row0));
-  for (int i = threadIdx.x; i < here * pairs; i += kRotThreads) {
+  for (int i = threadIdx.x; i < here * pairs; i += blockDim.x) {
     const int k = i / here, r = i - k * here;  // lanes of a warp share few pairs
     const float2 t = turn_cos_sin(static_cast<uint64_t>(static_cast<int64_t>(s_pos[r])) * d.turns[k]);
     s_angle[r * pairs + k] = make_float2(t.x * d.magnitude, (d.inverse ? -t.y : t.y) * d.magnitude);
   }
   __syncthreads();
-  if (!active) return;
+  const int page = s_page[rb];
+  if (!active || (t.paged && page < 0)) return;
+  const bool rotate = turning && t.rotate;
   float2 cs[kPairs];
-  if (turning) {
+  if (rotate) {
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) cs[i] = s_angle[rb * pairs + u * kPairs + i];
   }
-  const int page = s_page[rb], slot = s_pos[rb] % kPage;
-  const int64_t page_at = (static_cast<int64_t>(page) * d.n_kv_heads * kPage + slot) * d.head_dim;
-  for (int h_base = h0; h_base < a.heads; h_base += kRotBatch * a.head_slots) {
-    if (h_base != h0) load(h_base);
+  const int64_t out_head = t.paged ? static_cast<int64_t>(kPage) * d.head_dim : t.out_head;
+  T* dst = static_cast<T*>(t.out) + head * out_head +
+           (t.paged ? (static_cast<int64_t>(page) * d.n_kv_heads * kPage + s_pos[rb] % kPage) * d.head_dim : row * t.out_row);
 #pragma unroll
-    for (int b = 0; b < kRotBatch; ++b) {
-      const int h = h_base + b * a.head_slots;
-      if (h >= a.heads) continue;
-      const int p = part_of(h);
-      const RotPart& t = d.part[p];
-      if (turning && t.rotate) {
+  for (int b = 0; b < kRotBatch; ++b) {
+    if (b < heads) {
+      if (rotate) {
+        float x[VEC], y[VEC];
+        unpack(lo[b], x);
+        if (kTwo) unpack(hi[b], y);
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-          T& xe = kTwo ? lo[b].e[i] : lo[b].e[(2 * i) % VEC];
-          T& ye = kTwo ? hi[b].e[i] : lo[b].e[(2 * i + 1) % VEC];
-          const float xf = to_f(xe), yf = to_f(ye);
-          xe = from_f<T>(xf * cs[i].x - yf * cs[i].y);
-          ye = from_f<T>(yf * cs[i].x + xf * cs[i].y);
+          float& u0 = kTwo ? x[i] : x[(2 * i) % VEC];
+          float& u1 = kTwo ? y[i] : x[(2 * i + 1) % VEC];
+          const float xf = u0, yf = u1;
+          u0 = xf * cs[i].x - yf * cs[i].y;
+          u1 = yf * cs[i].x + xf * cs[i].y;
         }
+        pack(x, lo[b]);
+        if (kTwo) pack(y, hi[b]);
       }
-      if (t.paged && page < 0) continue;
-      const int64_t at = t.paged ? page_at + static_cast<int64_t>(h - first_of(p)) * kPage * d.head_dim
-                                 : row * t.out_row + (h - first_of(p)) * t.out_head;
-      T* dst = static_cast<T*>(t.out) + at;
       *reinterpret_cast<U*>(dst + e0) = lo[b];
       if (two) *reinterpret_cast<U*>(dst + e1) = hi[b];
     }
+    dst += out_head;
   }
 }
 
@@ -181,20 +217,33 @@ cudaError_t launch_vec(RotaryArgs& a, int num_sms, cudaStream_t stream) {
   const RotaryDesc& d = a.d;
   a.rot_units = VEC == 1 ? d.rot_dim / 2 : d.interleaved ? d.rot_dim / VEC : d.rot_dim / 2 / VEC;
   a.units = a.rot_units + (d.head_dim - d.rot_dim) / VEC;
-  a.heads = 0;
-  for (int p = 0; p < d.n_parts; ++p) a.heads += d.part[p].heads;
-  // A block's threads: units x rows x head slots. Slots of a batch of heads each where the rows fill the SMs (few
-  // angles are formed twice); more slots and fewer rows where they do not.
+  // Slots of four heads where the rows alone fill the SMs, of one head where they are few: a call of one row is then
+  // a block or two with one head a thread.
+  const bool few = d.n_rows < 4 * num_sms;
+  a.batch = few ? 1 : kRotBatch;
+  auto deal = [&]() {
+    a.slots = 0;
+    for (int p = 0; p < 3; ++p) {
+      a.slot0[p] = a.slots;
+      if (p < d.n_parts) a.slots += (d.part[p].heads + a.batch - 1) / a.batch;
+      else a.slot0[p] = 1 << 30;
+    }
+  };
+  deal();
+  if (a.batch == 1 && a.slots > 4096) {  // heads beyond any row's: keep the grid's second axis short
+    a.batch = kRotBatch;
+    deal();
+  }
   const int room = kRotThreads / a.units;
-  a.head_slots = std::max(1, std::min(room, (a.heads + 2 * kRotBatch - 1) / (2 * kRotBatch)));
-  a.rows_per_block = std::max(1, std::min(kRotMaxRows, room / a.head_slots));
-  while (a.rows_per_block > 1 && (static_cast<int64_t>(d.n_rows) + a.rows_per_block - 1) / a.rows_per_block < 4 * num_sms)
-    a.rows_per_block /= 2;
-  a.head_slots = std::min(a.heads, room / a.rows_per_block);
-  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(d.n_rows) + a.rows_per_block - 1) / a.rows_per_block));
+  a.block_slots = std::min(a.slots, room);
+  // rows of a block: about 128 threads (16384 bf16 rows of 32 heads: 44 us; 47 with 256, 50 with 72)
+  a.rows = few ? 1 : std::max(1, std::min(kRotMaxRows, 128 / (a.units * a.block_slots)));
+  const int threads = (a.units * a.block_slots * a.rows + 31) / 32 * 32;
+  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(d.n_rows) + a.rows - 1) / a.rows),
+                  (a.slots + a.block_slots - 1) / a.block_slots);
   PdlScope pdl;
-  return d.interleaved ? launch_kernel(rotary_kernel<T, VEC, true>, grid, dim3(kRotThreads), 0, stream, a)
-                       : launch_kernel(rotary_kernel<T, VEC, false>, grid, dim3(kRotThreads), 0, stream, a);
+  return d.interleaved ? launch_kernel(rotary_kernel<T, VEC, true>, grid, dim3(threads), 0, stream, a)
+                       : launch_kernel(rotary_kernel<T, VEC, false>, grid, dim3(threads), 0, stream, a);
 }
 
 template <typename T>
