@@ -361,7 +361,9 @@ crf_status crf_chunk_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int n
     s = fill_chunks(chunks, n_chunks, true, 1, &t);
     if (s == CRF_OK) s = check_attention(n_q_heads, n_kv_heads, window, t.row0[t.n]);
     if (s != CRF_OK) return s;
-    *bytes = align256(chunk_attention_workspace(t, n_q_heads, n_kv_heads, head_dim, causal != 0, window, ctx->num_sms));
+    ChunkPlan plan;
+    plan_chunk_attention(t, n_q_heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
+    *bytes = align256(chunk_attention_workspace(plan, head_dim));
     return CRF_OK;
   });
 }
@@ -392,8 +394,9 @@ crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer,
     s = check_out(q->out, q->out_row, q->out_head, q->heads, rows, head_dim, "q");
     if (s != CRF_OK) return s;
     if (q->x == q->out) return fail(CRF_EINVAL, "q: o may not be written over q");
-    s = check_workspace(workspace, ws_bytes,
-                        chunk_attention_workspace(t, q->heads, n_kv_heads, head_dim, causal != 0, window, ctx->num_sms));
+    ChunkPlan plan;
+    plan_chunk_attention(t, q->heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
+    s = check_workspace(workspace, ws_bytes, chunk_attention_workspace(plan, head_dim));
     if (s != CRF_OK) return s;
     ChunkAttnDesc d;
     d.q = static_cast<const __nv_bfloat16*>(q->x);
@@ -415,8 +418,8 @@ crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer,
     DeviceScope dev(ctx->device);
     CRF_CUDA(dev.error());
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    ProfScope ps(ctx, kPChunkAttn, st, chunk_attention_launches(t, q->heads, n_kv_heads, head_dim, d.causal, window, ctx->num_sms));
-    CRF_CUDA(launch_chunk_attention(d, t, workspace, ctx->num_sms, st));
+    ProfScope ps(ctx, kPChunkAttn, st, plan.cuts ? 2 : 1);
+    CRF_CUDA(launch_chunk_attention(d, t, plan, workspace, ctx->num_sms, st));
     return CRF_OK;
   });
 }

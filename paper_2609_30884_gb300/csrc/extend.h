@@ -56,12 +56,29 @@ struct ChunkAttnDesc {
   int window;                  // 0: none
   int* status;
 };
-size_t chunk_attention_workspace(const ChunkTable& c, int n_q_heads, int n_kv_heads, int head_dim, bool causal,
-                                 int window, int num_sms);
-int chunk_attention_launches(const ChunkTable& c, int n_q_heads, int n_kv_heads, int head_dim, bool causal, int window,
-                             int num_sms);
-cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, void* workspace, int num_sms,
-                                   cudaStream_t stream);
+constexpr int kMaxCtas = 256;
+// Where a CTA's run begins: step `step` of item (request, query tile or pair qt, kv head g); request = c.n: the end.
+// Items go through the requests in order, query tiles from the last down, heads.
+struct RunStart {
+  int req, qt, g, step;
+};
+// A cut item: part k is in slot first_slot (k = 0) or 2 (cta + k).
+struct CutItem {
+  int row0, q0, g, first_slot, cta, parts;
+};
+// How a call's work is dealt: one run a CTA, and the items that runs cut.
+struct ChunkPlan {
+  int ctas, cuts;
+  int part_rows, merge_rows;  // rows of the largest cut item, of all
+  RunStart run[kMaxCtas + 1];
+  int rows[kMaxCtas + 1];     // packed rows of the cut items before each
+  CutItem cut[kMaxCtas];
+};
+void plan_chunk_attention(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms,
+                          ChunkPlan* p);
+size_t chunk_attention_workspace(const ChunkPlan& p, int head_dim);
+cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, const ChunkPlan& p, void* workspace,
+                                   int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------- pages
 // Entries [first[i], first[i + 1]) of a call are table i's.

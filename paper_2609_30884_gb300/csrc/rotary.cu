@@ -28,7 +28,7 @@ namespace {
 constexpr int kRotThreads = 256;    // at most
 constexpr int kRotBatch = 4;        // heads of a thread, at most
 constexpr int kRotMaxRows = 32;     // of a block
-constexpr int kRotMaxAngles = 2048; // of a block: at most 8 a thread
+constexpr int kRotMaxAngles = 1024; // of a block: 8 pairs a unit, about 128 threads, or one row
 
 struct RotaryArgs {
   RotaryDesc d;

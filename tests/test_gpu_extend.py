@@ -381,6 +381,21 @@ def test_attention_long_chunk(ctx):
     ctx.check()
 
 
+@pytest.mark.parametrize("hq,hkv,dim,chunks", [
+    (28, 4, 128, [(16, 20000)]), (12, 2, 128, [(9, 30001), (1, 100)]), (4, 2, 64, [(60, 25000)]), (5, 5, 64, [(100, 9000), (128, 7000)]),
+    (28, 4, 128, [(300, 12000), (2, 9000), (18, 11111)]), (4, 2, 64, [(700, 3000)]), (16, 1, 128, [(8, 40000), (40, 5000)]),
+])
+def test_attention_cut_items(ctx, hq, hkv, dim, chunks):
+    """Few query tiles over many keys: every item is cut among CTAs, whatever the number of rows in its tile."""
+    s = Setup(25, hq, hkv, dim, chunks)
+    out, lse = s.run(ctx)
+    s.verify(out, lse)
+    for _ in range(3):
+        again, lse2 = s.run(ctx)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
+    ctx.check()
+
+
 def test_attention_values_that_only_later_rows_see(ctx):
     """NaN and infinities in keys' values reach the rows that see them and no other."""
     for hq, hkv, dim in ((4, 2, 64), (28, 4, 128)):
