@@ -107,7 +107,7 @@ class KVPool:
         n = len(self.k_pages)
         self._k = (c_void_p * n)(*[t.data_ptr() for t in self.k_pages])
         self._v = (c_void_p * n)(*[t.data_ptr() for t in self.v_pages])
-        self.num_pages = int(self.k_pages[0].shape[0])
+        self.num_pages, self.n_kv_heads, _, self.head_dim = (int(x) for x in self.k_pages[0].shape)
         self.c = abi.KVPool(self._k, self._v, self.num_pages)
 
 
@@ -151,6 +151,13 @@ def _int32_on_device(name: str, t: torch.Tensor, n: int) -> torch.Tensor:
     return t
 
 
+def _one_device(tensors: Sequence[torch.Tensor]) -> int:
+    devices = {t.get_device() for t in tensors}
+    if len(devices) > 1:
+        raise ValueError("the page tables are on different devices")
+    return devices.pop() if devices else -1
+
+
 class Chunks:
     """The new rows of a step's requests (see crf_chunk), packed in order: ``n_new[i]`` rows at positions
     ``pos[i]`` on of the request cached on ``page_tables[i]``. ``n_keys[i]`` (default ``pos + n_new``)
@@ -163,6 +170,7 @@ class Chunks:
             raise ValueError("page_tables, n_new, pos and n_keys must have one entry a request")
         self.page_tables = list(page_tables)
         self.n, self.rows = n, sum(n_new)
+        self.device = _one_device(self.page_tables)
         self.append_entries, self.attend_entries = [], []
         self.c = (abi.Chunk * max(1, n))()
         for i, t in enumerate(self.page_tables):
@@ -187,6 +195,7 @@ class PageTables:
         if len(n_tokens) != n or (outs is not None and len(outs) != n):
             raise ValueError("tables, n_tokens and outs must have one entry a request")
         self.tables, self.outs = list(tables), None if outs is None else list(outs)
+        self.device = _one_device(self.tables + (self.outs or []))
         self.n = n
         self.c = (abi.Pages * max(1, n))()
         for i, t in enumerate(self.tables):
@@ -197,6 +206,7 @@ class PageTables:
             self.c[i] = abi.Pages(int(n_tokens[i]), t.data_ptr(), None if outs is None else outs[i].data_ptr())
 
 
+_HeadsPair = abi.Heads * 2
 _TYPES = {torch.bfloat16: abi.BF16, torch.float16: abi.FP16, torch.float32: abi.FP32}
 
 
@@ -327,9 +337,10 @@ class Context:
         return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else _stream(stream)
 
     def _here(self, *tensors: Optional[torch.Tensor]) -> None:
+        device = self.device
         for t in tensors:
-            if t is not None and t.get_device() != self.device:
-                raise ValueError(f"every tensor of the call must be on cuda:{self.device}")
+            if t is not None and t.get_device() != device:
+                raise ValueError(f"every tensor of the call must be on cuda:{device}")
 
     def rotary(self, rope: Rope, positions: torch.Tensor, x: torch.Tensor, out: Optional[torch.Tensor] = None,
                k: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, inverse: bool = False,
@@ -342,20 +353,28 @@ class Context:
         if x.dtype not in _TYPES:
             raise ValueError("x must be bfloat16, float16 or float32")
         _int32_on_device("positions", positions, n)
-        parts = (abi.Heads * 2)()
-        parts[0] = _heads("x", x, x if out is None else out, rope.head_dim)
-        if k is not None:
+        first = _heads("x", x, x if out is None else out, rope.head_dim)
+        if k is None:
+            parts = byref(first)
+        else:
             if k.dtype != x.dtype or k.shape[0] != n:
                 raise ValueError("k must have x's type and rows")
-            parts[1] = _heads("k", k, k if k_out is None else k_out, rope.head_dim)
-        abi.check(self.lib.crf_rotary(self.h, byref(rope.c), parts, 1 if k is None else 2, _TYPES[x.dtype], n,
-                                      positions.data_ptr(), int(inverse), self._stream_here(stream)))
+            parts = _HeadsPair(first, _heads("k", k, k if k_out is None else k_out, rope.head_dim))
+        status = self.lib.crf_rotary(self.h, byref(rope.c), parts, 1 if k is None else 2, _TYPES[x.dtype], n,
+                                     positions.data_ptr(), inverse, self._stream_here(stream))
+        if status:
+            abi.check(status)
 
     def _pool_layer(self, pool: KVPool, layer: int) -> Tuple[int, int]:
         if not 0 <= layer < len(pool.k_pages):
             raise ValueError(f"layer {layer} is not in the pool")
-        k = pool.k_pages[layer]
-        return int(k.shape[1]), int(k.shape[3])
+        if pool.k_pages[layer].get_device() != self.device:
+            raise ValueError(f"the pool must be on cuda:{self.device}")
+        return pool.n_kv_heads, pool.head_dim
+
+    def _tables_here(self, device: int) -> None:
+        if device != self.device:
+            raise ValueError(f"the page tables must be on cuda:{self.device}")
 
     def cache_append(self, pool: KVPool, layer: int, chunks: Chunks, k: torch.Tensor, v: torch.Tensor,
                      q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
@@ -364,15 +383,18 @@ class Context:
         position when ``rope`` is given; and ``q`` rotated into ``q_out`` (default: in place)."""
         hkv, dim = self._pool_layer(pool, layer)
         self._here(k, v, q, q_out)
+        self._tables_here(chunks.device)
         if not chunks.append_ok:
             raise ValueError(f"page tables need {chunks.append_entries} entries to append")
         for name, t in (("k", k), ("v", v), ("q", q)):
             if t is not None and (t.dtype != torch.bfloat16 or t.shape[0] != chunks.rows):
                 raise ValueError(f"{name} must be bfloat16 with {chunks.rows} rows")
         qh = None if q is None else byref(_heads("q", q, q if q_out is None else q_out, dim))
-        abi.check(self.lib.crf_cache_append(self.h, None if rope is None else byref(rope.c), byref(pool.c), layer,
-                                            hkv, dim, chunks.c, chunks.n, qh, byref(_heads("k", k, None, dim)),
-                                            byref(_heads("v", v, None, dim)), self._stream_here(stream)))
+        status = self.lib.crf_cache_append(self.h, None if rope is None else byref(rope.c), byref(pool.c), layer, hkv, dim,
+                                           chunks.c, chunks.n, qh, byref(_heads("k", k, None, dim)),
+                                           byref(_heads("v", v, None, dim)), self._stream_here(stream))
+        if status:
+            abi.check(status)
 
     def chunk_attention_workspace(self, pool: KVPool, chunks: Chunks, n_q_heads: int, causal: bool = True,
                                   window: int = 0) -> torch.Tensor:
@@ -390,16 +412,20 @@ class Context:
         ``layer`` (see crf_chunk_attention); ``lse`` fp32 [rows, heads]; ``scale`` 0: 1 / sqrt(head_dim)."""
         hkv, dim = self._pool_layer(pool, layer)
         self._here(q, out, workspace, lse)
+        self._tables_here(chunks.device)
         if not chunks.attend_ok:
             raise ValueError(f"page tables need {chunks.attend_entries} entries to attend")
         if q.dtype != torch.bfloat16 or q.shape[0] != chunks.rows:
             raise ValueError(f"q must be bfloat16 with {chunks.rows} rows")
-        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.shape != q.shape[:2]):
+        heads = _heads("q", q, out, dim)
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
+                                or tuple(lse.shape) != (chunks.rows, heads.heads)):
             raise ValueError("lse must be a contiguous float32 [rows, heads]")
-        abi.check(self.lib.crf_chunk_attention(self.h, byref(pool.c), layer, hkv, dim, chunks.c, chunks.n,
-                                               byref(_heads("q", q, out, dim)), _ptr(lse), scale, int(causal),
-                                               window, workspace.data_ptr(), workspace.numel(),
-                                               self._stream_here(stream)))
+        status = self.lib.crf_chunk_attention(self.h, byref(pool.c), layer, hkv, dim, chunks.c, chunks.n, byref(heads),
+                                              None if lse is None else lse.data_ptr(), scale, causal, window,
+                                              workspace.data_ptr(), workspace.numel(), self._stream_here(stream))
+        if status:
+            abi.check(status)
 
     # -------------------------------------------------------------- pages
     def pages_workspace(self, num_pages: int, tables: PageTables) -> torch.Tensor:
@@ -433,17 +459,23 @@ class Context:
         if tables.outs is None:
             raise ValueError("the tables need outs")
         self._here(workspace)
+        self._tables_here(tables.device)
         a, b = self._refs(pool.num_pages, refs, refs_out)
-        abi.check(call(self.h, byref(pool.c), len(pool.k_pages), hkv, dim, a, b, tables.c, tables.n, *flags,
-                       workspace.data_ptr(), workspace.numel(), self._stream_here(stream)))
+        status = call(self.h, byref(pool.c), len(pool.k_pages), hkv, dim, a, b, tables.c, tables.n, *flags,
+                      workspace.data_ptr(), workspace.numel(), self._stream_here(stream))
+        if status:
+            abi.check(status)
 
     def pages_release(self, refs: torch.Tensor, tables: PageTables, workspace: torch.Tensor,
                       refs_out: Optional[torch.Tensor] = None, stream=None) -> None:
         """Every table entry gives its reference back."""
         self._here(workspace)
+        self._tables_here(tables.device)
         a, b = self._refs(refs.numel(), refs, refs_out)
-        abi.check(self.lib.crf_pages_release(self.h, refs.numel(), a, b, tables.c, tables.n, workspace.data_ptr(),
-                                             workspace.numel(), self._stream_here(stream)))
+        status = self.lib.crf_pages_release(self.h, refs.numel(), a, b, tables.c, tables.n, workspace.data_ptr(),
+                                            workspace.numel(), self._stream_here(stream))
+        if status:
+            abi.check(status)
 
     def check(self, stream=None) -> None:
         abi.check(self.lib.crf_check(self.h, _stream(stream)))

@@ -65,8 +65,9 @@ crf_status check_rope(const crf_rope& r) {
 void fill_turns(const crf_rope& r, uint64_t* turns) {
   const double two_pi = 6.283185307179586476925286766559;
   const double theta = r.scaling == CRF_ROPE_BASE ? r.theta * std::pow(r.factor, r.rot_dim / (r.rot_dim - 2.0)) : r.theta;
+  const double step = -2.0 / r.rot_dim * std::log2(theta);
   for (int i = 0; i < r.rot_dim / 2; ++i) {
-    double f = std::pow(theta, -2.0 * i / r.rot_dim);
+    double f = std::exp2(step * i);
     if (r.scaling == CRF_ROPE_LINEAR) f /= r.factor;
     if (r.scaling == CRF_ROPE_BANDS) {
       double g = (r.original * f / two_pi - r.low) / (r.high - r.low);
@@ -108,6 +109,8 @@ RotPart part_of(const crf_heads& h, bool rotate) {
   return p;
 }
 
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
+
 // Outputs of rows and heads must not share elements: the strides are at least the extents they step over,
 // in one order or the other.
 crf_status check_out(const void* out, int64_t row, int64_t head, int heads, int64_t rows, int dim, const char* name) {
@@ -132,6 +135,7 @@ crf_status fill_chunks(const crf_chunk* chunks, int n, bool attend, int num_page
       return fail(CRF_EINVAL, "chunk %d: n_new, pos or n_keys out of range", i);
     if (!c.page_table && (attend ? c.n_new > 0 && c.n_keys > 0 : c.n_new > 0))
       return fail(CRF_EINVAL, "chunk %d: page table is null", i);
+    if (!aligned4(c.page_table)) return fail(CRF_EINVAL, "chunk %d: page table misaligned", i);
     t->row0[i] = static_cast<int>(rows);
     t->pos[i] = c.pos;
     t->n_keys[i] = c.n_keys;
@@ -190,6 +194,7 @@ crf_status fill_tables(const crf_pages* tables, int n, int num_pages, bool has_o
     const crf_pages& p = tables[i];
     if (p.n_tokens < 0 || p.n_tokens > (1 << 30)) return fail(CRF_EINVAL, "table %d: n_tokens out of range", i);
     if (p.n_tokens > 0 && (!p.table || (has_out && !p.out))) return fail(CRF_EINVAL, "table %d: null pointer", i);
+    if (!aligned4(p.table) || (has_out && !aligned4(p.out))) return fail(CRF_EINVAL, "table %d: misaligned pointer", i);
     t->first[i] = static_cast<int>(entries);
     t->fresh0[i] = static_cast<int>(fresh);
     t->n_tokens[i] = p.n_tokens;
@@ -211,7 +216,8 @@ crf_status run_pages(crf_ctx* ctx, PageOp op, const crf_kv_pool* pool, int n_lay
                      int num_pages, const int32_t* refs_in, int32_t* refs_out, const crf_pages* tables, int n_tables,
                      bool deep, void* workspace, size_t ws_bytes, void* stream) {
   if (!ctx) return fail(CRF_EINVAL, "ctx is null");
-  if (!refs_in || !refs_out) return fail(CRF_EINVAL, "reference counts are null");
+  if (!refs_in || !refs_out || !aligned4(refs_in) || !aligned4(refs_out))
+    return fail(CRF_EINVAL, "reference counts null or misaligned");
   if (op != kPageRelease) {
     if (n_layers < 1) return fail(CRF_EINVAL, "n_layers must be positive");
     crf_status s = check_pool_shape(n_kv_heads, head_dim, num_pages);
@@ -250,7 +256,7 @@ crf_status crf_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts
     if (type < CRF_BF16 || type > CRF_FP32) return fail(CRF_EUNSUPPORTED, "unknown element type %d", type);
     if (n_rows < 0) return fail(CRF_EINVAL, "n_rows must be >= 0");
     if (n_rows == 0) return CRF_OK;
-    if (!positions) return fail(CRF_EINVAL, "positions is null");
+    if (!positions || !aligned4(positions)) return fail(CRF_EINVAL, "positions null or misaligned");
     RotaryDesc d;
     std::memset(&d, 0, sizeof(d));
     for (int p = 0; p < n_parts; ++p) {
@@ -394,6 +400,7 @@ crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer,
     s = check_out(q->out, q->out_row, q->out_head, q->heads, rows, head_dim, "q");
     if (s != CRF_OK) return s;
     if (q->x == q->out) return fail(CRF_EINVAL, "q: o may not be written over q");
+    if (!aligned4(lse)) return fail(CRF_EINVAL, "lse misaligned");
     ChunkPlan plan;
     plan_chunk_attention(t, q->heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
     s = check_workspace(workspace, ws_bytes, chunk_attention_workspace(plan, head_dim));

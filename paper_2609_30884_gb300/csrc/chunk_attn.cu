@@ -1064,13 +1064,18 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_attn_merge(const __grid_c
 }
 
 // ---------------------------------------------------------------- plan (host)
-// A segment costs about kSegment steps beside its own (q, the masks, the end): 8192 rows from nothing 427 us with 4,
-// 369 with 6, 370 with 8, 377 with 10; 8 rows of 4K-16K keys 37.6, 38.0, 39.5, 39.5.
+// What runs are dealt by, in units of a wide step's time. A narrow step reads two tiles; a segment costs something beside
+// its steps (q, the masks, the end): 8192 rows from nothing took 427 us with 4 units, 369 with 6, 370 with 8, 377 with 10;
+// 64 single rows over 2000 keys 60 us with 2 or 4, 55 with 6.
 constexpr int kSegment = 6;
+inline int step_units(bool narrow) { return narrow ? 2 : 1; }
+// The merge's launch and run.
+constexpr int kMerge = 2;
 
-// Deals the items' steps to at most `ctas` runs of `budget` (steps and segments' costs), the last one taking what is
-// left; false if that is more.
-bool deal(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int window, int ctas, int64_t budget, ChunkPlan* p) {
+// Deals the items' steps to at most `ctas` runs of at most `budget` units each; false if they do not fit. `whole`:
+// an item a run.
+bool deal(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int window, int ctas, int64_t budget, bool whole,
+          ChunkPlan* p) {
   const int grp = n_q_heads / n_kv_heads;
   p->ctas = 0;
   p->part_rows = p->cuts = p->merge_rows = 0;
@@ -1085,7 +1090,7 @@ bool deal(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int w
     const int rows = (c.row0[i + 1] - c.row0[i]) * grp;
     if (rows == 0) continue;
     const bool narrow = narrow_form(rows);
-    const int tile = narrow ? kM : 2 * kM, tiles = (rows + tile - 1) / tile;
+    const int unit = step_units(narrow), tile = narrow ? kM : 2 * kM, tiles = (rows + tile - 1) / tile;
     for (int qt = tiles - 1; qt >= 0; --qt) {
       const int q0 = qt * tile, q1 = std::min(q0 + tile, rows) - 1;
       const int steps = tiles_of(keys_of_rows(c.pos[i] + q0 / grp, c.pos[i] + q1 / grp, c.n_keys[i], causal, window), narrow).steps;
@@ -1093,18 +1098,18 @@ bool deal(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int w
         int step = 0, first_cta = -1, first_slot = 0, parts = 0;
         do {
           // a segment of at least one step (or the whole of an empty item) starts only where it fits the budget
-          if (p->ctas == 0 || left < kSegment + std::min(steps - step, 1)) {
+          if (p->ctas == 0 || whole || left < kSegment + std::min(steps - step, 1) * unit) {
             if (p->ctas == ctas) return false;
             open(i, qt, g, step);
           }
           left -= kSegment;
-          const int take = static_cast<int>(std::min<int64_t>(steps - step, left));
+          const int take = whole ? steps : static_cast<int>(std::min<int64_t>(steps - step, left / unit));
           if (parts++ == 0) {
             first_cta = p->ctas - 1;
             first_slot = 2 * first_cta + (here > 0 ? 1 : 0);
           }
           ++here;
-          left -= take;
+          left -= take * unit;
           step += take;
         } while (step < steps);
         if (parts > 1) {
@@ -1125,25 +1130,30 @@ bool deal(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int w
 
 void plan_chunk_attention(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms, ChunkPlan* p) {
   const int grp = n_q_heads / n_kv_heads, ctas = std::min(num_sms, kMaxCtas);
-  int64_t total = 0;
+  int64_t total = 0, items = 0;
+  int longest = 0, least = 1;  // units of the longest item's steps, of a segment of one step
   for (int i = 0; i < c.n; ++i) {
     const int rows = (c.row0[i + 1] - c.row0[i]) * grp;
     if (rows == 0) continue;
     const bool narrow = narrow_form(rows);
-    const int tile = narrow ? kM : 2 * kM;
+    const int unit = step_units(narrow), tile = narrow ? kM : 2 * kM;
+    least = std::max(least, kSegment + unit);
     for (int q0 = 0; q0 < rows; q0 += tile) {
       const int q1 = std::min(q0 + tile, rows) - 1;
       const int steps = tiles_of(keys_of_rows(c.pos[i] + q0 / grp, c.pos[i] + q1 / grp, c.n_keys[i], causal, window), narrow).steps;
-      total += static_cast<int64_t>(n_kv_heads) * (steps + kSegment);
+      total += static_cast<int64_t>(n_kv_heads) * (steps * unit + kSegment);
+      items += n_kv_heads;
+      longest = std::max(longest, steps * unit);
     }
   }
-  // an even share, and the cost of the segment that a run continues; runs that end early for want of a whole step
-  // may need a little more
-  int64_t budget = (total + ctas - 1) / ctas;
-  budget = std::max<int64_t>(kSegment + 1, total > ctas ? budget + kSegment : budget);
+  // An even share at first; runs that end early for want of a whole step, and the segments that they continue, need some
+  // more. Few short items stay whole: the merge costs more than the steps that it saves.
+  int64_t budget = std::max<int64_t>(least, (total + ctas - 1) / ctas);
+  const bool whole = items <= ctas && longest <= budget - kSegment + kMerge;
+  if (items > 2 * ctas) budget += kSegment;  // nearly every run continues a segment: fewer tries
   for (int tries = 0;; ++tries) {
-    if (deal(c, n_q_heads, n_kv_heads, causal, window, ctas, budget, p)) return;
-    budget += 1 + (tries < 4 ? 0 : budget / 8);
+    if (deal(c, n_q_heads, n_kv_heads, causal, window, ctas, budget, whole, p)) return;
+    budget += tries < 12 ? 1 : budget / 8 + 1;
   }
 }
 

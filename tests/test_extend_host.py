@@ -145,6 +145,7 @@ def test_rotary_argument_refusals(lib, ctx):
     assert lib.crf_rotary(ctx, ref(rope()), None, 1, 0, 1, A16, 0, None) == EINVAL
     assert call_rotary(lib, ctx, n_parts=0) == EINVAL and call_rotary(lib, ctx, n_parts=3) == EINVAL
     assert call_rotary(lib, ctx, type=3) == EUNSUPPORTED and call_rotary(lib, ctx, type=-1) == EUNSUPPORTED
+    assert call_rotary(lib, ctx, positions=A16 + 1) == EINVAL
     assert call_rotary(lib, ctx, rows=-1) == EINVAL and call_rotary(lib, ctx, positions=None) == EINVAL
     assert call_rotary(lib, ctx, rows=0, positions=None) == abi.OK  # nothing to do
 
@@ -174,10 +175,10 @@ def test_append_of_no_rows_is_nothing(lib, ctx):
 
 
 def call_attention(lib, ctx, pl=None, layer=0, hkv=2, d=64, ch=((3, 5, 8, A16),), q=None, scale=0.0, window=0, ws=A16,
-                   ws_bytes=1 << 30, n=None):
+                   ws_bytes=1 << 30, n=None, lse=None):
     c = chunks(*ch)
     return lib.crf_chunk_attention(ctx, ref(pl or pool()), layer, hkv, d, c, len(ch) if n is None else n, ref(q or heads()),
-                                   None, scale, 1, window, ws, ws_bytes, None)
+                                   lse, scale, 1, window, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -186,7 +187,8 @@ def call_attention(lib, ctx, pl=None, layer=0, hkv=2, d=64, ch=((3, 5, 8, A16),)
     (dict(ch=((1, 5, -1, A16),)), EINVAL), (dict(ch=((1, 5, (1 << 30) + 1, A16),)), EINVAL), (dict(ch=((1, 5, 6, None),)), EINVAL),
     (dict(q=heads(x=A16 + 2)), EINVAL), (dict(q=heads(x_row=260)), EUNSUPPORTED), (dict(q=heads(out_head=68)), EUNSUPPORTED),
     (dict(q=heads(out=A16)), EINVAL), (dict(q=heads(out_row=64)), ESHAPE), (dict(q=heads(heads=3)), ESHAPE),
-    (dict(pl=pool(k=None)), EINVAL),
+    (dict(pl=pool(k=None)), EINVAL), (dict(ch=((1, 5, 6, A16 + 2),)), EINVAL), (dict(lse=A16 + 2), EINVAL),
+    (dict(ch=((1 << 29, 0, 1 << 29, A16),)), EUNSUPPORTED),
 ])
 def test_attention_refusals(lib, ctx, kw, status):
     assert call_attention(lib, ctx, **kw) == status
@@ -218,6 +220,7 @@ def tables(*t):
 
 PAGE_BAD = [
     (dict(t=((-1, A16, A16),)), EINVAL), (dict(t=(((1 << 30) + 1, A16, A16),)), EINVAL), (dict(t=((1, None, A16),)), EINVAL),
+    (dict(t=((1, A16 + 1, A16),)), EINVAL), (dict(refs=A16 + 2), EINVAL),
     (dict(n=0), EINVAL), (dict(n=513), EINVAL), (dict(refs=None), EINVAL), (dict(refs_out=None), EINVAL),
     (dict(ws=None), EINVAL), (dict(ws=A16 + 64), EINVAL), (dict(ws_bytes=64), ENOMEM),
 ]
@@ -286,6 +289,28 @@ def test_page_tables_marshalling():
                 lambda: crf.PageTables([t, t], [40]), lambda: crf.PageTables([t.float()], [40])):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_a_context_of_a_gpu_refuses_tensors_elsewhere(lib):
+    """The binding looks at where tensors are before it takes their addresses."""
+    ctx = crf.Context.__new__(crf.Context)
+    ctx.device, ctx.h, ctx.lib = 0, None, lib
+    t, x = torch.zeros(4, dtype=torch.int32), torch.zeros(2, 3, 64, dtype=torch.bfloat16)
+    ws = torch.zeros(256, dtype=torch.uint8)
+    pool = crf.KVPool([torch.zeros(4, 3, 16, 64, dtype=torch.bfloat16)], [torch.zeros(4, 3, 16, 64, dtype=torch.bfloat16)])
+    assert (pool.n_kv_heads, pool.head_dim) == (3, 64)
+    with pytest.raises(ValueError):
+        ctx.rotary(crf.Rope(64), t, x)
+    with pytest.raises(ValueError):
+        ctx.cache_append(pool, 0, crf.Chunks([t], [2], [0]), x, x)
+    with pytest.raises(ValueError):
+        ctx.chunk_attention(pool, 0, crf.Chunks([t], [2], [0]), x, torch.zeros_like(x), ws)
+    with pytest.raises(ValueError):
+        ctx.chunk_attention(pool, 1, crf.Chunks([t], [2], [0]), x, torch.zeros_like(x), ws)
+    with pytest.raises(ValueError):
+        ctx.pages_fork(pool, t, crf.PageTables([t], [16], [t]), ws)
+    with pytest.raises(ValueError):
+        ctx.pages_release(t, crf.PageTables([t], [16]), ws)
 
 
 def test_heads_marshalling():

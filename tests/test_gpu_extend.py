@@ -706,6 +706,171 @@ def test_calls_on_other_streams_and_captured(ctx):
     ctx.check()
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_calls_see_what_was_just_written(ctx, captured):
+    """Inputs made by a copy, a fill and a kernel right before each call, on two joined streams; every kernel of these
+    calls may become resident early, and none may read early."""
+    s = Setup(44, 12, 2, 128, [(3, 700), (1, 2500)], poison=False)
+    p = Pool(45, [100, 40], 20, layers=1)
+    tables, outs = p.page_tables()
+    pws, refs2 = ctx.pages_workspace(p.total, tables), torch.empty_like(p.refs)
+    b = s.batch()
+    ws = ctx.chunk_attention_workspace(s.pool, b, s.hq)
+    rope = crf.Rope(128, theta=1e6)
+    src = [normal(gen(46 + i), s.rows, h, 128) for i, h in enumerate((12, 2, 2))]
+    x, k, v = (torch.empty_like(t) for t in src)
+    q, out, lse, refs = torch.empty_like(x), torch.empty_like(x), torch.empty(s.rows, 12, device=DEV), torch.empty_like(p.refs)
+    counts, side = p.refs.clone(), torch.cuda.Stream()
+    big = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+
+    def calls():
+        here = torch.cuda.current_stream()
+        side.wait_stream(here)
+        with torch.cuda.stream(side):
+            big.fill_(1)                      # a while
+            refs.copy_(counts)                # device to device
+            ctx.pages_fork(p.pool, refs, tables, pws, refs_out=refs2)
+            k.copy_(src[1])
+        x.zero_()
+        x.add_(src[0])                        # a kernel
+        v.copy_(src[2])
+        here.wait_stream(side)
+        ctx.cache_append(s.pool, 0, b, k, v, q=x, q_out=q, rope=rope)
+        ctx.chunk_attention(s.pool, 0, b, q, out, ws, lse=lse)
+        out.mul_(2)                           # and a kernel behind
+
+    calls()
+    torch.cuda.synchronize()
+    first = [t.clone() for t in (q, out, lse, refs2, *outs)]
+    assert torch.equal(refs2, fork_counts(p, counts))
+    graph = None
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls()
+    for i in range(20):
+        for t in (x, k, v, q, out, lse, refs, refs2, *outs):
+            t.fill_(i)
+        for t in src:
+            t.neg_()
+        counts[p.tables[0].long()[0]] += 1
+        graph.replay() if captured else calls()
+        torch.cuda.synchronize()
+        # q and k change their signs together: the same scores, the values' signs turned for the new rows alone
+        assert torch.equal(q, first[0] if i % 2 else -first[0])
+        assert torch.equal(refs2, fork_counts(p, counts)) and all(torch.equal(a, c) for a, c in zip(outs, first[4:]))
+        if i % 2:
+            assert torch.equal(out, first[1]) and torch.equal(lse, first[2])
+    ctx.check()
+
+
+def fork_counts(p, refs):
+    """Counts after a shallow fork of the pool's tables."""
+    out, free = refs.clone(), (refs == 0).nonzero().squeeze(1)
+    fresh = 0
+    for t, n in zip(p.tables, p.tokens):
+        out.index_add_(0, t[: n // PAGE].long(), torch.ones_like(t[: n // PAGE]))
+        fresh += n % PAGE > 0
+    out[free[:fresh]] = 1
+    return out
+
+
+def test_calls_at_the_end_of_a_large_pool(ctx):
+    """Pages whose elements lie behind 2^31: a layer's pool of 4.5 GB."""
+    hq, hkv, dim, pages = 28, 4, 128, 275000
+    assert pages * hkv * PAGE * dim > 2**31
+    kp, vp = (torch.empty(pages, hkv, PAGE, dim, dtype=BF16, device=DEV) for _ in range(2))
+    g = gen(47)
+    table = ints(pages - 1, pages - 7, 3, pages - 2, pages - 3)
+    n, m = 70, 9
+    k, v = normal(g, n, hkv, dim), normal(g, n, hkv, dim)
+    pool = crf.KVPool([kp], [vp])
+    ctx.cache_append(pool, 0, crf.Chunks([table], [n], [0]), k, v)
+    at = torch.arange(n, device=DEV)
+    assert torch.equal(kp[table.long()[at // PAGE], :, at % PAGE], k)
+    assert torch.equal(vp[table.long()[at // PAGE], :, at % PAGE], v)
+    q, out = normal(g, m, hq, dim), torch.empty(m, hq, dim, dtype=BF16, device=DEV)
+    b = crf.Chunks([table], [m], [n - m])
+    ctx.chunk_attention(pool, 0, b, q, out, ctx.chunk_attention_workspace(pool, b, hq))
+    z = torch.einsum("mgrd,ngd->mgrn", q.double().view(m, hkv, -1, dim), k.double()) * dim**-0.5
+    z = z.masked_fill((at > torch.arange(n - m, n, device=DEV)[:, None])[:, None, None], -math.inf)
+    w = z.softmax(-1)
+    want = torch.einsum("mgrn,ngd->mgrd", w, v.double()).reshape(m, hq, dim)
+    size = torch.einsum("mgrn,ngd->mgrd", w, v.double().abs()).reshape(m, hq, dim)
+    assert bool(((out.double() - want).abs() <= size * (2.0**-8 + 2.0**-12) + want.abs() * 2.0**-8 * 1.01).all())
+    refs = torch.zeros(pages, dtype=torch.int32, device=DEV)
+    refs[:-60] = 1  # nearly full: the new pages are the last ones
+    refs[table.long()] = 1
+    child = torch.empty_like(table)
+    t = crf.PageTables([table], [n], [child])
+    free = (refs == 0).nonzero().squeeze(1)
+    ctx.pages_fork(pool, refs, t, ctx.pages_workspace(pages, t), deep=True)
+    ctx.check()
+    assert torch.equal(child.long(), free[:5])
+    assert torch.equal(kp[child.long()[at // PAGE], :, at % PAGE], k) and torch.equal(vp[child.long()[at // PAGE], :, at % PAGE], v)
+
+
+def test_one_parent_forked_twice_in_a_call(ctx):
+    s = Pool(48, [100, 40], 20, layers=2)
+    lists = [s.tables[0].tolist()] * 2
+    want, refs, k, v = fork_model(lists, [100, 100], s.refs.tolist(), s.k, s.v, False)
+    outs = [torch.full_like(s.tables[0], -7) for _ in range(2)]
+    t = crf.PageTables([s.tables[0]] * 2, [100, 100], outs)
+    ctx.pages_fork(s.pool, s.refs, t, ctx.pages_workspace(s.total, t))
+    ctx.check()
+    assert [o.tolist() for o in outs] == want and s.refs.tolist() == refs and torch.equal(s.k, k) and torch.equal(s.v, v)
+
+
+def test_continuation_matches_recomputation(ctx):
+    """A prefix's cache from crf_recompute_window, extended by new rows layer by layer with these calls, against the
+    window call over the whole: the same rotation, layout and attention."""
+    import synth
+    from tests.harness import DeviceAdapter, DeviceModel, make_pool, split_page_tables
+    from tests.gpu_util import REL_KVH, rel_frob, request_kv, to_np
+    cfg, n, m = synth.TINY, 203, 70
+    dm, ad = DeviceModel(cfg, DEV), DeviceAdapter(cfg, synth.LORA_TINY, 1, DEV)
+    total = pages_for(n + m) + 4
+    tokens = synth.token_ids(cfg, n + m).to(DEV)
+    table = split_page_tables([n + m], total, seed=5, device=DEV)[0]
+    whole, part = make_pool(cfg, total, DEV, fill="zeros"), make_pool(cfg, total, DEV, fill="zeros")
+    H = [torch.empty(n + m, cfg.hidden, dtype=BF16, device=DEV) for _ in range(cfg.n_layers)]
+    for pool, count, hidden in ((whole, n + m, H), (part, n, None)):
+        r = crf.Request(table, 0, cfg.n_layers, n_tokens=count, tokens=tokens, hidden_out=hidden)
+        ctx.recompute_window(dm.crf, ad.crf, pool, [r], ctx.workspace(dm.crf, ad.crf, [r]))
+    ctx.check()
+    scale = ad.lcfg.alpha / ad.lcfg.rank
+
+    def project(x, l, name):
+        w = dm.layers[l][f"W_{name}"].float()
+        if name in ad.layers[l]:
+            a, b = ad.layers[l][name]
+            w = w + scale * b.float() @ a.float()
+        return x.float() @ w.T
+
+    def norm(x, gain):
+        x = x.float()
+        return (x * torch.rsqrt((x * x).mean(-1, keepdim=True) + cfg.rms_eps) * gain.float()).to(BF16)
+
+    b = crf.Chunks([table], [m], [n])
+    rope = crf.Rope(cfg.head_dim, theta=cfg.rope_theta)
+    ws = ctx.chunk_attention_workspace(part, b, cfg.n_q_heads)
+    x = dm.embed[tokens[n:].long()]
+    for l in range(cfg.n_layers):
+        y = norm(x, dm.layers[l]["ln1"])
+        q, k, v = (project(y, l, name).to(BF16).view(m, -1, cfg.head_dim) for name in "qkv")
+        out = torch.empty_like(q)
+        ctx.cache_append(part, l, b, k, v, q=q, rope=rope)
+        ctx.chunk_attention(part, l, b, q, out, ws)
+        x = (x.float() + project(out.view(m, -1), l, "o")).to(BF16)
+        y = norm(x, dm.layers[l]["ln2"])
+        g = project(y, l, "gate")
+        x = (x.float() + project((torch.nn.functional.silu(g) * project(y, l, "up")).to(BF16), l, "down")).to(BF16)
+        assert rel_frob(to_np(x), to_np(H[l][n:])) <= REL_KVH, l
+        for a, c in ((part.k_pages[l], whole.k_pages[l]), (part.v_pages[l], whole.v_pages[l])):
+            assert rel_frob(request_kv(a, table, n + m), request_kv(c, table, n + m)) <= REL_KVH, l
+    ctx.check()
+
+
 def test_two_continuations_of_a_recovered_prefix(ctx):
     """Fork, append, attend, release, compact: two continuations of one prefix against plain caches."""
     g = gen(51)
