@@ -27,6 +27,7 @@ A recovered cache is extended with new tokens by calls of one layer and of the p
 from __future__ import annotations
 
 import ctypes
+import struct
 from ctypes import POINTER, byref, c_size_t, c_void_p
 from typing import Dict, List, Optional, Sequence, Tuple
 
@@ -109,6 +110,7 @@ class KVPool:
         self._v = (c_void_p * n)(*[t.data_ptr() for t in self.v_pages])
         self.num_pages, self.n_kv_heads, _, self.head_dim = (int(x) for x in self.k_pages[0].shape)
         self.c = abi.KVPool(self._k, self._v, self.num_pages)
+        self.address = ctypes.addressof(self.c)
 
 
 class Request:
@@ -143,6 +145,7 @@ class Rope:
         self.head_dim = head_dim
         self.c = abi.Rope(head_dim, head_dim if rot_dim is None else rot_dim, abi.ROPE_LAYOUTS[layout],
                           abi.ROPE_SCALINGS[scaling], theta, factor, low, high, original, magnitude)
+        self.address = ctypes.addressof(self.c)
 
 
 def _int32_on_device(name: str, t: torch.Tensor, n: int) -> torch.Tensor:
@@ -181,6 +184,7 @@ class Chunks:
             self.append_entries.append((p + m + 15) // 16 if m else 0)
             self.attend_entries.append((k + 15) // 16 if m else 0)
             self.c[i] = abi.Chunk(m, p, k, t.data_ptr())
+        self.address = ctypes.addressof(self.c)
         self.append_ok = all(t.numel() >= e for t, e in zip(self.page_tables, self.append_entries))
         self.attend_ok = all(t.numel() >= e for t, e in zip(self.page_tables, self.attend_entries))
 
@@ -204,28 +208,40 @@ class PageTables:
             if outs is not None:
                 _int32_on_device(f"outs[{i}]", outs[i], need)
             self.c[i] = abi.Pages(int(n_tokens[i]), t.data_ptr(), None if outs is None else outs[i].data_ptr())
+        self.address = ctypes.addressof(self.c)
 
 
-_HeadsPair = abi.Heads * 2
 _TYPES = {torch.bfloat16: abi.BF16, torch.float16: abi.FP16, torch.float32: abi.FP32}
+# The current stream's handle: a torch.cuda.Stream object costs a small call as much as half its launch.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda d: torch.cuda.current_stream(d).cuda_stream)
+# crf_heads, packed into a context's buffer: building the ctypes structures takes three times as long.
+_pack_heads = struct.Struct("PPiqqqq").pack_into
+_HEADS = ctypes.sizeof(abi.Heads)
 
 
-def _heads(name: str, x: torch.Tensor, out: Optional[torch.Tensor], dim: int) -> abi.Heads:
-    """crf_heads of x [rows, heads, dim] and out, of any row and head strides."""
+def _put_heads(buf, at: int, device: int, name: str, x: torch.Tensor, out: Optional[torch.Tensor], dim: int) -> int:
+    """crf_heads of x [rows, heads, dim] and out (any row and head strides) at ``buf[at:]``; the heads."""
     shape = x.shape
     if len(shape) != 3 or shape[2] != dim:
         raise ValueError(f"{name} must be [rows, heads, {dim}]")
+    if x.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device}")
     row, head, one = x.stride()
     if out is None:
-        if one != 1:
+        _pack_heads(buf, at, x.data_ptr(), 0, shape[1], row, head, 0, 0)
+    elif out is x:
+        p = x.data_ptr()
+        _pack_heads(buf, at, p, p, shape[1], row, head, row, head)
+    else:
+        if out.shape != shape or out.dtype != x.dtype or out.get_device() != device:
+            raise ValueError(f"{name}: the output must have the input's shape, type and device")
+        out_row, out_head, out_one = out.stride()
+        if out_one != 1:
             raise ValueError(f"{name}: the elements of a head must be adjacent")
-        return abi.Heads(x.data_ptr(), None, shape[1], row, head, 0, 0)
-    if out is not x and (out.shape != shape or out.dtype != x.dtype):
-        raise ValueError(f"{name}: the output must have the input's shape and type")
-    out_row, out_head, out_one = out.stride()
-    if one != 1 or out_one != 1:
+        _pack_heads(buf, at, x.data_ptr(), out.data_ptr(), shape[1], row, head, out_row, out_head)
+    if one != 1:
         raise ValueError(f"{name}: the elements of a head must be adjacent")
-    return abi.Heads(x.data_ptr(), out.data_ptr(), shape[1], row, head, out_row, out_head)
+    return shape[1]
 
 
 def _req_array(reqs: Sequence[Request]):
@@ -244,6 +260,7 @@ class Context:
         h = c_void_p()
         abi.check(self.lib.crf_create(byref(h), device))
         self.h = h
+        self._parts = ctypes.create_string_buffer(3 * _HEADS)
 
     def close(self) -> None:
         if self.h:
@@ -333,8 +350,7 @@ class Context:
 
     # -------------------------------------------------------------- extension by new tokens
     def _stream_here(self, stream) -> int:
-        # the raw handle: a torch.cuda.Stream object costs a small call as much as its launch
-        return torch._C._cuda_getCurrentRawStream(self.device) if stream is None else _stream(stream)
+        return _raw_stream(self.device) if stream is None else _stream(stream)
 
     def _here(self, *tensors: Optional[torch.Tensor]) -> None:
         device = self.device
@@ -348,20 +364,19 @@ class Context:
         """x [rows, heads, head_dim] (bf16, fp16 or fp32, any row and head strides) rotated at
         ``positions`` [rows] into ``out`` (default: in place), and ``k`` likewise into ``k_out``.
         ``inverse``: the transposed map, the gradient of the call without it."""
-        self._here(positions, x, out, k, k_out)
-        n = x.shape[0]
-        if x.dtype not in _TYPES:
+        device, buf, dim = self.device, self._parts, rope.head_dim
+        n, kind = x.shape[0], _TYPES.get(x.dtype)
+        if kind is None:
             raise ValueError("x must be bfloat16, float16 or float32")
+        self._here(positions)
         _int32_on_device("positions", positions, n)
-        first = _heads("x", x, x if out is None else out, rope.head_dim)
-        if k is None:
-            parts = byref(first)
-        else:
+        _put_heads(buf, 0, device, "x", x, x if out is None else out, dim)
+        if k is not None:
             if k.dtype != x.dtype or k.shape[0] != n:
                 raise ValueError("k must have x's type and rows")
-            parts = _HeadsPair(first, _heads("k", k, k if k_out is None else k_out, rope.head_dim))
-        status = self.lib.crf_rotary(self.h, byref(rope.c), parts, 1 if k is None else 2, _TYPES[x.dtype], n,
-                                     positions.data_ptr(), inverse, self._stream_here(stream))
+            _put_heads(buf, _HEADS, device, "k", k, k if k_out is None else k_out, dim)
+        status = self.lib.crf_rotary(self.h, rope.address, buf, 1 if k is None else 2, kind, n, positions.data_ptr(),
+                                     inverse, _raw_stream(device) if stream is None else _stream(stream))
         if status:
             abi.check(status)
 
@@ -382,17 +397,23 @@ class Context:
         """Rows k, v [rows, kv heads, head_dim] into the requests' pages of ``layer``, k rotated at its
         position when ``rope`` is given; and ``q`` rotated into ``q_out`` (default: in place)."""
         hkv, dim = self._pool_layer(pool, layer)
-        self._here(k, v, q, q_out)
-        self._tables_here(chunks.device)
+        device, buf, n = self.device, self._parts, chunks.rows
+        if chunks.device != device:
+            raise ValueError(f"the page tables must be on cuda:{device}")
         if not chunks.append_ok:
             raise ValueError(f"page tables need {chunks.append_entries} entries to append")
-        for name, t in (("k", k), ("v", v), ("q", q)):
-            if t is not None and (t.dtype != torch.bfloat16 or t.shape[0] != chunks.rows):
-                raise ValueError(f"{name} must be bfloat16 with {chunks.rows} rows")
-        qh = None if q is None else byref(_heads("q", q, q if q_out is None else q_out, dim))
-        status = self.lib.crf_cache_append(self.h, None if rope is None else byref(rope.c), byref(pool.c), layer, hkv, dim,
-                                           chunks.c, chunks.n, qh, byref(_heads("k", k, None, dim)),
-                                           byref(_heads("v", v, None, dim)), self._stream_here(stream))
+        bf16 = torch.bfloat16
+        if k.dtype != bf16 or v.dtype != bf16 or k.shape[0] != n or v.shape[0] != n or (
+                q is not None and (q.dtype != bf16 or q.shape[0] != n)):
+            raise ValueError(f"q, k and v must be bfloat16 with {n} rows")
+        at = ctypes.addressof(buf)
+        _put_heads(buf, _HEADS, device, "k", k, None, dim)
+        _put_heads(buf, 2 * _HEADS, device, "v", v, None, dim)
+        if q is not None:
+            _put_heads(buf, 0, device, "q", q, q if q_out is None else q_out, dim)
+        status = self.lib.crf_cache_append(self.h, None if rope is None else rope.address, pool.address, layer, hkv, dim,
+                                           chunks.address, chunks.n, None if q is None else at, at + _HEADS,
+                                           at + 2 * _HEADS, _raw_stream(device) if stream is None else _stream(stream))
         if status:
             abi.check(status)
 
@@ -401,7 +422,7 @@ class Context:
         """Workspace of a chunk_attention call; the same one serves every layer of the step."""
         hkv, dim = self._pool_layer(pool, 0)
         n = c_size_t()
-        abi.check(self.lib.crf_chunk_attention_workspace_size(self.h, n_q_heads, hkv, dim, chunks.c, chunks.n,
+        abi.check(self.lib.crf_chunk_attention_workspace_size(self.h, n_q_heads, hkv, dim, chunks.address, chunks.n,
                                                               int(causal), window, byref(n)))
         return torch.empty(max(256, n.value), dtype=torch.uint8, device=f"cuda:{self.device}")
 
@@ -411,26 +432,28 @@ class Context:
         """out = attention of the rows q [rows, heads, head_dim] (bf16) over their requests' cached keys of
         ``layer`` (see crf_chunk_attention); ``lse`` fp32 [rows, heads]; ``scale`` 0: 1 / sqrt(head_dim)."""
         hkv, dim = self._pool_layer(pool, layer)
-        self._here(q, out, workspace, lse)
-        self._tables_here(chunks.device)
+        device, buf, n = self.device, self._parts, chunks.rows
+        if chunks.device != device:
+            raise ValueError(f"the page tables must be on cuda:{device}")
         if not chunks.attend_ok:
             raise ValueError(f"page tables need {chunks.attend_entries} entries to attend")
-        if q.dtype != torch.bfloat16 or q.shape[0] != chunks.rows:
-            raise ValueError(f"q must be bfloat16 with {chunks.rows} rows")
-        heads = _heads("q", q, out, dim)
-        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
-                                or tuple(lse.shape) != (chunks.rows, heads.heads)):
+        if q.dtype != torch.bfloat16 or q.shape[0] != n:
+            raise ValueError(f"q must be bfloat16 with {n} rows")
+        heads = _put_heads(buf, 0, device, "q", q, out, dim)
+        self._here(workspace, lse)
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (n, heads)):
             raise ValueError("lse must be a contiguous float32 [rows, heads]")
-        status = self.lib.crf_chunk_attention(self.h, byref(pool.c), layer, hkv, dim, chunks.c, chunks.n, byref(heads),
+        status = self.lib.crf_chunk_attention(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, buf,
                                               None if lse is None else lse.data_ptr(), scale, causal, window,
-                                              workspace.data_ptr(), workspace.numel(), self._stream_here(stream))
+                                              workspace.data_ptr(), workspace.numel(),
+                                              _raw_stream(device) if stream is None else _stream(stream))
         if status:
             abi.check(status)
 
     # -------------------------------------------------------------- pages
     def pages_workspace(self, num_pages: int, tables: PageTables) -> torch.Tensor:
         n = c_size_t()
-        abi.check(self.lib.crf_pages_workspace_size(self.h, num_pages, tables.c, tables.n, byref(n)))
+        abi.check(self.lib.crf_pages_workspace_size(self.h, num_pages, tables.address, tables.n, byref(n)))
         return torch.empty(max(256, n.value), dtype=torch.uint8, device=f"cuda:{self.device}")
 
     def _refs(self, num_pages: int, refs: torch.Tensor, refs_out: Optional[torch.Tensor]) -> Tuple[int, int]:
@@ -461,7 +484,7 @@ class Context:
         self._here(workspace)
         self._tables_here(tables.device)
         a, b = self._refs(pool.num_pages, refs, refs_out)
-        status = call(self.h, byref(pool.c), len(pool.k_pages), hkv, dim, a, b, tables.c, tables.n, *flags,
+        status = call(self.h, pool.address, len(pool.k_pages), hkv, dim, a, b, tables.address, tables.n, *flags,
                       workspace.data_ptr(), workspace.numel(), self._stream_here(stream))
         if status:
             abi.check(status)
@@ -472,7 +495,7 @@ class Context:
         self._here(workspace)
         self._tables_here(tables.device)
         a, b = self._refs(refs.numel(), refs, refs_out)
-        status = self.lib.crf_pages_release(self.h, refs.numel(), a, b, tables.c, tables.n, workspace.data_ptr(),
+        status = self.lib.crf_pages_release(self.h, refs.numel(), a, b, tables.address, tables.n, workspace.data_ptr(),
                                             workspace.numel(), self._stream_here(stream))
         if status:
             abi.check(status)

@@ -295,6 +295,7 @@ def test_a_context_of_a_gpu_refuses_tensors_elsewhere(lib):
     """The binding looks at where tensors are before it takes their addresses."""
     ctx = crf.Context.__new__(crf.Context)
     ctx.device, ctx.h, ctx.lib = 0, None, lib
+    ctx._parts = ctypes.create_string_buffer(3 * crf._HEADS)
     t, x = torch.zeros(4, dtype=torch.int32), torch.zeros(2, 3, 64, dtype=torch.bfloat16)
     ws = torch.zeros(256, dtype=torch.uint8)
     pool = crf.KVPool([torch.zeros(4, 3, 16, 64, dtype=torch.bfloat16)], [torch.zeros(4, 3, 16, 64, dtype=torch.bfloat16)])
@@ -314,12 +315,21 @@ def test_a_context_of_a_gpu_refuses_tensors_elsewhere(lib):
 
 
 def test_heads_marshalling():
+    buf = ctypes.create_string_buffer(2 * crf._HEADS)
+
+    def put(x, out, dim=64, device=-1):
+        n = crf._put_heads(buf, crf._HEADS, device, "x", x, out, dim)
+        h = abi.Heads.from_buffer(buf, crf._HEADS)
+        assert n == h.heads
+        return h.x, h.out, h.heads, h.x_row, h.x_head, h.out_row, h.out_head
+
     x = torch.zeros(5, 7, 64, dtype=torch.bfloat16)[:, 1:4]
-    h = crf._heads("x", x, None, 64)
-    assert (h.x, h.out, h.heads, h.x_row, h.x_head) == (x.data_ptr(), None, 3, 448, 64)
-    with pytest.raises(ValueError):
-        crf._heads("x", x, None, 32)
-    with pytest.raises(ValueError):
-        crf._heads("x", torch.zeros(2, 3, 128)[..., ::2], None, 64)
-    with pytest.raises(ValueError):
-        crf._heads("x", x, torch.zeros(5, 3, 64), 64)
+    y = torch.zeros(3, 5, 64, dtype=torch.bfloat16).transpose(0, 1)
+    assert put(x, None) == (x.data_ptr(), None, 3, 448, 64, 0, 0)
+    assert put(x, x) == (x.data_ptr(), x.data_ptr(), 3, 448, 64, 448, 64)
+    assert put(x, y) == (x.data_ptr(), y.data_ptr(), 3, 448, 64, 64, 320)
+    z = torch.zeros(2, 3, 128, dtype=torch.bfloat16)[..., ::2]
+    for bad in ((x, None, 32), (x, None, 64, 0), (z, None), (x, torch.zeros(5, 3, 64)), (x, y[:4]), (x[0], None),
+                (torch.zeros(2, 3, 64, dtype=torch.bfloat16), z)):
+        with pytest.raises(ValueError):
+            put(*bad)
