@@ -296,6 +296,7 @@ CRF_API crf_status crf_kl_logits_noalloc(int device, const float* z_ref, const f
 
 #define CRF_MAX_CHUNKS 128  /* requests of one append or attention call */
 #define CRF_MAX_TABLES 512  /* page tables of one crf_pages_* call */
+#define CRF_MAX_KEYS (1 << 26)  /* cached positions of a request that attention sees */
 
 enum { CRF_BF16 = 0, CRF_FP16 = 1, CRF_FP32 = 2 };                  /* element types of crf_rotary */
 enum { CRF_ROPE_HALF = 0, CRF_ROPE_INTERLEAVED = 1 };               /* pairs (i, i + rot/2) or (2i, 2i + 1) */
@@ -340,7 +341,7 @@ CRF_API crf_status crf_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_head
  * The rows of a call's requests are packed in order. page_table: device int32,
  * ceil((pos + n_new) / 16) entries to append, ceil(n_keys / 16) to attend.
  * n_keys: cached positions that attention may see, the new rows' own (appended
- * before) among them; usually pos + n_new. */
+ * before) among them; usually pos + n_new, at most CRF_MAX_KEYS. pos + n_new <= 2^30. */
 typedef struct crf_chunk {
   int n_new, pos, n_keys;
   const int32_t* page_table;

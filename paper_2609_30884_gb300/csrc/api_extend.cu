@@ -133,6 +133,8 @@ crf_status fill_chunks(const crf_chunk* chunks, int n, bool attend, int num_page
     // 2^30 leaves room for tile arithmetic in 32 bits
     if (c.n_new < 0 || c.pos < 0 || c.n_keys < 0 || c.n_keys > (1 << 30) || static_cast<int64_t>(c.pos) + c.n_new > (1 << 30))
       return fail(CRF_EINVAL, "chunk %d: n_new, pos or n_keys out of range", i);
+    // a query tile's keys have to pass within the kernels' wait limit (1.6 us for 128 of them: 0.8 s)
+    if (attend && c.n_keys > CRF_MAX_KEYS) return fail(CRF_EUNSUPPORTED, "chunk %d: n_keys over %d", i, CRF_MAX_KEYS);
     if (!c.page_table && (attend ? c.n_new > 0 && c.n_keys > 0 : c.n_new > 0))
       return fail(CRF_EINVAL, "chunk %d: page table is null", i);
     if (!aligned4(c.page_table)) return fail(CRF_EINVAL, "chunk %d: page table misaligned", i);

@@ -188,7 +188,8 @@ def call_attention(lib, ctx, pl=None, layer=0, hkv=2, d=64, ch=((3, 5, 8, A16),)
     (dict(q=heads(x=A16 + 2)), EINVAL), (dict(q=heads(x_row=260)), EUNSUPPORTED), (dict(q=heads(out_head=68)), EUNSUPPORTED),
     (dict(q=heads(out=A16)), EINVAL), (dict(q=heads(out_row=64)), ESHAPE), (dict(q=heads(heads=3)), ESHAPE),
     (dict(pl=pool(k=None)), EINVAL), (dict(ch=((1, 5, 6, A16 + 2),)), EINVAL), (dict(lse=A16 + 2), EINVAL),
-    (dict(ch=((1 << 29, 0, 1 << 29, A16),)), EUNSUPPORTED),
+    (dict(ch=((1, 1 << 26, (1 << 26) + 1, A16),)), EUNSUPPORTED),
+    (dict(ch=((1 << 29, 0, 1 << 20, A16),)), EUNSUPPORTED),
 ])
 def test_attention_refusals(lib, ctx, kw, status):
     assert call_attention(lib, ctx, **kw) == status
