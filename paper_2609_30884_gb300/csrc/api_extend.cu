@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstring>
 #include <exception>
+#include <limits>
 
 using namespace crf;
 
@@ -44,6 +45,10 @@ crf_status guarded(F&& f) {
 }
 
 // ---------------------------------------------------------------- rotary positions
+double rope_base(const crf_rope& r) {
+  return r.scaling == CRF_ROPE_BASE ? r.theta * std::pow(r.factor, r.rot_dim / (r.rot_dim - 2.0)) : r.theta;
+}
+
 crf_status check_rope(const crf_rope& r) {
   if (r.head_dim < 2 || r.head_dim > 2 * kMaxPairs || r.rot_dim < 2 || r.rot_dim % 2 || r.rot_dim > r.head_dim)
     return fail(CRF_EUNSUPPORTED, "rope: rot_dim %d must be even, 2..head_dim, and head_dim %d 2..%d", r.rot_dim,
@@ -58,14 +63,17 @@ crf_status check_rope(const crf_rope& r) {
   if (r.scaling == CRF_ROPE_BANDS &&
       (!(r.low >= 0) || !(r.high > r.low) || !std::isfinite(r.high) || !(r.original > 0) || !std::isfinite(r.original)))
     return fail(CRF_EINVAL, "rope: bands need 0 <= low < high and original > 0, all finite");
+  // the base in use; from the smallest normal number on, every frequency is finite
+  const double base = rope_base(r);
+  if (!std::isfinite(base) || base < std::numeric_limits<double>::min())
+    return fail(CRF_EINVAL, "rope: the base is out of range");
   return CRF_OK;
 }
 
 // Turns a position of every pair, as a fraction of one turn in units of 2^-64.
 void fill_turns(const crf_rope& r, uint64_t* turns) {
   const double two_pi = 6.283185307179586476925286766559;
-  const double theta = r.scaling == CRF_ROPE_BASE ? r.theta * std::pow(r.factor, r.rot_dim / (r.rot_dim - 2.0)) : r.theta;
-  const double step = -2.0 / r.rot_dim * std::log2(theta);
+  const double step = -2.0 / r.rot_dim * std::log2(rope_base(r));
   for (int i = 0; i < r.rot_dim / 2; ++i) {
     double f = std::exp2(step * i);
     if (r.scaling == CRF_ROPE_LINEAR) f /= r.factor;

@@ -116,6 +116,15 @@ def test_rope_refusals(lib, ctx, kw, status):
     assert call_rotary(lib, ctx, rope(**kw)) == status
 
 
+@pytest.mark.parametrize("kw", [
+    dict(theta=5e-324), dict(theta=1e-308, rot_dim=64), dict(theta=1e300, scaling="base", factor=1e20, rot_dim=4),
+    dict(scaling="base", factor=1e308, rot_dim=4),
+])
+def test_rope_refuses_a_base_out_of_range(lib, ctx, kw):
+    # the frequencies or the base itself would be infinite
+    assert call_rotary(lib, ctx, rope(**kw)) == EINVAL
+
+
 def test_rope_unknown_layout_or_scaling(lib, ctx):
     for field in ("layout", "scaling"):
         for bad in (-1, 4):
