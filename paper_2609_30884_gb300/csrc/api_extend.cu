@@ -121,10 +121,13 @@ bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0;
 
 // Outputs of rows and heads must not share elements: the strides are at least the extents they step over,
 // in one order or the other.
-crf_status check_out(const void* out, int64_t row, int64_t head, int heads, int64_t rows, int dim, const char* name) {
-  const bool rows_outer = (heads == 1 || head >= dim) && (rows <= 1 || row >= (heads - 1) * head + dim);
-  const bool heads_outer = (rows <= 1 || row >= dim) && (heads == 1 || head >= (rows - 1) * row + dim);
-  if (!out || (!rows_outer && !heads_outer)) return fail(CRF_ESHAPE, "%s: the strides make output rows or heads overlap", name);
+crf_status check_out(const crf_heads& h, int64_t rows, int dim, const char* name) {
+  // n steps and dim more within `outer`; a product could overflow
+  auto fits = [dim](int64_t n, int64_t step, int64_t outer) { return outer >= dim && n <= (outer - dim) / step; };
+  const bool head_ok = h.heads == 1 || h.out_head >= dim, row_ok = rows <= 1 || h.out_row >= dim;
+  const bool rows_outer = head_ok && (rows <= 1 || (h.heads == 1 ? row_ok : fits(h.heads - 1, h.out_head, h.out_row)));
+  const bool heads_outer = row_ok && (h.heads == 1 || (rows <= 1 ? head_ok : fits(rows - 1, h.out_row, h.out_head)));
+  if (!rows_outer && !heads_outer) return fail(CRF_ESHAPE, "%s: the strides make output rows or heads overlap", name);
   return CRF_OK;
 }
 
@@ -273,7 +276,7 @@ crf_status crf_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts
       const char* name = p ? "part 1" : "part 0";
       s = check_heads(parts[p], type == CRF_FP32 ? 4 : 2, true, name);
       if (s != CRF_OK) return s;
-      s = check_out(parts[p].out, parts[p].out_row, parts[p].out_head, parts[p].heads, n_rows, rope->head_dim, name);
+      s = check_out(parts[p], n_rows, rope->head_dim, name);
       if (s != CRF_OK) return s;
       if (parts[p].x == parts[p].out && (parts[p].x_row != parts[p].out_row || parts[p].x_head != parts[p].out_head))
         return fail(CRF_ESHAPE, "%s: in place with other strides", name);
@@ -330,7 +333,7 @@ crf_status crf_cache_append(crf_ctx* ctx, const crf_rope* rope, const crf_kv_poo
     if (q) {
       s = check_heads(*q, 2, true, "q");
       if (s != CRF_OK) return s;
-      s = check_out(q->out, q->out_row, q->out_head, q->heads, rows, head_dim, "q");
+      s = check_out(*q, rows, head_dim, "q");
       if (s != CRF_OK) return s;
       if (q->x == q->out && (q->x_row != q->out_row || q->x_head != q->out_head))
         return fail(CRF_ESHAPE, "q: in place with other strides");
@@ -407,7 +410,7 @@ crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer,
     if (s != CRF_OK) return s;
     if ((q->x_row | q->x_head | q->out_row | q->out_head) % 8)
       return fail(CRF_EUNSUPPORTED, "q: strides must be multiples of 8 elements");
-    s = check_out(q->out, q->out_row, q->out_head, q->heads, rows, head_dim, "q");
+    s = check_out(*q, rows, head_dim, "q");
     if (s != CRF_OK) return s;
     if (q->x == q->out) return fail(CRF_EINVAL, "q: o may not be written over q");
     if (!aligned4(lse)) return fail(CRF_EINVAL, "lse misaligned");

@@ -148,6 +148,13 @@ def test_rotary_refusals(lib, ctx, kw, status):
     assert call_rotary(lib, ctx, p=(heads(), heads(**kw)), n_parts=2) == status
 
 
+def test_rotary_refuses_rows_too_far_apart_to_multiply(lib, ctx):
+    # (rows - 1) x row is over 2^63: rows and heads interleave, whatever the product wraps to
+    far = heads(out_row=1 << 40, out_head=1 << 40)
+    for rows in ((1 << 23) + 1, (1 << 24) + 1, (1 << 31) - 1):
+        assert call_rotary(lib, ctx, p=(far, heads()), rows=rows) == ESHAPE
+
+
 def test_rotary_argument_refusals(lib, ctx):
     assert lib.crf_rotary(None, ref(rope()), ref(heads()), 1, 0, 1, A16, 0, None) == EINVAL
     assert lib.crf_rotary(ctx, None, ref(heads()), 1, 0, 1, A16, 0, None) == EINVAL
