@@ -319,8 +319,9 @@ typedef struct crf_rope {
 } crf_rope;
 
 /* Heads of a batch of rows: element e of head h of row r of `x` is at
- * x[r x_row + h x_head + e] (strides in elements, >= 0), `out` likewise. `out`
- * may be `x` itself with the same strides; otherwise the two do not overlap. */
+ * x[r x_row + h x_head + e] (strides in elements, >= 0; that of an axis of one
+ * row or head is not read), `out` likewise. `out` may be `x` itself with the
+ * same strides; otherwise the two do not overlap. */
 typedef struct crf_heads {
   const void* x;
   void* out;
@@ -394,7 +395,7 @@ typedef struct crf_pages {
  * (the slots behind them are left as they were). New pages are the lowest free ones, dealt
  * in order of tables and entries. A table id outside the pool or of count 0, or a
  * negative count, rejects the call (CRF_EINVAL from crf_check), and so do too few free pages
- * (CRF_ENOMEM from crf_check). `out` overlaps no table of the call. */
+ * (CRF_ENOMEM from crf_check). `out` overlaps no table of the call and no other `out`. */
 CRF_API crf_status crf_pages_fork(crf_ctx* ctx, const crf_kv_pool* pool, int n_layers, int n_kv_heads,
                                   int head_dim, const int32_t* refs_in, int32_t* refs_out,
                                   const crf_pages* tables, int n_tables, int deep, void* workspace,

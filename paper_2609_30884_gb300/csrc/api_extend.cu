@@ -103,6 +103,14 @@ crf_status check_heads(const crf_heads& h, size_t size, bool has_out, const char
   return CRF_OK;
 }
 
+// The stride of an axis of one says nothing, whatever its value: it is set to one that every form takes.
+crf_heads settled(crf_heads h, int64_t rows, int dim) {
+  const int64_t step = (dim + 7) / 8 * 8;
+  if (rows <= 1) h.x_row = h.out_row = step;
+  if (h.heads == 1) h.x_head = h.out_head = step;
+  return h;
+}
+
 RotPart part_of(const crf_heads& h, bool rotate) {
   RotPart p;
   p.x = h.x;
@@ -274,13 +282,14 @@ crf_status crf_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts
     std::memset(&d, 0, sizeof(d));
     for (int p = 0; p < n_parts; ++p) {
       const char* name = p ? "part 1" : "part 0";
-      s = check_heads(parts[p], type == CRF_FP32 ? 4 : 2, true, name);
+      const crf_heads h = settled(parts[p], n_rows, rope->head_dim);
+      s = check_heads(h, type == CRF_FP32 ? 4 : 2, true, name);
       if (s != CRF_OK) return s;
-      s = check_out(parts[p], n_rows, rope->head_dim, name);
+      s = check_out(h, n_rows, rope->head_dim, name);
       if (s != CRF_OK) return s;
-      if (parts[p].x == parts[p].out && (parts[p].x_row != parts[p].out_row || parts[p].x_head != parts[p].out_head))
+      if (h.x == h.out && (h.x_row != h.out_row || h.x_head != h.out_head))
         return fail(CRF_ESHAPE, "%s: in place with other strides", name);
-      d.part[p] = part_of(parts[p], true);
+      d.part[p] = part_of(h, true);
     }
     d.n_parts = n_parts;
     d.head_dim = rope->head_dim;
@@ -322,24 +331,26 @@ crf_status crf_cache_append(crf_ctx* ctx, const crf_rope* rope, const crf_kv_poo
     if (s != CRF_OK) return s;
     const int rows = t.row0[t.n];
     if (rows == 0) return CRF_OK;
-    s = check_heads(*k, 2, false, "k");
+    const crf_heads hk = settled(*k, rows, head_dim), hv = settled(*v, rows, head_dim);
+    s = check_heads(hk, 2, false, "k");
     if (s != CRF_OK) return s;
-    s = check_heads(*v, 2, false, "v");
+    s = check_heads(hv, 2, false, "v");
     if (s != CRF_OK) return s;
     if (k->heads != n_kv_heads || v->heads != n_kv_heads)
       return fail(CRF_ESHAPE, "k has %d and v %d heads, the pool %d", k->heads, v->heads, n_kv_heads);
     RotaryDesc d;
     std::memset(&d, 0, sizeof(d));
     if (q) {
-      s = check_heads(*q, 2, true, "q");
+      const crf_heads hq = settled(*q, rows, head_dim);
+      s = check_heads(hq, 2, true, "q");
       if (s != CRF_OK) return s;
-      s = check_out(*q, rows, head_dim, "q");
+      s = check_out(hq, rows, head_dim, "q");
       if (s != CRF_OK) return s;
-      if (q->x == q->out && (q->x_row != q->out_row || q->x_head != q->out_head))
+      if (hq.x == hq.out && (hq.x_row != hq.out_row || hq.x_head != hq.out_head))
         return fail(CRF_ESHAPE, "q: in place with other strides");
-      d.part[d.n_parts++] = part_of(*q, true);
+      d.part[d.n_parts++] = part_of(hq, true);
     }
-    RotPart kp = part_of(*k, rope != nullptr), vp = part_of(*v, false);
+    RotPart kp = part_of(hk, rope != nullptr), vp = part_of(hv, false);
     kp.paged = vp.paged = true;
     kp.out = pool->k_pages[layer];
     vp.out = pool->v_pages[layer];
@@ -406,11 +417,12 @@ crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer,
     if (rows == 0) return CRF_OK;
     s = check_attention(q->heads, n_kv_heads, window, rows);
     if (s != CRF_OK) return s;
-    s = check_heads(*q, 16, true, "q");
+    const crf_heads hq = settled(*q, rows, head_dim);
+    s = check_heads(hq, 16, true, "q");
     if (s != CRF_OK) return s;
-    if ((q->x_row | q->x_head | q->out_row | q->out_head) % 8)
+    if ((hq.x_row | hq.x_head | hq.out_row | hq.out_head) % 8)
       return fail(CRF_EUNSUPPORTED, "q: strides must be multiples of 8 elements");
-    s = check_out(*q, rows, head_dim, "q");
+    s = check_out(hq, rows, head_dim, "q");
     if (s != CRF_OK) return s;
     if (q->x == q->out) return fail(CRF_EINVAL, "q: o may not be written over q");
     if (!aligned4(lse)) return fail(CRF_EINVAL, "lse misaligned");
@@ -421,10 +433,10 @@ crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer,
     ChunkAttnDesc d;
     d.q = static_cast<const __nv_bfloat16*>(q->x);
     d.out = static_cast<__nv_bfloat16*>(q->out);
-    d.q_row = q->x_row;
-    d.q_head = q->x_head;
-    d.out_row = q->out_row;
-    d.out_head = q->out_head;
+    d.q_row = hq.x_row;
+    d.q_head = hq.x_head;
+    d.out_row = hq.out_row;
+    d.out_head = hq.out_head;
     d.lse = lse;
     d.kpages = static_cast<const __nv_bfloat16*>(pool->k_pages[layer]);
     d.vpages = static_cast<const __nv_bfloat16*>(pool->v_pages[layer]);

@@ -211,6 +211,21 @@ def test_attention_refusals(lib, ctx, kw, status):
     assert call_attention(lib, ctx, **kw) == status
 
 
+def test_strides_of_axes_of_one_are_not_refused(lib, ctx):
+    # what stands behind the strides is refused instead: a missing workspace, misaligned positions
+    long = dict(ch=((1, 100000, 100001, A16),), ws=A16 + 16)
+    assert call_attention(lib, ctx, q=heads(x_row=3, out_row=0), **long) == EINVAL
+    assert b"workspace" in lib.crf_last_error()
+    one = heads(heads=1, x_head=5, out_head=0)
+    assert call_attention(lib, ctx, hkv=1, q=one, **long) == EINVAL
+    assert b"workspace" in lib.crf_last_error()
+    bad = heads(out=None)
+    assert call_rotary(lib, ctx, p=(heads(x_row=-1, out_row=0), bad), n_parts=2, rows=1) == EINVAL
+    assert b"part 1" in lib.crf_last_error()
+    assert call_rotary(lib, ctx, p=(heads(heads=1, x_head=-1, out_head=0), bad), n_parts=2) == EINVAL
+    assert b"part 1" in lib.crf_last_error()
+
+
 def test_attention_workspace(lib, ctx):
     n = ctypes.c_size_t()
     long = chunks((1, 100000, 100001, A16))

@@ -434,6 +434,39 @@ def test_attention_strides_and_rows_behind(ctx):
     assert torch.equal(out, want)
 
 
+def test_strides_of_axes_of_one_are_not_read(ctx):
+    # one row, or one head: a tensor may carry any stride there
+    def odd(t, row, head):
+        return t.as_strided(t.shape, (row, head, 1))
+
+    s = Setup(23, 8, 2, 128, [(1, 300)])
+    want, _ = s.run(ctx)
+    out = torch.empty_like(s.q)
+    got, _ = s.run(ctx, q=odd(s.q, 3, 128), out=odd(out, 5, 128))
+    assert torch.equal(got, want)
+    s = Setup(24, 1, 1, 64, [(37, 300)])
+    want, _ = s.run(ctx)
+    out = torch.empty_like(s.q)
+    got, _ = s.run(ctx, q=odd(s.q, 64, 1), out=odd(out, 64, 0))
+    assert torch.equal(got, want)
+    x, pos = normal(gen(25), 1, 8, 64), ints(77)
+    want, got = torch.empty_like(x), torch.empty_like(x)
+    ctx.rotary(crf.Rope(64), pos, x, want)
+    ctx.rotary(crf.Rope(64), pos, odd(x, 0, 64), odd(got, 1, 64))
+    assert torch.equal(got, want)
+    pool = [torch.zeros(2, 1, 16, 64, dtype=BF16, device=DEV) for _ in range(4)]
+    k, q = normal(gen(26), 1, 1, 64), normal(gen(27), 1, 1, 64)
+    q_out = torch.empty_like(q)
+    c = crf.Chunks([ints(1)], [1], [3])
+    rope = crf.Rope(64)
+    ctx.cache_append(crf.KVPool(pool[:1], pool[1:2]), 0, c, k, k, q=q.clone(), rope=rope)
+    ctx.cache_append(crf.KVPool(pool[2:3], pool[3:]), 0, c, odd(k, 1, 7), odd(k, 0, 0), q=odd(q, 1, 1), q_out=odd(q_out, 0, 0),
+                     rope=rope)
+    ctx.rotary(rope, ints(3), q)
+    assert torch.equal(pool[0], pool[2]) and torch.equal(pool[1], pool[3]) and torch.equal(q_out, q)
+    ctx.check()
+
+
 def test_attention_shared_pages_and_same_bits(ctx):
     s = Setup(22, 28, 4, 128, [(1, 2000), (1, 1500), (9, 700)])
     s.tables = [s.tables[0]] * 3  # three requests on one prefix
