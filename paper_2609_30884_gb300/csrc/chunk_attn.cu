@@ -212,7 +212,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool firs
 __device__ __forceinline__ bool not_finite_bf16(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
 
 // LEAN: every request of the call has at most 64 packed rows (single tokens and short drafts), so that o at a segment's
-// end takes half the space and the ring a slot more: 8 rows of 4K-16K keys 41.4 -> 38.7 us.
+// end takes half the space and the ring a slot more: 8 rows of 4K-16K keys, replayed from a graph, take 37.4 us instead of 39.5.
 constexpr int kLeanRows = 64;
 template <int D, bool LEAN>
 struct Tile {
