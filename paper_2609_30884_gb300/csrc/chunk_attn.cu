@@ -463,6 +463,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = sh.tmem_base;
+  // Pages, their tables and q may come from the kernel before. Every role waits for it here, so that the bounded waits
+  // below measure this kernel alone (the issuer's for q, say, would run out behind a kernel of over two seconds).
+  griddep_wait();
 
   if (warp < 4) {
     regs_dec_ctl();
@@ -472,7 +475,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       bool ok = true;
       int slot = 0, armed = 0;
       uint32_t ph = 0;
-      griddep_wait();  // the pages and their tables may come from the kernel before
       for (int n = 0; ok; ++n) {
         ok = mbar_wait_warp(&sh.seg_full[n % kSegRing], (n / kSegRing) & 1, &sh.abort_flag, d.status);
         if (!ok) break;
@@ -684,7 +686,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
     const int grp = d.n_q_heads / d.n_kv_heads;
     bool ok = true;
     int base = 0, work = 0, done = 0;  // ring items, segments with tiles, steps of the chain before this segment
-    griddep_wait();                    // q may come from the kernel before
     for (int n = 0;; ++n) {
       // The warps go from segment to segment together: the stage is free for q once all have left it
       if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sh.seg_full[n % kSegRing], (n / kSegRing) & 1, &sh.abort_flag, d.status));
