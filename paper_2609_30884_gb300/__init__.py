@@ -101,14 +101,17 @@ class Adapter:
 
 
 class KVPool:
-    """Per-layer K and V page pools, bf16 [num_pages, Hkv, 16, d]."""
+    """Per-layer K and V page pools, bf16 [num_pages, Hkv, 16, d]. Calls that are given the model take flat views
+    of that memory too; those that extend a cache read the heads and their size from the shape."""
 
     def __init__(self, k_pages: Sequence[torch.Tensor], v_pages: Sequence[torch.Tensor]):
         self.k_pages, self.v_pages = list(k_pages), list(v_pages)
         n = len(self.k_pages)
         self._k = (c_void_p * n)(*[t.data_ptr() for t in self.k_pages])
         self._v = (c_void_p * n)(*[t.data_ptr() for t in self.v_pages])
-        self.num_pages, self.n_kv_heads, _, self.head_dim = (int(x) for x in self.k_pages[0].shape)
+        shape = [int(x) for x in self.k_pages[0].shape]
+        self.num_pages = shape[0]
+        self.n_kv_heads, self.head_dim = (shape[1], shape[3]) if len(shape) == 4 else (None, None)
         self.c = abi.KVPool(self._k, self._v, self.num_pages)
         self.address = ctypes.addressof(self.c)
 
@@ -383,6 +386,8 @@ class Context:
     def _pool_layer(self, pool: KVPool, layer: int) -> Tuple[int, int]:
         if not 0 <= layer < len(pool.k_pages):
             raise ValueError(f"layer {layer} is not in the pool")
+        if pool.head_dim is None:
+            raise ValueError("the pool's tensors must be [num_pages, kv heads, 16, head_dim]")
         if pool.k_pages[layer].get_device() != self.device:
             raise ValueError(f"the pool must be on cuda:{self.device}")
         return pool.n_kv_heads, pool.head_dim
