@@ -112,8 +112,25 @@ class KVPool:
         shape = [int(x) for x in self.k_pages[0].shape]
         self.num_pages = shape[0]
         self.n_kv_heads, self.head_dim = (shape[1], shape[3]) if len(shape) == 4 else (None, None)
+        self.device = self.k_pages[0].get_device()
+        self.not_paged = self._not_paged(shape)
         self.c = abi.KVPool(self._k, self._v, self.num_pages)
         self.address = ctypes.addressof(self.c)
+
+    def _not_paged(self, shape: List[int]) -> Optional[str]:
+        """Why the tensors do not all hold ``shape[0]`` pages of layer 0's keys' shape, or None: the calls that extend a
+        cache write by that shape alone."""
+        if len(shape) != 4 or shape[2] != abi.PAGE_SIZE:
+            return f"the pool's tensors must be [num_pages, kv heads, {abi.PAGE_SIZE}, head_dim]"
+        if len(self.v_pages) != len(self.k_pages):
+            return "the pool has a different number of K and V layers"
+        for name, layers in (("k_pages", self.k_pages), ("v_pages", self.v_pages)):
+            for l, t in enumerate(layers):
+                if t.dtype != torch.bfloat16 or t.device != self.k_pages[0].device or not t.is_contiguous():
+                    return f"{name}[{l}] must be contiguous bfloat16 on the device of k_pages[0]"
+                if t.dim() != 4 or list(t.shape[1:]) != shape[1:] or t.shape[0] < shape[0]:
+                    return f"{name}[{l}] must hold {shape[0]} pages {shape[1:]} like k_pages[0], not {list(t.shape)}"
+        return None
 
 
 class Request:
@@ -386,9 +403,9 @@ class Context:
     def _pool_layer(self, pool: KVPool, layer: int) -> Tuple[int, int]:
         if not 0 <= layer < len(pool.k_pages):
             raise ValueError(f"layer {layer} is not in the pool")
-        if pool.head_dim is None:
-            raise ValueError("the pool's tensors must be [num_pages, kv heads, 16, head_dim]")
-        if pool.k_pages[layer].get_device() != self.device:
+        if pool.not_paged:
+            raise ValueError(pool.not_paged)
+        if pool.device != self.device:
             raise ValueError(f"the pool must be on cuda:{self.device}")
         return pool.n_kv_heads, pool.head_dim
 

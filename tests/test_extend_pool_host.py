@@ -63,3 +63,44 @@ def test_flat_views_of_the_pages_make_a_pool(ctx, shape):
     for name, call in extension_calls(ctx, pool).items():
         with pytest.raises(ValueError, match="kv heads, 16, head_dim"):
             call()
+
+
+def wrong_pools():
+    k, v = (lambda: pages(5, 2, 16, 64)), (lambda: pages(5, 2, 16, 64))  # noqa: E731
+    return {
+        "V of fewer pages": ([k(), k()], [v(), pages(4, 2, 16, 64)]),
+        "K of fewer pages in a later layer": ([k(), pages(4, 2, 16, 64)], [v(), v()]),
+        "V of fewer heads": ([k()], [pages(5, 1, 16, 64)]),
+        "another layer's head size": ([k(), pages(5, 2, 16, 32)], [v(), v()]),
+        "a flat later layer": ([k(), k().view(5, 2048)], [v(), v()]),
+        "V flat": ([k()], [v().view(-1)]),
+        "pages of eight": ([pages(5, 2, 8, 64)], [pages(5, 2, 8, 64)]),
+        "fp16": ([pages(5, 2, 16, 64, dtype=torch.float16)], [pages(5, 2, 16, 64, dtype=torch.float16)]),
+        "V of fp32": ([k()], [pages(5, 2, 16, 64, dtype=torch.float32)]),
+        "every other page": ([pages(10, 2, 16, 64)[::2]], [v()]),
+        "V of heads outside": ([k()], [pages(2, 5, 16, 64).transpose(0, 1)]),
+        "V elsewhere": ([k()], [torch.empty(5, 2, 16, 64, dtype=BF16, device="meta")]),
+    }
+
+
+@pytest.mark.parametrize("name", sorted(wrong_pools()))
+def test_a_pool_that_is_not_pages_throughout_is_refused(ctx, name):
+    """Its tensors' addresses would be read and written by layer 0's keys' shape, behind the end of a smaller one."""
+    pool = crf.KVPool(*wrong_pools()[name])
+    for call in extension_calls(ctx, pool).values():
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_layers_of_more_pages_than_the_first_are_fine(ctx):
+    pool = crf.KVPool([pages(5, 2, 16, 64), pages(7, 2, 16, 64)], [pages(6, 2, 16, 64), pages(5, 2, 16, 64)])
+    with pytest.raises(AssertionError, match="was called"):
+        extension_calls(ctx, pool)["append"]()
+
+
+@pytest.mark.parametrize("layers", [(2, 1)])
+def test_layers_without_values_are_refused(ctx, layers):
+    pool = crf.KVPool([pages(5, 2, 16, 64) for _ in range(layers[0])], [pages(5, 2, 16, 64) for _ in range(layers[1])])
+    for call in extension_calls(ctx, pool).values():
+        with pytest.raises(ValueError):
+            call()
