@@ -150,6 +150,15 @@ class Request:
                              self._hout, _ptr(final_hidden_out))
 
 
+_INT32 = 1 << 31  # ctypes drops the bits of an int that its field has no room for
+
+
+def _fits(name: str, v: int) -> int:
+    if not -_INT32 <= v < _INT32:
+        raise ValueError(f"{name} {v} does not fit 32 bits")
+    return v
+
+
 class Rope:
     """Rotary positions (see crf_rope): the first ``rot_dim`` elements of a head turn in pairs of ``layout``
     ("half" or "interleaved"); ``scaling`` "none", "linear", "base" or "bands" for contexts ``factor`` times
@@ -162,8 +171,8 @@ class Rope:
             raise ValueError(f"layout must be one of {sorted(abi.ROPE_LAYOUTS)}")
         if scaling not in abi.ROPE_SCALINGS:
             raise ValueError(f"scaling must be one of {sorted(abi.ROPE_SCALINGS)}")
-        self.head_dim = head_dim
-        self.c = abi.Rope(head_dim, head_dim if rot_dim is None else rot_dim, abi.ROPE_LAYOUTS[layout],
+        self.head_dim = _fits("head_dim", head_dim)
+        self.c = abi.Rope(head_dim, head_dim if rot_dim is None else _fits("rot_dim", rot_dim), abi.ROPE_LAYOUTS[layout],
                           abi.ROPE_SCALINGS[scaling], theta, factor, low, high, original, magnitude)
         self.address = ctypes.addressof(self.c)
 
@@ -199,6 +208,8 @@ class Chunks:
         for i, t in enumerate(self.page_tables):
             m, p = int(n_new[i]), int(pos[i])
             k = p + m if n_keys is None else int(n_keys[i])
+            if not (-_INT32 <= m < _INT32 and -_INT32 <= p < _INT32 and -_INT32 <= k < _INT32):
+                raise ValueError(f"request {i}: n_new, pos or n_keys does not fit 32 bits")
             if t.dtype != torch.int32 or not t.is_contiguous():
                 raise ValueError(f"page table {i} must be a contiguous int32 tensor")
             self.append_entries.append((p + m + 15) // 16 if m else 0)
@@ -223,7 +234,7 @@ class PageTables:
         self.n = n
         self.c = (abi.Pages * max(1, n))()
         for i, t in enumerate(self.tables):
-            need = (int(n_tokens[i]) + 15) // 16
+            need = (_fits("n_tokens", int(n_tokens[i])) + 15) // 16
             _int32_on_device(f"table {i}", t, need)
             if outs is not None:
                 _int32_on_device(f"outs[{i}]", outs[i], need)
@@ -444,8 +455,9 @@ class Context:
         """Workspace of a chunk_attention call; the same one serves every layer of the step."""
         hkv, dim = self._pool_layer(pool, 0)
         n = c_size_t()
-        abi.check(self.lib.crf_chunk_attention_workspace_size(self.h, n_q_heads, hkv, dim, chunks.address, chunks.n,
-                                                              int(causal), window, byref(n)))
+        abi.check(self.lib.crf_chunk_attention_workspace_size(self.h, _fits("n_q_heads", n_q_heads), hkv, dim,
+                                                              chunks.address, chunks.n, int(causal),
+                                                              _fits("window", window), byref(n)))
         return torch.empty(max(256, n.value), dtype=torch.uint8, device=f"cuda:{self.device}")
 
     def chunk_attention(self, pool: KVPool, layer: int, chunks: Chunks, q: torch.Tensor, out: torch.Tensor,
@@ -465,6 +477,8 @@ class Context:
         self._here(workspace, lse)
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (n, heads)):
             raise ValueError("lse must be a contiguous float32 [rows, heads]")
+        if window:
+            _fits("window", window)
         status = self.lib.crf_chunk_attention(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, buf,
                                               None if lse is None else lse.data_ptr(), scale, causal, window,
                                               workspace.data_ptr(), workspace.numel(),
@@ -475,7 +489,7 @@ class Context:
     # -------------------------------------------------------------- pages
     def pages_workspace(self, num_pages: int, tables: PageTables) -> torch.Tensor:
         n = c_size_t()
-        abi.check(self.lib.crf_pages_workspace_size(self.h, num_pages, tables.address, tables.n, byref(n)))
+        abi.check(self.lib.crf_pages_workspace_size(self.h, _fits("num_pages", num_pages), tables.address, tables.n, byref(n)))
         return torch.empty(max(256, n.value), dtype=torch.uint8, device=f"cuda:{self.device}")
 
     def _refs(self, num_pages: int, refs: torch.Tensor, refs_out: Optional[torch.Tensor]) -> Tuple[int, int]:
