@@ -366,7 +366,8 @@ CRF_API crf_status crf_cache_append(crf_ctx* ctx, const crf_rope* rope, const cr
  *   q: x bf16 [rows] x heads, out the same shape (not overlapping x); heads a
  *      multiple of n_kv_heads; head_dim 64 or 128; strides multiples of 8, 16-byte aligned.
  *   lse: NULL, or device fp32 [rows][heads]: log of the sum of exp(scale q k).
- *   scale: > 0, or 0 for 1 / sqrt(head_dim).
+ *   scale: > 0, or 0 for 1 / sqrt(head_dim); scores are kept as scale log2(e) q k in fp32, and both the
+ *      factor and the scores have to be in its range.
  * Slots that a row does not see may hold anything, infinities and NaN
  * included. Softmax weights enter the product with v in bf16; sums, maxima
  * and o are fp32. `workspace` >= crf_chunk_attention_workspace_size bytes for

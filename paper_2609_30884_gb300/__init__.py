@@ -479,6 +479,8 @@ class Context:
             raise ValueError("lse must be a contiguous float32 [rows, heads]")
         if window:
             _fits("window", window)
+        if 0 < scale < 2.0**-149:
+            raise ValueError("scale would be 0 in float32, which stands for 1 / sqrt(head_dim)")
         status = self.lib.crf_chunk_attention(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, buf,
                                               None if lse is None else lse.data_ptr(), scale, causal, window,
                                               workspace.data_ptr(), workspace.numel(),

@@ -409,7 +409,9 @@ crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer,
     if (s != CRF_OK) return s;
     s = check_attention(q->heads, n_kv_heads, window, 0);
     if (s != CRF_OK) return s;
-    if (!(scale >= 0.f) || !std::isfinite(scale)) return fail(CRF_EINVAL, "scale must be positive, or 0 for 1/sqrt(head_dim)");
+    // the kernel multiplies scores by scale log2(e), in fp32
+    if (!(scale >= 0.f) || !std::isfinite(scale * 1.4426950408889634f))
+      return fail(CRF_EINVAL, "scale must be positive and under 2.35e38, or 0 for 1/sqrt(head_dim)");
     ChunkTable t;
     s = fill_chunks(chunks, n_chunks, true, pool->num_pages, &t);
     if (s != CRF_OK) return s;
