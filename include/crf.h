@@ -394,9 +394,10 @@ typedef struct crf_pages {
  * shared (their count rises by one); a last page that is part filled, or with deep != 0 every
  * page, gets a page of its own, count 1, into which the live slots of all n_layers layers are copied
  * (the slots behind them are left as they were). New pages are the lowest free ones, dealt
- * in order of tables and entries. A table id outside the pool or of count 0, or a
- * negative count, rejects the call (CRF_EINVAL from crf_check), and so do too few free pages
- * (CRF_ENOMEM from crf_check). `out` overlaps no table of the call and no other `out`. */
+ * in order of tables and entries. The call is rejected (CRF_EINVAL from crf_check) by a table id
+ * outside the pool or of count 0, a negative count, and, where pages are shared, a table id whose
+ * count is over 2^31 - 1 less the call's entries; and by too few free pages (CRF_ENOMEM from crf_check).
+ * `out` overlaps no table of the call and no other `out`. */
 CRF_API crf_status crf_pages_fork(crf_ctx* ctx, const crf_kv_pool* pool, int n_layers, int n_kv_heads,
                                   int head_dim, const int32_t* refs_in, int32_t* refs_out,
                                   const crf_pages* tables, int n_tables, int deep, void* workspace,

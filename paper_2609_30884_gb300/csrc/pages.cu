@@ -192,7 +192,7 @@ __global__ void __cluster_dims__(kPlanCtas, 1, 1) __launch_bounds__(kPlanThreads
     if (id < 0 || id >= P)
       bad = 1;
     else if (OP == kPageFork)
-      bad |= a.refs_in[id] < 1;
+      bad |= a.refs_in[id] < 1 || (!a.deep && a.refs_in[id] > 0x7fffffff - t.first[t.n]);  // room for the call's entries
     else
       atomicAdd(&a.s.mark[id], 1);
   });
