@@ -13,6 +13,9 @@ using namespace crf;
 
 namespace {
 
+// The arrays that kernels take are sized by the one and filled up to the other.
+static_assert(kMaxChunks == CRF_MAX_CHUNKS && kMaxTables == CRF_MAX_TABLES, "limits of the ABI and of the kernels differ");
+
 // The context's device for the length of a call, then the caller's again.
 class DeviceScope {
  public:

@@ -6,7 +6,7 @@
 
 namespace crf {
 
-constexpr int kMaxChunks = 128;  // equals CRF_MAX_CHUNKS
+constexpr int kMaxChunks = 128;  // equals CRF_MAX_CHUNKS (api_extend.cu checks that)
 constexpr int kMaxTables = 512;  // equals CRF_MAX_TABLES
 constexpr int kMaxPairs = 128;   // rotary pairs of a head
 
