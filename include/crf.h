@@ -311,6 +311,8 @@ enum { CRF_ROPE_PLAIN = 0, CRF_ROPE_LINEAR = 1, CRF_ROPE_BASE = 2, CRF_ROPE_BAND
  *   CRF_ROPE_BANDS   f_i (g + (1 - g) / factor), g = clamp((r - low) / (high - low), 0, 1) of the
  *                    r = original f_i / (2 pi) turns that the pair makes over the `original` trained
  *                    positions (0 <= low < high): fast pairs stay, slow ones are interpolated.
+ *                    g is a ramp over turns. Models whose ramp runs over the pair's index i between two
+ *                    rounded bounds have other frequencies, which this scaling does not give.
  * head_dim 2..256; rot_dim even, 2..head_dim. `factor` is not read with
  * CRF_ROPE_PLAIN; low, high and original are read with CRF_ROPE_BANDS alone. */
 typedef struct crf_rope {

@@ -162,7 +162,7 @@ def _fits(name: str, v: int) -> int:
 class Rope:
     """Rotary positions (see crf_rope): the first ``rot_dim`` elements of a head turn in pairs of ``layout``
     ("half" or "interleaved"); ``scaling`` "none", "linear", "base" or "bands" for contexts ``factor`` times
-    as long."""
+    as long. "bands" ramps over the turns that a pair makes in ``original`` positions, not over its index."""
 
     def __init__(self, head_dim: int, rot_dim: Optional[int] = None, theta: float = 1e4, layout: str = "half",
                  scaling: str = "none", factor: float = 1.0, low: float = 1.0, high: float = 32.0,

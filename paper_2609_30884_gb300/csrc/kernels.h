@@ -47,7 +47,9 @@ constexpr int kBxCols = 64;
 // behind it count on all before it having ended. Weights, and cached K/V pages that the call does not
 // write, may be read before that wait, so a chain with such reads opens with an ordinary launch or a
 // memset: what the caller enqueued before has then ended and is visible. Window calls, generation
-// steps, the LM head pass of a KL call, the KL reduction over few rows and drift open a scope.
+// steps, the LM head pass of a KL call, the KL reduction over few rows and drift open a scope. So do the
+// calls that extend a cache, from their first kernel on: their kernels read no global memory before
+// the wait (nor begin a bounded wait of their own, which would count the predecessor's time).
 class PdlScope {
  public:
   PdlScope();

@@ -3,9 +3,11 @@
 // p f, with f the pair's radians a position; the inverse map takes -sin (the transpose, hence the gradient).
 //
 // Angles: f / 2 pi is a fraction of a turn, held as a 64-bit integer in units of 2^-64 turns, so the product
-// with the position drops whole turns by itself (integer arithmetic modulo 2^64) and is exact for the held f:
-// at p = 2^31 the angle is off by at most 2^-33 turns. Its top 32 bits are split into a quadrant and a
-// remainder of at most an eighth of a turn, whose sine and cosine are fp32 functions.
+// with the position drops whole turns by itself (integer arithmetic modulo 2^64). Three things are rounded: the
+// fraction itself, formed in 64-bit floating point, is off by a few 2^-53 of its value, which the position multiplies
+// (2^-24 turns for the fastest pair at p = 2^31, 2^-38 at 131072); its units cost p 2^-64 turns; and the product's
+// top 32 bits are kept, which costs up to 2^-32 turns. They are split into a quadrant and a remainder of at most an
+// eighth of a turn, whose sine and cosine are fp32 functions.
 //
 // Bound by memory: every element is read once and written once. A thread owns one 16-byte unit of a row (for the
 // half layout two, the pair's halves) in up to four neighbouring heads and asks for all of them before the angles are
