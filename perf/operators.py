@@ -338,8 +338,16 @@ def plain_release(s):
 HELD = {}
 
 
+def page_tables(s):
+    """The tables of one call. The requests that fork, move or end are other ones at every call, and have grown: no
+    program has this at hand."""
+    import paper_2609_30884_gb300 as crf
+
+    return crf.PageTables(s["tables"], s["tokens"], None if s["kind"] == "release" else s["tables_out"])
+
+
 def held(s):
-    """What a program keeps across its layers and steps: the context, the pool, the batch's descriptors, a workspace."""
+    """What a program keeps across its layers and steps: the context, the pool, a step's chunks, a workspace."""
     import paper_2609_30884_gb300 as crf
 
     if "ctx" not in HELD:
@@ -354,8 +362,7 @@ def held(s):
     if kind == "attention":
         h["ws"] = ctx.chunk_attention_workspace(h["pool"], h["chunks"], s["q"].shape[1], window=case["window"])
     if kind in ("fork", "compact", "release"):
-        h["tables"] = crf.PageTables(s["tables"], s["tokens"], s["tables_out"])
-        h["ws"] = ctx.pages_workspace(len(s["refs"]), h["tables"])
+        h["ws"] = ctx.pages_workspace(len(s["refs"]), page_tables(s))
         if kind != "release":
             h["pool"] = crf.KVPool(list(s["k_pages"]), list(s["v_pages"]))
     return h
@@ -376,12 +383,12 @@ def own_run(s):
         ctx.chunk_attention(h["pool"], 0, h["chunks"], s["q"], s["out"], h["ws"], lse=s["lse"], window=s["case"]["window"])
         return s["out"], s["lse"]
     if kind == "fork":
-        ctx.pages_fork(h["pool"], s["refs"], h["tables"], h["ws"], refs_out=s["refs_out"], deep=s["case"]["deep"])
+        ctx.pages_fork(h["pool"], s["refs"], page_tables(s), h["ws"], refs_out=s["refs_out"], deep=s["case"]["deep"])
         return s["new_tables"], s["refs_out"], s["k_pages"], s["v_pages"]
     if kind == "compact":
-        ctx.pages_compact(h["pool"], s["refs"], h["tables"], h["ws"], refs_out=s["refs_out"])
+        ctx.pages_compact(h["pool"], s["refs"], page_tables(s), h["ws"], refs_out=s["refs_out"])
         return s["new_tables"], s["refs_out"], s["k_pages"], s["v_pages"]
-    ctx.pages_release(s["refs"], h["tables"], h["ws"], refs_out=s["refs_out"])
+    ctx.pages_release(s["refs"], page_tables(s), h["ws"], refs_out=s["refs_out"])
     return s["refs_out"]
 
 
