@@ -45,6 +45,12 @@ constexpr int kPagesPerTile = kN / kPage;
 constexpr int kThreads = 384;
 constexpr int kMaxSlots = 6; // K/V ring
 constexpr int kSegRing = 4;  // segments found ahead
+// Steps of a chain after which its o starts anew. The tensor cores drop the low bits of every sum: in one chain of products
+// o comes out short by 0.76e-6 of itself a tile (v of mean 1, standard deviation 0.5: 6e-3 over 2^20 keys, 0.1 over 2^24).
+// So after this many tiles, 1e-4, o and the sum of weights are added to fp32 totals in the workspace, rounded to nearest
+// (9728 rows over 2^24 keys: 2e-7). 2048 rows over 65536 keys take 1216 us with it, 1188 without; calls whose runs are
+// shorter take what they took.
+constexpr int kChain = 128;
 // setmaxnreg split: the first warpgroup (producer, issuer, finder) keeps kRegsCtl, the softmax warpgroups take
 // kRegsSoftmax; the sum must fit what the CTA launched with.
 constexpr int kRegsCtl = 80;
@@ -64,6 +70,7 @@ struct ChunkArgs {
   float* part;
   float* part_ml;
   int part_rows;
+  float* total;  // of chains longer than kChain: [CTA][chain][kTotals][row]
 };
 
 struct MergeArgs {
@@ -207,6 +214,52 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool firs
   f32x2_split(rs2[0], r0, r1);
   f32x2_split(rs2[1], r2, r3);
   l_run += (r0 + r1) + (r2 + r3);
+}
+
+// The totals of a thread's row: o's columns, the sum of weights and the maximum that they were formed under, element i at
+// total[i kM]. They are added to between two loops over tiles: a test in the one loop, with the maximum and the sum in
+// registers, cost every call 2-6%.
+template <int D>
+constexpr int kTotals = D + 2;
+// o and the sum of a chain's last steps into the row's totals; the first time there is nothing to add to.
+template <int D>
+__device__ __forceinline__ void add_to_totals(uint32_t tO, float* total, bool first, float sl2, float m_run, float& l_run) {
+  const float m_was = first ? -INFINITY : __ldcg(total + (D + 1) * kM);
+  const float keep = m_was == -INFINITY ? 0.f : ex2_approx((m_was - m_run) * sl2);
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t o[32];
+    float was[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) was[i] = first ? 0.f : __ldcg(total + (c * 32 + i) * kM);
+    tmem_ld32(tO + c * 32, o);
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) __stcg(total + (c * 32 + i) * kM, was[i] * keep + __uint_as_float(o[i]));
+  }
+  __stcg(total + D * kM, (first ? 0.f : __ldcg(total + D * kM)) * keep + l_run);
+  __stcg(total + (D + 1) * kM, m_run);
+  l_run = 0.f;
+}
+// The totals into o and the sum, at a segment's end.
+template <int D>
+__device__ __forceinline__ void add_totals(uint32_t tO, const float* total, float sl2, float m_run, float& l_run) {
+  const float m_was = __ldcg(total + (D + 1) * kM);
+  const float keep = m_was == -INFINITY ? 0.f : ex2_approx((m_was - m_run) * sl2);
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t o[32];
+    float was[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) was[i] = __ldcg(total + (c * 32 + i) * kM);
+    tmem_ld32(tO + c * 32, o);
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(was[i] * keep + __uint_as_float(o[i]));
+    tmem_st32(tO + c * 32, o);
+  }
+  tmem_st_wait();
+  l_run += __ldcg(total + D * kM) * keep;
 }
 
 __device__ __forceinline__ bool not_finite_bf16(uint32_t h) { return (h & 0x7F80u) == 0x7F80u; }
@@ -595,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
               // a last odd tile of the narrow form has its V next to its K
               const int vslot = narrow && t == 0 && s > 0 && j + 1 == J ? slot_after<kSlots>(vs[t], kSlots - 1) : vs[t];
               const uint64_t v = vd + static_cast<uint32_t>(vslot * (KV_BYTES >> 4));
-              const bool full = pg0 == 0 && pg1 == kPagesPerTile;
+              const bool full = pg0 == 0 && pg1 == kPagesPerTile, anew = s % kChain == 0;
               // P of this step is in TMEM, and its V and the chain's next K have landed
               ok = mbar_wait_warp(&sh.p_full[t], ((t ? done1 : done0) + s) & 1, &sh.abort_flag, d.status);
               if (!ok) continue;
@@ -605,13 +658,13 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
 #pragma unroll
                   for (int kk = 0; kk < kN / 16; ++kk)
                     mma_bf16_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, v + kk * (2 * GROUP_BYTES >> 4), idesc_o,
-                                (s > 0 || kk > 0) ? 1u : 0u);
+                                (!anew || kk > 0) ? 1u : 0u);
                 } else {
                   // 16 keys, one page, an MMA: pages that no row sees are left out
 #pragma unroll 1
                   for (int kk = pg0; kk < pg1; ++kk)
                     mma_bf16_ts(tmem + 256 + t * 128, tmem + t * 128 + kk * 8, v + kk * (2 * GROUP_BYTES >> 4), idesc_o,
-                                (s > 0 || kk > pg0) ? 1u : 0u);
+                                (!anew || kk > pg0) ? 1u : 0u);
                 }
               }
               if (s + 1 < steps) issue_s(t, ks[t]);
@@ -738,6 +791,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       const int row = min(R, last_row) / grp;
       const KeyRange mine = keys_of_rows(w.pos + row, w.pos + row, w.n_keys, d.causal, d.window);
       float m_run = -INFINITY, l_run = 0.f;  // maximum in raw score units
+      auto totals = [&]() { return a.total + static_cast<size_t>(2 * blockIdx.x + t) * (kTotals<D> * kM) + r; };
       const KeyRange full = t ? w.full1 : w.full0;  // keys that all rows of the chain see, and of the CTA
       const bool both = !narrow && n1 > 0 && n0 > 0;
       const int cta_lo = both ? max(w.full0.lo, w.full1.lo) : full.lo;
@@ -754,46 +808,56 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
         const int stride = narrow ? 4 : 2;
         int ki = base + item_k(narrow, tile_of(narrow, t, 0)), vi = base + item_v(narrow, tile_of(narrow, t, 0), J);
         int ks = ki % kSlots, vs = vi % kSlots, last_vs = 0;
-        for (int s = 0; s < steps && ok; ++s) {
-          const int j = tile_of(narrow, t, s), k0 = (jb + j) * kN;
-          if (narrow && t == 0 && s > 0 && j + 1 == J) {  // a last odd tile: its V is next to its K
-            --vi;
-            vs = slot_after<kSlots>(vs, kSlots - 1);
-          }
-          ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[t], (done + s) & 1, &sh.abort_flag, d.status));
-          if (!ok) break;
-          tc_fence_after();
-          // S of this step complete: so is P V of the step before; this chain is done with that V and this K
-          release_slot(ks);
-          if (s > 0) release_slot(last_vs);
-          // the products that read this P also need V and the chain's next K: seen early, they need no wait later
-          const int need = (s + 1 < steps ? max(vi, ki + stride) : vi) + 1;
-          bool here = static_cast<int>(ld_acquire_shared(&sh.landed) - static_cast<uint32_t>(need)) >= 0;
-          __syncwarp();
-          if (k0 < full.lo || k0 + kN > full.hi) mask_tile(tS, mine.lo - k0, mine.hi - k0);
-          softmax_tile<D>(tS, tO, s == 0, sl2, m_run, l_run);
-          if (k0 < cta_lo || k0 + kN > cta_hi) {
-            ok = wait_landed(sh, vi + 1, d.status);
+        for (int s0 = 0; s0 < steps && ok; s0 += kChain) {
+          const int s1 = min(steps, s0 + kChain);
+          if (s0 > 0) {
+            // S of the step complete: so is o of the steps before, which this step's P V overwrites
+            ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[t], (done + s0) & 1, &sh.abort_flag, d.status));
             if (!ok) break;
-            // the fetched pages' keys before those that all rows see, and behind them
-            const int a0 = pages.first(j) * kPage, a1 = min(pages.last(j) * kPage, max(a0, cta_lo - k0));
-            const int b1 = pages.last(j) * kPage, b0 = min(b1, max(a1, cta_hi - k0));
-            clean_v<D>(sKV + vs * KV_BYTES, a0, a1, b0, b1, w.all_lo - k0, w.all_hi - k0, quarter * 32 + lane,
-                       32 * quarters, &sh.dirty);
-            fence_proxy_async_smem();
+            tc_fence_after();
+            add_to_totals<D>(tO, totals(), s0 == kChain, sl2, m_run, l_run);
           }
-          if (quarter == 0 && !__all_sync(0xffffffffu, here)) {
-            ok = wait_landed(sh, need, d.status);
+          for (int s = s0; s < s1 && ok; ++s) {
+            const int j = tile_of(narrow, t, s), k0 = (jb + j) * kN;
+            if (narrow && t == 0 && s > 0 && j + 1 == J) {  // a last odd tile: its V is next to its K
+              --vi;
+              vs = slot_after<kSlots>(vs, kSlots - 1);
+            }
+            ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[t], (done + s) & 1, &sh.abort_flag, d.status));
             if (!ok) break;
+            tc_fence_after();
+            // S of this step complete: so is P V of the step before; this chain is done with that V and this K
+            release_slot(ks);
+            if (s > 0) release_slot(last_vs);
+            // the products that read this P also need V and the chain's next K: seen early, they need no wait later
+            const int need = (s + 1 < steps ? max(vi, ki + stride) : vi) + 1;
+            bool here = static_cast<int>(ld_acquire_shared(&sh.landed) - static_cast<uint32_t>(need)) >= 0;
+            __syncwarp();
+            if (k0 < full.lo || k0 + kN > full.hi) mask_tile(tS, mine.lo - k0, mine.hi - k0);
+            softmax_tile<D>(tS, tO, s == s0, sl2, m_run, l_run);
+            if (k0 < cta_lo || k0 + kN > cta_hi) {
+              ok = wait_landed(sh, vi + 1, d.status);
+              if (!ok) break;
+              // the fetched pages' keys before those that all rows see, and behind them
+              const int a0 = pages.first(j) * kPage, a1 = min(pages.last(j) * kPage, max(a0, cta_lo - k0));
+              const int b1 = pages.last(j) * kPage, b0 = min(b1, max(a1, cta_hi - k0));
+              clean_v<D>(sKV + vs * KV_BYTES, a0, a1, b0, b1, w.all_lo - k0, w.all_hi - k0, quarter * 32 + lane,
+                         32 * quarters, &sh.dirty);
+              fence_proxy_async_smem();
+            }
+            if (quarter == 0 && !__all_sync(0xffffffffu, here)) {
+              ok = wait_landed(sh, need, d.status);
+              if (!ok) break;
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_n(&sh.p_full[t], quarter == 0 ? 5 - quarters : 1);
+            last_vs = vs;
+            ki += stride;
+            vi += stride;
+            ks = slot_after<kSlots>(ks, stride);
+            vs = slot_after<kSlots>(vs, stride);
           }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_n(&sh.p_full[t], quarter == 0 ? 5 - quarters : 1);
-          last_vs = vs;
-          ki += stride;
-          vi += stride;
-          ks = slot_after<kSlots>(ks, stride);
-          vs = slot_after<kSlots>(vs, stride);
         }
       }
       if (J > 0) {
@@ -811,6 +875,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       }
       __syncwarp();
       const bool rows_here = ok && quarter < quarters;
+      if (rows_here && steps > kChain) add_totals<D>(tO, totals(), sl2, m_run, l_run);
       if (rows_here && J > 0 && sh.dirty != 0 && steps > 0) {
         // the zeroed elements of v, to the rows that see them
 #pragma unroll 1
@@ -1079,7 +1144,7 @@ bool deal(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int w
           ChunkPlan* p) {
   const int grp = n_q_heads / n_kv_heads;
   p->ctas = 0;
-  p->part_rows = p->cuts = p->merge_rows = 0;
+  p->part_rows = p->cuts = p->merge_rows = p->longest = 0;
   int64_t left = 0;     // of the current CTA's budget
   int here = 0;         // segments of the current CTA
   auto open = [&](int req, int qt, int g, int step) {
@@ -1105,6 +1170,7 @@ bool deal(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int w
           }
           left -= kSegment;
           const int take = whole ? steps : static_cast<int>(std::min<int64_t>(steps - step, left / unit));
+          p->longest = std::max(p->longest, take);
           if (parts++ == 0) {
             first_cta = p->ctas - 1;
             first_slot = 2 * first_cta + (here > 0 ? 1 : 0);
@@ -1199,11 +1265,14 @@ size_t part_floats(const ChunkPlan& p, int head_dim, bool ml) {
   if (p.cuts == 0) return 0;
   return (static_cast<size_t>(2 * p.ctas) * p.part_rows * (ml ? 2 : head_dim) + 63) & ~static_cast<size_t>(63);
 }
+size_t total_floats(const ChunkPlan& p, int head_dim) {
+  return p.longest > kChain ? static_cast<size_t>(2 * p.ctas) * (head_dim + 2) * kM : 0;
+}
 
 }  // namespace
 
 size_t chunk_attention_workspace(const ChunkPlan& p, int head_dim) {
-  return (part_floats(p, head_dim, false) + part_floats(p, head_dim, true)) * sizeof(float);
+  return (part_floats(p, head_dim, false) + part_floats(p, head_dim, true) + total_floats(p, head_dim)) * sizeof(float);
 }
 
 cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, const ChunkPlan& p, void* workspace,
@@ -1219,6 +1288,7 @@ cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, 
   a.part = static_cast<float*>(workspace);
   a.part_ml = a.part + part_floats(p, d.head_dim, false);
   a.part_rows = p.part_rows;
+  a.total = a.part_ml + part_floats(p, d.head_dim, true);
   bool lean = true;
   for (int i = 0; i < c.n; ++i) lean = lean && static_cast<int64_t>(c.row0[i + 1] - c.row0[i]) * (d.n_q_heads / d.n_kv_heads) <= kLeanRows;
   if (d.head_dim == 128) return lean ? launch_tc<128, true>(a, p, num_sms, stream) : launch_tc<128, false>(a, p, num_sms, stream);

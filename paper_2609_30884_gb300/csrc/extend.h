@@ -70,6 +70,7 @@ struct CutItem {
 struct ChunkPlan {
   int ctas, cuts;
   int part_rows, merge_rows;  // rows of the largest cut item, of all
+  int longest;                // steps of the longest segment
   RunStart run[kMaxCtas + 1];
   int rows[kMaxCtas + 1];     // packed rows of the cut items before each
   CutItem cut[kMaxCtas];

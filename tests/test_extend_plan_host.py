@@ -11,6 +11,7 @@ from paper_2609_30884_gb300 import abi, build
 from tests.test_extend_host import A16, call_attention, chunks, ctx, lib, ref  # noqa: F401
 
 TILE, CTAS = 128, 256  # rows of a query tile and keys of a K/V tile; CTAs at most
+SUM = 128  # steps after which a sum starts anew
 
 SHIM = r"""
 #include "chunk_attn.cu"
@@ -30,8 +31,8 @@ extern "C" size_t plan(int n, const int* n_new, const int* pos, const int* n_key
   }
   static crf::ChunkPlan p;
   crf::plan_chunk_attention(t, hq, hkv, causal != 0, window, sms, &p);
-  const int v[4] = {p.ctas, p.cuts, p.part_rows, p.merge_rows};
-  for (int i = 0; i < 4; ++i) info[i] = v[i];
+  const int v[5] = {p.ctas, p.cuts, p.part_rows, p.merge_rows, p.longest};
+  for (int i = 0; i < 5; ++i) info[i] = v[i];
   for (int i = 0; i <= p.ctas; ++i) {
     const int r[4] = {p.run[i].req, p.run[i].qt, p.run[i].g, p.run[i].step};
     for (int k = 0; k < 4; ++k) runs[4 * i + k] = r[k];
@@ -62,10 +63,10 @@ def planner(tmp_path_factory):
     def plan(reqs, hq, hkv, dim, causal, window, sms):
         ints = lambda n: (ctypes.c_int * n)()  # noqa: E731
         cols = [(ctypes.c_int * len(reqs))(*c) for c in zip(*reqs)]
-        info, runs, rows, cuts = ints(4), ints(4 * (CTAS + 1)), ints(CTAS + 1), ints(6 * CTAS)
+        info, runs, rows, cuts = ints(5), ints(4 * (CTAS + 1)), ints(CTAS + 1), ints(6 * CTAS)
         need = so.plan(len(reqs), *cols, hq, hkv, dim, int(causal), window, sms, info, runs, rows, cuts)
-        ctas, n_cuts, part_rows, merge_rows = info
-        return dict(ctas=ctas, part_rows=part_rows, merge_rows=merge_rows, need=need, rows=list(rows)[:n_cuts + 1],
+        ctas, n_cuts, part_rows, merge_rows, longest = info
+        return dict(ctas=ctas, part_rows=part_rows, merge_rows=merge_rows, longest=longest, need=need, rows=list(rows)[:n_cuts + 1],
                     runs=[tuple(runs[4 * i:4 * i + 4]) for i in range(ctas + 1)],
                     cuts=[tuple(cuts[6 * i:6 * i + 6]) for i in range(n_cuts)])
 
@@ -122,8 +123,13 @@ def check(p, reqs, hq, hkv, dim, causal, window, sms):
     assert p["cuts"] == want and p["rows"] == rows and p["merge_rows"] == rows[-1]
     most = max((items[k][5] for k in inside), default=0)
     assert p["part_rows"] == most
-    # every slot: a row's o, its maximum and its sum
-    assert p["need"] >= 4 * 2 * p["ctas"] * most * (dim + 2) if inside else p["need"] == 0
+    # every slot: a row's o, its maximum and its sum; and where a segment has more steps than a sum, both chains' totals
+    ends = starts[1:] + [(len(items), 0)]
+    longest = max(e - b for (k0, s0), (k1, s1) in zip(starts, ends) for k in range(k0, k1 + 1)
+                  for b, e in [(s0 if k == k0 else 0, s1 if k == k1 else items[k][3])])
+    assert p["longest"] == longest
+    need = 4 * 2 * p["ctas"] * most * (dim + 2) + (4 * 2 * p["ctas"] * TILE * (dim + 2) if longest > SUM else 0)
+    assert need <= p["need"] <= need + 512 and (p["need"] > 0) == (need > 0)
 
 
 @pytest.mark.parametrize("seed", range(12))
