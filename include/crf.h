@@ -373,8 +373,9 @@ CRF_API crf_status crf_cache_append(crf_ctx* ctx, const crf_rope* rope, const cr
  * Slots that a row does not see may hold anything, infinities and NaN
  * included. Softmax weights enter the product with v in bf16; sums, maxima
  * and o are fp32, and weights of up to 2^8 are summed before the division: 2^8 times
- * the sum of |v| over a row's keys has to be in fp32's range. `workspace` >= crf_chunk_attention_workspace_size bytes for
- * these chunks, 256-byte aligned. Pages may be shared by requests. */
+ * the sum of |v| over a row's keys has to be in fp32's range. `workspace` >=
+ * crf_chunk_attention_workspace_size bytes for these chunks, 256-byte aligned.
+ * Pages may be shared by requests. */
 CRF_API crf_status crf_chunk_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim,
                                                       const crf_chunk* chunks, int n_chunks, int causal,
                                                       int window, size_t* bytes);

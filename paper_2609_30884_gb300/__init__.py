@@ -234,11 +234,14 @@ class PageTables:
         self.n = n
         self.c = (abi.Pages * max(1, n))()
         for i, t in enumerate(self.tables):
-            need = (_fits("n_tokens", int(n_tokens[i])) + 15) // 16
+            count = int(n_tokens[i])
+            if not -_INT32 <= count < _INT32:
+                raise ValueError(f"table {i}: n_tokens does not fit 32 bits")
+            need = (count + 15) // 16
             _int32_on_device(f"table {i}", t, need)
             if outs is not None:
                 _int32_on_device(f"outs[{i}]", outs[i], need)
-            self.c[i] = abi.Pages(int(n_tokens[i]), t.data_ptr(), None if outs is None else outs[i].data_ptr())
+            self.c[i] = abi.Pages(count, t.data_ptr(), None if outs is None else outs[i].data_ptr())
         self.address = ctypes.addressof(self.c)
 
 

@@ -48,8 +48,8 @@ constexpr int kSegRing = 4;  // segments found ahead
 // Steps of a chain after which its o starts anew. The tensor cores drop the low bits of every sum: in one chain of products
 // o comes out short by 0.76e-6 of itself a tile (v of mean 1, standard deviation 0.5: 6e-3 over 2^20 keys, 0.1 over 2^24).
 // So after this many tiles, 1e-4, o and the sum of weights are added to fp32 totals in the workspace, rounded to nearest
-// (9728 rows over 2^24 keys: 2e-7). 2048 rows over 65536 keys take 1216 us with it, 1188 without; calls whose runs are
-// shorter take what they took.
+// (9728 rows over 2^24 keys: 2e-7). 2048 rows over 65536 keys take 1216 us with it, 1188 without; shorter runs
+// have no totals.
 constexpr int kChain = 128;
 // setmaxnreg split: the first warpgroup (producer, issuer, finder) keeps kRegsCtl, the softmax warpgroups take
 // kRegsSoftmax; the sum must fit what the CTA launched with.
