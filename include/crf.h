@@ -297,6 +297,8 @@ CRF_API crf_status crf_kl_logits_noalloc(int device, const float* z_ref, const f
 #define CRF_MAX_CHUNKS 128  /* requests of one append or attention call */
 #define CRF_MAX_TABLES 512  /* page tables of one crf_pages_* call */
 #define CRF_MAX_KEYS (1 << 26)  /* cached positions of a request that attention sees */
+#define CRF_MAX_TOP 32      /* alternatives of a row of logits */
+#define CRF_MAX_VOCAB (1 << 20)  /* entries of a row of logits */
 
 enum { CRF_BF16 = 0, CRF_FP16 = 1, CRF_FP32 = 2 };                  /* element types of crf_rotary */
 enum { CRF_ROPE_HALF = 0, CRF_ROPE_INTERLEAVED = 1 };               /* pairs (i, i + rot/2) or (2i, 2i + 1) */
@@ -340,6 +342,28 @@ typedef struct crf_heads {
 CRF_API crf_status crf_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts, int n_parts,
                               int type, int n_rows, const int32_t* positions, int inverse, void* stream);
 
+/* RMS norm of a head: gain [head_dim] of the heads' type, aligned to its elements; eps >= 0. */
+typedef struct crf_norm {
+  const void* gain;
+  float eps;
+} crf_norm;
+
+/* crf_rotary's heads, normed on the way: y = R(gain x r), r = 1 / sqrt(mean(x^2) + eps) over the head_dim elements of a
+ * head, R the rotation of its first rot_dim elements; norms[i] belongs to parts[i]. Arithmetic is fp32, y is rounded once
+ * to `type`; the sum of squares has to be in fp32's range. */
+CRF_API crf_status crf_norm_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts, const crf_norm* norms,
+                                   int n_parts, int type, int n_rows, const int32_t* positions, void* stream);
+
+/* Its gradient: parts[i].x is the forward call's x, grads[i].x the gradient of y (its `out` members are not read), parts[i].out
+ * receives that of x and dgains[i] (host array of device fp32 [head_dim]) that of the gain, summed over rows and heads in
+ * a fixed order. parts[i].out may be parts[i].x or grads[i].x, with the same strides; otherwise nothing overlaps. Where x has a
+ * stride of 0, every row or head still gets a gradient of its own. With n_rows == 0 the gains' gradients are
+ * zeros. `workspace` >= crf_norm_rotary_workspace_size bytes, 256-byte aligned. */
+CRF_API crf_status crf_norm_rotary_workspace_size(crf_ctx* ctx, int head_dim, int n_rows, size_t* bytes);
+CRF_API crf_status crf_norm_rotary_grad(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts, const crf_norm* norms,
+                                        const crf_heads* grads, float* const* dgains, int n_parts, int type, int n_rows,
+                                        const int32_t* positions, void* workspace, size_t ws_bytes, void* stream);
+
 /* New rows of one request: n_new (>= 0) rows at positions pos .. pos + n_new - 1.
  * The rows of a call's requests are packed in order. page_table: device int32,
  * ceil((pos + n_new) / 16) entries to append, ceil(n_keys / 16) to attend.
@@ -359,6 +383,13 @@ typedef struct crf_chunk {
 CRF_API crf_status crf_cache_append(crf_ctx* ctx, const crf_rope* rope, const crf_kv_pool* pool, int layer,
                                     int n_kv_heads, int head_dim, const crf_chunk* chunks, int n_chunks,
                                     const crf_heads* q, const crf_heads* k, const crf_heads* v, void* stream);
+
+/* crf_cache_append with normed heads: k is normed by k_norm and rotated, q (if given) by q_norm, as crf_norm_rotary
+ * does; v is copied. */
+CRF_API crf_status crf_cache_append_normed(crf_ctx* ctx, const crf_rope* rope, const crf_kv_pool* pool, int layer,
+                                           int n_kv_heads, int head_dim, const crf_chunk* chunks, int n_chunks,
+                                           const crf_heads* q, const crf_norm* q_norm, const crf_heads* k,
+                                           const crf_norm* k_norm, const crf_heads* v, void* stream);
 
 /* Attention of the rows over their requests' cached keys of `layer`. Row r of a
  * request (position p = pos + r) sees the keys
@@ -427,6 +458,31 @@ CRF_API crf_status crf_pages_release(crf_ctx* ctx, int num_pages, const int32_t*
 /* Workspace bytes (256-byte aligned) of any crf_pages_* call on these tables. */
 CRF_API crf_status crf_pages_workspace_size(crf_ctx* ctx, int num_pages, const crf_pages* tables, int n_tables,
                                             size_t* bytes);
+
+/* Log probabilities. Row r of the logits z (element v at logits[r row_stride + v], of `type`, aligned to its elements,
+ * row_stride >= vocab; that of one row is not read) gives, each output NULL if it is not wanted,
+ *   lse[r]      log sum exp z
+ *   logprob[r]  z_t - lse of the token t = targets[r] (device int32); 0 where t is -1, a padded row. Any other id
+ *               outside [0, vocab) is read as token 0 and reported by crf_check
+ *   entropy[r]  lse - sum p z, p = exp(z - lse)
+ *   top_ids, top_logprobs [n_rows][n_top]: the n_top (0..CRF_MAX_TOP, at most vocab) most probable tokens, descending, the lower
+ *               id first among equal logits, and their log probabilities
+ * in fp32 whatever the type. Logits of -inf (ruled out) have no part in the sums. A row of nothing else has lse and log
+ * probabilities of -inf and entropy 0. A row with NaN or +inf has NaN for all of them but the ids, where NaN
+ * comes last. vocab 1..CRF_MAX_VOCAB, n_rows <= 2^24 (0: nothing to do). No workspace. */
+CRF_API crf_status crf_logprobs(crf_ctx* ctx, const void* logits, int type, int n_rows, int vocab, int64_t row_stride,
+                                const int32_t* targets, float* logprob, float* entropy, float* lse, int n_top,
+                                int32_t* top_ids, float* top_logprobs, void* stream);
+
+/* Its gradient with respect to the logits, from the forward call's lse and entropy:
+ *   d_logits = g_logprob (1[v = t] - p) - g_entropy p (log p + entropy),
+ * fp32 rounded once to `type`. g_logprob (with targets) or g_entropy (with entropy), device fp32 [n_rows], may be
+ * NULL: no such term. Rows whose target is -1 have no first term; a row of lse -inf has gradient 0. d_logits has rows of
+ * d_row_stride >= vocab and may be the logits themselves with the same stride; otherwise it does not overlap them. */
+CRF_API crf_status crf_logprobs_grad(crf_ctx* ctx, const void* logits, int type, int n_rows, int vocab, int64_t row_stride,
+                                     const int32_t* targets, const float* lse, const float* entropy,
+                                     const float* g_logprob, const float* g_entropy, void* d_logits,
+                                     int64_t d_row_stride, void* stream);
 
 /* Per-kernel timing, for measurement: while enabled, every kernel launch and
  * device copy the library issues is bracketed by CUDA events recorded on the

@@ -23,6 +23,12 @@ A recovered cache is extended with new tokens by calls of one layer and of the p
     ctx.cache_append(pool, layer, chunks, k, v, q=q, q_out=q_rot, rope=rope)
     ctx.chunk_attention(pool, layer, chunks, q_rot, o, ctx.chunk_attention_workspace(pool, chunks, n_heads))
     ctx.pages_fork(pool, refs, PageTables(tables, n_tokens, child_tables), ctx.pages_workspace(...))
+
+Decoders that norm their query and key heads give the gains (and have norm_rotary, norm_rotary_grad for rows outside a cache);
+rows of logits are scored by logprobs, with logprobs_grad for what learns from the score:
+
+    ctx.cache_append(pool, layer, chunks, k, v, q=q, q_out=q_rot, rope=rope, q_gain=gq, k_gain=gk)
+    ctx.logprobs(logits, targets, logprob=lp, entropy=h, lse=lse, top_ids=ids, top_logprobs=alternatives)
 """
 from __future__ import annotations
 
@@ -251,6 +257,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda d: torch.cud
 # crf_heads, packed into a context's buffer: building the ctypes structures takes three times as long.
 _pack_heads = struct.Struct("PPiqqqq").pack_into
 _HEADS = ctypes.sizeof(abi.Heads)
+_pack_norm = struct.Struct("Pf").pack_into
+_NORM = ctypes.sizeof(abi.Norm)
 
 
 def _put_heads(buf, at: int, device: int, name: str, x: torch.Tensor, out: Optional[torch.Tensor], dim: int) -> int:
@@ -278,6 +286,13 @@ def _put_heads(buf, at: int, device: int, name: str, x: torch.Tensor, out: Optio
     return shape[1]
 
 
+def _put_norm(buf, at: int, device: int, name: str, gain: torch.Tensor, kind: torch.dtype, dim: int, eps: float) -> None:
+    """crf_norm of ``gain`` [dim] at ``buf[at:]``."""
+    if gain.shape != (dim,) or gain.dtype != kind or gain.get_device() != device or (dim > 1 and gain.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous [{dim}] of the heads' type on cuda:{device}")
+    _pack_norm(buf, at, gain.data_ptr(), eps)
+
+
 def _req_array(reqs: Sequence[Request]):
     arr = (abi.Request * len(reqs))()
     for i, r in enumerate(reqs):
@@ -294,7 +309,9 @@ class Context:
         h = c_void_p()
         abi.check(self.lib.crf_create(byref(h), device))
         self.h = h
-        self._parts = ctypes.create_string_buffer(3 * _HEADS)
+        self._parts = ctypes.create_string_buffer(4 * _HEADS)
+        self._norms = ctypes.create_string_buffer(2 * _NORM)
+        self._dgains = (c_void_p * 2)()
 
     def close(self) -> None:
         if self.h:
@@ -414,6 +431,133 @@ class Context:
         if status:
             abi.check(status)
 
+    def _norm_parts(self, rope: Rope, positions: torch.Tensor, x, gain, out, k, k_gain, k_out, eps: float) -> Tuple[int, int, int]:
+        """Rows, type and parts of a call on normed heads, its descriptors packed."""
+        device, buf, dim = self.device, self._parts, rope.head_dim
+        n, kind = x.shape[0], _TYPES.get(x.dtype)
+        if kind is None:
+            raise ValueError("x must be bfloat16, float16 or float32")
+        self._here(positions)
+        _int32_on_device("positions", positions, n)
+        _put_heads(buf, 0, device, "x", x, x if out is None else out, dim)
+        _put_norm(self._norms, 0, device, "gain", gain, x.dtype, dim, eps)
+        if k is None:
+            return n, kind, 1
+        if k.dtype != x.dtype or k.shape[0] != n:
+            raise ValueError("k must have x's type and rows")
+        if k_gain is None:
+            raise ValueError("k needs k_gain")
+        _put_heads(buf, _HEADS, device, "k", k, k if k_out is None else k_out, dim)
+        _put_norm(self._norms, _NORM, device, "k_gain", k_gain, x.dtype, dim, eps)
+        return n, kind, 2
+
+    def norm_rotary(self, rope: Rope, positions: torch.Tensor, x: torch.Tensor, gain: torch.Tensor,
+                    out: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None,
+                    k_gain: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    stream=None) -> None:
+        """Heads x [rows, heads, head_dim] divided by their root mean square, times ``gain`` [head_dim] (x's type), rotated
+        at ``positions`` into ``out`` (default: in place), in one pass; ``k`` likewise (see crf_norm_rotary)."""
+        n, kind, parts = self._norm_parts(rope, positions, x, gain, out, k, k_gain, k_out, eps)
+        status = self.lib.crf_norm_rotary(self.h, rope.address, self._parts, self._norms, parts, kind, n, positions.data_ptr(),
+                                          _raw_stream(self.device) if stream is None else _stream(stream))
+        if status:
+            abi.check(status)
+
+    def norm_rotary_workspace(self, rope: Rope, n_rows: int) -> torch.Tensor:
+        """Workspace of a norm_rotary_grad call on up to ``n_rows`` rows."""
+        n = c_size_t()
+        abi.check(self.lib.crf_norm_rotary_workspace_size(self.h, rope.head_dim, _fits("n_rows", n_rows), byref(n)))
+        return torch.empty(max(256, n.value), dtype=torch.uint8, device=f"cuda:{self.device}")
+
+    def norm_rotary_grad(self, rope: Rope, positions: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, grad: torch.Tensor,
+                         dx: torch.Tensor, dgain: torch.Tensor, workspace: torch.Tensor, k: Optional[torch.Tensor] = None,
+                         k_gain: Optional[torch.Tensor] = None, k_grad: Optional[torch.Tensor] = None,
+                         k_dx: Optional[torch.Tensor] = None, k_dgain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                         stream=None) -> None:
+        """The gradient of norm_rotary: ``grad`` is that of its output; ``dx`` (which may be x or grad) receives that of x and
+        ``dgain`` (float32 [head_dim]) that of the gain, summed over rows and heads; ``k`` likewise."""
+        if k is not None and (k_grad is None or k_dx is None or k_dgain is None):
+            raise ValueError("k needs k_grad, k_dx and k_dgain")
+        n, kind, parts = self._norm_parts(rope, positions, x, gain, dx, k, k_gain, k_dx, eps)
+        device, buf, dim = self.device, self._parts, rope.head_dim
+        self._here(workspace)
+        for i, (name, g, like, dg) in enumerate((("grad", grad, x, dgain), ("k_grad", k_grad, k, k_dgain))[:parts]):
+            if g.shape != like.shape or g.dtype != like.dtype:
+                raise ValueError(f"{name} must have the heads' shape and type")
+            _put_heads(buf, (2 + i) * _HEADS, device, name, g, None, dim)
+            if dg.shape != (dim,) or dg.dtype != torch.float32 or dg.get_device() != device or not dg.is_contiguous():
+                raise ValueError(f"the gain's gradient must be a contiguous float32 [{dim}] on cuda:{device}")
+            self._dgains[i] = dg.data_ptr()
+        status = self.lib.crf_norm_rotary_grad(self.h, rope.address, buf, self._norms, ctypes.addressof(buf) + 2 * _HEADS,
+                                               self._dgains, parts, kind, n, positions.data_ptr(), workspace.data_ptr(),
+                                               workspace.numel(), _raw_stream(device) if stream is None else _stream(stream))
+        if status:
+            abi.check(status)
+
+    # -------------------------------------------------------------- log probabilities
+    def _logits(self, name: str, z: torch.Tensor) -> int:
+        kind = _TYPES.get(z.dtype)
+        if kind is None or z.dim() != 2 or z.get_device() != self.device or (z.shape[1] > 1 and z.stride(1) != 1):
+            raise ValueError(f"{name} must be [rows, vocab] bfloat16, float16 or float32 on cuda:{self.device}, a row's entries adjacent")
+        if z.shape[0] >= _INT32 or z.shape[1] >= _INT32:
+            raise ValueError(f"{name}: a size does not fit 32 bits")
+        return kind
+
+    def _a_row(self, name: str, t: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> Optional[int]:
+        if t is None:
+            return None
+        if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous() or t.get_device() != self.device:
+            raise ValueError(f"{name} must be a contiguous {dtype} [{n}] on cuda:{self.device}")
+        return t.data_ptr()
+
+    def logprobs(self, logits: torch.Tensor, targets: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None,
+                 entropy: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                 top_ids: Optional[torch.Tensor] = None, top_logprobs: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Of rows of logits [rows, vocab] (bf16, fp16 or fp32; decode_step's, kl's): the log probability of ``targets`` [rows]
+        (int32; -1: none, 0), the entropy and the log of the sum of exponentials (fp32 [rows]); the most probable tokens (int32
+        [rows, n], n at most 32, the lower id first among equals) and their log probabilities (fp32 [rows, n]). See crf_logprobs."""
+        kind = self._logits("logits", logits)
+        n, vocab = logits.shape
+        t = self._a_row("targets", targets, n, torch.int32)
+        a = self._a_row("logprob", logprob, n, torch.float32)
+        b = self._a_row("entropy", entropy, n, torch.float32)
+        c = self._a_row("lse", lse, n, torch.float32)
+        k = 0
+        for name, x, dtype in (("top_ids", top_ids, torch.int32), ("top_logprobs", top_logprobs, torch.float32)):
+            if x is not None:
+                if x.dim() != 2 or x.shape[0] != n or x.dtype != dtype or not x.is_contiguous() or x.get_device() != self.device:
+                    raise ValueError(f"{name} must be a contiguous {dtype} [{n}, alternatives] on cuda:{self.device}")
+                k = x.shape[1]
+        if top_ids is not None and top_logprobs is not None and top_ids.shape != top_logprobs.shape:
+            raise ValueError("top_ids and top_logprobs must have one shape")
+        status = self.lib.crf_logprobs(self.h, logits.data_ptr(), kind, n, vocab, logits.stride(0), t, a, b, c, k,
+                                       _ptr(top_ids), _ptr(top_logprobs),
+                                       _raw_stream(self.device) if stream is None else _stream(stream))
+        if status:
+            abi.check(status)
+
+    def logprobs_grad(self, logits: torch.Tensor, targets: Optional[torch.Tensor], lse: torch.Tensor, d_logits: torch.Tensor,
+                      g_logprob: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                      g_entropy: Optional[torch.Tensor] = None, stream=None) -> None:
+        """The gradient of logprobs' ``logprob`` and ``entropy`` (theirs are ``g_logprob`` and ``g_entropy``, fp32 [rows]) with
+        respect to the logits, into ``d_logits`` (which may be the logits); ``lse`` and ``entropy`` as logprobs gave them."""
+        kind = self._logits("logits", logits)
+        if self._logits("d_logits", d_logits) != kind or d_logits.shape != logits.shape:
+            raise ValueError("d_logits must have the logits' shape and type")
+        n, vocab = logits.shape
+        if lse is None:
+            raise ValueError("lse is needed")
+        t = self._a_row("targets", targets, n, torch.int32)
+        e = self._a_row("lse", lse, n, torch.float32)
+        h = self._a_row("entropy", entropy, n, torch.float32)
+        a = self._a_row("g_logprob", g_logprob, n, torch.float32)
+        b = self._a_row("g_entropy", g_entropy, n, torch.float32)
+        status = self.lib.crf_logprobs_grad(self.h, logits.data_ptr(), kind, n, vocab, logits.stride(0), t, e, h, a, b,
+                                            d_logits.data_ptr(), d_logits.stride(0),
+                                            _raw_stream(self.device) if stream is None else _stream(stream))
+        if status:
+            abi.check(status)
+
     def _pool_layer(self, pool: KVPool, layer: int) -> Tuple[int, int]:
         if not 0 <= layer < len(pool.k_pages):
             raise ValueError(f"layer {layer} is not in the pool")
@@ -429,9 +573,11 @@ class Context:
 
     def cache_append(self, pool: KVPool, layer: int, chunks: Chunks, k: torch.Tensor, v: torch.Tensor,
                      q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
-                     rope: Optional[Rope] = None, stream=None) -> None:
+                     rope: Optional[Rope] = None, stream=None, q_gain: Optional[torch.Tensor] = None,
+                     k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6) -> None:
         """Rows k, v [rows, kv heads, head_dim] into the requests' pages of ``layer``, k rotated at its
-        position when ``rope`` is given; and ``q`` rotated into ``q_out`` (default: in place)."""
+        position when ``rope`` is given; and ``q`` rotated into ``q_out`` (default: in place). With ``k_gain``
+        (and ``q_gain`` for q) the heads are normed first, as norm_rotary does."""
         hkv, dim = self._pool_layer(pool, layer)
         device, buf, n = self.device, self._parts, chunks.rows
         if chunks.device != device:
@@ -447,6 +593,20 @@ class Context:
         _put_heads(buf, 2 * _HEADS, device, "v", v, None, dim)
         if q is not None:
             _put_heads(buf, 0, device, "q", q, q if q_out is None else q_out, dim)
+        if q_gain is not None or k_gain is not None:
+            if rope is None or k_gain is None or (q is None) != (q_gain is None):
+                raise ValueError("normed heads need rope, k_gain, and q_gain exactly where there is q")
+            norms, to = self._norms, ctypes.addressof(self._norms)
+            _put_norm(norms, _NORM, device, "k_gain", k_gain, bf16, dim, eps)
+            if q is not None:
+                _put_norm(norms, 0, device, "q_gain", q_gain, bf16, dim, eps)
+            status = self.lib.crf_cache_append_normed(
+                self.h, rope.address, pool.address, layer, hkv, dim, chunks.address, chunks.n, None if q is None else at,
+                None if q is None else to, at + _HEADS, to + _NORM, at + 2 * _HEADS,
+                _raw_stream(device) if stream is None else _stream(stream))
+            if status:
+                abi.check(status)
+            return
         status = self.lib.crf_cache_append(self.h, None if rope is None else rope.address, pool.address, layer, hkv, dim,
                                            chunks.address, chunks.n, None if q is None else at, at + _HEADS,
                                            at + 2 * _HEADS, _raw_stream(device) if stream is None else _stream(stream))

@@ -24,6 +24,8 @@ PAGE_SIZE = 16
 MAX_REQUESTS = 32
 MAX_CHUNKS = 128
 MAX_TABLES = 512
+MAX_TOP = 32
+MAX_VOCAB = 1 << 20
 BF16, FP16, FP32 = range(3)
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "bands": 3}
@@ -35,7 +37,9 @@ EXPORTS = ("crf_create", "crf_destroy", "crf_last_error", "crf_check", "crf_work
            "crf_profile_read", "crf_decode_workspace_size", "crf_decode_step",
            "crf_selftest_timeout", "crf_rotary", "crf_cache_append",
            "crf_chunk_attention_workspace_size", "crf_chunk_attention", "crf_pages_workspace_size",
-           "crf_pages_fork", "crf_pages_compact", "crf_pages_release")
+           "crf_pages_fork", "crf_pages_compact", "crf_pages_release", "crf_norm_rotary",
+           "crf_norm_rotary_workspace_size", "crf_norm_rotary_grad", "crf_cache_append_normed",
+           "crf_logprobs", "crf_logprobs_grad")
 
 
 class ModelDims(ctypes.Structure):
@@ -86,6 +90,10 @@ class Rope(ctypes.Structure):
 class Heads(ctypes.Structure):
     _fields_ = [("x", c_void_p), ("out", c_void_p), ("heads", c_int), ("x_row", c_int64),
                 ("x_head", c_int64), ("out_row", c_int64), ("out_head", c_int64)]
+
+
+class Norm(ctypes.Structure):
+    _fields_ = [("gain", c_void_p), ("eps", c_float)]
 
 
 class Chunk(ctypes.Structure):
@@ -140,6 +148,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "crf_pages_fork": ([P, P, c_int, c_int, c_int, P, P, P, c_int, c_int, P, c_size_t, P], c_int),
         "crf_pages_compact": ([P, P, c_int, c_int, c_int, P, P, P, c_int, P, c_size_t, P], c_int),
         "crf_pages_release": ([P, c_int, P, P, P, c_int, P, c_size_t, P], c_int),
+        "crf_norm_rotary": ([P, P, P, P, c_int, c_int, c_int, P, P], c_int),
+        "crf_norm_rotary_workspace_size": ([P, c_int, c_int, POINTER(c_size_t)], c_int),
+        "crf_norm_rotary_grad": ([P, P, P, P, P, P, c_int, c_int, c_int, P, P, c_size_t, P], c_int),
+        "crf_cache_append_normed": ([P, P, P, c_int, c_int, c_int, P, c_int, P, P, P, P, P, P], c_int),
+        "crf_logprobs": ([P, P, c_int, c_int, c_int, c_int64, P, P, P, P, c_int, P, P, P], c_int),
+        "crf_logprobs_grad": ([P, P, c_int, c_int, c_int, c_int64, P, P, P, P, P, P, c_int64, P], c_int),
         "crf_kl_logits_noalloc": ([c_int, P, P, c_int, c_int, P, P], c_int),
         "crf_profile_enable": ([P, c_int, c_int], c_int),
         "crf_profile_read": ([P, c_int, ctypes.c_char_p, POINTER(ctypes.c_double), POINTER(c_int),

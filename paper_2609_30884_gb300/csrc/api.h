@@ -27,7 +27,8 @@ namespace crf {
 
 enum ProfKind : int {
   kPQkv, kPO, kPGateUp, kPDown, kPAttn, kPNorm, kPEmbed, kPCopy,
-  kPDecode, kPLmHead, kPKl, kPDrift, kPCheck, kPRotary, kPAppend, kPChunkAttn, kPPagePlan, kPPageCopy, kPNumKinds
+  kPDecode, kPLmHead, kPKl, kPDrift, kPCheck, kPRotary, kPAppend, kPChunkAttn, kPPagePlan, kPPageCopy,
+  kPHeadNorm, kPHeadNormGrad, kPLogprobs, kPLogprobsGrad, kPNumKinds
 };
 
 // Brackets the launches issued in its lifetime with two events on `st` when

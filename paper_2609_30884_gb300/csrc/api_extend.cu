@@ -14,7 +14,8 @@ using namespace crf;
 namespace {
 
 // The arrays that kernels take are sized by the one and filled up to the other.
-static_assert(kMaxChunks == CRF_MAX_CHUNKS && kMaxTables == CRF_MAX_TABLES, "limits of the ABI and of the kernels differ");
+static_assert(kMaxChunks == CRF_MAX_CHUNKS && kMaxTables == CRF_MAX_TABLES && kMaxTop == CRF_MAX_TOP && kMaxVocab == CRF_MAX_VOCAB,
+              "limits of the ABI and of the kernels differ");
 
 // The context's device for the length of a call, then the caller's again.
 class DeviceScope {
@@ -205,6 +206,130 @@ crf_status check_attention(int n_q_heads, int n_kv_heads, int window, int64_t ro
   return CRF_OK;
 }
 
+// ---------------------------------------------------------------- heads of a call
+// The arguments that calls on rows of heads share, checked, and their descriptor; it is left unset where there are no rows.
+crf_status rotary_call(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts, int n_parts, int type, int n_rows,
+                       const int32_t* positions, RotaryDesc* d) {
+  if (!ctx || !rope || !parts) return fail(CRF_EINVAL, "null argument");
+  crf_status s = check_rope(*rope);
+  if (s != CRF_OK) return s;
+  if (n_parts < 1 || n_parts > 2) return fail(CRF_EINVAL, "n_parts %d out of range (1 or 2)", n_parts);
+  if (type < CRF_BF16 || type > CRF_FP32) return fail(CRF_EUNSUPPORTED, "unknown element type %d", type);
+  if (n_rows < 0) return fail(CRF_EINVAL, "n_rows must be >= 0");
+  if (n_rows == 0) return CRF_OK;
+  if (!positions || !aligned4(positions)) return fail(CRF_EINVAL, "positions null or misaligned");
+  std::memset(d, 0, sizeof(*d));
+  for (int p = 0; p < n_parts; ++p) {
+    const char* name = p ? "part 1" : "part 0";
+    const crf_heads h = settled(parts[p], n_rows, rope->head_dim);
+    s = check_heads(h, type == CRF_FP32 ? 4 : 2, true, name);
+    if (s != CRF_OK) return s;
+    s = check_out(h, n_rows, rope->head_dim, name);
+    if (s != CRF_OK) return s;
+    if (h.x == h.out && (h.x_row != h.out_row || h.x_head != h.out_head))
+      return fail(CRF_ESHAPE, "%s: in place with other strides", name);
+    d->part[p] = part_of(h, true);
+  }
+  d->n_parts = n_parts;
+  d->head_dim = rope->head_dim;
+  d->rot_dim = rope->rot_dim;
+  d->interleaved = rope->layout == CRF_ROPE_INTERLEAVED;
+  d->magnitude = static_cast<float>(rope->magnitude);
+  d->n_rows = n_rows;
+  d->positions = positions;
+  d->type = type;
+  d->status = ctx->status_dev;
+  fill_turns(*rope, d->turns);
+  return CRF_OK;
+}
+
+// The same of an append; no rows: t->row0[t->n] is 0 and *d unset.
+crf_status append_call(crf_ctx* ctx, const crf_rope* rope, const crf_kv_pool* pool, int layer, int n_kv_heads, int head_dim,
+                       const crf_chunk* chunks, int n_chunks, const crf_heads* q, const crf_heads* k, const crf_heads* v,
+                       RotaryDesc* d, ChunkTable* t) {
+  if (!ctx || !pool || !k || !v) return fail(CRF_EINVAL, "null argument");
+  crf_status s = check_pool_shape(n_kv_heads, head_dim, pool->num_pages);
+  if (s != CRF_OK) return s;
+  s = check_layer(pool, layer);
+  if (s != CRF_OK) return s;
+  if (q && !rope) return fail(CRF_EINVAL, "q needs rope: there is nothing else to do with it");
+  if (rope) {
+    s = check_rope(*rope);
+    if (s != CRF_OK) return s;
+    if (rope->head_dim != head_dim) return fail(CRF_ESHAPE, "rope head_dim %d != head_dim %d", rope->head_dim, head_dim);
+  }
+  s = fill_chunks(chunks, n_chunks, false, pool->num_pages, t);
+  if (s != CRF_OK) return s;
+  const int rows = t->row0[t->n];
+  if (rows == 0) return CRF_OK;
+  const crf_heads hk = settled(*k, rows, head_dim), hv = settled(*v, rows, head_dim);
+  s = check_heads(hk, 2, false, "k");
+  if (s != CRF_OK) return s;
+  s = check_heads(hv, 2, false, "v");
+  if (s != CRF_OK) return s;
+  if (k->heads != n_kv_heads || v->heads != n_kv_heads)
+    return fail(CRF_ESHAPE, "k has %d and v %d heads, the pool %d", k->heads, v->heads, n_kv_heads);
+  std::memset(d, 0, sizeof(*d));
+  if (q) {
+    const crf_heads hq = settled(*q, rows, head_dim);
+    s = check_heads(hq, 2, true, "q");
+    if (s != CRF_OK) return s;
+    s = check_out(hq, rows, head_dim, "q");
+    if (s != CRF_OK) return s;
+    if (hq.x == hq.out && (hq.x_row != hq.out_row || hq.x_head != hq.out_head))
+      return fail(CRF_ESHAPE, "q: in place with other strides");
+    d->part[d->n_parts++] = part_of(hq, true);
+  }
+  RotPart kp = part_of(hk, rope != nullptr), vp = part_of(hv, false);
+  kp.paged = vp.paged = true;
+  kp.out = pool->k_pages[layer];
+  vp.out = pool->v_pages[layer];
+  d->part[d->n_parts++] = kp;
+  d->part[d->n_parts++] = vp;
+  d->head_dim = head_dim;
+  d->rot_dim = rope ? rope->rot_dim : 2;
+  if (rope) {
+    d->interleaved = rope->layout == CRF_ROPE_INTERLEAVED;
+    d->magnitude = static_cast<float>(rope->magnitude);
+    fill_turns(*rope, d->turns);
+  } else {
+    d->rot_dim = head_dim;  // whole heads of units that no part rotates
+  }
+  d->n_rows = rows;
+  d->n_kv_heads = n_kv_heads;
+  d->type = CRF_BF16;
+  d->status = ctx->status_dev;
+  return CRF_OK;
+}
+
+crf_status check_norms(const crf_norm* norms, int n, int type, const void** gain, float* eps) {
+  if (!norms) return fail(CRF_EINVAL, "norms is null");
+  for (int i = 0; i < n; ++i) {
+    if (!norms[i].gain || (reinterpret_cast<uintptr_t>(norms[i].gain) & (type == CRF_FP32 ? 3 : 1)))
+      return fail(CRF_EINVAL, "norm %d: gain null or misaligned", i);
+    if (!(norms[i].eps >= 0.f) || !std::isfinite(norms[i].eps)) return fail(CRF_EINVAL, "norm %d: eps must be finite and at least 0", i);
+    gain[i] = norms[i].gain;
+    eps[i] = norms[i].eps;
+  }
+  return CRF_OK;
+}
+
+// ---------------------------------------------------------------- logits
+crf_status check_logits(int type, int n_rows, int vocab) {
+  if (type < CRF_BF16 || type > CRF_FP32) return fail(CRF_EUNSUPPORTED, "unknown element type %d", type);
+  if (vocab < 1 || vocab > CRF_MAX_VOCAB) return fail(CRF_EUNSUPPORTED, "vocab %d out of range (1..%d)", vocab, CRF_MAX_VOCAB);
+  if (n_rows < 0) return fail(CRF_EINVAL, "n_rows must be >= 0");
+  if (n_rows > (1 << 24)) return fail(CRF_EUNSUPPORTED, "n_rows %d over 2^24", n_rows);
+  return CRF_OK;
+}
+crf_status check_rows_of(const void* x, int type, int n_rows, int vocab, int64_t stride, const char* name) {
+  if (!x) return fail(CRF_EINVAL, "%s is null", name);
+  if (reinterpret_cast<uintptr_t>(x) & (type == CRF_FP32 ? 3 : 1)) return fail(CRF_EINVAL, "%s: not aligned to its elements", name);
+  if (n_rows > 1 && (stride < vocab || stride > (int64_t{1} << 40)))
+    return fail(CRF_ESHAPE, "%s: row stride under vocab, or over 2^40", name);
+  return CRF_OK;
+}
+
 // ---------------------------------------------------------------- pages
 crf_status fill_tables(const crf_pages* tables, int n, int num_pages, bool has_out, bool deep, PageTables* t) {
   if (!tables) return fail(CRF_EINVAL, "tables is null");
@@ -273,38 +398,10 @@ extern "C" {
 crf_status crf_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts, int n_parts, int type, int n_rows,
                       const int32_t* positions, int inverse, void* stream) {
   return guarded([&]() -> crf_status {
-    if (!ctx || !rope || !parts) return fail(CRF_EINVAL, "null argument");
-    crf_status s = check_rope(*rope);
-    if (s != CRF_OK) return s;
-    if (n_parts < 1 || n_parts > 2) return fail(CRF_EINVAL, "n_parts %d out of range (1 or 2)", n_parts);
-    if (type < CRF_BF16 || type > CRF_FP32) return fail(CRF_EUNSUPPORTED, "unknown element type %d", type);
-    if (n_rows < 0) return fail(CRF_EINVAL, "n_rows must be >= 0");
-    if (n_rows == 0) return CRF_OK;
-    if (!positions || !aligned4(positions)) return fail(CRF_EINVAL, "positions null or misaligned");
     RotaryDesc d;
-    std::memset(&d, 0, sizeof(d));
-    for (int p = 0; p < n_parts; ++p) {
-      const char* name = p ? "part 1" : "part 0";
-      const crf_heads h = settled(parts[p], n_rows, rope->head_dim);
-      s = check_heads(h, type == CRF_FP32 ? 4 : 2, true, name);
-      if (s != CRF_OK) return s;
-      s = check_out(h, n_rows, rope->head_dim, name);
-      if (s != CRF_OK) return s;
-      if (h.x == h.out && (h.x_row != h.out_row || h.x_head != h.out_head))
-        return fail(CRF_ESHAPE, "%s: in place with other strides", name);
-      d.part[p] = part_of(h, true);
-    }
-    d.n_parts = n_parts;
-    d.head_dim = rope->head_dim;
-    d.rot_dim = rope->rot_dim;
-    d.interleaved = rope->layout == CRF_ROPE_INTERLEAVED;
+    const crf_status s = rotary_call(ctx, rope, parts, n_parts, type, n_rows, positions, &d);
+    if (s != CRF_OK || n_rows == 0) return s;
     d.inverse = inverse != 0;
-    d.magnitude = static_cast<float>(rope->magnitude);
-    d.n_rows = n_rows;
-    d.positions = positions;
-    d.type = type;
-    d.status = ctx->status_dev;
-    fill_turns(*rope, d.turns);
     DeviceScope dev(ctx->device);
     CRF_CUDA(dev.error());
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -314,69 +411,192 @@ crf_status crf_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts
   });
 }
 
+crf_status crf_norm_rotary(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts, const crf_norm* norms, int n_parts,
+                           int type, int n_rows, const int32_t* positions, void* stream) {
+  return guarded([&]() -> crf_status {
+    HeadNormDesc d;
+    std::memset(&d, 0, sizeof(d));
+    crf_status s = rotary_call(ctx, rope, parts, n_parts, type, n_rows, positions, &d.r);
+    if (s != CRF_OK) return s;
+    s = check_norms(norms, n_parts, type, d.gain, d.eps);
+    if (s != CRF_OK || n_rows == 0) return s;
+    d.inv_dim = 1.0f / rope->head_dim;
+    DeviceScope dev(ctx->device);
+    CRF_CUDA(dev.error());
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    ProfScope ps(ctx, kPHeadNorm, st);
+    CRF_CUDA(launch_head_norm(d, nullptr, ctx->num_sms, st));
+    return CRF_OK;
+  });
+}
+
+crf_status crf_norm_rotary_workspace_size(crf_ctx* ctx, int head_dim, int n_rows, size_t* bytes) {
+  return guarded([&]() -> crf_status {
+    if (!ctx || !bytes) return fail(CRF_EINVAL, "null argument");
+    if (head_dim < 2 || head_dim > 2 * kMaxPairs) return fail(CRF_EUNSUPPORTED, "head_dim %d unsupported", head_dim);
+    if (n_rows < 0) return fail(CRF_EINVAL, "n_rows must be >= 0");
+    *bytes = align256(head_norm_grad_workspace(n_rows, head_dim, ctx->num_sms));
+    return CRF_OK;
+  });
+}
+
+crf_status crf_norm_rotary_grad(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts, const crf_norm* norms,
+                                const crf_heads* grads, float* const* dgains, int n_parts, int type, int n_rows,
+                                const int32_t* positions, void* workspace, size_t ws_bytes, void* stream) {
+  return guarded([&]() -> crf_status {
+    HeadNormGradDesc d;
+    std::memset(&d, 0, sizeof(d));
+    crf_status s = rotary_call(ctx, rope, parts, n_parts, type, n_rows, positions, &d.r);
+    if (s != CRF_OK) return s;
+    s = check_norms(norms, n_parts, type, d.gain, d.eps);
+    if (s != CRF_OK) return s;
+    if (!grads || !dgains) return fail(CRF_EINVAL, "null argument");
+    d.r.n_parts = n_parts;
+    d.r.head_dim = rope->head_dim;
+    d.r.inverse = true;
+    d.inv_dim = 1.0f / rope->head_dim;
+    for (int p = 0; p < n_parts; ++p) {
+      if (!dgains[p] || !aligned4(dgains[p])) return fail(CRF_EINVAL, "dgains[%d] null or misaligned", p);
+      d.dgain[p] = dgains[p];
+      if (n_rows == 0) continue;
+      const char* name = p ? "grads 1" : "grads 0";
+      const crf_heads g = settled(grads[p], n_rows, rope->head_dim);
+      s = check_heads(g, type == CRF_FP32 ? 4 : 2, false, name);
+      if (s != CRF_OK) return s;
+      if (g.heads != parts[p].heads) return fail(CRF_ESHAPE, "%s: %d heads, x has %d", name, g.heads, parts[p].heads);
+      if (g.x == d.r.part[p].out && (g.x_row != d.r.part[p].out_row || g.x_head != d.r.part[p].out_head))
+        return fail(CRF_ESHAPE, "%s: written over with other strides", name);
+      d.grad[p] = g.x;
+      d.g_row[p] = g.x_row;
+      d.g_head[p] = g.x_head;
+    }
+    s = check_workspace(workspace, ws_bytes, head_norm_grad_workspace(n_rows, rope->head_dim, ctx->num_sms));
+    if (s != CRF_OK) return s;
+    DeviceScope dev(ctx->device);
+    CRF_CUDA(dev.error());
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    ProfScope ps(ctx, kPHeadNormGrad, st, n_rows ? 2 : 0);
+    CRF_CUDA(launch_head_norm_grad(d, static_cast<float*>(workspace), ctx->num_sms, st));
+    return CRF_OK;
+  });
+}
+
 crf_status crf_cache_append(crf_ctx* ctx, const crf_rope* rope, const crf_kv_pool* pool, int layer, int n_kv_heads,
                             int head_dim, const crf_chunk* chunks, int n_chunks, const crf_heads* q, const crf_heads* k,
                             const crf_heads* v, void* stream) {
   return guarded([&]() -> crf_status {
-    if (!ctx || !pool || !k || !v) return fail(CRF_EINVAL, "null argument");
-    crf_status s = check_pool_shape(n_kv_heads, head_dim, pool->num_pages);
-    if (s != CRF_OK) return s;
-    s = check_layer(pool, layer);
-    if (s != CRF_OK) return s;
-    if (q && !rope) return fail(CRF_EINVAL, "q needs rope: there is nothing else to do with it");
-    if (rope) {
-      s = check_rope(*rope);
-      if (s != CRF_OK) return s;
-      if (rope->head_dim != head_dim) return fail(CRF_ESHAPE, "rope head_dim %d != head_dim %d", rope->head_dim, head_dim);
-    }
-    ChunkTable t;
-    s = fill_chunks(chunks, n_chunks, false, pool->num_pages, &t);
-    if (s != CRF_OK) return s;
-    const int rows = t.row0[t.n];
-    if (rows == 0) return CRF_OK;
-    const crf_heads hk = settled(*k, rows, head_dim), hv = settled(*v, rows, head_dim);
-    s = check_heads(hk, 2, false, "k");
-    if (s != CRF_OK) return s;
-    s = check_heads(hv, 2, false, "v");
-    if (s != CRF_OK) return s;
-    if (k->heads != n_kv_heads || v->heads != n_kv_heads)
-      return fail(CRF_ESHAPE, "k has %d and v %d heads, the pool %d", k->heads, v->heads, n_kv_heads);
     RotaryDesc d;
-    std::memset(&d, 0, sizeof(d));
-    if (q) {
-      const crf_heads hq = settled(*q, rows, head_dim);
-      s = check_heads(hq, 2, true, "q");
-      if (s != CRF_OK) return s;
-      s = check_out(hq, rows, head_dim, "q");
-      if (s != CRF_OK) return s;
-      if (hq.x == hq.out && (hq.x_row != hq.out_row || hq.x_head != hq.out_head))
-        return fail(CRF_ESHAPE, "q: in place with other strides");
-      d.part[d.n_parts++] = part_of(hq, true);
-    }
-    RotPart kp = part_of(hk, rope != nullptr), vp = part_of(hv, false);
-    kp.paged = vp.paged = true;
-    kp.out = pool->k_pages[layer];
-    vp.out = pool->v_pages[layer];
-    d.part[d.n_parts++] = kp;
-    d.part[d.n_parts++] = vp;
-    d.head_dim = head_dim;
-    d.rot_dim = rope ? rope->rot_dim : 2;
-    if (rope) {
-      d.interleaved = rope->layout == CRF_ROPE_INTERLEAVED;
-      d.magnitude = static_cast<float>(rope->magnitude);
-      fill_turns(*rope, d.turns);
-    } else {
-      d.rot_dim = head_dim;  // whole heads of units that no part rotates
-    }
-    d.n_rows = rows;
-    d.n_kv_heads = n_kv_heads;
-    d.type = CRF_BF16;
-    d.status = ctx->status_dev;
+    ChunkTable t;
+    const crf_status s = append_call(ctx, rope, pool, layer, n_kv_heads, head_dim, chunks, n_chunks, q, k, v, &d, &t);
+    if (s != CRF_OK || t.row0[t.n] == 0) return s;
     DeviceScope dev(ctx->device);
     CRF_CUDA(dev.error());
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     ProfScope ps(ctx, kPAppend, st);
     CRF_CUDA(launch_rotary(d, &t, ctx->num_sms, st));
+    return CRF_OK;
+  });
+}
+
+crf_status crf_cache_append_normed(crf_ctx* ctx, const crf_rope* rope, const crf_kv_pool* pool, int layer, int n_kv_heads,
+                                   int head_dim, const crf_chunk* chunks, int n_chunks, const crf_heads* q,
+                                   const crf_norm* q_norm, const crf_heads* k, const crf_norm* k_norm, const crf_heads* v,
+                                   void* stream) {
+  return guarded([&]() -> crf_status {
+    if (!rope || !k_norm || (q && !q_norm)) return fail(CRF_EINVAL, "null argument");
+    HeadNormDesc d;
+    std::memset(&d, 0, sizeof(d));
+    crf_norm norms[2] = {q ? *q_norm : *k_norm, *k_norm};  // part 0 is q, or k without it
+    crf_status s = check_norms(norms, q ? 2 : 1, CRF_BF16, d.gain, d.eps);
+    if (s != CRF_OK) return s;
+    ChunkTable t;
+    s = append_call(ctx, rope, pool, layer, n_kv_heads, head_dim, chunks, n_chunks, q, k, v, &d.r, &t);
+    if (s != CRF_OK || t.row0[t.n] == 0) return s;
+    d.inv_dim = 1.0f / head_dim;
+    DeviceScope dev(ctx->device);
+    CRF_CUDA(dev.error());
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    ProfScope ps(ctx, kPHeadNorm, st);
+    CRF_CUDA(launch_head_norm(d, &t, ctx->num_sms, st));
+    return CRF_OK;
+  });
+}
+
+crf_status crf_logprobs(crf_ctx* ctx, const void* logits, int type, int n_rows, int vocab, int64_t row_stride,
+                        const int32_t* targets, float* logprob, float* entropy, float* lse, int n_top, int32_t* top_ids,
+                        float* top_logprobs, void* stream) {
+  return guarded([&]() -> crf_status {
+    if (!ctx) return fail(CRF_EINVAL, "ctx is null");
+    crf_status s = check_logits(type, n_rows, vocab);
+    if (s != CRF_OK) return s;
+    if (n_top < 0 || n_top > CRF_MAX_TOP || n_top > vocab)
+      return fail(CRF_EUNSUPPORTED, "n_top %d out of range (0..%d, at most vocab)", n_top, CRF_MAX_TOP);
+    if (n_rows == 0) return CRF_OK;
+    s = check_rows_of(logits, type, n_rows, vocab, row_stride, "logits");
+    if (s != CRF_OK) return s;
+    if (logprob && !targets) return fail(CRF_EINVAL, "logprob needs targets");
+    if (n_top && !top_ids && !top_logprobs) return fail(CRF_EINVAL, "n_top without an output for it");
+    if (!aligned4(targets) || !aligned4(logprob) || !aligned4(entropy) || !aligned4(lse) || !aligned4(top_ids) || !aligned4(top_logprobs))
+      return fail(CRF_EINVAL, "targets or an output misaligned");
+    LogprobsDesc d;
+    d.z = logits;
+    d.z_row = n_rows == 1 ? 0 : row_stride;
+    d.type = type;
+    d.n_rows = n_rows;
+    d.vocab = vocab;
+    d.n_top = n_top;
+    d.targets = targets;
+    d.logprob = logprob;
+    d.entropy = entropy;
+    d.lse = lse;
+    d.top_ids = top_ids;
+    d.top_logprobs = top_logprobs;
+    d.status = ctx->status_dev;
+    DeviceScope dev(ctx->device);
+    CRF_CUDA(dev.error());
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    ProfScope ps(ctx, kPLogprobs, st);
+    CRF_CUDA(launch_logprobs(d, ctx->num_sms, st));
+    return CRF_OK;
+  });
+}
+
+crf_status crf_logprobs_grad(crf_ctx* ctx, const void* logits, int type, int n_rows, int vocab, int64_t row_stride,
+                             const int32_t* targets, const float* lse, const float* entropy, const float* g_logprob,
+                             const float* g_entropy, void* d_logits, int64_t d_row_stride, void* stream) {
+  return guarded([&]() -> crf_status {
+    if (!ctx) return fail(CRF_EINVAL, "ctx is null");
+    crf_status s = check_logits(type, n_rows, vocab);
+    if (s != CRF_OK || n_rows == 0) return s;
+    s = check_rows_of(logits, type, n_rows, vocab, row_stride, "logits");
+    if (s != CRF_OK) return s;
+    s = check_rows_of(d_logits, type, n_rows, vocab, d_row_stride, "d_logits");
+    if (s != CRF_OK) return s;
+    if (logits == d_logits && n_rows > 1 && row_stride != d_row_stride) return fail(CRF_ESHAPE, "d_logits: in place with another stride");
+    if (!lse) return fail(CRF_EINVAL, "lse is null");
+    if (g_logprob && !targets) return fail(CRF_EINVAL, "g_logprob needs targets");
+    if (g_entropy && !entropy) return fail(CRF_EINVAL, "g_entropy needs entropy");
+    if (!aligned4(targets) || !aligned4(lse) || !aligned4(entropy) || !aligned4(g_logprob) || !aligned4(g_entropy))
+      return fail(CRF_EINVAL, "targets, lse, entropy or a gradient misaligned");
+    LogprobsGradDesc d;
+    d.z = logits;
+    d.dz = d_logits;
+    d.z_row = n_rows == 1 ? 0 : row_stride;
+    d.dz_row = n_rows == 1 ? 0 : d_row_stride;
+    d.type = type;
+    d.n_rows = n_rows;
+    d.vocab = vocab;
+    d.targets = g_logprob ? targets : nullptr;
+    d.lse = lse;
+    d.entropy = entropy;
+    d.g_logprob = g_logprob;
+    d.g_entropy = g_entropy;
+    d.status = ctx->status_dev;
+    DeviceScope dev(ctx->device);
+    CRF_CUDA(dev.error());
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    ProfScope ps(ctx, kPLogprobsGrad, st);
+    CRF_CUDA(launch_logprobs_grad(d, st));
     return CRF_OK;
   });
 }

@@ -1,5 +1,5 @@
-// Launchers of the calls that extend a cache with new tokens: rotary positions, writes of new keys and
-// values, attention of a chunk over the pages, and the pages' reference counts.
+// Launchers of the calls that extend a cache with new tokens: rotary positions, norms of heads, writes of new keys and
+// values, attention of a chunk over the pages, the pages' reference counts, and log probabilities of tokens.
 #pragma once
 
 #include "kernels.h"
@@ -9,6 +9,8 @@ namespace crf {
 constexpr int kMaxChunks = 128;  // equals CRF_MAX_CHUNKS (api_extend.cu checks that)
 constexpr int kMaxTables = 512;  // equals CRF_MAX_TABLES
 constexpr int kMaxPairs = 128;   // rotary pairs of a head
+constexpr int kMaxTop = 32;      // equals CRF_MAX_TOP
+constexpr int kMaxVocab = 1 << 20;  // equals CRF_MAX_VOCAB
 
 // The requests of a call: rows [row0[i], row0[i + 1]) are request i's, at positions pos[i] on.
 struct ChunkTable {
@@ -41,6 +43,56 @@ struct RotaryDesc {
   int* status;
 };
 cudaError_t launch_rotary(const RotaryDesc& d, const ChunkTable* chunks, int num_sms, cudaStream_t stream);
+
+// ---------------------------------------------------------------- norms of heads
+// Parts that are rotated are normed first, with the gain and eps of their number.
+struct HeadNormDesc {
+  RotaryDesc r;
+  const void* gain[2];
+  float eps[2];
+  float inv_dim;               // 1 / head_dim
+};
+cudaError_t launch_head_norm(const HeadNormDesc& d, const ChunkTable* chunks, int num_sms, cudaStream_t stream);
+// r.part: x and, as out, its gradient; r.inverse is set.
+struct HeadNormGradDesc {
+  RotaryDesc r;
+  const void* gain[2];
+  const void* grad[2];         // of the outputs
+  int64_t g_row[2], g_head[2];
+  float eps[2];
+  float inv_dim;
+  float* dgain[2];
+};
+size_t head_norm_grad_workspace(int n_rows, int head_dim, int num_sms);
+cudaError_t launch_head_norm_grad(const HeadNormGradDesc& d, float* partial, int num_sms, cudaStream_t stream);
+
+// ---------------------------------------------------------------- log probabilities
+struct LogprobsDesc {
+  const void* z;
+  int64_t z_row;
+  int type, n_rows, vocab, n_top;
+  const int32_t* targets;      // null with logprob
+  float* logprob;              // each output may be null
+  float* entropy;
+  float* lse;
+  int32_t* top_ids;            // [n_rows][n_top]
+  float* top_logprobs;
+  int* status;
+};
+cudaError_t launch_logprobs(const LogprobsDesc& d, int num_sms, cudaStream_t stream);
+struct LogprobsGradDesc {
+  const void* z;
+  void* dz;
+  int64_t z_row, dz_row;
+  int type, n_rows, vocab;
+  const int32_t* targets;
+  const float* lse;
+  const float* entropy;        // read with g_entropy
+  const float* g_logprob;      // may be null
+  const float* g_entropy;      // may be null
+  int* status;
+};
+cudaError_t launch_logprobs_grad(const LogprobsGradDesc& d, cudaStream_t stream);
 
 // ---------------------------------------------------------------- chunk attention
 struct ChunkAttnDesc {
