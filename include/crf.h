@@ -415,6 +415,37 @@ CRF_API crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, in
                                        const crf_heads* q, float* lse, float scale, int causal, int window,
                                        void* workspace, size_t ws_bytes, void* stream);
 
+/* The same with sinks: the first `sinks` (>= 0) keys of a request stay in sight of its rows whatever the window:
+ *   j < n_keys, and j <= p unless causal == 0, and (j < sinks or j > p - window).
+ * With window == 0, which hides nothing, or sinks == 0 it is crf_chunk_attention. Pages between the sinks and the rows' windows
+ * are not read, nor are their table entries. */
+CRF_API crf_status crf_chunk_attention_sinks_workspace_size(crf_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim,
+                                                            const crf_chunk* chunks, int n_chunks, int causal,
+                                                            int window, int sinks, size_t* bytes);
+CRF_API crf_status crf_chunk_attention_sinks(crf_ctx* ctx, const crf_kv_pool* pool, int layer, int n_kv_heads,
+                                             int head_dim, const crf_chunk* chunks, int n_chunks, const crf_heads* q,
+                                             float* lse, float scale, int causal, int window, int sinks,
+                                             void* workspace, size_t ws_bytes, void* stream);
+
+/* The next n_chunks (>= 1) requests of a call share their first n_shared (>= 0) keys: their page tables lead to the same keys and values
+ * there, in the same pages or, for the part of a page that crf_pages_fork copied, in equal ones. Those of the first of them that
+ * has rows are read. n_shared is at most the n_keys of each that has rows, and its pos unless causal == 0. */
+typedef struct crf_prefix {
+  int n_chunks, n_shared;
+} crf_prefix;
+
+/* crf_chunk_attention (without a window) of requests that share prefixes: keys and values that a group shares are read and
+ * multiplied once for all its rows. `prefixes` (host array) take the call's requests in order, all of them; a request
+ * of its own is a group of one. Where a group gains nothing by sharing, its requests are attended one by one. */
+CRF_API crf_status crf_prefix_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim,
+                                                       const crf_chunk* chunks, int n_chunks,
+                                                       const crf_prefix* prefixes, int n_prefixes, int causal,
+                                                       size_t* bytes);
+CRF_API crf_status crf_prefix_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer, int n_kv_heads, int head_dim,
+                                        const crf_chunk* chunks, int n_chunks, const crf_prefix* prefixes,
+                                        int n_prefixes, const crf_heads* q, float* lse, float scale, int causal,
+                                        void* workspace, size_t ws_bytes, void* stream);
+
 /* Pages are shared through a reference count a page (device int32 [num_pages];
  * 0: free). One table of a request of n_tokens (>= 0) tokens: `table` device int32
  * [ceil(n_tokens / 16)], `out` of the same length (see the calls). The counts go from refs_in to

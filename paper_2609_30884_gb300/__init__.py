@@ -23,6 +23,8 @@ A recovered cache is extended with new tokens by calls of one layer and of the p
     ctx.cache_append(pool, layer, chunks, k, v, q=q, q_out=q_rot, rope=rope)
     ctx.chunk_attention(pool, layer, chunks, q_rot, o, ctx.chunk_attention_workspace(pool, chunks, n_heads))
     ctx.pages_fork(pool, refs, PageTables(tables, n_tokens, child_tables), ctx.pages_workspace(...))
+    shared = Prefixes([n_requests], [n_shared])      # forks of one prefix
+    ctx.prefix_attention(pool, layer, chunks, shared, q_rot, o, ctx.prefix_attention_workspace(pool, chunks, shared, n_heads))
 
 Decoders that norm their query and key heads give the gains (and have norm_rotary, norm_rotary_grad for rows outside a cache);
 rows of logits are scored by logprobs, with logprobs_grad for what learns from the score:
@@ -44,8 +46,8 @@ from .abi import CrfError
 
 MODULES = ("q", "k", "v", "o", "gate", "up", "down")
 
-__all__ = ["Context", "Model", "Adapter", "KVPool", "Request", "Rope", "Chunks", "PageTables", "CrfError",
-           "MODULES", "abi", "kl_logits_noalloc"]
+__all__ = ["Context", "Model", "Adapter", "KVPool", "Request", "Rope", "Chunks", "PageTables", "Prefixes",
+           "CrfError", "MODULES", "abi", "kl_logits_noalloc"]
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -224,6 +226,20 @@ class Chunks:
         self.address = ctypes.addressof(self.c)
         self.append_ok = all(t.numel() >= e for t, e in zip(self.page_tables, self.append_entries))
         self.attend_ok = all(t.numel() >= e for t, e in zip(self.page_tables, self.attend_entries))
+
+
+class Prefixes:
+    """Which requests of a call share keys (see crf_prefix): in the order of the Chunks, the next ``counts[i]`` requests share
+    their first ``n_shared[i]`` keys. One object serves every layer of a step."""
+
+    def __init__(self, counts: Sequence[int], n_shared: Sequence[int]):
+        if len(counts) != len(n_shared):
+            raise ValueError("counts and n_shared must have one entry a group")
+        self.n = len(counts)
+        self.c = (abi.Prefix * max(1, self.n))()
+        for i in range(self.n):
+            self.c[i] = abi.Prefix(_fits("count", int(counts[i])), _fits("n_shared", int(n_shared[i])))
+        self.address = ctypes.addressof(self.c)
 
 
 class PageTables:
@@ -613,41 +629,69 @@ class Context:
         if status:
             abi.check(status)
 
-    def chunk_attention_workspace(self, pool: KVPool, chunks: Chunks, n_q_heads: int, causal: bool = True,
-                                  window: int = 0) -> torch.Tensor:
-        """Workspace of a chunk_attention call; the same one serves every layer of the step."""
+    def _attention_workspace(self, call, pool: KVPool, chunks: Chunks, n_q_heads: int, *more) -> torch.Tensor:
         hkv, dim = self._pool_layer(pool, 0)
         n = c_size_t()
-        abi.check(self.lib.crf_chunk_attention_workspace_size(self.h, _fits("n_q_heads", n_q_heads), hkv, dim,
-                                                              chunks.address, chunks.n, int(causal),
-                                                              _fits("window", window), byref(n)))
+        abi.check(call(self.h, _fits("n_q_heads", n_q_heads), hkv, dim, chunks.address, chunks.n, *more, byref(n)))
         return torch.empty(max(256, n.value), dtype=torch.uint8, device=f"cuda:{self.device}")
 
-    def chunk_attention(self, pool: KVPool, layer: int, chunks: Chunks, q: torch.Tensor, out: torch.Tensor,
-                        workspace: torch.Tensor, lse: Optional[torch.Tensor] = None, scale: float = 0.0,
-                        causal: bool = True, window: int = 0, stream=None) -> None:
-        """out = attention of the rows q [rows, heads, head_dim] (bf16) over their requests' cached keys of
-        ``layer`` (see crf_chunk_attention); ``lse`` fp32 [rows, heads]; ``scale`` 0: 1 / sqrt(head_dim)."""
+    def chunk_attention_workspace(self, pool: KVPool, chunks: Chunks, n_q_heads: int, causal: bool = True,
+                                  window: int = 0, sinks: int = 0) -> torch.Tensor:
+        """Workspace of a chunk_attention call; the same one serves every layer of the step."""
+        return self._attention_workspace(self.lib.crf_chunk_attention_sinks_workspace_size, pool, chunks, n_q_heads, int(causal),
+                                         _fits("window", window), _fits("sinks", sinks))
+
+    def prefix_attention_workspace(self, pool: KVPool, chunks: Chunks, prefixes: Prefixes, n_q_heads: int,
+                                   causal: bool = True) -> torch.Tensor:
+        """Workspace of a prefix_attention call; the same one serves every layer of the step."""
+        return self._attention_workspace(self.lib.crf_prefix_attention_workspace_size, pool, chunks, n_q_heads, prefixes.address,
+                                         prefixes.n, int(causal))
+
+    def _put_attention(self, pool: KVPool, layer: int, chunks: Chunks, q, out, workspace, lse, scale: float) -> Tuple[int, int]:
+        """Checks of an attention call's tensors; its heads are packed. KV heads and head_dim."""
         hkv, dim = self._pool_layer(pool, layer)
-        device, buf, n = self.device, self._parts, chunks.rows
+        device, n = self.device, chunks.rows
         if chunks.device != device:
             raise ValueError(f"the page tables must be on cuda:{device}")
         if not chunks.attend_ok:
             raise ValueError(f"page tables need {chunks.attend_entries} entries to attend")
         if q.dtype != torch.bfloat16 or q.shape[0] != n:
             raise ValueError(f"q must be bfloat16 with {n} rows")
-        heads = _put_heads(buf, 0, device, "q", q, out, dim)
+        heads = _put_heads(self._parts, 0, device, "q", q, out, dim)
         self._here(workspace, lse)
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (n, heads)):
             raise ValueError("lse must be a contiguous float32 [rows, heads]")
-        if window:
-            _fits("window", window)
         if 0 < scale < 2.0**-149:
             raise ValueError("scale would be 0 in float32, which stands for 1 / sqrt(head_dim)")
-        status = self.lib.crf_chunk_attention(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, buf,
-                                              None if lse is None else lse.data_ptr(), scale, causal, window,
-                                              workspace.data_ptr(), workspace.numel(),
-                                              _raw_stream(device) if stream is None else _stream(stream))
+        return hkv, dim
+
+    def chunk_attention(self, pool: KVPool, layer: int, chunks: Chunks, q: torch.Tensor, out: torch.Tensor,
+                        workspace: torch.Tensor, lse: Optional[torch.Tensor] = None, scale: float = 0.0,
+                        causal: bool = True, window: int = 0, stream=None, sinks: int = 0) -> None:
+        """out = attention of the rows q [rows, heads, head_dim] (bf16) over their requests' cached keys of
+        ``layer`` (see crf_chunk_attention); ``lse`` fp32 [rows, heads]; ``scale`` 0: 1 / sqrt(head_dim). With a
+        ``window``, the first ``sinks`` keys stay in sight (see crf_chunk_attention_sinks)."""
+        hkv, dim = self._put_attention(pool, layer, chunks, q, out, workspace, lse, scale)
+        if window or sinks:
+            _fits("window", window)
+            _fits("sinks", sinks)
+        status = self.lib.crf_chunk_attention_sinks(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, self._parts,
+                                                    None if lse is None else lse.data_ptr(), scale, causal, window, sinks,
+                                                    workspace.data_ptr(), workspace.numel(),
+                                                    _raw_stream(self.device) if stream is None else _stream(stream))
+        if status:
+            abi.check(status)
+
+    def prefix_attention(self, pool: KVPool, layer: int, chunks: Chunks, prefixes: Prefixes, q: torch.Tensor, out: torch.Tensor,
+                         workspace: torch.Tensor, lse: Optional[torch.Tensor] = None, scale: float = 0.0, causal: bool = True,
+                         stream=None) -> None:
+        """chunk_attention of requests that share prefixes: the keys and values that the requests of a group share are read once
+        for all of them (see crf_prefix_attention)."""
+        hkv, dim = self._put_attention(pool, layer, chunks, q, out, workspace, lse, scale)
+        status = self.lib.crf_prefix_attention(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, prefixes.address,
+                                               prefixes.n, self._parts, None if lse is None else lse.data_ptr(), scale, causal,
+                                               workspace.data_ptr(), workspace.numel(),
+                                               _raw_stream(self.device) if stream is None else _stream(stream))
         if status:
             abi.check(status)
 

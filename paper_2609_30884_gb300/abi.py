@@ -39,7 +39,8 @@ EXPORTS = ("crf_create", "crf_destroy", "crf_last_error", "crf_check", "crf_work
            "crf_chunk_attention_workspace_size", "crf_chunk_attention", "crf_pages_workspace_size",
            "crf_pages_fork", "crf_pages_compact", "crf_pages_release", "crf_norm_rotary",
            "crf_norm_rotary_workspace_size", "crf_norm_rotary_grad", "crf_cache_append_normed",
-           "crf_logprobs", "crf_logprobs_grad")
+           "crf_logprobs", "crf_logprobs_grad", "crf_chunk_attention_sinks_workspace_size",
+           "crf_chunk_attention_sinks", "crf_prefix_attention_workspace_size", "crf_prefix_attention")
 
 
 class ModelDims(ctypes.Structure):
@@ -100,6 +101,10 @@ class Chunk(ctypes.Structure):
     _fields_ = [("n_new", c_int), ("pos", c_int), ("n_keys", c_int), ("page_table", c_void_p)]
 
 
+class Prefix(ctypes.Structure):
+    _fields_ = [("n_chunks", c_int), ("n_shared", c_int)]
+
+
 class Pages(ctypes.Structure):
     _fields_ = [("n_tokens", c_int), ("table", c_void_p), ("out", c_void_p)]
 
@@ -148,6 +153,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "crf_pages_fork": ([P, P, c_int, c_int, c_int, P, P, P, c_int, c_int, P, c_size_t, P], c_int),
         "crf_pages_compact": ([P, P, c_int, c_int, c_int, P, P, P, c_int, P, c_size_t, P], c_int),
         "crf_pages_release": ([P, c_int, P, P, P, c_int, P, c_size_t, P], c_int),
+        "crf_chunk_attention_sinks_workspace_size": ([P, c_int, c_int, c_int, P, c_int, c_int, c_int, c_int,
+                                                      POINTER(c_size_t)], c_int),
+        "crf_chunk_attention_sinks": ([P, P, c_int, c_int, c_int, P, c_int, P, P, c_float, c_int, c_int, c_int, P,
+                                       c_size_t, P], c_int),
+        "crf_prefix_attention_workspace_size": ([P, c_int, c_int, c_int, P, c_int, P, c_int, c_int, POINTER(c_size_t)], c_int),
+        "crf_prefix_attention": ([P, P, c_int, c_int, c_int, P, c_int, P, c_int, P, P, c_float, c_int, P, c_size_t, P], c_int),
         "crf_norm_rotary": ([P, P, P, P, c_int, c_int, c_int, P, P], c_int),
         "crf_norm_rotary_workspace_size": ([P, c_int, c_int, POINTER(c_size_t)], c_int),
         "crf_norm_rotary_grad": ([P, P, P, P, P, P, c_int, c_int, c_int, P, P, c_size_t, P], c_int),

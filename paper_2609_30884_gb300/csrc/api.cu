@@ -31,7 +31,8 @@ const char* const kProfNames[kPNumKinds] = {
     "gemm_qkv_rope_paged", "gemm_o_resid", "gemm_gateup_swiglu", "gemm_down_resid",
     "attn_prefill_paged", "rmsnorm", "embed_gather", "row_copy",
     "tail_decode", "lm_head", "kl_reduce", "drift_gram", "page_check", "rotary", "cache_append",
-    "chunk_attention", "page_plan", "page_copy", "head_norm", "head_norm_grad", "logprobs", "logprobs_grad"};
+    "chunk_attention", "page_plan", "page_copy", "head_norm", "head_norm_grad", "logprobs", "logprobs_grad",
+    "prefix_attention"};
 
 thread_local std::string g_err;
 

@@ -28,7 +28,7 @@ namespace crf {
 enum ProfKind : int {
   kPQkv, kPO, kPGateUp, kPDown, kPAttn, kPNorm, kPEmbed, kPCopy,
   kPDecode, kPLmHead, kPKl, kPDrift, kPCheck, kPRotary, kPAppend, kPChunkAttn, kPPagePlan, kPPageCopy,
-  kPHeadNorm, kPHeadNormGrad, kPLogprobs, kPLogprobsGrad, kPNumKinds
+  kPHeadNorm, kPHeadNormGrad, kPLogprobs, kPLogprobsGrad, kPPrefixAttn, kPNumKinds
 };
 
 // Brackets the launches issued in its lifetime with two events on `st` when

@@ -4,6 +4,7 @@
 #include "common.cuh"
 #include "extend.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <exception>
@@ -14,7 +15,8 @@ using namespace crf;
 namespace {
 
 // The arrays that kernels take are sized by the one and filled up to the other.
-static_assert(kMaxChunks == CRF_MAX_CHUNKS && kMaxTables == CRF_MAX_TABLES && kMaxTop == CRF_MAX_TOP && kMaxVocab == CRF_MAX_VOCAB,
+static_assert(kMaxChunks == CRF_MAX_CHUNKS && kMaxTables == CRF_MAX_TABLES && kMaxTop == CRF_MAX_TOP && kMaxVocab == CRF_MAX_VOCAB &&
+                  kMaxKeys == CRF_MAX_KEYS,
               "limits of the ABI and of the kernels differ");
 
 // The context's device for the length of a call, then the caller's again.
@@ -330,6 +332,121 @@ crf_status check_rows_of(const void* x, int type, int n_rows, int vocab, int64_t
   return CRF_OK;
 }
 
+// The sizes of an attention call, checked, and its table.
+crf_status attention_sizes(crf_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim, const crf_chunk* chunks, int n_chunks,
+                           int window, int sinks, ChunkTable* t) {
+  if (!ctx) return fail(CRF_EINVAL, "ctx is null");
+  crf_status s = check_attention(n_q_heads, n_kv_heads, window, 0);
+  if (s != CRF_OK) return s;
+  if (sinks < 0) return fail(CRF_EINVAL, "sinks must be >= 0");
+  s = check_pool_shape(n_kv_heads, head_dim, 1);
+  if (s != CRF_OK) return s;
+  s = fill_chunks(chunks, n_chunks, true, 1, t);
+  return s != CRF_OK ? s : check_attention(n_q_heads, n_kv_heads, window, t->row0[t->n]);
+}
+
+// The arguments that attention calls share, checked, and their descriptor; it is left unset where there are no rows.
+crf_status attention_call(crf_ctx* ctx, const crf_kv_pool* pool, int layer, int n_kv_heads, int head_dim, const crf_chunk* chunks,
+                          int n_chunks, const crf_heads* q, float* lse, float scale, int causal, int window, ChunkTable* t,
+                          ChunkAttnDesc* d) {
+  if (!ctx || !pool || !q) return fail(CRF_EINVAL, "null argument");
+  crf_status s = check_pool_shape(n_kv_heads, head_dim, pool->num_pages);
+  if (s != CRF_OK) return s;
+  s = check_layer(pool, layer);
+  if (s != CRF_OK) return s;
+  s = check_attention(q->heads, n_kv_heads, window, 0);
+  if (s != CRF_OK) return s;
+  // the kernel multiplies scores by scale log2(e), in fp32
+  if (!(scale >= 0.f) || !std::isfinite(scale * 1.4426950408889634f))
+    return fail(CRF_EINVAL, "scale must be positive and under 2.35e38, or 0 for 1/sqrt(head_dim)");
+  s = fill_chunks(chunks, n_chunks, true, pool->num_pages, t);
+  if (s != CRF_OK) return s;
+  const int rows = t->row0[t->n];
+  if (rows == 0) return CRF_OK;
+  s = check_attention(q->heads, n_kv_heads, window, rows);
+  if (s != CRF_OK) return s;
+  const crf_heads hq = settled(*q, rows, head_dim);
+  s = check_heads(hq, 16, true, "q");
+  if (s != CRF_OK) return s;
+  if ((hq.x_row | hq.x_head | hq.out_row | hq.out_head) % 8)
+    return fail(CRF_EUNSUPPORTED, "q: strides must be multiples of 8 elements");
+  s = check_out(hq, rows, head_dim, "q");
+  if (s != CRF_OK) return s;
+  if (q->x == q->out) return fail(CRF_EINVAL, "q: o may not be written over q");
+  if (!aligned4(lse)) return fail(CRF_EINVAL, "lse misaligned");
+  d->q = static_cast<const __nv_bfloat16*>(q->x);
+  d->out = static_cast<__nv_bfloat16*>(q->out);
+  d->q_row = hq.x_row;
+  d->q_head = hq.x_head;
+  d->out_row = hq.out_row;
+  d->out_head = hq.out_head;
+  d->lse = lse;
+  d->kpages = static_cast<const __nv_bfloat16*>(pool->k_pages[layer]);
+  d->vpages = static_cast<const __nv_bfloat16*>(pool->v_pages[layer]);
+  d->n_q_heads = q->heads;
+  d->n_kv_heads = n_kv_heads;
+  d->head_dim = head_dim;
+  d->scale = scale > 0.f ? scale : static_cast<float>(1.0 / std::sqrt(static_cast<double>(head_dim)));
+  d->causal = causal != 0;
+  d->window = window;
+  d->status = ctx->status_dev;
+  return CRF_OK;
+}
+
+crf_status run_chunk_attention(crf_ctx* ctx, const ChunkAttnDesc& d, const ChunkTable& t, void* workspace, size_t ws_bytes,
+                               cudaStream_t st) {
+  ChunkPlan plan;
+  plan_chunk_attention(t, d.n_q_heads, d.n_kv_heads, d.causal, d.window, ctx->num_sms, &plan);
+  const crf_status s = check_workspace(workspace, ws_bytes, chunk_attention_workspace(plan, d.head_dim));
+  if (s != CRF_OK) return s;
+  DeviceScope dev(ctx->device);
+  CRF_CUDA(dev.error());
+  ProfScope ps(ctx, kPChunkAttn, st, plan.cuts ? 2 : 1);
+  CRF_CUDA(launch_chunk_attention(d, t, plan, workspace, ctx->num_sms, st));
+  return CRF_OK;
+}
+
+void table_with_sinks(const ChunkTable& t, int sinks, AttnTable* a) {
+  std::memset(a, 0, sizeof(*a));
+  a->n = t.n;
+  a->num_pages = t.num_pages;
+  a->sinks = std::min(sinks, CRF_MAX_KEYS);
+  for (int i = 0; i < t.n; ++i) {
+    a->row0[i] = t.row0[i];
+    a->rows[i] = t.row0[i + 1] - t.row0[i];
+    a->pos[i] = t.pos[i];
+    a->n_keys[i] = t.n_keys[i];
+    a->pt[i] = t.pt[i];
+  }
+}
+
+// The requests' groups, checked, and the table of those that share.
+crf_status prefix_groups(const ChunkTable& t, const crf_prefix* prefixes, int n, int n_q_heads, int n_kv_heads, bool causal,
+                         AttnTable* a, PrefixGroups* g) {
+  if (!prefixes) return fail(CRF_EINVAL, "prefixes is null");
+  if (n < 1 || n > t.n) return fail(CRF_EINVAL, "n_prefixes %d out of range (1..%d)", n, t.n);
+  int count[CRF_MAX_CHUNKS], keys[CRF_MAX_CHUNKS], at = 0;
+  for (int i = 0; i < n; ++i) {
+    count[i] = prefixes[i].n_chunks;
+    keys[i] = prefixes[i].n_shared;
+    if (count[i] < 1 || count[i] > t.n - at) return fail(CRF_EINVAL, "prefix %d: n_chunks %d, %d requests are left", i, count[i], t.n - at);
+    for (int j = at; j < at + count[i]; ++j) {
+      if (t.row0[j + 1] == t.row0[j]) continue;
+      if (keys[i] < 0 || keys[i] > t.n_keys[j] || (causal && keys[i] > t.pos[j]))
+        return fail(CRF_EINVAL, "prefix %d: n_shared %d beyond the keys of chunk %d, or its new rows", i, keys[i], j);
+    }
+    at += count[i];
+  }
+  if (at != t.n) return fail(CRF_EINVAL, "the prefixes have %d requests, the call %d", at, t.n);
+  share_prefixes(t, count, keys, n, n_q_heads, n_kv_heads, a, g);
+  return CRF_OK;
+}
+
+crf_status check_parts(const AttnPlan& p) {
+  if (p.part_rows > (1 << 30)) return fail(CRF_EUNSUPPORTED, "the rows' parts are over 2^30");
+  return CRF_OK;
+}
+
 // ---------------------------------------------------------------- pages
 crf_status fill_tables(const crf_pages* tables, int n, int num_pages, bool has_out, bool deep, PageTables* t) {
   if (!tables) return fail(CRF_EINVAL, "tables is null");
@@ -604,19 +721,30 @@ crf_status crf_logprobs_grad(crf_ctx* ctx, const void* logits, int type, int n_r
 crf_status crf_chunk_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim,
                                               const crf_chunk* chunks, int n_chunks, int causal, int window,
                                               size_t* bytes) {
+  return crf_chunk_attention_sinks_workspace_size(ctx, n_q_heads, n_kv_heads, head_dim, chunks, n_chunks, causal, window, 0, bytes);
+}
+
+crf_status crf_chunk_attention_sinks_workspace_size(crf_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim,
+                                                    const crf_chunk* chunks, int n_chunks, int causal, int window,
+                                                    int sinks, size_t* bytes) {
   return guarded([&]() -> crf_status {
-    if (!ctx || !bytes) return fail(CRF_EINVAL, "null argument");
-    crf_status s = check_attention(n_q_heads, n_kv_heads, window, 0);
-    if (s != CRF_OK) return s;
-    s = check_pool_shape(n_kv_heads, head_dim, 1);
-    if (s != CRF_OK) return s;
+    if (!bytes) return fail(CRF_EINVAL, "null argument");
     ChunkTable t;
-    s = fill_chunks(chunks, n_chunks, true, 1, &t);
-    if (s == CRF_OK) s = check_attention(n_q_heads, n_kv_heads, window, t.row0[t.n]);
+    crf_status s = attention_sizes(ctx, n_q_heads, n_kv_heads, head_dim, chunks, n_chunks, window, sinks, &t);
     if (s != CRF_OK) return s;
-    ChunkPlan plan;
-    plan_chunk_attention(t, n_q_heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
-    *bytes = align256(chunk_attention_workspace(plan, head_dim));
+    size_t need;
+    if (window > 0 && sinks > 0) {
+      AttnTable a;
+      AttnPlan plan;
+      table_with_sinks(t, sinks, &a);
+      plan_attention(a, false, n_q_heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
+      need = attention_workspace(plan, head_dim);
+    } else {
+      ChunkPlan plan;
+      plan_chunk_attention(t, n_q_heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
+      need = chunk_attention_workspace(plan, head_dim);
+    }
+    *bytes = align256(need);
     return CRF_OK;
   });
 }
@@ -624,59 +752,92 @@ crf_status crf_chunk_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int n
 crf_status crf_chunk_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer, int n_kv_heads, int head_dim,
                                const crf_chunk* chunks, int n_chunks, const crf_heads* q, float* lse, float scale,
                                int causal, int window, void* workspace, size_t ws_bytes, void* stream) {
+  return crf_chunk_attention_sinks(ctx, pool, layer, n_kv_heads, head_dim, chunks, n_chunks, q, lse, scale, causal, window, 0,
+                                   workspace, ws_bytes, stream);
+}
+
+crf_status crf_chunk_attention_sinks(crf_ctx* ctx, const crf_kv_pool* pool, int layer, int n_kv_heads, int head_dim,
+                                     const crf_chunk* chunks, int n_chunks, const crf_heads* q, float* lse, float scale,
+                                     int causal, int window, int sinks, void* workspace, size_t ws_bytes, void* stream) {
   return guarded([&]() -> crf_status {
-    if (!ctx || !pool || !q) return fail(CRF_EINVAL, "null argument");
-    crf_status s = check_pool_shape(n_kv_heads, head_dim, pool->num_pages);
-    if (s != CRF_OK) return s;
-    s = check_layer(pool, layer);
-    if (s != CRF_OK) return s;
-    s = check_attention(q->heads, n_kv_heads, window, 0);
-    if (s != CRF_OK) return s;
-    // the kernel multiplies scores by scale log2(e), in fp32
-    if (!(scale >= 0.f) || !std::isfinite(scale * 1.4426950408889634f))
-      return fail(CRF_EINVAL, "scale must be positive and under 2.35e38, or 0 for 1/sqrt(head_dim)");
     ChunkTable t;
-    s = fill_chunks(chunks, n_chunks, true, pool->num_pages, &t);
-    if (s != CRF_OK) return s;
-    const int rows = t.row0[t.n];
-    if (rows == 0) return CRF_OK;
-    s = check_attention(q->heads, n_kv_heads, window, rows);
-    if (s != CRF_OK) return s;
-    const crf_heads hq = settled(*q, rows, head_dim);
-    s = check_heads(hq, 16, true, "q");
-    if (s != CRF_OK) return s;
-    if ((hq.x_row | hq.x_head | hq.out_row | hq.out_head) % 8)
-      return fail(CRF_EUNSUPPORTED, "q: strides must be multiples of 8 elements");
-    s = check_out(hq, rows, head_dim, "q");
-    if (s != CRF_OK) return s;
-    if (q->x == q->out) return fail(CRF_EINVAL, "q: o may not be written over q");
-    if (!aligned4(lse)) return fail(CRF_EINVAL, "lse misaligned");
-    ChunkPlan plan;
-    plan_chunk_attention(t, q->heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
-    s = check_workspace(workspace, ws_bytes, chunk_attention_workspace(plan, head_dim));
-    if (s != CRF_OK) return s;
     ChunkAttnDesc d;
-    d.q = static_cast<const __nv_bfloat16*>(q->x);
-    d.out = static_cast<__nv_bfloat16*>(q->out);
-    d.q_row = hq.x_row;
-    d.q_head = hq.x_head;
-    d.out_row = hq.out_row;
-    d.out_head = hq.out_head;
-    d.lse = lse;
-    d.kpages = static_cast<const __nv_bfloat16*>(pool->k_pages[layer]);
-    d.vpages = static_cast<const __nv_bfloat16*>(pool->v_pages[layer]);
-    d.n_q_heads = q->heads;
-    d.n_kv_heads = n_kv_heads;
-    d.head_dim = head_dim;
-    d.scale = scale > 0.f ? scale : static_cast<float>(1.0 / std::sqrt(static_cast<double>(head_dim)));
-    d.causal = causal != 0;
-    d.window = window;
-    d.status = ctx->status_dev;
+    crf_status s = attention_call(ctx, pool, layer, n_kv_heads, head_dim, chunks, n_chunks, q, lse, scale, causal, window, &t, &d);
+    if (s != CRF_OK) return s;
+    if (sinks < 0) return fail(CRF_EINVAL, "sinks must be >= 0");
+    if (t.row0[t.n] == 0) return CRF_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (window > 0 && sinks > 0) {
+      AttnTable a;
+      AttnPlan plan;
+      table_with_sinks(t, sinks, &a);
+      plan_attention(a, false, q->heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
+      s = check_workspace(workspace, ws_bytes, attention_workspace(plan, head_dim));
+      if (s != CRF_OK) return s;
+      DeviceScope dev(ctx->device);
+      CRF_CUDA(dev.error());
+      ProfScope ps(ctx, kPChunkAttn, st, attention_launches(plan));
+      CRF_CUDA(launch_attention(d, a, nullptr, plan, workspace, ctx->num_sms, st));
+      return CRF_OK;
+    }
+    return run_chunk_attention(ctx, d, t, workspace, ws_bytes, st);
+  });
+}
+
+crf_status crf_prefix_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int n_kv_heads, int head_dim,
+                                               const crf_chunk* chunks, int n_chunks, const crf_prefix* prefixes,
+                                               int n_prefixes, int causal, size_t* bytes) {
+  return guarded([&]() -> crf_status {
+    if (!bytes) return fail(CRF_EINVAL, "null argument");
+    ChunkTable t;
+    crf_status s = attention_sizes(ctx, n_q_heads, n_kv_heads, head_dim, chunks, n_chunks, 0, 0, &t);
+    if (s != CRF_OK) return s;
+    AttnTable a;
+    PrefixGroups g;
+    s = prefix_groups(t, prefixes, n_prefixes, n_q_heads, n_kv_heads, causal != 0, &a, &g);
+    if (s != CRF_OK) return s;
+    size_t need;
+    if (g.groups > 0) {
+      AttnPlan plan;
+      plan_attention(a, true, n_q_heads, n_kv_heads, causal != 0, 0, ctx->num_sms, &plan);
+      s = check_parts(plan);
+      if (s != CRF_OK) return s;
+      need = attention_workspace(plan, head_dim);
+    } else {
+      ChunkPlan plan;
+      plan_chunk_attention(t, n_q_heads, n_kv_heads, causal != 0, 0, ctx->num_sms, &plan);
+      need = chunk_attention_workspace(plan, head_dim);
+    }
+    *bytes = align256(need);
+    return CRF_OK;
+  });
+}
+
+crf_status crf_prefix_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer, int n_kv_heads, int head_dim,
+                                const crf_chunk* chunks, int n_chunks, const crf_prefix* prefixes, int n_prefixes,
+                                const crf_heads* q, float* lse, float scale, int causal, void* workspace, size_t ws_bytes,
+                                void* stream) {
+  return guarded([&]() -> crf_status {
+    ChunkTable t;
+    ChunkAttnDesc d;
+    crf_status s = attention_call(ctx, pool, layer, n_kv_heads, head_dim, chunks, n_chunks, q, lse, scale, causal, 0, &t, &d);
+    if (s != CRF_OK) return s;
+    AttnTable a;
+    PrefixGroups g;
+    s = prefix_groups(t, prefixes, n_prefixes, q->heads, n_kv_heads, causal != 0, &a, &g);
+    if (s != CRF_OK || t.row0[t.n] == 0) return s;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (g.groups == 0) return run_chunk_attention(ctx, d, t, workspace, ws_bytes, st);
+    AttnPlan plan;
+    plan_attention(a, true, q->heads, n_kv_heads, causal != 0, 0, ctx->num_sms, &plan);
+    s = check_parts(plan);
+    if (s != CRF_OK) return s;
+    s = check_workspace(workspace, ws_bytes, attention_workspace(plan, head_dim));
+    if (s != CRF_OK) return s;
     DeviceScope dev(ctx->device);
     CRF_CUDA(dev.error());
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    ProfScope ps(ctx, kPChunkAttn, st, plan.cuts ? 2 : 1);
-    CRF_CUDA(launch_chunk_attention(d, t, plan, workspace, ctx->num_sms, st));
+    ProfScope ps(ctx, kPPrefixAttn, st, attention_launches(plan));
+    CRF_CUDA(launch_attention(d, a, &g, plan, workspace, ctx->num_sms, st));
     return CRF_OK;
   });
 }

@@ -1,0 +1,286 @@
+// Attention of new rows over cached keys (chunk_attn.cu) in two more forms, both instances of its kernel.
+//
+// Sinks: row r of a request at position p sees the window p - window < j <= p and, whatever the window, the keys j < sinks. An item's
+// tiles are those of the sinks, then those of its rows' windows; nothing between is read.
+//
+// Shared prefixes: requests whose first n keys are the same (pages_fork makes such tables) are attended in two parts, joined by their
+// maxima and sums:
+//   o = (e^(m1 - m) o1 + e^(m2 - m) o2) / (e^(m1 - m) l1 + e^(m2 - m) l2),  m = max(m1, m2)
+// with (m, l, o) the maximum, the sum of exponentials and their unnormalised product with v. The rows of all requests of a group
+// are packed into one axis for the shared keys, as rows and heads are within a request, so that the keys and values of the prefix
+// are read, and multiplied, once for the group and not once a request. Each request's own keys are items like any other. Every
+// segment writes its part; one merge joins an output row's parts of the group's item and of its request's, in order.
+//
+// Where the rows of each request fill tiles of their own, sharing saves no products: the parts would cost more than they save,
+// and such groups are attended request by request (share_prefixes).
+#include "chunk_attn.cuh"
+
+namespace crf {
+
+namespace {
+
+struct JoinArgs {
+  ChunkAttnDesc d;
+  AttnTable c;
+  PrefixGroups g;
+  int item0[kMaxEntries];
+  const int* first;
+  const int* last;
+  const float* part;
+  const float* part_ml;
+  int rows;  // output rows times query heads
+};
+
+// The parts of one output row in one item: `count` of them, `rows` rows apart.
+struct Parts {
+  int64_t at, base;  // row of the first part's row; first row of the first part
+  int rows, r, count;
+};
+__device__ __forceinline__ Parts parts_of(const JoinArgs& a, int e, int row, int h) {
+  const int grp = a.d.n_q_heads / a.d.n_kv_heads;
+  const int packed = (row - a.c.row0[e]) * grp + h % grp, all = a.c.rows[e] * grp, tile = narrow_form(all) ? kM : 2 * kM;
+  const int qt = packed / tile, item = a.item0[e] + ((all + tile - 1) / tile - 1 - qt) * a.d.n_kv_heads + h / grp;
+  Parts p;
+  p.r = packed - qt * tile;
+  p.rows = min(tile, all - qt * tile);
+  p.base = __ldcg(a.first + item);
+  p.count = static_cast<int>(__ldcg(a.last + item) - p.base) / p.rows + 1;
+  p.at = p.base + p.r;
+  return p;
+}
+
+// As chunk_attn_merge: a row by GROUPS groups of D / 4 lanes.
+template <int D, int GROUPS>
+__global__ void __launch_bounds__(kMergeThreads) chunk_attn_join(const __grid_constant__ JoinArgs a) {
+  constexpr int kLanes = D / 4, kRows = kMergeThreads / (kLanes * GROUPS), kBatch = 4;
+  __shared__ float4 red_o[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? kRows * kLanes : 1];
+  __shared__ float2 red_ml[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? kRows : 1];
+  griddep_launch_dependents();
+  const ChunkAttnDesc& d = a.d;
+  const int c = threadIdx.x % kLanes, q = threadIdx.x / kLanes % GROUPS, rr = threadIdx.x / (kLanes * GROUPS);
+  const int b = min(static_cast<int>(blockIdx.x) * kRows + rr, a.rows - 1);  // a last block's spare rows repeat the last
+  const int row = b / d.n_q_heads, h = b - row * d.n_q_heads;
+  int lo = a.g.groups, hi = a.c.n - 1;  // the row's request
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.c.row0[mid] <= row) lo = mid; else hi = mid - 1;
+  }
+  const int group = a.g.of[lo - a.g.groups];
+  griddep_wait();
+  const Parts own = parts_of(a, lo, row, h);
+  Parts shared = own;
+  shared.count = 0;
+  if (group >= 0) shared = parts_of(a, group, row, h);
+  const int parts = shared.count + own.count;
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = q; k0 < parts; k0 += kBatch * GROUPS) {
+    float2 ml[kBatch];
+    float4 v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int k = k0 + i * GROUPS;
+      ml[i] = make_float2(-INFINITY, 0.f);
+      if (k < parts) {
+        const bool s = k < shared.count;
+        const int rows = s ? shared.rows : own.rows, r = s ? shared.r : own.r;
+        const int64_t base = (s ? shared.base : own.base) + static_cast<int64_t>(s ? k : k - shared.count) * rows;
+        ml[i] = __ldcg(reinterpret_cast<const float2*>(a.part_ml) + base + r);
+        v[i] = __ldcg(reinterpret_cast<const float4*>(a.part) + base * kLanes + (static_cast<int64_t>(c / 8) * rows + r) * 8 + row_unit(r, c % 8));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (ml[i].y == 0.f) continue;  // nothing seen (its o holds no number)
+      const float mn = fmaxf(m, ml[i].x), keep = m == -INFINITY ? 0.f : ex2_approx(m - mn), add = ex2_approx(ml[i].x - mn);
+      o.x = o.x * keep + v[i].x * add;
+      o.y = o.y * keep + v[i].y * add;
+      o.z = o.z * keep + v[i].z * add;
+      o.w = o.w * keep + v[i].w * add;
+      l = l * keep + ml[i].y * add;
+      m = mn;
+    }
+  }
+  if (GROUPS > 1) {
+    red_o[q][rr * kLanes + c] = o;
+    if (c == 0) red_ml[q][rr] = make_float2(m, l);
+    __syncthreads();
+    if (q != 0) return;
+    float M = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) M = fmaxf(M, red_ml[i][rr].x);
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      const float2 ml = red_ml[i][rr];
+      if (ml.y == 0.f) continue;
+      const float e = ex2_approx(ml.x - M);
+      const float4 v = red_o[i][rr * kLanes + c];
+      o.x += v.x * e;
+      o.y += v.y * e;
+      o.z += v.z * e;
+      o.w += v.w * e;
+      L += ml.y * e;
+    }
+    m = M;
+    l = L;
+  }
+  const float inv = l != 0.f ? 1.0f / l : 0.f;
+  *reinterpret_cast<uint2*>(d.out + row * d.out_row + h * d.out_head + c * 4) =
+      make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+  if (d.lse && c == 0) d.lse[static_cast<size_t>(row) * d.n_q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// Floats of a workspace's pieces, each a multiple of 64.
+size_t round64(size_t n) { return (n + 63) & ~static_cast<size_t>(63); }
+struct Pieces {
+  size_t part, ml, items, total;
+};
+Pieces pieces_of(const AttnPlan& p, int head_dim) {
+  Pieces x;
+  if (p.shared) {
+    x.part = round64(static_cast<size_t>(p.part_rows) * head_dim);
+    x.ml = round64(static_cast<size_t>(p.part_rows) * 2);
+    x.items = round64(2 * static_cast<size_t>(p.items));
+  } else {
+    x.part = part_floats(p.runs, head_dim, false);
+    x.ml = part_floats(p.runs, head_dim, true);
+    x.items = 0;
+  }
+  x.total = total_floats(p.runs, head_dim);
+  return x;
+}
+
+template <int D, bool LEAN>
+cudaError_t launch_wider(const ChunkArgs<true>& a, const PrefixGroups* g, const AttnPlan& p, int num_sms, cudaStream_t stream) {
+  PdlScope pdl;
+  const cudaError_t e = launch_kernel_tc<D, LEAN, true>(a, p.runs.ctas, stream);
+  if (e != cudaSuccess) return e;
+  if (!p.shared) return launch_merge<D>(a.d, p.runs, a.part, a.part_ml, num_sms, stream);
+  JoinArgs j;
+  std::memset(&j, 0, sizeof(j));
+  j.d = a.d;
+  j.c = a.c;
+  j.g = *g;
+  std::memcpy(j.item0, p.item0, sizeof(j.item0));
+  j.first = a.prefix.first;
+  j.last = a.prefix.last;
+  j.part = a.part;
+  j.part_ml = a.part_ml;
+  int rows = 0;
+  for (int i = g->groups; i < a.c.n; ++i) rows += a.c.rows[i];
+  j.rows = rows * a.d.n_q_heads;
+  constexpr int kRow = kMergeThreads / (D / 4);  // rows a block with one group each
+  if (j.rows < 4 * kRow * num_sms) {
+    constexpr int kRows8 = kRow / 8;
+    return launch_kernel(chunk_attn_join<D, 8>, dim3((j.rows + kRows8 - 1) / kRows8), dim3(kMergeThreads), 0, stream, j);
+  }
+  return launch_kernel(chunk_attn_join<D, 1>, dim3((j.rows + kRow - 1) / kRow), dim3(kMergeThreads), 0, stream, j);
+}
+
+}  // namespace
+
+void plan_attention(const AttnTable& a, bool shared, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms,
+                    AttnPlan* p) {
+  std::memset(p->run_rows, 0, sizeof(p->run_rows));
+  p->shared = shared;
+  p->items = 0;
+  p->part_rows = 0;
+  const int grp = n_q_heads / n_kv_heads;
+  for (int i = 0; i < a.n; ++i) {
+    const int rows = a.rows[i] * grp, tile = narrow_form(rows) ? kM : 2 * kM;
+    p->item0[i] = p->items;
+    p->items += (rows + tile - 1) / tile * n_kv_heads;
+  }
+  plan_runs(a, n_q_heads, n_kv_heads, causal, window, num_sms, shared ? p->run_rows : nullptr, &p->runs);
+  if (shared)
+    for (int b = 0; b < p->runs.ctas; ++b) p->part_rows += p->run_rows[b];
+}
+
+void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int n, int n_q_heads, int n_kv_heads,
+                    AttnTable* a, PrefixGroups* g) {
+  std::memset(a, 0, sizeof(*a));
+  std::memset(g, 0, sizeof(*g));
+  const int grp = n_q_heads / n_kv_heads;
+  // units of one kv head's items of `rows` rows over keys [0, n)
+  auto units = [&](int rows, int n) {
+    const int packed = rows * grp, tile = narrow_form(packed) ? kM : 2 * kM;
+    const int64_t steps = tiles_of(KeyRange{0, n}, narrow_form(packed)).steps;
+    return static_cast<int64_t>((packed + tile - 1) / tile) * steps * step_units(narrow_form(packed));
+  };
+  a->num_pages = c.num_pages;
+  for (int i = 0, r = 0; i < n; r += count[i++]) {
+    const int rows = c.row0[r + count[i]] - c.row0[r], packed = rows * grp, tile = narrow_form(packed) ? kM : 2 * kM;
+    int64_t apart = 0;
+    int first = -1;
+    for (int j = r; j < r + count[i]; ++j) {
+      g->of[j] = -1;
+      if (rows_of(c, j) == 0) continue;
+      if (first < 0) first = j;
+      apart += units(rows_of(c, j), keys[i]);
+    }
+    // the shared items' own ends have to be earned, beside their steps
+    if (first < 0 || keys[i] == 0 || apart - units(rows, keys[i]) <= kSegment * ((packed + tile - 1) / tile)) continue;
+    const int e = g->groups++;
+    a->row0[e] = c.row0[r];
+    a->rows[e] = rows;
+    a->pos[e] = kMaxKeys;  // behind every key
+    a->n_keys[e] = keys[i];
+    a->pt[e] = c.pt[first];
+    for (int j = r; j < r + count[i]; ++j) g->of[j] = static_cast<int16_t>(e);
+  }
+  a->n = g->groups + c.n;
+  for (int i = 0, r = 0; i < n; r += count[i++])
+    for (int j = r; j < r + count[i]; ++j) {
+      const int e = g->groups + j;
+      a->row0[e] = c.row0[j];
+      a->rows[e] = rows_of(c, j);
+      a->pos[e] = c.pos[j];
+      a->key0[e] = g->of[j] >= 0 ? keys[i] : 0;
+      a->n_keys[e] = c.n_keys[j];
+      a->pt[e] = c.pt[j];
+    }
+}
+
+size_t attention_workspace(const AttnPlan& p, int head_dim) {
+  const Pieces x = pieces_of(p, head_dim);
+  return (x.part + x.ml + x.items + x.total) * sizeof(float);
+}
+
+int attention_launches(const AttnPlan& p) { return p.shared || p.runs.cuts ? 2 : 1; }
+
+cudaError_t launch_attention(const ChunkAttnDesc& d, const AttnTable& c, const PrefixGroups* g, const AttnPlan& p,
+                             void* workspace, int num_sms, cudaStream_t stream) {
+  if (p.runs.ctas == 0) return cudaSuccess;
+  ChunkArgs<true> a;
+  std::memset(&a, 0, sizeof(a));
+  const long pool_rows = static_cast<long>(c.num_pages) * d.n_kv_heads * kPage;
+  if (!tensor_map_pool(&a.tmK, d.kpages, pool_rows, d.head_dim) || !tensor_map_pool(&a.tmV, d.vpages, pool_rows, d.head_dim))
+    return cudaErrorInvalidValue;
+  a.d = d;
+  a.c = c;
+  std::memcpy(a.run, p.runs.run, (p.runs.ctas + 1) * sizeof(RunStart));
+  const Pieces x = pieces_of(p, d.head_dim);
+  a.part = static_cast<float*>(workspace);
+  a.part_ml = a.part + x.part;
+  a.part_rows = p.runs.part_rows;
+  a.total = a.part_ml + x.ml + x.items;
+  a.prefix.on = p.shared;
+  if (p.shared) {
+    a.prefix.first = reinterpret_cast<int*>(a.part_ml + x.ml);
+    a.prefix.last = a.prefix.first + p.items;
+    std::memcpy(a.prefix.item0, p.item0, sizeof(a.prefix.item0));
+    int row = 0;
+    for (int b = 0; b < p.runs.ctas; ++b) {
+      a.prefix.row0[b] = row;
+      row += static_cast<int>(p.run_rows[b]);
+    }
+  }
+  bool lean = true;
+  for (int i = 0; i < c.n; ++i) lean = lean && static_cast<int64_t>(c.rows[i]) * (d.n_q_heads / d.n_kv_heads) <= kLeanRows;
+  if (d.head_dim == 128)
+    return lean ? launch_wider<128, true>(a, g, p, num_sms, stream) : launch_wider<128, false>(a, g, p, num_sms, stream);
+  return lean ? launch_wider<64, true>(a, g, p, num_sms, stream) : launch_wider<64, false>(a, g, p, num_sms, stream);
+}
+
+}  // namespace crf

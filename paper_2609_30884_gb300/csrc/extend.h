@@ -9,6 +9,7 @@ namespace crf {
 constexpr int kMaxChunks = 128;  // equals CRF_MAX_CHUNKS (api_extend.cu checks that)
 constexpr int kMaxTables = 512;  // equals CRF_MAX_TABLES
 constexpr int kMaxPairs = 128;   // rotary pairs of a head
+constexpr int kMaxKeys = 1 << 26;  // equals CRF_MAX_KEYS
 constexpr int kMaxTop = 32;      // equals CRF_MAX_TOP
 constexpr int kMaxVocab = 1 << 20;  // equals CRF_MAX_VOCAB
 
@@ -108,6 +109,19 @@ struct ChunkAttnDesc {
   int window;                  // 0: none
   int* status;
 };
+// The entries of a call whose rows see sinks, or whose requests share prefixes: entry i's rows [row0[i], row0[i] + rows[i]) over the keys
+// from key0[i] on. With prefixes, groups of requests over the keys that they share come first (at positions behind all of them).
+constexpr int kMaxEntries = kMaxChunks + kMaxChunks / 2;
+struct AttnTable {
+  int n, num_pages;
+  int sinks;
+  int row0[kMaxEntries];
+  int rows[kMaxEntries];
+  int pos[kMaxEntries];
+  int key0[kMaxEntries];
+  int n_keys[kMaxEntries];
+  const int32_t* pt[kMaxEntries];
+};
 constexpr int kMaxCtas = 256;
 // Where a CTA's run begins: step `step` of item (request, query tile or pair qt, kv head g); request = c.n: the end.
 // Items go through the requests in order, query tiles from the last down, heads.
@@ -132,6 +146,30 @@ void plan_chunk_attention(const ChunkTable& c, int n_q_heads, int n_kv_heads, bo
 size_t chunk_attention_workspace(const ChunkPlan& p, int head_dim);
 cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, const ChunkPlan& p, void* workspace,
                                    int num_sms, cudaStream_t stream);
+
+// Attention with sinks, and of requests that share prefixes.
+struct AttnPlan {
+  ChunkPlan runs;
+  bool shared;                      // the table's first entries are groups; every segment is a part
+  int items;
+  int64_t part_rows;                // of all parts
+  int64_t run_rows[kMaxCtas];
+  int item0[kMaxEntries];           // items of the entries before
+};
+// Which requests share: group[i] of request i is an entry of `a`, or -1.
+struct PrefixGroups {
+  int groups;
+  int16_t of[kMaxChunks];
+};
+void plan_attention(const AttnTable& a, bool shared, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms,
+                    AttnPlan* p);
+// The table of requests in runs of count[i] that share their first keys[i] keys; groups that gain nothing by it are none.
+void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int n, int n_q_heads, int n_kv_heads,
+                    AttnTable* a, PrefixGroups* g);
+size_t attention_workspace(const AttnPlan& p, int head_dim);
+int attention_launches(const AttnPlan& p);
+cudaError_t launch_attention(const ChunkAttnDesc& d, const AttnTable& a, const PrefixGroups* g, const AttnPlan& p,
+                             void* workspace, int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------- pages
 // Entries [first[i], first[i + 1]) of a call are table i's.
