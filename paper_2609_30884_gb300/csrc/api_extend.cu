@@ -552,7 +552,7 @@ crf_status crf_norm_rotary_workspace_size(crf_ctx* ctx, int head_dim, int n_rows
     if (!ctx || !bytes) return fail(CRF_EINVAL, "null argument");
     if (head_dim < 2 || head_dim > 2 * kMaxPairs) return fail(CRF_EUNSUPPORTED, "head_dim %d unsupported", head_dim);
     if (n_rows < 0) return fail(CRF_EINVAL, "n_rows must be >= 0");
-    *bytes = align256(head_norm_grad_workspace(n_rows, head_dim, ctx->num_sms));
+    *bytes = align256(head_norm_grad_workspace(head_dim, ctx->num_sms));
     return CRF_OK;
   });
 }
@@ -587,7 +587,7 @@ crf_status crf_norm_rotary_grad(crf_ctx* ctx, const crf_rope* rope, const crf_he
       d.g_row[p] = g.x_row;
       d.g_head[p] = g.x_head;
     }
-    s = check_workspace(workspace, ws_bytes, head_norm_grad_workspace(n_rows, rope->head_dim, ctx->num_sms));
+    s = check_workspace(workspace, ws_bytes, head_norm_grad_workspace(rope->head_dim, ctx->num_sms));
     if (s != CRF_OK) return s;
     DeviceScope dev(ctx->device);
     CRF_CUDA(dev.error());

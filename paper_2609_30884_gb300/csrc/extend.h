@@ -64,7 +64,7 @@ struct HeadNormGradDesc {
   float inv_dim;
   float* dgain[2];
 };
-size_t head_norm_grad_workspace(int n_rows, int head_dim, int num_sms);
+size_t head_norm_grad_workspace(int head_dim, int num_sms);
 cudaError_t launch_head_norm_grad(const HeadNormGradDesc& d, float* partial, int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------- log probabilities

@@ -7,13 +7,17 @@
 // values of new rows into the pages of a layer (values neither normed nor turned).
 //
 // Bound by memory: every element is read once and written once. As in rotary.cu a thread owns one 16-byte unit of a head (for
-// the half layout two, the pair's halves); here the lanes of a head, a power of two, are neighbours in a warp and join the sum
-// of squares by shuffles. Heads whose units are no such thing (odd sizes, strides or alignments) take a warp each, an element
-// or a pair a lane.
+// the half layout two, the pair's halves), in four neighbouring heads, two in a gradient; here the lanes of a head, a power of
+// two, are neighbours in a warp and join the sum of squares by shuffles. What it takes to stay near memory is few instructions: 512
+// elements of a warp's step took 283 of them at first (16384 bf16 rows of 32 heads 58 us, the gradient 155). So places are
+// found by shifts, arithmetic is on two elements an instruction, gains and angles are multiplied once for a thread's heads, and all
+// of its heads' shuffles go level by level. Heads whose units are no such thing (odd sizes, strides or alignments) take a warp
+// each, an element or a pair a lane.
 //
-// The gains' gradient: a thread keeps the same elements of its part's heads over all the rows that its block walks, so
+// The gains' gradient: a thread keeps the same elements of its heads' part over all the rows that its block walks, so
 // their sums stay in its registers; a block's sums meet in shared memory, the blocks' in a second small kernel, both in a
-// fixed order: the same inputs give the same bits.
+// fixed order: the same inputs give the same bits. The next row's loads are on their way, and its angles formed, before the block's one
+// barrier a row.
 #include "../../include/crf.h"
 #include "rotary.cuh"
 
@@ -24,62 +28,49 @@ namespace crf {
 
 namespace {
 
-constexpr int kNormBatch = 4;   // heads of a thread, at most
-constexpr int kGradBatch = 2;
-constexpr int kMaxGradColumns = 4;  // blocks side by side over a row's heads
+constexpr int kNormBatch = 4;   // heads of a thread
 constexpr int kLoose = 8;       // elements of a lane in the form of a warp a head: 256 / 32
 
+// How a call's heads lie in blocks.
+struct Tiling {
+  int log_lanes;            // of a head
+  int units, rot_units;     // 16-byte units of a head, those that rotate
+  int log_rows;             // of a block
+  int slot0[3];             // each part's first slot (of a batch of heads)
+  int slots, block_slots;   // of all parts; of a block
+};
 struct NormArgs {
   HeadNormDesc d;
   ChunkTable c;
-  int lanes;                // of a head, a power of two
-  int units, rot_units;     // 16-byte units of a head, those that rotate
-  int rows;                 // of a block
-  int batch;                // heads of a slot
-  int slot0[3];             // each part's first slot
-  int slots, block_slots;   // of all parts; of a block
+  Tiling t;
 };
 
-// Sum over the `lanes` neighbours that share a head.
-__device__ __forceinline__ float head_sum(float v, int lanes) {
-  for (int o = lanes / 2; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
-// A thread's place: unit u of head slot `slot` of row `row`.
+// A thread's place: unit u of the heads [head, head + heads) of a part, row rb of the block's.
 struct Place {
-  int u, rb, slot, part, head, heads;
+  int rb, part, head, heads;
   bool turning;
   int e0, e1;  // first elements of its piece(s)
+  int pair;    // its first pair
 };
-template <int VEC, bool INTER, typename Args>
-__device__ __forceinline__ Place place_of(const Args& a, const RotaryDesc& d) {
+template <int VEC, bool INTER, int BATCH>
+__device__ __forceinline__ Place place_of(const Tiling& a, const RotaryDesc& d) {
   Place t;
-  t.u = threadIdx.x % a.lanes;
-  const int rest = threadIdx.x / a.lanes;
-  t.rb = rest % a.rows;
-  t.slot = rest / a.rows + blockIdx.y * a.block_slots;
-  const bool there = rest / a.rows < a.block_slots && t.slot < a.slots && t.u < a.units;
-  t.part = t.slot >= a.slot0[2] ? 2 : t.slot >= a.slot0[1] ? 1 : 0;
+  const int u = threadIdx.x & ((1 << a.log_lanes) - 1), rest = threadIdx.x >> a.log_lanes;
+  t.rb = rest & ((1 << a.log_rows) - 1);
+  const int at = rest >> a.log_rows, slot = at + blockIdx.y * a.block_slots;
+  const bool there = at < a.block_slots && slot < a.slots && u < a.units;
+  t.part = slot >= a.slot0[2] ? 2 : slot >= a.slot0[1] ? 1 : 0;
   const int first = t.part == 0 ? 0 : t.part == 1 ? a.slot0[1] : a.slot0[2];
   const int all = t.part == 0 ? d.part[0].heads : t.part == 1 ? d.part[1].heads : d.part[2].heads;
-  t.head = (t.slot - first) * a.batch;
-  t.heads = there ? min(a.batch, all - t.head) : 0;
-  t.turning = t.u < a.rot_units;
-  t.e0 = t.turning ? t.u * VEC : d.rot_dim + (t.u - a.rot_units) * VEC;
+  t.head = (slot - first) * BATCH;
+  t.heads = there ? min(BATCH, all - t.head) : 0;
+  t.turning = u < a.rot_units;
+  t.e0 = t.turning ? u * VEC : d.rot_dim + (u - a.rot_units) * VEC;
   t.e1 = t.turning && !INTER ? t.e0 + d.rot_dim / 2 : t.e0;
+  t.pair = u * (INTER ? VEC / 2 : VEC);
   return t;
 }
 
-// Angles of `here` rows from row0 on: [row][pair].
-__device__ __forceinline__ void form_angles(const RotaryDesc& d, const int* pos, int here, float2* angle) {
-  const int pairs = d.rot_dim / 2;
-  for (int i = threadIdx.x; i < here * pairs; i += blockDim.x) {
-    const int k = i / here, r = i - k * here;  // lanes of a warp share few pairs
-    const float2 t = turn_cos_sin(static_cast<uint64_t>(static_cast<int64_t>(pos[r])) * d.turns[k]);
-    angle[r * pairs + k] = make_float2(t.x * d.magnitude, (d.inverse ? -t.y : t.y) * d.magnitude);
-  }
-}
 // Positions, and the pages of rows that go into a cache (-1: no page of the pool).
 __device__ __forceinline__ void find_row(const RotaryDesc& d, const ChunkTable& c, int r, int* pos, int* page) {
   *page = 0;
@@ -103,99 +94,191 @@ __device__ __forceinline__ int64_t out_step(const RotaryDesc& d, const RotPart& 
   return t.paged ? static_cast<int64_t>(kPage) * d.head_dim : t.out_head;
 }
 
-// The pair(s) of two pieces, or of one with its pairs side by side.
-template <int VEC, bool INTER>
-__device__ __forceinline__ void turn(float (&x)[VEC], float (&y)[VEC], const float2* cs) {
+// ---------------------------------------------------------------- two elements a word
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float sum_f32x2(uint64_t a) {
+  float x, y;
+  f32x2_split(a, x, y);
+  return x + y;
+}
+__device__ __forceinline__ uint64_t swap_f32x2(uint64_t a) {
+  float x, y;
+  f32x2_split(a, x, y);
+  return f32x2(y, x);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void unpack_pairs(const uint4& raw, uint64_t (&p)[VEC / 2]) {
+  Unit<T, VEC> u;
+  *reinterpret_cast<uint4*>(&u) = raw;
+  float f[VEC];
+  unpack(u, f);
 #pragma unroll
-  for (int i = 0; i < (INTER ? VEC / 2 : VEC); ++i) {
-    float& a = INTER ? x[(2 * i) % VEC] : x[i];
-    float& b = INTER ? x[(2 * i + 1) % VEC] : y[i];
-    const float af = a, bf = b;
-    a = af * cs[i].x - bf * cs[i].y;
-    b = bf * cs[i].x + af * cs[i].y;
+  for (int i = 0; i < VEC / 2; ++i) p[i] = f32x2(f[2 * i], f[2 * i + 1]);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ uint4 pack_pairs(const uint64_t (&p)[VEC / 2]) {
+  float f[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC / 2; ++i) f32x2_split(p[i], f[2 * i], f[2 * i + 1]);
+  Unit<T, VEC> u;
+  pack(f, u);
+  return *reinterpret_cast<const uint4*>(&u);
+}
+// Sums over the lanes of a head, of N heads level by level.
+template <int N>
+__device__ __forceinline__ void head_sums(float (&v)[N], int log_lanes) {
+  for (int o = (1 << log_lanes) >> 1; o > 0; o >>= 1) {
+#pragma unroll
+    for (int b = 0; b < N; ++b) v[b] += __shfl_xor_sync(0xffffffffu, v[b], o);
+  }
+}
+// Angles of `rows` rows: cosines and sines [row][pair].
+struct Angles {
+  float cos[kRotMaxAngles], sin[kRotMaxAngles];
+};
+__device__ __forceinline__ void form_angles(const RotaryDesc& d, const int* pos, int log_rows, int rows, Angles& to) {
+  const int pairs = d.rot_dim / 2;
+  for (int i = threadIdx.x; i < pairs << log_rows; i += blockDim.x) {
+    const int k = i >> log_rows, r = i & ((1 << log_rows) - 1);  // lanes of a warp share pairs
+    if (r >= rows) continue;
+    const float2 t = turn_cos_sin(static_cast<uint64_t>(static_cast<int64_t>(pos[r])) * d.turns[k]);
+    to.cos[r * pairs + k] = t.x * d.magnitude;
+    to.sin[r * pairs + k] = t.y * d.magnitude;
   }
 }
 
 // ---------------------------------------------------------------- forward, 16-byte units
-template <typename T, int VEC, bool INTER>
-__global__ void __launch_bounds__(kRotThreads) head_norm_kernel(const __grid_constant__ NormArgs a) {
-  using U = Unit<T, VEC>;
+template <typename T, int VEC, bool INTER, int BATCH>
+__global__ void __launch_bounds__(kRotThreads, BATCH == 1 ? 1 : 3) head_norm_kernel(const __grid_constant__ NormArgs a) {
   constexpr bool kTwo = !INTER;
-  constexpr int kPairs = INTER ? VEC / 2 : VEC;
+  constexpr int P = VEC / 2, H = kTwo ? P : 1;
   __shared__ int s_pos[kRotMaxRows], s_page[kRotMaxRows];
-  __shared__ float2 s_angle[kRotMaxAngles];
+  __shared__ __align__(16) Angles s_angle;
   griddep_launch_dependents();
   const RotaryDesc& d = a.d.r;
-  const Place p = place_of<VEC, INTER>(a, d);
-  const int64_t row0 = static_cast<int64_t>(blockIdx.x) * a.rows, row = row0 + p.rb;
-  const int heads = row < d.n_rows ? p.heads : 0;
+  const Place p = place_of<VEC, INTER, BATCH>(a.t, d);
+  const int64_t row0 = static_cast<int64_t>(blockIdx.x) << a.t.log_rows, row = row0 + p.rb;
+  const int heads = row < d.n_rows ? p.heads : 0, here = static_cast<int>(min(static_cast<int64_t>(1) << a.t.log_rows, d.n_rows - row0));
   const RotPart t = p.part == 0 ? d.part[0] : p.part == 1 ? d.part[1] : d.part[2];
-  const T* gain = static_cast<const T*>(p.part == 0 ? a.d.gain[0] : p.part == 1 ? a.d.gain[1] : nullptr);
-  const float eps = p.part == 0 ? a.d.eps[0] : a.d.eps[1];
   const bool two = kTwo && p.turning;
-  U lo[kNormBatch], hi[kNormBatch], wl, wh;
+  uint4 lo[BATCH], hi[kTwo ? BATCH : 1], wl, wh;
   griddep_wait();
   {
-    const T* src = static_cast<const T*>(t.x) + row * t.x_row + p.head * t.x_head;
+    const T* src = static_cast<const T*>(t.x) + row * t.x_row + p.head * t.x_head + p.e0;
 #pragma unroll
-    for (int b = 0; b < kNormBatch; ++b) {
+    for (int b = 0; b < BATCH; ++b) {
       if (b < heads) {
-        lo[b] = *reinterpret_cast<const U*>(src + p.e0);
-        if (two) hi[b] = *reinterpret_cast<const U*>(src + p.e1);
+        lo[b] = *reinterpret_cast<const uint4*>(src);
+        if constexpr (kTwo)
+          if (two) hi[b] = *reinterpret_cast<const uint4*>(src + (p.e1 - p.e0));
       }
       src += t.x_head;
     }
   }
-  if (gain && heads > 0) {
-    wl = *reinterpret_cast<const U*>(gain + p.e0);
-    if (two) wh = *reinterpret_cast<const U*>(gain + p.e1);
+  if (t.rotate && heads > 0) {
+    const T* gain = static_cast<const T*>(p.part == 0 ? a.d.gain[0] : a.d.gain[1]);
+    wl = *reinterpret_cast<const uint4*>(gain + p.e0);
+    if (two) wh = *reinterpret_cast<const uint4*>(gain + p.e1);
   }
-  if (threadIdx.x < a.rows && row0 + threadIdx.x < d.n_rows)
-    find_row(d, a.c, static_cast<int>(row0) + threadIdx.x, &s_pos[threadIdx.x], &s_page[threadIdx.x]);
+  if (threadIdx.x < here) find_row(d, a.c, static_cast<int>(row0) + threadIdx.x, &s_pos[threadIdx.x], &s_page[threadIdx.x]);
   __syncthreads();
-  form_angles(d, s_pos, static_cast<int>(min(static_cast<int64_t>(a.rows), d.n_rows - row0)), s_angle);
+  form_angles(d, s_pos, a.t.log_rows, here, s_angle);
   __syncthreads();
+  if (__all_sync(0xffffffffu, heads == 0)) return;
   const int page = s_page[p.rb];
-  const bool rotate = p.turning && t.rotate;
-  float2 cs[kPairs];
-  if (rotate && heads > 0) {
-#pragma unroll
-    for (int i = 0; i < kPairs; ++i) cs[i] = s_angle[p.rb * (d.rot_dim / 2) + p.u * kPairs + i];
-  }
   const int64_t step = out_step(d, t);
-  T* dst = static_cast<T*>(t.out) + (heads > 0 ? p.head * step + out_at(d, t, row, s_pos[p.rb], page) : 0);
+  T* dst = static_cast<T*>(t.out) + (heads > 0 ? p.head * step + out_at(d, t, row, s_pos[p.rb], page) + p.e0 : 0);
   const bool write = heads > 0 && !(t.paged && page < 0);
+  if (!t.rotate) {
+    // (a warp may have normed heads beside these, so their lanes go on to the sums)
+    if (write) {
 #pragma unroll
-  for (int b = 0; b < kNormBatch; ++b) {
-    float x[VEC], y[VEC], ss = 0.f;
-    if (b < heads && t.rotate) {
-      unpack(lo[b], x);
-      if (two) unpack(hi[b], y);
+      for (int b = 0; b < BATCH; ++b)
+        if (b < heads) {
+          *reinterpret_cast<uint4*>(dst + b * step) = lo[b];
+          if constexpr (kTwo)
+            if (two) *reinterpret_cast<uint4*>(dst + b * step + (p.e1 - p.e0)) = hi[b];
+        }
+    }
+  }
+  const bool norm = t.rotate && heads > 0;
+  float ss[BATCH];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        ss += x[i] * x[i];
-        if (two) ss += y[i] * y[i];
+  for (int b = 0; b < BATCH; ++b) {
+    uint64_t sum = 0;
+    if (norm && b < heads) {
+      uint64_t x[P];
+      unpack_pairs<T, VEC>(lo[b], x);
+#pragma unroll
+      for (int i = 0; i < P; ++i) sum = fma_f32x2(x[i], x[i], sum);
+      if constexpr (kTwo)
+        if (two) {
+          unpack_pairs<T, VEC>(hi[b], x);
+#pragma unroll
+          for (int i = 0; i < P; ++i) sum = fma_f32x2(x[i], x[i], sum);
+        }
+    }
+    ss[b] = sum_f32x2(sum);
+  }
+  head_sums(ss, a.t.log_lanes);
+  if (!norm || !write) return;
+  // Gains and angles: x' = x k0 + y k1, y' = y k2 + x k3 (half layout), (x, y) k0 + (y, x) k1 (interleaved); a unit that does not
+  // turn has its gain alone.
+  uint64_t k0[P], k1[P], k2[H], k3[H];
+  unpack_pairs<T, VEC>(wl, k0);
+  if (p.turning) {
+    const float* c = s_angle.cos + p.rb * (d.rot_dim / 2) + p.pair;
+    const float* n = s_angle.sin + p.rb * (d.rot_dim / 2) + p.pair;
+    if constexpr (INTER) {
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        k1[i] = swap_f32x2(mul_f32x2(k0[i], f32x2(n[i], -n[i])));  // (-s w_y, s w_x)
+        k0[i] = mul_f32x2(k0[i], f32x2(c[i], c[i]));
+      }
+    } else {
+      unpack_pairs<T, VEC>(wh, k2);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float c0 = c[2 * i], c1 = c[2 * i + 1], n0 = n[2 * i], n1 = n[2 * i + 1];
+        k1[i] = mul_f32x2(k2[i], f32x2(-n0, -n1));
+        k3[i] = mul_f32x2(k0[i], f32x2(n0, n1));
+        k0[i] = mul_f32x2(k0[i], f32x2(c0, c1));
+        k2[i] = mul_f32x2(k2[i], f32x2(c0, c1));
       }
     }
-    ss = head_sum(ss, a.lanes);  // every lane takes part
-    if (b < heads && write) {
-      if (t.rotate) {
-        const float r = rsqrtf(ss * a.d.inv_dim + eps);
-        float w[VEC];
-        unpack(wl, w);
+  }
+  const float eps = p.part == 0 ? a.d.eps[0] : a.d.eps[1];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) x[i] *= r * w[i];
-        if (two) {
-          unpack(wh, w);
+  for (int b = 0; b < BATCH; ++b) {
+    if (b < heads) {
+      const float r = rsqrtf(ss[b] * a.d.inv_dim + eps);
+      const uint64_t r2 = f32x2(r, r);
+      uint64_t x[P], o[P];
+      unpack_pairs<T, VEC>(lo[b], x);
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) y[i] *= r * w[i];
+      for (int i = 0; i < P; ++i) x[i] = mul_f32x2(x[i], r2);
+      if (!p.turning) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) o[i] = mul_f32x2(x[i], k0[i]);
+      } else if constexpr (INTER) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) o[i] = fma_f32x2(swap_f32x2(x[i]), k1[i], mul_f32x2(x[i], k0[i]));
+      } else {
+        uint64_t y[P];
+        unpack_pairs<T, VEC>(hi[b], y);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          y[i] = mul_f32x2(y[i], r2);
+          o[i] = fma_f32x2(y[i], k1[i], mul_f32x2(x[i], k0[i]));
+          y[i] = fma_f32x2(x[i], k3[i], mul_f32x2(y[i], k2[i]));
         }
-        if (rotate) turn<VEC, INTER>(x, y, cs);
-        pack(x, lo[b]);
-        if (two) pack(y, hi[b]);
+        *reinterpret_cast<uint4*>(dst + (p.e1 - p.e0)) = pack_pairs<T, VEC>(y);
       }
-      *reinterpret_cast<U*>(dst + p.e0) = lo[b];
-      if (two) *reinterpret_cast<U*>(dst + p.e1) = hi[b];
+      *reinterpret_cast<uint4*>(dst) = pack_pairs<T, VEC>(o);
     }
     dst += step;
   }
@@ -222,7 +305,7 @@ __device__ __forceinline__ void store1(T* p, float v) {
 template <typename T>
 __global__ void __launch_bounds__(kRotThreads) head_norm_loose_kernel(const __grid_constant__ NormArgs a) {
   __shared__ int s_pos[1], s_page[1];
-  __shared__ float2 s_angle[kMaxPairs];
+  __shared__ Angles s_angle;
   griddep_launch_dependents();
   const RotaryDesc& d = a.d.r;
   const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -230,13 +313,13 @@ __global__ void __launch_bounds__(kRotThreads) head_norm_loose_kernel(const __gr
   griddep_wait();
   if (threadIdx.x == 0) find_row(d, a.c, row, s_pos, s_page);
   __syncthreads();
-  form_angles(d, s_pos, 1, s_angle);
+  form_angles(d, s_pos, 0, 1, s_angle);
   __syncthreads();
   const int page = s_page[0];
-  for (int s = warp; s < a.slots; s += blockDim.x / 32) {
-    const int p = s >= a.slot0[2] ? 2 : s >= a.slot0[1] ? 1 : 0;
+  for (int s = warp; s < a.t.slots; s += blockDim.x / 32) {
+    const int p = s >= a.t.slot0[2] ? 2 : s >= a.t.slot0[1] ? 1 : 0;
     const RotPart t = p == 0 ? d.part[0] : p == 1 ? d.part[1] : d.part[2];
-    const int head = s - (p == 0 ? 0 : p == 1 ? a.slot0[1] : a.slot0[2]);
+    const int head = s - (p == 0 ? 0 : p == 1 ? a.t.slot0[1] : a.t.slot0[2]);
     const T* src = static_cast<const T*>(t.x) + row * t.x_row + head * t.x_head;
     if (t.paged && page < 0) continue;
     T* dst = static_cast<T*>(t.out) + head * out_step(d, t) + out_at(d, t, row, s_pos[0], page);
@@ -263,7 +346,7 @@ __global__ void __launch_bounds__(kRotThreads) head_norm_loose_kernel(const __gr
     for (int i = 0; i < kLoose / 2; ++i)
       if (lane + 32 * i < pairs) {
         const int2 e = pair_at(d, lane + 32 * i);
-        const float2 cs = s_angle[lane + 32 * i];
+        const float2 cs = make_float2(s_angle.cos[lane + 32 * i], s_angle.sin[lane + 32 * i]);
         const float u = x[i] * (r * load1(gain + e.x)), v = y[i] * (r * load1(gain + e.y));
         store1(dst + e.x, u * cs.x - v * cs.y);
         store1(dst + e.y, v * cs.x + u * cs.y);
@@ -274,149 +357,227 @@ __global__ void __launch_bounds__(kRotThreads) head_norm_loose_kernel(const __gr
 }
 
 // ---------------------------------------------------------------- gradient, 16-byte units
-struct GradArgs {
+struct NormGradArgs {
   HeadNormGradDesc d;
-  int lanes, units, rot_units;
-  int rows, batch, slot0[3], slots, block_slots;
-  int row_blocks;           // blocks along the rows: each takes every row_blocks-th group of rows
+  Tiling t;
+  int row_blocks;           // blocks along the rows: each takes every row_blocks-th tile of rows
   float* partial;           // [part][block][head_dim]
 };
+// A thread's heads: as many as make four units of x and g.
+template <bool INTER>
+constexpr int kGradBatch = INTER ? 2 : 1;
+constexpr int kGradUnits = 4;
+// A thread's units of the next two tiles are on their way into places of its own in shared memory: in registers one tile took 128
+// of them and two blocks an SM had too few bytes in flight. Positions go three tiles ahead, because the next tile's angles are
+// formed before the barrier that follows their landing.
+constexpr int kStages = 3, kPositions = 4;
+struct NormGradShared {
+  Angles angle[2];
+  int pos[kPositions][kRotMaxRows];
+};
+
+__device__ __forceinline__ void copy_async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async4(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <typename T, int VEC, bool INTER>
-__global__ void __launch_bounds__(kRotThreads) head_norm_grad_kernel(const __grid_constant__ GradArgs a) {
-  using U = Unit<T, VEC>;
+__global__ void __launch_bounds__(kRotThreads, 2) head_norm_grad_kernel(const __grid_constant__ NormGradArgs a) {
   constexpr bool kTwo = !INTER;
-  constexpr int kPairs = INTER ? VEC / 2 : VEC;
-  __shared__ int s_pos[kRotMaxRows];
-  __shared__ float2 s_angle[kRotMaxAngles];
-  extern __shared__ float s_sum[];  // [lane group][head_dim]
+  constexpr int P = VEC / 2, H = kTwo ? P : 1, B = kGradBatch<INTER>;
+  __shared__ __align__(16) NormGradShared sh;
+  extern __shared__ __align__(16) uint4 s_unit[];  // [stage][x, its second or next, g likewise][thread]; then sums [head's lanes][head_dim]
   griddep_launch_dependents();
   const RotaryDesc& d = a.d.r;
-  const Place p = place_of<VEC, INTER>(a, d);
-  const RotPart t = p.part == 0 ? d.part[0] : d.part[1];
-  const T* gain = static_cast<const T*>(a.d.gain[p.part & 1]);
-  const float eps = a.d.eps[p.part & 1];
-  const int64_t g_row = a.d.g_row[p.part & 1], g_head = a.d.g_head[p.part & 1];
+  const Place p = place_of<VEC, INTER, B>(a.t, d);
+  const int q = p.part & 1, threads = blockDim.x;
+  const RotPart t = q == 0 ? d.part[0] : d.part[1];
+  const int64_t g_row = q == 0 ? a.d.g_row[0] : a.d.g_row[1], g_head = q == 0 ? a.d.g_head[0] : a.d.g_head[1];
   const bool two = kTwo && p.turning;
-  float acc_lo[VEC], acc_hi[VEC];
+  const int e1 = p.e1 - p.e0, log_rows = a.t.log_rows;
+  const int64_t tiles = (static_cast<int64_t>(d.n_rows) + (1 << log_rows) - 1) >> log_rows;
+  uint64_t acc_x[P], acc_y[H], wx[P], wy[H];
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) acc_lo[i] = acc_hi[i] = 0.f;
+  for (int i = 0; i < P; ++i) acc_x[i] = wx[i] = 0;
+#pragma unroll
+  for (int i = 0; i < H; ++i) acc_y[i] = wy[i] = 0;
+  const int64_t first_row = (static_cast<int64_t>(blockIdx.x) << log_rows) + p.rb, jump = static_cast<int64_t>(a.row_blocks) << log_rows;
+  // where the thread reads next, two tiles ahead, and writes
+  const T* x_at = static_cast<const T*>(t.x) + first_row * t.x_row + p.head * t.x_head + p.e0;
+  const T* g_at = static_cast<const T*>(q == 0 ? a.d.grad[0] : a.d.grad[1]) + first_row * g_row + p.head * g_head + p.e0;
+  T* o_at = static_cast<T*>(t.out) + first_row * t.out_row + p.head * t.out_head + p.e0;
+  const int64_t x_jump = jump * t.x_row, g_jump = jump * g_row, o_jump = jump * t.out_row;
+  int64_t f_row = first_row, pos_row = (static_cast<int64_t>(blockIdx.x) << log_rows) + threadIdx.x;
+  const int heads = p.heads;
   griddep_wait();
-  U wl, wh;
-  if (p.heads > 0) {
-    wl = *reinterpret_cast<const U*>(gain + p.e0);
-    if (two) wh = *reinterpret_cast<const U*>(gain + p.e1);
+  auto fetch_pos = [&](int slot) {
+    if (threadIdx.x < 1 << log_rows && pos_row < d.n_rows) copy_async4(&sh.pos[slot][threadIdx.x], d.positions + pos_row);
+    pos_row += jump;
+  };
+  auto fetch = [&](int stage) {
+    if (f_row < d.n_rows) {
+      uint4* to = s_unit + stage * kGradUnits * threads + threadIdx.x;
+      if (heads > 0) {
+        copy_async16(to, x_at);
+        copy_async16(to + 2 * threads, g_at);
+      }
+      if (kTwo ? two : heads > 1) {
+        copy_async16(to + threads, x_at + (kTwo ? e1 : t.x_head));
+        copy_async16(to + 3 * threads, g_at + (kTwo ? e1 : g_head));
+      }
+    }
+    f_row += jump;
+    x_at += x_jump;
+    g_at += g_jump;
+  };
+  fetch_pos(0);
+  copy_async_commit();
+  fetch_pos(1);
+  fetch(0);
+  copy_async_commit();
+  fetch_pos(2);
+  fetch(1);
+  copy_async_commit();
+  if (heads > 0) {
+    const T* gain = static_cast<const T*>(q == 0 ? a.d.gain[0] : a.d.gain[1]);
+    unpack_pairs<T, VEC>(*reinterpret_cast<const uint4*>(gain + p.e0), wx);
+    if constexpr (kTwo)
+      if (two) unpack_pairs<T, VEC>(*reinterpret_cast<const uint4*>(gain + p.e1), wy);
   }
-  for (int64_t row0 = static_cast<int64_t>(blockIdx.x) * a.rows; row0 < d.n_rows; row0 += static_cast<int64_t>(a.row_blocks) * a.rows) {
-    const int64_t row = row0 + p.rb;
-    const int heads = row < d.n_rows ? p.heads : 0;
-    U xl[kGradBatch], xh[kGradBatch], gl[kGradBatch], gh[kGradBatch];
-    {
-      const T* src = static_cast<const T*>(t.x) + row * t.x_row + p.head * t.x_head;
-      const T* grad = static_cast<const T*>(a.d.grad[p.part & 1]) + row * g_row + p.head * g_head;
+  copy_async_wait<1>();
+  __syncthreads();  // the first two tiles' positions
+  int64_t row = first_row;
+  auto angles = [&](int64_t at, int slot, Angles& to) {
+    const int64_t row0 = at - p.rb;
+    if (row0 < d.n_rows) form_angles(d, sh.pos[slot], log_rows, static_cast<int>(min(static_cast<int64_t>(1) << log_rows, d.n_rows - row0)), to);
+  };
+  angles(row, 0, sh.angle[0]);
+  __syncthreads();
+  int stage = 0, ahead = 2, pos = 0, buffer = 0;
+  for (int64_t tile = blockIdx.x; tile < tiles; tile += a.row_blocks) {
+    // (the stage and the positions of the tile before are free: all have passed the barrier behind them)
+    fetch_pos((pos + 3) & (kPositions - 1));
+    fetch(ahead);
+    copy_async_commit();
+    copy_async_wait<2>();
+    const float* c = sh.angle[buffer].cos + p.rb * (d.rot_dim / 2) + p.pair;
+    const float* n = sh.angle[buffer].sin + p.rb * (d.rot_dim / 2) + p.pair;
+    const uint4* from = s_unit + stage * kGradUnits * threads + threadIdx.x;
+    const int now = row < d.n_rows ? heads : 0;
+    // u: the gradient, turned back
+    uint64_t x[B][P], y[H], u[B][P], v[H];
+    float ss[B], dot[B];
 #pragma unroll
-      for (int b = 0; b < kGradBatch; ++b) {
-        if (b < heads) {
-          xl[b] = *reinterpret_cast<const U*>(src + p.e0);
-          gl[b] = *reinterpret_cast<const U*>(grad + p.e0);
+    for (int b = 0; b < B; ++b) {
+      uint64_t s2 = 0, d2 = 0;
+      if (b < now) {
+        unpack_pairs<T, VEC>(from[b * threads], x[b]);
+        unpack_pairs<T, VEC>(from[(2 + b) * threads], u[b]);
+        if constexpr (kTwo) {
           if (two) {
-            xh[b] = *reinterpret_cast<const U*>(src + p.e1);
-            gh[b] = *reinterpret_cast<const U*>(grad + p.e1);
+            unpack_pairs<T, VEC>(from[threads], y);
+            unpack_pairs<T, VEC>(from[3 * threads], v);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+              const float c0 = c[2 * i], c1 = c[2 * i + 1], n0 = n[2 * i], n1 = n[2 * i + 1];
+              const uint64_t g = u[b][i], c2 = f32x2(c0, c1);
+              u[b][i] = fma_f32x2(v[i], f32x2(n0, n1), mul_f32x2(g, c2));
+              v[i] = fma_f32x2(g, f32x2(-n0, -n1), mul_f32x2(v[i], c2));
+              s2 = fma_f32x2(y[i], y[i], s2);
+              d2 = fma_f32x2(mul_f32x2(v[i], wy[i]), y[i], d2);
+            }
           }
+        } else if (p.turning) {
+#pragma unroll
+          for (int i = 0; i < P; ++i) u[b][i] = fma_f32x2(swap_f32x2(u[b][i]), f32x2(n[i], -n[i]), mul_f32x2(u[b][i], f32x2(c[i], c[i])));
         }
-        src += t.x_head;
-        grad += g_head;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          s2 = fma_f32x2(x[b][i], x[b][i], s2);
+          d2 = fma_f32x2(mul_f32x2(u[b][i], wx[i]), x[b][i], d2);
+        }
+      }
+      ss[b] = sum_f32x2(s2);
+      dot[b] = sum_f32x2(d2);
+    }
+    head_sums(ss, a.t.log_lanes);
+    head_sums(dot, a.t.log_lanes);
+    const float eps = q == 0 ? a.d.eps[0] : a.d.eps[1];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      if (b < now) {
+        const float r = rsqrtf(ss[b] * a.d.inv_dim + eps), m = -r * (r * r * (dot[b] * a.d.inv_dim));
+        const uint64_t r2 = f32x2(r, r), m2 = f32x2(m, m);
+        T* dst = o_at + b * t.out_head;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const uint64_t ur = mul_f32x2(u[b][i], r2);
+          acc_x[i] = fma_f32x2(ur, x[b][i], acc_x[i]);
+          u[b][i] = fma_f32x2(ur, wx[i], mul_f32x2(x[b][i], m2));
+        }
+        *reinterpret_cast<uint4*>(dst) = pack_pairs<T, VEC>(u[b]);
+        if constexpr (kTwo)
+          if (two) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+              const uint64_t vr = mul_f32x2(v[i], r2);
+              acc_y[i] = fma_f32x2(vr, y[i], acc_y[i]);
+              v[i] = fma_f32x2(vr, wy[i], mul_f32x2(y[i], m2));
+            }
+            *reinterpret_cast<uint4*>(dst + e1) = pack_pairs<T, VEC>(v);
+          }
       }
     }
-    if (threadIdx.x < a.rows && row0 + threadIdx.x < d.n_rows) s_pos[threadIdx.x] = d.positions[row0 + threadIdx.x];
+    o_at += o_jump;
+    row += jump;
+    buffer ^= 1;
+    pos = (pos + 1) & (kPositions - 1);
+    stage = stage == kStages - 1 ? 0 : stage + 1;
+    ahead = ahead == kStages - 1 ? 0 : ahead + 1;
+    angles(row, pos, sh.angle[buffer]);
     __syncthreads();
-    form_angles(d, s_pos, static_cast<int>(min(static_cast<int64_t>(a.rows), d.n_rows - row0)), s_angle);
-    __syncthreads();
-    float2 cs[kPairs];
-    if (p.turning && heads > 0) {
-#pragma unroll
-      for (int i = 0; i < kPairs; ++i) cs[i] = s_angle[p.rb * (d.rot_dim / 2) + p.u * kPairs + i];
-    }
-    T* dst = static_cast<T*>(t.out) + row * t.out_row + p.head * t.out_head;
-#pragma unroll
-    for (int b = 0; b < kGradBatch; ++b) {
-      float x[VEC], y[VEC], u[VEC], v[VEC], w[VEC], ss = 0.f, dot = 0.f;
-      if (b < heads) {
-        unpack(xl[b], x);
-        unpack(gl[b], u);
-        if (two) {
-          unpack(xh[b], y);
-          unpack(gh[b], v);
-        }
-        if (p.turning) turn<VEC, INTER>(u, v, cs);
-        unpack(wl, w);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          ss += x[i] * x[i];
-          dot += u[i] * w[i] * x[i];
-        }
-        if (two) {
-          unpack(wh, w);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            ss += y[i] * y[i];
-            dot += v[i] * w[i] * y[i];
-          }
-        }
-      }
-      ss = head_sum(ss, a.lanes);
-      dot = head_sum(dot, a.lanes);
-      if (b < heads) {
-        const float r = rsqrtf(ss * a.d.inv_dim + eps), c = r * r * (dot * a.d.inv_dim);
-        unpack(wl, w);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          acc_lo[i] += u[i] * (x[i] * r);
-          u[i] = r * (u[i] * w[i] - x[i] * c);
-        }
-        pack(u, xl[b]);
-        *reinterpret_cast<U*>(dst + p.e0) = xl[b];
-        if (two) {
-          unpack(wh, w);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            acc_hi[i] += v[i] * (y[i] * r);
-            v[i] = r * (v[i] * w[i] - y[i] * c);
-          }
-          pack(v, xh[b]);
-          *reinterpret_cast<U*>(dst + p.e1) = xh[b];
-        }
-      }
-      dst += t.out_head;
-    }
-    // (the next rows' positions are written behind the reads of this round's: the angles' barrier lies between; the
-    // angles themselves are written behind the next round's first barrier)
   }
-  // the block's sums: lane groups side by side, then a thread an element, group after group
-  float* mine = s_sum + threadIdx.x / a.lanes * d.head_dim;
-  if (p.u < a.units) {
+  copy_async_wait<0>();
+  __syncthreads();
+  // the block's sums: a head's lanes side by side, then a thread an element, head after head
+  float* s_sum = reinterpret_cast<float*>(s_unit);
+  float* mine = s_sum + (threadIdx.x >> a.t.log_lanes) * d.head_dim + p.e0;
+  if (heads > 0) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      mine[p.e0 + i] = acc_lo[i];
-      if (two) mine[p.e1 + i] = acc_hi[i];
-    }
+    for (int i = 0; i < P; ++i) f32x2_split(acc_x[i], mine[2 * i], mine[2 * i + 1]);
+    if constexpr (kTwo)
+      if (two) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) f32x2_split(acc_y[i], mine[e1 + 2 * i], mine[e1 + 2 * i + 1]);
+      }
   }
   __syncthreads();
   const int block = blockIdx.y * a.row_blocks + blockIdx.x, blocks = a.row_blocks * gridDim.y;
-  const int first = blockIdx.y * a.block_slots;  // the block's slots of part 0 come before those of part 1
-  const int split = min(max(a.slot0[1] - first, 0), a.block_slots) * a.rows, all = min(a.slots - first, a.block_slots) * a.rows;
+  const int first = blockIdx.y * a.t.block_slots;  // the block's slots of part 0 come before those of part 1
+  const int slots = min(a.t.slots - first, a.t.block_slots);
+  const int all = slots << log_rows, split = min(max(a.t.slot0[1] - first, 0), slots) << log_rows;
   for (int i = threadIdx.x; i < d.n_parts * d.head_dim; i += blockDim.x) {
-    const int q = i / d.head_dim, e = i - q * d.head_dim;
+    const int part = i >= d.head_dim, e = i - part * d.head_dim;
     float sum = 0.f;
-    for (int g = q ? split : 0; g < (q ? all : min(split, all)); ++g) sum += s_sum[g * d.head_dim + e];
-    a.partial[(static_cast<size_t>(q) * blocks + block) * d.head_dim + e] = sum;
+    for (int g = part ? split : 0; g < (part ? all : split); ++g) sum += s_sum[g * d.head_dim + e];
+    a.partial[(static_cast<size_t>(part) * blocks + block) * d.head_dim + e] = sum;
   }
 }
+
+struct GradArgs {  // of the loose form
+  HeadNormGradDesc d;
+  float* partial;           // [part][block][head_dim]
+};
 
 // ---------------------------------------------------------------- gradient, a warp a head
 template <typename T>
 __global__ void __launch_bounds__(kRotThreads) head_norm_grad_loose_kernel(const __grid_constant__ GradArgs a) {
-  __shared__ float2 s_angle[kMaxPairs];
+  __shared__ Angles s_angle;
   __shared__ float s_sum[kRotThreads / 32][2 * kMaxPairs];
   griddep_launch_dependents();
   const RotaryDesc& d = a.d.r;
@@ -430,9 +591,9 @@ __global__ void __launch_bounds__(kRotThreads) head_norm_grad_loose_kernel(const
 #pragma unroll
   for (int i = 0; i < kLoose; ++i) acc_r[i] = 0.f;
   griddep_wait();
-  for (int64_t row = blockIdx.x; row < d.n_rows; row += a.row_blocks) {
+  for (int64_t row = blockIdx.x; row < d.n_rows; row += gridDim.x) {
     __syncthreads();  // the angles of the row before have been read
-    form_angles(d, d.positions + row, 1, s_angle);
+    form_angles(d, d.positions + row, 0, 1, s_angle);
     __syncthreads();
     for (int head = warp; head < t.heads; head += warps) {
       const T* src = static_cast<const T*>(t.x) + row * t.x_row + head * t.x_head;
@@ -443,7 +604,7 @@ __global__ void __launch_bounds__(kRotThreads) head_norm_grad_loose_kernel(const
       for (int i = 0; i < kLoose / 2; ++i)
         if (lane + 32 * i < pairs) {
           const int2 e = pair_at(d, lane + 32 * i);
-          const float2 cs = s_angle[lane + 32 * i];
+          const float2 cs = make_float2(s_angle.cos[lane + 32 * i], -s_angle.sin[lane + 32 * i]);
           x[i] = load1(src + e.x);
           y[i] = load1(src + e.y);
           const float g = load1(grad + e.x), h = load1(grad + e.y);
@@ -498,33 +659,32 @@ __global__ void __launch_bounds__(kRotThreads) head_norm_grad_loose_kernel(const
   for (int e = threadIdx.x; e < d.head_dim; e += blockDim.x) {
     float sum = 0.f;
     for (int w = 0; w < warps; ++w) sum += s_sum[w][e];
-    a.partial[(static_cast<size_t>(q) * a.row_blocks + blockIdx.x) * d.head_dim + e] = sum;
+    a.partial[(static_cast<size_t>(q) * gridDim.x + blockIdx.x) * d.head_dim + e] = sum;
   }
 }
 
-// The blocks' sums of one part's gain: a warp takes eight elements, four lanes to each.
+// The blocks' sums of one part's gain: a block 32 elements, each warp every 32nd of the sums.
 struct GainArgs {
   const float* partial;  // [part][block][head_dim]
   float* dgain[2];
   int blocks, head_dim;
 };
-__global__ void __launch_bounds__(256) head_norm_gain_kernel(const __grid_constant__ GainArgs a) {
-  __shared__ float s_sum[8][32];
+__global__ void __launch_bounds__(1024) head_norm_gain_kernel(const __grid_constant__ GainArgs a) {
+  __shared__ float s_sum[32][33];
   griddep_launch_dependents();
-  const int lane = threadIdx.x % 32, group = threadIdx.x / 32, e = blockIdx.x * 32 + lane, q = blockIdx.y;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, e = blockIdx.x * 32 + lane, q = blockIdx.y;
+  const float* partial = a.partial + static_cast<size_t>(q) * a.blocks * a.head_dim;
   griddep_wait();
   float sum = 0.f;
   if (e < a.head_dim) {
-    const float* at = a.partial + static_cast<size_t>(q) * a.blocks * a.head_dim + e;
-    for (int b = group; b < a.blocks; b += 8) sum += __ldcg(at + static_cast<size_t>(b) * a.head_dim);
+#pragma unroll 8
+    for (int b = warp; b < a.blocks; b += 32) sum += __ldcg(partial + static_cast<size_t>(b) * a.head_dim + e);
   }
-  s_sum[group][lane] = sum;
+  s_sum[warp][lane] = sum;
   __syncthreads();
-  if (group == 0 && e < a.head_dim) {
-#pragma unroll
-    for (int g = 1; g < 8; ++g) sum += s_sum[g][lane];
-    (q == 0 ? a.dgain[0] : a.dgain[1])[e] = sum;
-  }
+  // element `warp` of the block's, over the warps' sums
+  sum = warp_sum(s_sum[lane][warp]);
+  if (lane == 0 && blockIdx.x * 32 + warp < a.head_dim) (q == 0 ? a.dgain[0] : a.dgain[1])[blockIdx.x * 32 + warp] = sum;
 }
 
 // ---------------------------------------------------------------- launches
@@ -533,92 +693,111 @@ bool units_align(const RotPart& t, int vec) {
          (reinterpret_cast<uintptr_t>(t.out) & 15) == 0 && (t.paged || (t.out_row % vec == 0 && t.out_head % vec == 0));
 }
 // Units of a head in the vector form and the lanes that they take; false where a head has no such form.
-template <typename Args>
-bool vector_form(const RotaryDesc& d, int vec, Args* a) {
+bool vector_form(const RotaryDesc& d, int vec, Tiling* a) {
   if (d.head_dim % vec || d.rot_dim % vec || (!d.interleaved && d.rot_dim / 2 % vec)) return false;
   a->rot_units = d.interleaved ? d.rot_dim / vec : d.rot_dim / 2 / vec;
   a->units = a->rot_units + (d.head_dim - d.rot_dim) / vec;
-  a->lanes = 1;
-  while (a->lanes < a->units) a->lanes *= 2;
-  return a->lanes <= 32;
+  a->log_lanes = 0;
+  while (1 << a->log_lanes < a->units) ++a->log_lanes;
+  return a->log_lanes <= 5;
 }
-// Deals the parts' heads to slots of at most `batch`, and slots and rows to blocks of about `threads` threads.
-template <typename Args>
-void deal_slots(const RotaryDesc& d, int batch, bool few, int threads, Args* a) {
-  a->batch = batch;
+// Deals the parts' heads to slots of at most `batch`, and slots and rows to blocks of about 128 threads.
+void deal_slots(const RotaryDesc& d, int batch, bool few, Tiling* a) {
   a->slots = 0;
   for (int p = 0; p < 3; ++p) {
     a->slot0[p] = a->slots;
     if (p < d.n_parts) a->slots += (d.part[p].heads + batch - 1) / batch;
     else a->slot0[p] = 1 << 30;
   }
-  a->block_slots = std::min(a->slots, kRotThreads / a->lanes);
-  a->rows = few ? 1 : std::max(1, std::min(kRotMaxRows, threads / (a->lanes * a->block_slots)));
+  a->block_slots = std::min(a->slots, kRotThreads >> a->log_lanes);
+  a->log_rows = 0;
+  while (!few && (a->block_slots << a->log_lanes << (a->log_rows + 1)) <= 128 && (2 << a->log_rows) <= kRotMaxRows &&
+         (d.rot_dim / 2) << (a->log_rows + 1) <= kRotMaxAngles)
+    ++a->log_rows;
 }
-template <typename Args>
-int block_threads(const Args& a) {
-  return (a.lanes * a.block_slots * a.rows + 31) / 32 * 32;
-}
+int block_threads(const Tiling& a) { return ((a.block_slots << a.log_lanes << a.log_rows) + 31) / 32 * 32; }
+unsigned columns_of(const Tiling& a) { return (a.slots + a.block_slots - 1) / a.block_slots; }
 
+template <typename T, int BATCH>
+cudaError_t launch_units(const NormArgs& a, cudaStream_t stream) {
+  constexpr int VEC = 16 / sizeof(T);
+  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(a.d.r.n_rows) + (1 << a.t.log_rows) - 1) >> a.t.log_rows), columns_of(a.t));
+  return a.d.r.interleaved ? launch_kernel(head_norm_kernel<T, VEC, true, BATCH>, grid, dim3(block_threads(a.t)), 0, stream, a)
+                           : launch_kernel(head_norm_kernel<T, VEC, false, BATCH>, grid, dim3(block_threads(a.t)), 0, stream, a);
+}
 template <typename T>
 cudaError_t launch_norm(NormArgs& a, int num_sms, cudaStream_t stream) {
   constexpr int VEC = 16 / sizeof(T);
   const RotaryDesc& d = a.d.r;
-  bool vec = vector_form(d, VEC, &a);
+  bool vec = vector_form(d, VEC, &a.t);
   for (int p = 0; p < d.n_parts; ++p)
     vec = vec && units_align(d.part[p], VEC) && (!d.part[p].rotate || (reinterpret_cast<uintptr_t>(a.d.gain[p]) & 15) == 0);
   PdlScope pdl;
   if (!vec) {
-    a.lanes = 32;
-    deal_slots(d, 1, true, 32, &a);
-    const int threads = std::min(kRotThreads, 32 * a.slots);
+    a.t.log_lanes = 5;
+    deal_slots(d, 1, true, &a.t);
+    const int threads = std::min(kRotThreads, 32 * a.t.slots);
     return launch_kernel(head_norm_loose_kernel<T>, dim3(d.n_rows), dim3(threads), 0, stream, a);
   }
-  // as in rotary.cu: slots of four heads where the rows alone fill the SMs, of one where they are few
+  // as in rotary.cu: four heads a thread where the rows alone fill the SMs, one where they are few
   const bool few = d.n_rows < 4 * num_sms;
-  deal_slots(d, few ? 1 : kNormBatch, few, 128, &a);
-  if (few && a.slots > 4096) deal_slots(d, kNormBatch, few, 128, &a);  // keep the grid's second axis short
-  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(d.n_rows) + a.rows - 1) / a.rows),
-                  (a.slots + a.block_slots - 1) / a.block_slots);
-  return d.interleaved ? launch_kernel(head_norm_kernel<T, VEC, true>, grid, dim3(block_threads(a)), 0, stream, a)
-                       : launch_kernel(head_norm_kernel<T, VEC, false>, grid, dim3(block_threads(a)), 0, stream, a);
+  if (few) {
+    deal_slots(d, 1, true, &a.t);
+    if (a.t.slots <= 4096) return launch_units<T, 1>(a, stream);  // (more: keep the grid's second axis short)
+  }
+  deal_slots(d, kNormBatch, few, &a.t);
+  return launch_units<T, kNormBatch>(a, stream);
 }
 
-// Blocks along the rows of a gradient, and so sums to join: up to six an SM.
-int row_blocks_of(int64_t groups, int num_sms) { return static_cast<int>(std::min<int64_t>(groups, 6 * num_sms)); }
+// Sums of a gradient's blocks, two parts, to join.
+int most_blocks(int num_sms) { return 8 * num_sms; }
 
-template <typename T>
-cudaError_t launch_grad(GradArgs& a, int num_sms, cudaStream_t stream) {
-  constexpr int VEC = 16 / sizeof(T);
-  const RotaryDesc& d = a.d.r;
-  bool vec = vector_form(d, VEC, &a);
-  for (int p = 0; p < d.n_parts; ++p)
-    vec = vec && units_align(d.part[p], VEC) && a.d.g_row[p] % VEC == 0 && a.d.g_head[p] % VEC == 0 &&
-          ((reinterpret_cast<uintptr_t>(a.d.gain[p]) | reinterpret_cast<uintptr_t>(a.d.grad[p])) & 15) == 0;
-  PdlScope pdl;
-  int blocks;
-  cudaError_t e;
-  if (vec) {
-    const bool few = d.n_rows < 4 * num_sms;
-    deal_slots(d, kGradBatch, few, 128, &a);
-    vec = a.slots <= a.block_slots * kMaxGradColumns;
+template <typename T, bool INTER>
+cudaError_t launch_grad_units(const NormGradArgs& a, int threads, int columns, cudaStream_t stream) {
+  constexpr int VEC = 16 / sizeof(T), kMost = kStages * kGradUnits * kRotThreads * 16;
+  static PerDevice once;
+  int dev = 0;
+  if (once.pending(&dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(head_norm_grad_kernel<T, VEC, INTER>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    if (e != cudaSuccess) return e;
+    once.done(dev);
   }
+  // (the sums need less: 64 bytes of a thread's two heads or two halves)
+  return launch_kernel(head_norm_grad_kernel<T, VEC, INTER>, dim3(a.row_blocks, columns), dim3(threads), kStages * kGradUnits * threads * 16, stream, a);
+}
+template <typename T>
+cudaError_t launch_grad(const HeadNormGradDesc& g, float* partial, int num_sms, cudaStream_t stream) {
+  constexpr int VEC = 16 / sizeof(T);
+  const RotaryDesc& d = g.r;
+  NormGradArgs a;
+  std::memset(&a, 0, sizeof(a));
+  bool vec = vector_form(d, VEC, &a.t);
+  for (int p = 0; p < d.n_parts; ++p)
+    vec = vec && units_align(d.part[p], VEC) && g.g_row[p] % VEC == 0 && g.g_head[p] % VEC == 0 &&
+          ((reinterpret_cast<uintptr_t>(g.gain[p]) | reinterpret_cast<uintptr_t>(g.grad[p])) & 15) == 0;
   if (vec) {
-    const int columns = (a.slots + a.block_slots - 1) / a.block_slots;
-    a.row_blocks = row_blocks_of((static_cast<int64_t>(d.n_rows) + a.rows - 1) / a.rows, num_sms);
-    blocks = a.row_blocks * columns;
-    const int threads = block_threads(a);
-    const size_t smem = static_cast<size_t>(threads / a.lanes) * d.head_dim * sizeof(float);  // at most 16 KB
-    const dim3 grid(a.row_blocks, columns);
-    e = d.interleaved ? launch_kernel(head_norm_grad_kernel<T, VEC, true>, grid, dim3(threads), smem, stream, a)
-                      : launch_kernel(head_norm_grad_kernel<T, VEC, false>, grid, dim3(threads), smem, stream, a);
+    deal_slots(d, d.interleaved ? kGradBatch<true> : kGradBatch<false>, d.n_rows < 4 * num_sms, &a.t);
+    vec = static_cast<int>(columns_of(a.t)) <= most_blocks(num_sms) / 8;
+  }
+  PdlScope pdl;
+  cudaError_t e;
+  GainArgs sums{partial, {g.dgain[0], g.dgain[1]}, 0, d.head_dim};
+  if (vec) {
+    a.d = g;
+    a.partial = partial;
+    // as many blocks as are resident at a time: two of 256 threads an SM (their registers), four of 128
+    const int columns = static_cast<int>(columns_of(a.t)), threads = block_threads(a.t), resident = std::min(8, 2 * kRotThreads / threads);
+    const int64_t tiles = (static_cast<int64_t>(d.n_rows) + (1 << a.t.log_rows) - 1) >> a.t.log_rows;
+    a.row_blocks = static_cast<int>(std::min<int64_t>(tiles, std::max(1, resident * num_sms / columns)));
+    sums.blocks = a.row_blocks * columns;
+    e = d.interleaved ? launch_grad_units<T, true>(a, threads, columns, stream) : launch_grad_units<T, false>(a, threads, columns, stream);
   } else {
-    a.row_blocks = blocks = row_blocks_of(d.n_rows, num_sms);
-    e = launch_kernel(head_norm_grad_loose_kernel<T>, dim3(blocks, d.n_parts), dim3(kRotThreads), 0, stream, a);
+    sums.blocks = std::min(d.n_rows, 4 * num_sms);
+    const GradArgs l{g, partial};
+    e = launch_kernel(head_norm_grad_loose_kernel<T>, dim3(sums.blocks, d.n_parts), dim3(kRotThreads), 0, stream, l);
   }
   if (e != cudaSuccess) return e;
-  GainArgs g{a.partial, {a.d.dgain[0], a.d.dgain[1]}, blocks, d.head_dim};
-  return launch_kernel(head_norm_gain_kernel, dim3((d.head_dim + 31) / 32, d.n_parts), dim3(256), 0, stream, g);
+  return launch_kernel(head_norm_gain_kernel, dim3((d.head_dim + 31) / 32, d.n_parts), dim3(1024), 0, stream, sums);
 }
 
 }  // namespace
@@ -637,8 +816,8 @@ cudaError_t launch_head_norm(const HeadNormDesc& d, const ChunkTable* chunks, in
   return cudaErrorInvalidValue;
 }
 
-size_t head_norm_grad_workspace(int n_rows, int head_dim, int num_sms) {
-  return 2ull * kMaxGradColumns * row_blocks_of(n_rows, num_sms) * head_dim * sizeof(float);
+size_t head_norm_grad_workspace(int head_dim, int num_sms) {
+  return 2 * static_cast<size_t>(most_blocks(num_sms)) * head_dim * sizeof(float);
 }
 
 cudaError_t launch_head_norm_grad(const HeadNormGradDesc& d, float* partial, int num_sms, cudaStream_t stream) {
@@ -649,14 +828,10 @@ cudaError_t launch_head_norm_grad(const HeadNormGradDesc& d, float* partial, int
     }
     return cudaSuccess;
   }
-  GradArgs a;
-  std::memset(&a, 0, sizeof(a));
-  a.d = d;
-  a.partial = partial;
   switch (d.r.type) {
-    case CRF_BF16: return launch_grad<__nv_bfloat16>(a, num_sms, stream);
-    case CRF_FP16: return launch_grad<__half>(a, num_sms, stream);
-    case CRF_FP32: return launch_grad<float>(a, num_sms, stream);
+    case CRF_BF16: return launch_grad<__nv_bfloat16>(d, partial, num_sms, stream);
+    case CRF_FP16: return launch_grad<__half>(d, partial, num_sms, stream);
+    case CRF_FP32: return launch_grad<float>(d, partial, num_sms, stream);
   }
   return cudaErrorInvalidValue;
 }

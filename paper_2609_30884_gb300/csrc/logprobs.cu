@@ -7,12 +7,13 @@
 // x = (z - m) log2 e, in fp32 (entropy = log s - d log 2 / s); differences are formed before the product, so that the rounding of
 // m log2 e stays out. A row is one CTA's, or the CTAs of a cluster's where rows are few; their sums meet in shared memory.
 //
-// The alternatives take no pass of their own over the row. The maximum of every 256 elements (a segment) is noted on the
-// way. Keys (value, then lower index) order all elements; the k greatest elements lie in the k segments of greatest maxima, because a
-// segment that is left out has k segments before it, each with an element of a greater key than any of its own. So k segments
-// are read again (from L2), and the elements that reach the k-th greatest maximum, some 1.5 k of them as a rule, are ranked by
-// counting. Where they are many (equal logits, rows that rise along the vocabulary), the k-th greatest key is found by
-// bisection first. Nothing here depends on the order in which threads run.
+// The alternatives take no pass of their own over the row. A lane's maximum is known when its sums are, and the lanes of a row are
+// groups of its elements (with a cluster, the same lane of every CTA): at least k elements reach the k-th greatest of the
+// groups' maxima, and those that reach it lie in groups that do. Sixteen rounds of counting over the block find that bound, to its
+// 16 leading bits; the few lanes that reach it have their elements read again (from L2), and the elements that do, some 1.1 k of
+// a long row, are ranked by counting. Keys (value, then lower index) order them, so the order in which threads
+// list them does not matter. Rows of many equal logits, and rows that rise along the vocabulary, are gone through again as a whole:
+// those equal to an exact bound are taken in order of index, or the k-th greatest key is found digit by digit.
 //
 // Rows start at any element: a row is cut at 16-byte addresses, its first and last pieces element by element.
 #include "../../include/crf.h"
@@ -27,9 +28,9 @@ namespace {
 
 constexpr int kLogThreads = 512;   // at most
 constexpr int kStrip = 1024;       // elements of a warp's step
-constexpr int kSegment = 256;      // elements that share a maximum
 constexpr int kList = 512;         // elements that are ranked by counting
-constexpr int kLogSmem = ((kMaxVocab + 16) / kSegment + 8 + kMaxTop * kSegment) * 4;
+constexpr int kChosen = 64;        // groups that are read again
+constexpr int kAhead = 4;          // units of them that a lane asks for at once
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFloor = -200.f;   // 2^x is 0 from here down; keeps an infinite x out of products
 
@@ -77,18 +78,16 @@ struct Sums {
   }
 };
 
-struct LogArgs {
-  LogprobsDesc d;
-  int segments;  // room for a row's
-};
-
 struct LogShared {
   Sums part[kLogThreads / 32];
-  Sums cta;                         // read by the cluster's first CTA
-  int count[2][kLogThreads / 32];
-  int chosen[kMaxTop];              // segments
+  Sums cta;                         // read by the cluster's first CTA, as is
+  uint32_t lane[kLogThreads];       // the order of each lane's maximum, 0 without elements
+  int chosen[kChosen];              // lanes
+  int n_chosen, n_list, n_equal[kLogThreads / 32];
   unsigned long long list[kList];
-  int n_list, n_above, n_equal[kLogThreads / 32];
+  int digits[256];
+  unsigned long long prefix;
+  int left;
 };
 
 __device__ __forceinline__ uint32_t ld_cluster_u32(const void* p, uint32_t rank) {
@@ -97,18 +96,6 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(const void* p, uint32_t rank)
   return v;
 }
 __device__ __forceinline__ float ld_cluster_f32(const void* p, uint32_t rank) { return __uint_as_float(ld_cluster_u32(p, rank)); }
-
-// Threads' counts, summed over the block. Calls take turns at the two rows of `count`, so one barrier a call is enough.
-__device__ __forceinline__ int block_count(LogShared& sh, int mine, int& turn) {
-  const int warps = blockDim.x / 32;
-  const int w = __reduce_add_sync(0xffffffffu, mine);
-  if (threadIdx.x % 32 == 0) sh.count[turn & 1][threadIdx.x / 32] = w;
-  __syncthreads();
-  int n = 0;
-  for (int i = 0; i < warps; ++i) n += sh.count[turn & 1][i];
-  ++turn;
-  return n;
-}
 
 template <typename T>
 __device__ __forceinline__ float load_logit(const T* p) {
@@ -119,45 +106,38 @@ __device__ __forceinline__ float load_logit(const T* p) {
 
 // C: CTAs of a row, a cluster.
 template <typename T, int C>
-__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logprobs_kernel(const __grid_constant__ LogArgs a) {
-  constexpr int VEC = 16 / sizeof(T), kLoads = kStrip / (32 * VEC), kPerSegment = kSegment / (32 * VEC);
-  static_assert(kPerSegment >= 1 && kLoads == 4 * kPerSegment, "a strip is four segments");
+__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logprobs_kernel(const __grid_constant__ LogprobsDesc d) {
+  using U = Unit<T, 16 / sizeof(T)>;
+  constexpr int VEC = 16 / sizeof(T), kLoads = kStrip / (32 * VEC);
   __shared__ LogShared sh;
-  extern __shared__ uint32_t s_dyn[];
-  uint32_t* s_max = s_dyn;                   // [segment of the row]: those of this CTA's strips; then of all
-  uint32_t* s_key = s_dyn + a.segments;      // [chosen segment][256]: orders
   griddep_launch_dependents();
-  const LogprobsDesc& d = a.d;
   const int row = blockIdx.x / C, rank = C > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
-  const bool top = d.n_top > 0;
   const T* z = static_cast<const T*>(d.z) + row * d.z_row;
   // virtual index v = element + skew: 16-byte aligned where v is a multiple of VEC
   const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
-  const int end = d.vocab + skew, strips = (end + kStrip - 1) / kStrip, segments = (end + kSegment - 1) / kSegment;
+  const int end = d.vocab + skew, strips = (end + kStrip - 1) / kStrip;
   const T* base = z - skew;  // never read before z
   Sums acc{-INFINITY, 0.f, 0.f};
+  bool any = false;
   griddep_wait();
   for (int st = rank * warps + warp; st < strips; st += C * warps) {
+    // lane l has units l, l + 32 ... of the strip
     const int v0 = st * kStrip;
-    float seg[4];
     if (v0 >= skew && v0 + kStrip <= end) {
-      Unit<T, VEC> u[kLoads];
+      U u[kLoads];
 #pragma unroll
-      for (int j = 0; j < kLoads; ++j) u[j] = *reinterpret_cast<const Unit<T, VEC>*>(base + v0 + (j * 32 + lane) * VEC);
+      for (int j = 0; j < kLoads; ++j) u[j] = *reinterpret_cast<const U*>(base + v0 + (j * 32 + lane) * VEC);
+      float mx = NAN;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        seg[g] = NAN;
+      for (int j = 0; j < kLoads; ++j) {
+        float x[VEC];
+        unpack(u[j], x);
 #pragma unroll
-        for (int j = g * kPerSegment; j < (g + 1) * kPerSegment; ++j) {
-          float x[VEC];
-          unpack(u[j], x);
-#pragma unroll
-          for (int i = 0; i < VEC; i += 2) seg[g] = fmax3(seg[g], x[i], x[i + 1]);
-        }
+        for (int i = 0; i < VEC; i += 2) mx = fmax3(mx, x[i], x[i + 1]);
       }
-      const float mx = fmaxf(fmaxf(seg[0], seg[1]), fmaxf(seg[2], seg[3]));
       if (mx > acc.m) acc.raise(mx);
+      any = true;
       const float neg = acc.m == -INFINITY ? 0.f : -acc.m;
       const uint64_t neg2 = f32x2(neg, neg), l2e = f32x2(kLog2e, kLog2e), one = f32x2(1.f, 1.f);
       uint64_t s2 = f32x2(0.f, 0.f), d2 = f32x2(0.f, 0.f);
@@ -182,37 +162,38 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
       f32x2_split(d2, s0, s1);
       acc.d += s0 + s1;
     } else {
-      // a first or last strip, element by element; what lies outside the row is NaN to the maxima and no part of the sums
-      float x[kStrip / 32];
-      auto inside = [&](int j) { const int v = v0 + j * 32 + lane; return v >= skew && v < end; };
+      // a first or last strip: units that lie inside the row as they are, the others element by element; what is outside is
+      // NaN to the maxima and no part of the sums
+      float x[kLoads * VEC];
+      auto inside = [&](int j, int i) { const int v = v0 + (j * 32 + lane) * VEC + i; return v >= skew && v < end; };
 #pragma unroll
-      for (int j = 0; j < kStrip / 32; ++j) x[j] = inside(j) ? load_logit(base + v0 + j * 32 + lane) : NAN;
+      for (int j = 0; j < kLoads; ++j) {
+        float y[VEC];
+        if (inside(j, 0) && inside(j, VEC - 1)) {
+          unpack(*reinterpret_cast<const U*>(base + v0 + (j * 32 + lane) * VEC), y);
+        } else {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        seg[g] = NAN;
+          for (int i = 0; i < VEC; ++i) y[i] = inside(j, i) ? load_logit(base + v0 + (j * 32 + lane) * VEC + i) : NAN;
+        }
 #pragma unroll
-        for (int j = 0; j < kSegment / 32; ++j) seg[g] = fmaxf(seg[g], x[g * (kSegment / 32) + j]);
+        for (int i = 0; i < VEC; ++i) x[j * VEC + i] = y[i];
       }
-      const float mx = fmaxf(fmaxf(seg[0], seg[1]), fmaxf(seg[2], seg[3]));
+      float mx = NAN;
+#pragma unroll
+      for (int i = 0; i < kLoads * VEC; ++i) mx = fmaxf(mx, x[i]);
       if (mx > acc.m) acc.raise(mx);
       const float m = acc.m == -INFINITY ? 0.f : acc.m;
 #pragma unroll
-      for (int j = 0; j < kStrip / 32; ++j) {
-        if (!inside(j)) continue;
-        const float t = max_nan((x[j] - m) * kLog2e, kFloor), e = ex2_approx(t);
+      for (int i = 0; i < kLoads * VEC; ++i) {
+        if (!inside(i / VEC, i % VEC)) continue;
+        any = true;
+        const float t = max_nan((x[i] - m) * kLog2e, kFloor), e = ex2_approx(t);
         acc.s += e;
         acc.d += e * t;
       }
     }
-    if (top) {
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        // (a lane without elements says 1, as one of NaN alone does)
-        const uint32_t o = __reduce_max_sync(0xffffffffu, order_of(seg[g]));
-        if (lane == 0 && st * 4 + g < segments) s_max[st * 4 + g] = o;
-      }
-    }
   }
+  sh.lane[threadIdx.x] = any ? order_of(acc.m) : 0u;
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) {
     Sums other;
@@ -226,13 +207,17 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
   if (threadIdx.x == 0) {
     for (int w = 1; w < warps; ++w) acc.add(sh.part[w]);
     sh.cta = acc;
+    sh.n_chosen = sh.n_list = 0;
   }
+  uint32_t mine = sh.lane[threadIdx.x];
   if (C > 1) {
     cluster_sync();
     if (rank != 0) {
       cluster_sync();  // the first CTA has read what it needs
       return;
     }
+#pragma unroll
+    for (int r = 1; r < C; ++r) mine = max(mine, ld_cluster_u32(&sh.lane[threadIdx.x], r));
     if (threadIdx.x == 0) {
       for (int r = 1; r < C; ++r) {
         Sums o;
@@ -243,11 +228,6 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
       }
       sh.cta = acc;
     }
-    if (top)
-      for (int i = threadIdx.x; i < segments; i += blockDim.x) {
-        const int r = i / 4 / warps % C;
-        if (r != 0) s_max[i] = ld_cluster_u32(s_max + i, r);
-      }
     cluster_sync();
   } else {
     __syncthreads();
@@ -267,88 +247,170 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
       d.logprob[row] = lp;
     }
   }
-  if (!top) return;
+  const int k = d.n_top;
+  if (k == 0) return;
 
-  // ---------------------------------------------------------------- the k segments of greatest maxima
-  int turn = 0;
-  const int k = d.n_top, take = min(k, segments);
-  uint32_t least = 0;  // the `take`-th greatest maximum
-  if (segments > take) {
+  // ---------------------------------------------------------------- lanes that reach the k-th greatest maximum
+  uint32_t least = 0;
+  int reached = __syncthreads_count(mine > 0);
+  if (reached >= k) {
+#pragma unroll 1
     for (int bit = 31; bit >= 0; --bit) {
       const uint32_t cand = least | (1u << bit);
-      int n = 0;
-      for (int i = threadIdx.x; i < segments; i += blockDim.x) n += s_max[i] >= cand;
-      if (block_count(sh, n, turn) >= take) least = cand;
-    }
-  }
-  // all above it, and the first of those equal to it
-  {
-    int above = 0;
-    for (int i = threadIdx.x; i < segments; i += blockDim.x) above += s_max[i] > least;
-    const int n_above = block_count(sh, above, turn);
-    if (threadIdx.x == 0) sh.n_above = sh.n_list = 0;
-    __syncthreads();
-    int before = 0;  // equal ones in the rounds and warps before
-    for (int i0 = 0; i0 < segments; i0 += blockDim.x) {
-      const int i = i0 + threadIdx.x;
-      const uint32_t v = i < segments ? s_max[i] : 0u;
-      const bool eq = i < segments && v == least;
-      if (i < segments && v > least) sh.chosen[atomicAdd(&sh.n_above, 1)] = i;
-      const uint32_t mask = __ballot_sync(0xffffffffu, eq);
-      if (lane == 0) sh.n_equal[warp] = __popc(mask);
-      __syncthreads();
-      int at = before;
-      for (int w = 0; w < warps; ++w) {
-        if (w < warp) at += sh.n_equal[w];
-        before += sh.n_equal[w];
+      const int n = __syncthreads_count(mine >= cand);
+      if (n >= k) {
+        least = cand;
+        reached = n;
       }
-      at += __popc(mask & ((1u << lane) - 1));
-      if (eq && n_above + at < take) sh.chosen[n_above + at] = i;
+      if (bit == 16 && reached <= kChosen) break;
+    }
+  }
+  least = max(least, 1u);  // (fewer lanes than k: every element is listed)
+  auto key = [&](uint32_t order, int v) { return static_cast<unsigned long long>(order) << 32 | ~static_cast<uint32_t>(v - skew); };
+  // Into the list; n_list counts those that it has no room for as well.
+  auto push = [&](bool in, uint32_t order, int v) {
+    const uint32_t ins = __ballot_sync(0xffffffffu, in);
+    if (ins == 0) return;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&sh.n_list, __popc(ins));
+    at = __shfl_sync(0xffffffffu, at, 0) + __popc(ins & ((1u << lane) - 1));
+    if (in && at < kList) sh.list[at] = key(order, v);
+  };
+  bool again = reached > kChosen;
+  if (!again) {
+    if (mine >= least) sh.chosen[atomicAdd(&sh.n_chosen, 1)] = threadIdx.x;
+    __syncthreads();
+    // warp w has the strips w, w + warps ... of the row, over the cluster's CTAs
+    const int turns = (strips + warps - 1) / warps, units = sh.n_chosen * turns * kLoads;
+    auto unit_at = [&](int e) {
+      const int pair = e / kLoads, at = sh.chosen[pair / turns];
+      return (at / 32 + pair % turns * warps) * kStrip + (e % kLoads * 32 + at % 32) * VEC;
+    };
+    for (int e0 = warp * 32; e0 < units; e0 += kAhead * blockDim.x) {
+      U u[kAhead];  // all in flight
+      int v[kAhead];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        const int e = e0 + q * blockDim.x + lane;
+        v[q] = e < units ? unit_at(e) : end;
+        if (v[q] >= skew && v[q] + VEC <= end) u[q] = *reinterpret_cast<const U*>(base + v[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) {
+        if (e0 + q * static_cast<int>(blockDim.x) >= units) break;
+        uint32_t o[VEC];
+        if (v[q] >= skew && v[q] + VEC <= end) {
+          float x[VEC];
+          unpack(u[q], x);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) o[i] = order_of(x[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) o[i] = v[q] + i >= skew && v[q] + i < end ? order_of(load_logit(base + v[q] + i)) : 0u;
+        }
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) push(o[i] >= least, o[i], v[q] + i);
+      }
+    }
+    __syncthreads();
+    again = sh.n_list > kList || sh.n_list < k;  // (fewer: where NaN hides behind a maximum of -inf)
+    if (sh.n_list < k) least = 1u;
+  }
+  if (again) {
+    // ---------------------------------------------------------------- the whole row again, a run of it a warp
+    const bool exact = reached > kChosen;
+    const int runs = (end + 31) / 32, c0 = static_cast<int>(static_cast<int64_t>(runs) * warp / warps), c1 = static_cast<int>(static_cast<int64_t>(runs) * (warp + 1) / warps);
+    auto order_at = [&](int v) { return v >= skew && v < end ? order_of(load_logit(base + v)) : 0u; };
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n_list = 0;
+    __syncthreads();
+    int above = kList + 1;
+    if (exact) {
+      int equal = 0;
+#pragma unroll 4
+      for (int c = c0; c < c1; ++c) {
+        const uint32_t o = order_at(c * 32 + lane);
+        push(o > least, o, c * 32 + lane);
+        equal += __popc(__ballot_sync(0xffffffffu, o == least));
+      }
+      if (lane == 0) sh.n_equal[warp] = equal;
+      __syncthreads();
+      above = sh.n_list;
       __syncthreads();
     }
-  }
-  // ---------------------------------------------------------------- their elements
-  for (int c = warp; c < take; c += warps) {
-    const int v0 = sh.chosen[c] * kSegment;
+    if (above <= kList - kMaxTop) {
+      // all above the bound, and the first of those equal to it
+      int at = above;
+      for (int w = 0; w < warp; ++w) at += sh.n_equal[w];
+      for (int c = c0; c < c1 && at < k; ++c) {
+        const uint32_t o = order_at(c * 32 + lane), eqs = __ballot_sync(0xffffffffu, o == least);
+        const int to = at + __popc(eqs & ((1u << lane) - 1));
+        if (o == least && to < k) sh.list[to] = key(o, c * 32 + lane);
+        at += __popc(eqs);
+      }
+      if (threadIdx.x == 0) sh.n_list = max(above, k);
+    } else {
+      // the k-th greatest key, a digit of eight bits at a time; then the keys that reach it
+      if (threadIdx.x == 0) {
+        sh.prefix = 0;
+        sh.left = k;
+        sh.n_list = 0;
+      }
+      for (int shift = 56; shift >= 0; shift -= 8) {
+        for (int i = threadIdx.x; i < 256; i += blockDim.x) sh.digits[i] = 0;
+        __syncthreads();
+        const unsigned long long prefix = sh.prefix;
+#pragma unroll 4
+        for (int c = c0; c < c1; ++c) {
+          const uint32_t o = order_at(c * 32 + lane);
+          const unsigned long long x = key(o, c * 32 + lane);
+          if (o >= least && (shift == 56 || x >> (shift + 8) == prefix >> (shift + 8))) atomicAdd(&sh.digits[static_cast<int>(x >> shift) & 255], 1);
+        }
+        __syncthreads();
+        if (warp == 0) {
+          // lane l has the digits from 255 - 8 l down
+          int sum = 0;
+          for (int i = 0; i < 8; ++i) sum += sh.digits[255 - 8 * lane - i];
+          int to = sum;
 #pragma unroll
-    for (int j = 0; j < kSegment; j += 32) {
-      const int v = v0 + j + lane;
-      s_key[c * kSegment + j + lane] = v >= skew && v < end ? order_of(load_logit(base + v)) : 0u;
+          for (int o = 1; o < 32; o *= 2) {
+            const int up = __shfl_up_sync(0xffffffffu, to, o);
+            if (lane >= o) to += up;
+          }
+          const int left = sh.left;
+          __syncwarp();
+          int at = to - sum;
+          if (at < left && to >= left) {
+            int i = 255 - 8 * lane;
+            while (at + sh.digits[i] < left) at += sh.digits[i--];
+            sh.prefix = prefix | static_cast<unsigned long long>(i) << shift;
+            sh.left = left - at;
+          }
+        }
+        __syncthreads();
+      }
+      const unsigned long long from = sh.prefix;
+#pragma unroll 4
+      for (int c = c0; c < c1; ++c) {
+        const uint32_t o = order_at(c * 32 + lane);
+        push(o != 0 && key(o, c * 32 + lane) >= from, o, c * 32 + lane);
+      }
     }
+    __syncthreads();
   }
-  __syncthreads();
-  auto key_of = [&](int e) {
-    const int v = sh.chosen[e / kSegment] * kSegment + e % kSegment - skew;
-    return static_cast<unsigned long long>(s_key[e]) << 32 | ~static_cast<uint32_t>(v);
-  };
-  // The list: elements that reach the k-th greatest maximum (every element where the segments are fewer than k).
-  const uint32_t reach = max(least, 1u);
-  const int elements = take * kSegment;
-  int n = 0;
-  for (int e = threadIdx.x; e < elements; e += blockDim.x) n += s_key[e] >= reach;
-  const int reached = block_count(sh, n, turn);
-  unsigned long long from = static_cast<unsigned long long>(reach) << 32;
-  if (reached > kList) {
-    from = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-      const unsigned long long cand = from | (1ull << bit);
-      n = 0;
-      for (int e = threadIdx.x; e < elements; e += blockDim.x) n += s_key[e] != 0 && key_of(e) >= cand;
-      if (block_count(sh, n, turn) >= k) from = cand;
-    }
-  }
-  for (int e = threadIdx.x; e < elements; e += blockDim.x)
-    if (s_key[e] != 0 && key_of(e) >= from) sh.list[atomicAdd(&sh.n_list, 1)] = key_of(e);
-  __syncthreads();
-  const int listed = sh.n_list;
-  for (int i = threadIdx.x; i < listed; i += blockDim.x) {
-    const unsigned long long mine = sh.list[i];
+  // ---------------------------------------------------------------- ranks: a key's lanes count those above it
+  const int listed = sh.n_list, share = listed * 8 <= static_cast<int>(blockDim.x) ? 8 : 1, part = threadIdx.x % share;
+  for (int i0 = 0; i0 < listed; i0 += blockDim.x / share) {
+    const int i = i0 + static_cast<int>(threadIdx.x) / share;
+    const unsigned long long it = i < listed ? sh.list[i] : 0ull;
     int before = 0;
-    for (int j = 0; j < listed; ++j) before += sh.list[j] > mine;
-    if (before < k) {
-      if (d.top_ids) d.top_ids[static_cast<int64_t>(row) * k + before] = static_cast<int32_t>(~static_cast<uint32_t>(mine));
+#pragma unroll 4
+    for (int j = part; j < listed; j += share) before += sh.list[j] > it;
+    for (int o = share / 2; o > 0; o /= 2) before += __shfl_xor_sync(0xffffffffu, before, o);
+    if (i < listed && before < k && part == 0) {
+      if (d.top_ids) d.top_ids[static_cast<int64_t>(row) * k + before] = static_cast<int32_t>(~static_cast<uint32_t>(it));
       if (d.top_logprobs) {
-        const float v = value_of(static_cast<uint32_t>(mine >> 32));
+        const float v = value_of(static_cast<uint32_t>(it >> 32));
         d.top_logprobs[static_cast<int64_t>(row) * k + before] = s == 0.f ? -INFINITY : v - lse;
       }
     }
@@ -422,36 +484,20 @@ __global__ void __launch_bounds__(kGradThreads) logprobs_grad_kernel(const __gri
 }
 
 // ---------------------------------------------------------------- launches
-template <typename T, int C>
-cudaError_t launch_log(const LogArgs& a, int threads, cudaStream_t stream) {
-  const size_t smem = a.d.n_top > 0 ? (static_cast<size_t>(a.segments) + static_cast<size_t>(a.d.n_top) * kSegment) * sizeof(uint32_t) : 0;
-  static PerDevice once;
-  int dev = 0;
-  if (once.pending(&dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(logprobs_kernel<T, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, kLogSmem);
-    if (e != cudaSuccess) return e;
-    once.done(dev);
-  }
-  PdlScope pdl;
-  return launch_kernel(logprobs_kernel<T, C>, dim3(static_cast<unsigned>(a.d.n_rows) * C), dim3(threads), smem, stream, a);
-}
-
 template <typename T>
 cudaError_t launch_type(const LogprobsDesc& d, int num_sms, cudaStream_t stream) {
-  LogArgs a;
-  a.d = d;
-  a.segments = ((d.vocab + 15) / kSegment + 1 + 3) / 4 * 4;
   const int strips = (d.vocab + 15 + kStrip - 1) / kStrip;
   // a row's CTAs: enough that few rows fill the SMs, each with a strip a warp at least
   int c = 1;
   while (c < 8 && static_cast<int64_t>(d.n_rows) * c < num_sms && strips >= 2 * c) c *= 2;
-  const int threads = 32 * std::min(kLogThreads / 32, (strips + c - 1) / c);
+  const dim3 grid(static_cast<unsigned>(d.n_rows) * c), block(32 * std::min(kLogThreads / 32, (strips + c - 1) / c));
+  PdlScope pdl;
   switch (c) {
-    case 1: return launch_log<T, 1>(a, threads, stream);
-    case 2: return launch_log<T, 2>(a, threads, stream);
-    case 4: return launch_log<T, 4>(a, threads, stream);
+    case 1: return launch_kernel(logprobs_kernel<T, 1>, grid, block, 0, stream, d);
+    case 2: return launch_kernel(logprobs_kernel<T, 2>, grid, block, 0, stream, d);
+    case 4: return launch_kernel(logprobs_kernel<T, 4>, grid, block, 0, stream, d);
   }
-  return launch_log<T, 8>(a, threads, stream);
+  return launch_kernel(logprobs_kernel<T, 8>, grid, block, 0, stream, d);
 }
 
 template <typename T>
