@@ -406,20 +406,6 @@ crf_status run_chunk_attention(crf_ctx* ctx, const ChunkAttnDesc& d, const Chunk
   return CRF_OK;
 }
 
-void table_with_sinks(const ChunkTable& t, int sinks, AttnTable* a) {
-  std::memset(a, 0, sizeof(*a));
-  a->n = t.n;
-  a->num_pages = t.num_pages;
-  a->sinks = std::min(sinks, CRF_MAX_KEYS);
-  for (int i = 0; i < t.n; ++i) {
-    a->row0[i] = t.row0[i];
-    a->rows[i] = t.row0[i + 1] - t.row0[i];
-    a->pos[i] = t.pos[i];
-    a->n_keys[i] = t.n_keys[i];
-    a->pt[i] = t.pt[i];
-  }
-}
-
 // The requests' groups, checked, and the table of those that share.
 crf_status prefix_groups(const ChunkTable& t, const crf_prefix* prefixes, int n, int n_q_heads, int n_kv_heads, bool causal,
                          AttnTable* a, PrefixGroups* g) {
@@ -438,7 +424,7 @@ crf_status prefix_groups(const ChunkTable& t, const crf_prefix* prefixes, int n,
     at += count[i];
   }
   if (at != t.n) return fail(CRF_EINVAL, "the prefixes have %d requests, the call %d", at, t.n);
-  share_prefixes(t, count, keys, n, n_q_heads, n_kv_heads, a, g);
+  share_prefixes(t, count, keys, n, n_q_heads, n_kv_heads, causal, a, g);
   return CRF_OK;
 }
 
@@ -734,11 +720,10 @@ crf_status crf_chunk_attention_sinks_workspace_size(crf_ctx* ctx, int n_q_heads,
     if (s != CRF_OK) return s;
     size_t need;
     if (window > 0 && sinks > 0) {
-      AttnTable a;
-      AttnPlan plan;
-      table_with_sinks(t, sinks, &a);
-      plan_attention(a, false, n_q_heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
-      need = attention_workspace(plan, head_dim);
+      const SinksTable a{t, sinks};
+      ChunkPlan plan;
+      plan_sinks_attention(a, n_q_heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
+      need = chunk_attention_workspace(plan, head_dim);
     } else {
       ChunkPlan plan;
       plan_chunk_attention(t, n_q_heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
@@ -768,16 +753,15 @@ crf_status crf_chunk_attention_sinks(crf_ctx* ctx, const crf_kv_pool* pool, int 
     if (t.row0[t.n] == 0) return CRF_OK;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (window > 0 && sinks > 0) {
-      AttnTable a;
-      AttnPlan plan;
-      table_with_sinks(t, sinks, &a);
-      plan_attention(a, false, q->heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
-      s = check_workspace(workspace, ws_bytes, attention_workspace(plan, head_dim));
+      const SinksTable a{t, sinks};
+      ChunkPlan plan;
+      plan_sinks_attention(a, q->heads, n_kv_heads, causal != 0, window, ctx->num_sms, &plan);
+      s = check_workspace(workspace, ws_bytes, chunk_attention_workspace(plan, head_dim));
       if (s != CRF_OK) return s;
       DeviceScope dev(ctx->device);
       CRF_CUDA(dev.error());
-      ProfScope ps(ctx, kPChunkAttn, st, attention_launches(plan));
-      CRF_CUDA(launch_attention(d, a, nullptr, plan, workspace, ctx->num_sms, st));
+      ProfScope ps(ctx, kPChunkAttn, st, plan.cuts ? 2 : 1);
+      CRF_CUDA(launch_sinks_attention(d, a, plan, workspace, ctx->num_sms, st));
       return CRF_OK;
     }
     return run_chunk_attention(ctx, d, t, workspace, ws_bytes, st);
@@ -797,12 +781,12 @@ crf_status crf_prefix_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int 
     s = prefix_groups(t, prefixes, n_prefixes, n_q_heads, n_kv_heads, causal != 0, &a, &g);
     if (s != CRF_OK) return s;
     size_t need;
-    if (g.groups > 0) {
+    if (g.any) {
       AttnPlan plan;
-      plan_attention(a, true, n_q_heads, n_kv_heads, causal != 0, 0, ctx->num_sms, &plan);
+      plan_prefix_attention(a, g.groups > 0, n_q_heads, n_kv_heads, causal != 0, ctx->num_sms, &plan);
       s = check_parts(plan);
       if (s != CRF_OK) return s;
-      need = attention_workspace(plan, head_dim);
+      need = prefix_attention_workspace(plan, head_dim);
     } else {
       ChunkPlan plan;
       plan_chunk_attention(t, n_q_heads, n_kv_heads, causal != 0, 0, ctx->num_sms, &plan);
@@ -827,17 +811,17 @@ crf_status crf_prefix_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer
     s = prefix_groups(t, prefixes, n_prefixes, q->heads, n_kv_heads, causal != 0, &a, &g);
     if (s != CRF_OK || t.row0[t.n] == 0) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (g.groups == 0) return run_chunk_attention(ctx, d, t, workspace, ws_bytes, st);
+    if (!g.any) return run_chunk_attention(ctx, d, t, workspace, ws_bytes, st);
     AttnPlan plan;
-    plan_attention(a, true, q->heads, n_kv_heads, causal != 0, 0, ctx->num_sms, &plan);
+    plan_prefix_attention(a, g.groups > 0, q->heads, n_kv_heads, causal != 0, ctx->num_sms, &plan);
     s = check_parts(plan);
     if (s != CRF_OK) return s;
-    s = check_workspace(workspace, ws_bytes, attention_workspace(plan, head_dim));
+    s = check_workspace(workspace, ws_bytes, prefix_attention_workspace(plan, head_dim));
     if (s != CRF_OK) return s;
     DeviceScope dev(ctx->device);
     CRF_CUDA(dev.error());
-    ProfScope ps(ctx, kPPrefixAttn, st, attention_launches(plan));
-    CRF_CUDA(launch_attention(d, a, &g, plan, workspace, ctx->num_sms, st));
+    ProfScope ps(ctx, kPPrefixAttn, st, plan.shared || plan.runs.cuts ? 2 : 1);
+    CRF_CUDA(launch_prefix_attention(d, a, g, plan, workspace, ctx->num_sms, st));
     return CRF_OK;
   });
 }

@@ -33,19 +33,8 @@
 namespace crf {
 
 void plan_chunk_attention(const ChunkTable& c, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms, ChunkPlan* p) {
-  plan_runs(c, n_q_heads, n_kv_heads, causal, window, num_sms, nullptr, p);
+  plan_runs(c, kCosts, n_q_heads, n_kv_heads, causal, window, num_sms, nullptr, p);
 }
-
-namespace {
-
-template <int D, bool LEAN>
-cudaError_t launch_tc(const ChunkArgs<false>& a, const ChunkPlan& p, int num_sms, cudaStream_t stream) {
-  PdlScope pdl;
-  const cudaError_t e = launch_kernel_tc<D, LEAN, false>(a, p.ctas, stream);
-  return e != cudaSuccess ? e : launch_merge<D>(a.d, p, a.part, a.part_ml, num_sms, stream);
-}
-
-}  // namespace
 
 size_t chunk_attention_workspace(const ChunkPlan& p, int head_dim) {
   return (part_floats(p, head_dim, false) + part_floats(p, head_dim, true) + total_floats(p, head_dim)) * sizeof(float);
@@ -53,22 +42,7 @@ size_t chunk_attention_workspace(const ChunkPlan& p, int head_dim) {
 
 cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, const ChunkPlan& p, void* workspace,
                                    int num_sms, cudaStream_t stream) {
-  if (p.ctas == 0) return cudaSuccess;
-  ChunkArgs<false> a;
-  const long pool_rows = static_cast<long>(c.num_pages) * d.n_kv_heads * kPage;
-  if (!tensor_map_pool(&a.tmK, d.kpages, pool_rows, d.head_dim) || !tensor_map_pool(&a.tmV, d.vpages, pool_rows, d.head_dim))
-    return cudaErrorInvalidValue;
-  a.d = d;
-  a.c = c;
-  std::memcpy(a.run, p.run, (p.ctas + 1) * sizeof(RunStart));
-  a.part = static_cast<float*>(workspace);
-  a.part_ml = a.part + part_floats(p, d.head_dim, false);
-  a.part_rows = p.part_rows;
-  a.total = a.part_ml + part_floats(p, d.head_dim, true);
-  bool lean = true;
-  for (int i = 0; i < c.n; ++i) lean = lean && static_cast<int64_t>(rows_of(c, i)) * (d.n_q_heads / d.n_kv_heads) <= kLeanRows;
-  if (d.head_dim == 128) return lean ? launch_tc<128, true>(a, p, num_sms, stream) : launch_tc<128, false>(a, p, num_sms, stream);
-  return lean ? launch_tc<64, true>(a, p, num_sms, stream) : launch_tc<64, false>(a, p, num_sms, stream);
+  return launch_rows<kPlain>(d, c, p, workspace, num_sms, stream);
 }
 
 }  // namespace crf

@@ -34,15 +34,16 @@ constexpr uint32_t kTmemCols = 512;  // S0 | S1 | O0 | O1, 128 each
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// WIDER: the form of calls whose rows see more than one range of keys (sinks), and of calls whose requests share a
-// prefix; its table's entries are requests, or groups of them over the keys that they share.
-template <bool WIDER>
-using TableOf = std::conditional_t<WIDER, AttnTable, ChunkTable>;
-template <bool WIDER>
+// The forms of the kernel: rows that see one range of keys; two (sinks); requests that share a prefix, whose table's entries are requests
+// or groups of them.
+enum Form : int { kPlain, kSinks, kPrefix };
+template <int FORM>
+using TableOf = std::conditional_t<FORM == kPlain, ChunkTable, std::conditional_t<FORM == kSinks, SinksTable, AttnTable>>;
+template <int FORM>
 struct ChunkArgs {
   CUtensorMap tmK, tmV;  // pages of the layer, box: one page of one kv head
   ChunkAttnDesc d;
-  TableOf<WIDER> c;
+  TableOf<FORM> c;
   RunStart run[kMaxCtas + 1];
   // parts of cut items: o [slot][32-column block][row][32] with the 16-byte units of a row swizzled by it, and
   // [slot][row] maximum (log2 units) and sum. A CTA's first segment has slot 2 b, a later one 2 b + 1.
@@ -61,7 +62,7 @@ struct PrefixArgs {
   int* last;               // [item] row of its last part
 };
 template <>
-struct ChunkArgs<true> {
+struct ChunkArgs<kPrefix> {
   CUtensorMap tmK, tmV;
   ChunkAttnDesc d;
   AttnTable c;
@@ -95,16 +96,58 @@ __host__ __device__ inline KeyRange keys_of_rows(int first_pos, int last_pos, in
   k.hi = causal && last_pos + 1 < n_keys ? last_pos + 1 : n_keys;
   return k;
 }
-__host__ __device__ inline KeyRange keys_of_rows(const ChunkTable& c, int i, int first_pos, int last_pos, bool causal, int window) {
-  return keys_of_rows(first_pos, last_pos, c.n_keys[i], causal, window);
+// The same of rows ra .. rb of entry i of a table; every_key: the keys that every one of them sees.
+__host__ __device__ inline KeyRange some_keys(const ChunkTable& c, int i, int ra, int rb, bool causal, int window) {
+  return keys_of_rows(c.pos[i] + ra, c.pos[i] + rb, c.n_keys[i], causal, window);
 }
-__host__ __device__ inline KeyRange keys_of_rows(const AttnTable& c, int i, int first_pos, int last_pos, bool causal, int window) {
-  KeyRange k = keys_of_rows(first_pos, last_pos, c.n_keys[i], causal, window);
+__host__ __device__ inline KeyRange every_key(const ChunkTable& c, int i, int ra, int rb, bool causal, int window) {
+  return keys_of_rows(c.pos[i] + rb, c.pos[i] + ra, c.n_keys[i], causal, window);
+}
+constexpr int kNowhere = 1 << 30;  // behind every key
+// Member of a folded entry that has row r.
+__host__ __device__ inline int member_of(const int* first, int m0, int members, int r) {
+  int lo = m0, hi = m0 + members - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (first[mid] <= r) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+// First key behind the tiles of a folded entry's shared keys.
+__host__ __device__ inline int own_key0(const AttnTable& c, int i) { return (c.sinks[i] + kN - 1) / kN * kN; }
+// Cached keys of member m that row r of entry i sees, and where key 0 of its table would lie among the entry's.
+__host__ __device__ inline int member_keys(const AttnTable& c, int i, int m, int r, bool causal) {
+  const int p = c.m_pos[m] + (r - c.m_row0[m]);
+  return causal && p + 1 < c.m_keys[m] ? p + 1 : c.m_keys[m];
+}
+__host__ __device__ inline int member_base(const AttnTable& c, int i, int m) { return own_key0(c, i) + (c.m_page0[m] - c.m_first[m]) * kPage; }
+__host__ __device__ inline KeyRange folded_row(const AttnTable& c, int i, int r, bool causal) {
+  const int m = member_of(c.m_row0, c.member0[i], c.members[i], r), base = member_base(c, i, m);
+  return KeyRange{base + c.sinks[i], base + member_keys(c, i, m, r, causal)};
+}
+__host__ __device__ inline KeyRange some_keys(const AttnTable& c, int i, int ra, int rb, bool causal, int window) {
+  if (c.members[i]) {
+    // whole pages: from the first member's on, up to the last that the last row needs
+    const int a = member_of(c.m_row0, c.member0[i], c.members[i], ra), b = member_of(c.m_row0, c.member0[i], c.members[i], rb);
+    const int keys = member_keys(c, i, b, rb, causal), pages = keys > c.sinks[i] ? (keys + kPage - 1) / kPage - c.m_first[b] : 0;
+    return KeyRange{own_key0(c, i) + c.m_page0[a] * kPage, own_key0(c, i) + (c.m_page0[b] + pages) * kPage};
+  }
+  KeyRange k = keys_of_rows(c.pos[i] + ra, c.pos[i] + rb, c.n_keys[i], causal, window);
+  if (k.lo < c.key0[i]) k.lo = c.key0[i];
+  return k;
+}
+// (of a folded entry the shared keys alone, which its `sinks` are: nothing behind them)
+__host__ __device__ inline KeyRange every_key(const AttnTable& c, int i, int ra, int rb, bool causal, int window) {
+  if (c.members[i]) return KeyRange{kNowhere, kNowhere};
+  KeyRange k = keys_of_rows(c.pos[i] + rb, c.pos[i] + ra, c.n_keys[i], causal, window);
   if (k.lo < c.key0[i]) k.lo = c.key0[i];
   return k;
 }
 __host__ __device__ inline int rows_of(const ChunkTable& c, int i) { return c.row0[i + 1] - c.row0[i]; }
 __host__ __device__ inline int rows_of(const AttnTable& c, int i) { return c.rows[i]; }
+// First keys that every row of entry i sees.
+__host__ __device__ inline int sinks_of(const SinksTable& c, int) { return c.sinks; }
+__host__ __device__ inline int sinks_of(const AttnTable& c, int i) { return c.sinks[i]; }
 // K/V tiles [first, first + count) of packed rows q0 .. q1 of a request, and the steps that they make.
 struct TileSpan {
   int first, count, steps;
@@ -134,13 +177,27 @@ __host__ __device__ inline SinkSpan tiles_with_sinks(const KeyRange& all, int la
   s.steps = narrow ? (s.count + 1) / 2 : s.count;
   return s;
 }
+// Steps of an item of entry i before those over a folded group's own keys.
+inline int shared_steps(const ChunkTable&, int, bool, int steps) { return steps; }
+inline int shared_steps(const AttnTable& c, int i, bool narrow, int steps) {
+  if (c.members[i] == 0) return steps;
+  const int tiles = (c.sinks[i] + kN - 1) / kN;
+  return std::min(steps, narrow ? tiles / 2 : tiles);
+}
 // Steps of packed rows q0 .. q1 of entry i.
 inline int steps_of(const ChunkTable& c, int i, int q0, int q1, int grp, bool causal, int window, bool narrow) {
   return tiles_of(keys_of_rows(c.pos[i] + q0 / grp, c.pos[i] + q1 / grp, c.n_keys[i], causal, window), narrow).steps;
 }
+template <typename Table>
+inline int steps_with_sinks(const Table& c, int i, int q0, int q1, int grp, bool causal, int window, bool narrow) {
+  const int r0 = q0 / grp, r1 = q1 / grp;
+  return tiles_with_sinks(some_keys(c, i, r0, r1, causal, window), every_key(c, i, r1, r1, causal, window).lo, sinks_of(c, i), narrow).steps;
+}
+inline int steps_of(const SinksTable& c, int i, int q0, int q1, int grp, bool causal, int window, bool narrow) {
+  return steps_with_sinks(c, i, q0, q1, grp, causal, window, narrow);
+}
 inline int steps_of(const AttnTable& c, int i, int q0, int q1, int grp, bool causal, int window, bool narrow) {
-  const int p0 = c.pos[i] + q0 / grp, p1 = c.pos[i] + q1 / grp;
-  return tiles_with_sinks(keys_of_rows(c, i, p0, p1, causal, window), keys_of_rows(c, i, p1, p1, causal, window).lo, c.sinks, narrow).steps;
+  return steps_with_sinks(c, i, q0, q1, grp, causal, window, narrow);
 }
 
 __device__ __forceinline__ void regs_dec_ctl() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsCtl)); }
@@ -252,6 +309,14 @@ __device__ __forceinline__ void softmax_tile(uint32_t tS, uint32_t tO, bool firs
   l_run += (r0 + r1) + (r2 + r3);
 }
 
+// P of a tile that no row of the warp sees a key of: zeros.
+__device__ __forceinline__ void no_weights(uint32_t tS) {
+  const uint32_t zero[16] = {};
+#pragma unroll
+  for (int c = 0; c < 4; ++c) tmem_st16(tS + 16 * c, zero);
+  tmem_st_wait();
+}
+
 // The totals of a thread's row: o's columns, the sum of weights and the maximum that they were formed under, element i at
 // total[i kM]. They are added to between two loops over tiles: a test in the one loop, with the maximum and the sum in
 // registers, cost every call 2-6%.
@@ -354,6 +419,49 @@ __device__ __forceinline__ void clean_v(uint8_t* slot, int a0, int a1, int b0, i
   }
 }
 
+// The same for the form in which whole tiles are cleaned (a folded group's own keys): all keys of the tile, a thread the same
+// 16-byte unit of every eighth key, so that its places are a constant stride apart, eight loads in flight, no branch between them; one
+// test for the two elements of a word, an exponent of ones plus one carrying into the sign's place. What no copy has
+// brought, behind the fetched pages' keys [k0, k1), is read as well and decides nothing.
+template <int D>
+__device__ __forceinline__ void clean_tile(uint8_t* slot, int k0, int k1, int lo, int hi, int thread, int threads, volatile int* dirty) {
+  constexpr int kUnits = D / 8, kAhead = 8;
+  const int unit = thread % kUnits;
+  if (k0 < lo || hi < k1) {
+    for (int key = k0 + thread / kUnits; key < k1; key += threads / kUnits)
+      if (key < lo || key >= hi) *slot_unit<D>(slot, key, unit) = make_uint4(0, 0, 0, 0);
+  }
+  for (int r = thread / kUnits; r < 8; r += threads / kUnits) {
+    uint8_t* const at = reinterpret_cast<uint8_t*>(slot_unit<D>(slot, r, unit));
+#pragma unroll
+    for (int g = 0; g < kN / 8; g += kAhead) {
+      uint4 v[kAhead];
+      uint32_t bad = 0;
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) v[k] = *reinterpret_cast<const uint4*>(at + (g + k) * Tile<D, false>::GROUP_BYTES);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        bad |= ((v[k].x & 0x7F807F80u) + 0x00800080u) | ((v[k].y & 0x7F807F80u) + 0x00800080u) |
+               ((v[k].z & 0x7F807F80u) + 0x00800080u) | ((v[k].w & 0x7F807F80u) + 0x00800080u);
+      if ((bad & 0x80008000u) == 0) continue;
+#pragma unroll 1
+      for (int k = 0; k < kAhead; ++k) {
+        const int key = (g + k) * 8 + r;
+        if (key < lo || key >= hi) continue;
+        uint32_t* e = reinterpret_cast<uint32_t*>(at + (g + k) * Tile<D, false>::GROUP_BYTES);
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t out = (not_finite_bf16(e[q]) ? 0x0000FFFFu : 0u) | (not_finite_bf16(e[q] >> 16) ? 0xFFFF0000u : 0u);
+          if (out) {
+            e[q] &= ~out;
+            *dirty = 1;
+          }
+        }
+      }
+    }
+  }
+}
+
 // A segment: the item's rows, and the keys that the CTA reads.
 struct Segment {
   int g, q0, rows;      // kv head; the item's first packed row; packed rows of the request
@@ -368,21 +476,23 @@ struct Segment {
   int n0, n1;           // steps of the chains
   int quarters0, quarters1;  // warps of a chain with rows
 };
-template <bool WIDER>
-struct SegmentOf : Segment {};
-template <>
-struct SegmentOf<true> : Segment {
+struct SegmentWider : Segment {
   int sinks, win_lo, ns, gap;  // as in SinkSpan; jb counts the numbered tiles
   int part_row, item_rows;     // prefix: the part's place
+  int entry;
 };
+template <int FORM>
+struct SegmentOf : SegmentWider {};
+template <>
+struct SegmentOf<kPlain> : Segment {};
 
-template <bool WIDER>
+template <int FORM>
 struct Shared {
   uint64_t q_full, o_full, drain;
   uint64_t kv_full[kMaxSlots], kv_empty[kMaxSlots];
   uint64_t s_full[2], p_full[2];
   uint64_t seg_full[kSegRing], seg_empty[kSegRing];
-  SegmentOf<WIDER> seg[kSegRing];
+  SegmentOf<FORM> seg[kSegRing];
   float2 ml[kM];       // narrow: chain 1's maxima and sums
   uint64_t tmem_free;  // the softmax warps are done with TMEM
   uint32_t landed;     // items of the ring that have landed, in order, over all segments
@@ -392,12 +502,12 @@ struct Shared {
 };
 
 // Walks a run's segments.
-template <bool WIDER>
+template <int FORM>
 struct Walk {
   RunStart at;
   bool first = true;
   int part_row;  // prefix: of the next segment
-  __host__ __device__ __forceinline__ void next(const ChunkArgs<WIDER>& a, int cta, SegmentOf<WIDER>& w) {
+  __host__ __device__ __forceinline__ void next(const ChunkArgs<FORM>& a, int cta, SegmentOf<FORM>& w) {
     const RunStart& to = a.run[cta + 1];
     w.end = at.req > to.req || (at.req == to.req && (at.qt < to.qt || (at.qt == to.qt && (at.g > to.g || (at.g == to.g && at.step >= to.step)))));
     if (w.end) return;
@@ -420,12 +530,19 @@ struct Walk {
     for (int t = 0; t < 2; ++t) {
       const int r0 = q0 + (narrow ? 0 : t * kM), r1 = min(r0 + kM, rows) - 1;
       valid[t] = max(0, r1 - r0 + 1);
-      const int p0 = w.pos + r0 / grp, p1 = w.pos + r1 / grp;
-      some[t] = keys_of_rows(a.c, i, p0, p1, a.d.causal, a.d.window);
-      full[t] = keys_of_rows(a.c, i, p1, p0, a.d.causal, a.d.window);
+      some[t] = some_keys(a.c, i, r0 / grp, r1 / grp, a.d.causal, a.d.window);
+      full[t] = every_key(a.c, i, r0 / grp, r1 / grp, a.d.causal, a.d.window);
       if (valid[t] == 0) some[t].hi = 0;
     }
     KeyRange all = {some[0].lo, max(some[0].hi, some[1].hi)};
+    // A chain gives back the tiles that it does not go through at the segment's end, so they may be two at most (five slots hold
+    // two tiles and a half): they are where keys end with the row or begin behind sinks. Of a folded entry, whose rows see
+    // runs of keys far apart, both chains go through every tile.
+    if constexpr (FORM == kPrefix)
+      if (a.c.members[i]) {
+        if (valid[0]) some[0].hi = all.hi;
+        if (valid[1]) some[1].hi = all.hi;
+      }
     w.all_lo = all.lo;
     w.all_hi = all.hi;
     w.full0 = full[0];
@@ -433,9 +550,10 @@ struct Walk {
     const bool last = to.req == i && to.qt == at.qt && to.g == at.g;  // the run ends within the item
     const int per = narrow ? 2 : 1;
     int steps, s1;
-    if constexpr (WIDER) {
-      const SinkSpan s = tiles_with_sinks(all, (valid[1] > 0 && !narrow ? full[1] : full[0]).lo, a.c.sinks, narrow);
-      if (a.c.sinks > 0 && s.sinks == 0) w.full0.lo = w.full1.lo = w.all_lo = 0;  // one range from 0 on
+    if constexpr (FORM != kPlain) {
+      const SinkSpan s = tiles_with_sinks(all, (valid[1] > 0 && !narrow ? full[1] : full[0]).lo, sinks_of(a.c, i), narrow);
+      if (sinks_of(a.c, i) > 0 && s.sinks == 0) w.full0.lo = w.full1.lo = w.all_lo = 0;  // one range from 0 on
+      w.entry = i;
       steps = s.steps;
       s1 = last ? min(to.step, steps) : steps;
       w.sinks = s.sinks;
@@ -450,12 +568,13 @@ struct Walk {
       w.n1 = narrow ? w.J / 2 : min(w.J, max(0, tiles_to(some[1].hi) - w.jb));
       w.item_rows = min(tile, rows - q0);
       w.part_row = part_row;
-      if (a.prefix.on) {
-        const int item = a.prefix.item0[i] + ((rows + tile - 1) / tile - 1 - at.qt) * a.d.n_kv_heads + at.g;
-        if (at.step == 0) a.prefix.first[item] = part_row;
-        if (s1 == steps) a.prefix.last[item] = part_row;
-        part_row += w.item_rows;
-      }
+      if constexpr (FORM == kPrefix)
+        if (a.prefix.on) {
+          const int item = a.prefix.item0[i] + ((rows + tile - 1) / tile - 1 - at.qt) * a.d.n_kv_heads + at.g;
+          if (at.step == 0) a.prefix.first[item] = part_row;
+          if (s1 == steps) a.prefix.last[item] = part_row;
+          part_row += w.item_rows;
+        }
     } else {
       const TileSpan s = tiles_of(all, narrow);
       steps = s.steps;
@@ -468,7 +587,7 @@ struct Walk {
     w.quarters0 = (valid[0] + 31) / 32;
     w.quarters1 = (valid[1] + 31) / 32;
     w.slot = at.step == 0 && s1 == steps ? -1 : 2 * cta + (first ? 0 : 1);
-    if constexpr (WIDER)
+    if constexpr (FORM == kPrefix)
       if (a.prefix.on) w.slot = 0;
     first = false;
     // the next item
@@ -497,7 +616,7 @@ __device__ __forceinline__ int item_v(bool narrow, int j, int J) {
 // K/V tile of a chain's step.
 __device__ __forceinline__ int tile_of(bool narrow, int t, int s) { return narrow ? 2 * s + t : s; }
 // Pages [first, last) of tile j that some row sees.
-template <bool WIDER>
+template <int FORM>
 struct PageSpan {
   int lo, hi;  // of the segment, from its first tile's first page on
   __host__ __device__ __forceinline__ explicit PageSpan(const Segment& w)
@@ -505,10 +624,9 @@ struct PageSpan {
   __host__ __device__ __forceinline__ int first(int j) const { return max(0, lo - j * kPagesPerTile); }
   __host__ __device__ __forceinline__ int last(int j) const { return min(kPagesPerTile, hi - j * kPagesPerTile); }
 };
-template <>
-struct PageSpan<true> {
-  const SegmentOf<true>& w;
-  __host__ __device__ __forceinline__ explicit PageSpan(const SegmentOf<true>& s) : w(s) {}
+struct PageSpanWider {
+  const SegmentWider& w;
+  __host__ __device__ __forceinline__ explicit PageSpanWider(const SegmentWider& s) : w(s) {}
   __host__ __device__ __forceinline__ int first(int j) const {
     const int c = w.jb + j;
     return c < w.ns ? 0 : max(0, w.win_lo / kPage - (c + w.gap) * kPagesPerTile);
@@ -518,13 +636,44 @@ struct PageSpan<true> {
     return min(kPagesPerTile, (hi + kPage - 1) / kPage - (c < w.ns ? c : c + w.gap) * kPagesPerTile);
   }
 };
+template <>
+struct PageSpan<kSinks> : PageSpanWider {
+  using PageSpanWider::PageSpanWider;
+};
+template <>
+struct PageSpan<kPrefix> : PageSpanWider {
+  using PageSpanWider::PageSpanWider;
+};
 // The cache's tile that a segment's tile j is, and what of a range of keys its rows see there.
-__host__ __device__ __forceinline__ int cache_tile(const SegmentOf<false>& w, int j) { return w.jb + j; }
-__host__ __device__ __forceinline__ int cache_tile(const SegmentOf<true>& w, int j) { return w.jb + j + (w.jb + j < w.ns ? 0 : w.gap); }
-__host__ __device__ __forceinline__ KeyRange range_in(const SegmentOf<false>&, int, const KeyRange& k) { return k; }
-__host__ __device__ __forceinline__ KeyRange range_in(const SegmentOf<true>& w, int j, const KeyRange& k) {
+__host__ __device__ __forceinline__ int cache_tile(const SegmentOf<kPlain>& w, int j) { return w.jb + j; }
+__host__ __device__ __forceinline__ int cache_tile(const SegmentWider& w, int j) { return w.jb + j + (w.jb + j < w.ns ? 0 : w.gap); }
+__host__ __device__ __forceinline__ KeyRange range_in(const SegmentOf<kPlain>&, int, const KeyRange& k) { return k; }
+__host__ __device__ __forceinline__ KeyRange range_in(const SegmentWider& w, int j, const KeyRange& k) {
   if (w.jb + j < w.ns) return KeyRange{0, min(w.sinks, k.hi)};
   return KeyRange{max(k.lo, w.sinks), k.hi};
+}
+// Keys that a row of the segment's request sees; of two ranges, the sinks' lies before it.
+__device__ __forceinline__ KeyRange row_keys(const ChunkTable&, const SegmentOf<kPlain>& w, int row, bool causal, int window) {
+  return keys_of_rows(w.pos + row, w.pos + row, w.n_keys, causal, window);
+}
+__host__ __device__ __forceinline__ KeyRange row_keys(const SinksTable& c, const SegmentWider& w, int row, bool causal, int window) {
+  KeyRange k = keys_of_rows(w.pos + row, w.pos + row, w.n_keys, causal, window);
+  if (c.sinks > 0 && w.sinks == 0) k.lo = 0;
+  return k;
+}
+__host__ __device__ __forceinline__ KeyRange row_keys(const AttnTable& c, const SegmentWider& w, int row, bool causal, int window) {
+  if (c.members[w.entry]) return folded_row(c, w.entry, row, causal);
+  KeyRange k = keys_of_rows(w.pos + row, w.pos + row, w.n_keys, causal, window);
+  if (k.lo < w.all_lo) k.lo = w.all_lo;  // a request's own keys begin behind the shared ones
+  return k;
+}
+// Page p of a segment's tile j, of the pool or not.
+// `member`: that the page of a folded entry is of, the last whose pages begin at or before it.
+__host__ __device__ __forceinline__ int page_of(const AttnTable& c, const SegmentWider& w, int j, int p, int member) {
+  const int page = cache_tile(w, j) * kPagesPerTile + p;
+  if (c.members[w.entry] == 0 || w.jb + j < w.ns) return w.pt[page];
+  const int m = c.member0[w.entry] + member;
+  return c.m_pt[m][c.m_first[m] + page - w.ns * kPagesPerTile - c.m_page0[m]];
 }
 // Wait until `items` items of the ring have landed: the count is monotonic, so no phase is mistaken for another. The
 // outcome is uniform over the warp.
@@ -536,8 +685,8 @@ __device__ __forceinline__ uint32_t ld_acquire_shared(const uint32_t* p) {
 __device__ __forceinline__ void st_release_shared(uint32_t* p, uint32_t v) {
   asm volatile("st.release.cta.shared::cta.u32 [%0], %1;" ::"r"(smem_u32(p)), "r"(v) : "memory");
 }
-template <bool WIDER>
-__device__ __forceinline__ bool wait_landed(Shared<WIDER>& sh, int items, int* status) {
+template <int FORM>
+__device__ __forceinline__ bool wait_landed(Shared<FORM>& sh, int items, int* status) {
   unsigned long long t0 = 0;
   for (uint32_t it = 1;; ++it) {
     if (__all_sync(0xffffffffu, static_cast<int>(ld_acquire_shared(&sh.landed) - static_cast<uint32_t>(items)) >= 0)) return true;
@@ -564,13 +713,13 @@ __device__ __forceinline__ int slot_after(int slot, int n) {
 // 16-byte unit u of row r's 128 bytes (32 columns of fp32, or of bf16 in the first four) in the stage.
 __device__ __forceinline__ int row_unit(int r, int u) { return u ^ (r & 7); }
 
-template <int D, bool LEAN, bool WIDER>
-__global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_constant__ ChunkArgs<WIDER> a) {
+template <int D, bool LEAN, int FORM>
+__global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_constant__ ChunkArgs<FORM> a) {
   using T = Tile<D, LEAN>;
   constexpr int kSlots = T::kSlots;
   constexpr int Q_BYTES = T::Q_BYTES, KV_BYTES = T::KV_BYTES, GROUP_BYTES = T::GROUP_BYTES;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) Shared<WIDER> sh;
+  __shared__ __align__(8) Shared<FORM> sh;
   griddep_launch_dependents();
   uint8_t* stage = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* sKV = stage + T::STAGE_BYTES;
@@ -602,15 +751,15 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
     sh.dirty = 0;
     fence_barrier_init();
   }
-  Walk<WIDER> walk;
+  Walk<FORM> walk;
   if (threadIdx.x == 64) {
     // the first segment, while the others set up
     walk.at = a.run[blockIdx.x];
-    if constexpr (WIDER) {
+    if constexpr (FORM == kPrefix) {
       walk.part_row = a.prefix.row0[blockIdx.x];
       if (a.prefix.on) griddep_wait();  // it writes to the workspace
     }
-    SegmentOf<WIDER> w;
+    SegmentOf<FORM> w;
     walk.next(a, blockIdx.x, w);
     sh.seg[0] = w;
   }
@@ -634,15 +783,35 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       for (int n = 0; ok; ++n) {
         ok = mbar_wait_warp(&sh.seg_full[n % kSegRing], (n / kSegRing) & 1, &sh.abort_flag, d.status);
         if (!ok) break;
-        const SegmentOf<WIDER>& w = sh.seg[n % kSegRing];
+        const SegmentOf<FORM>& w = sh.seg[n % kSegRing];
         if (w.end) break;
-        const PageSpan<WIDER> pages(w);
+        const PageSpan<FORM> pages(w);
         const int J = w.J, group = w.narrow ? 2 : 1;  // tiles whose K come before their V
+        // a folded group: where its members' pages begin, 32 members a register, so that eight pages' members are found by votes
+        int begins[FORM == kPrefix ? kMaxChunks / 32 : 1];
+        if constexpr (FORM == kPrefix) {
+#pragma unroll
+          for (int r = 0; r < kMaxChunks / 32; ++r)
+            begins[r] = r * 32 + lane < a.c.members[w.entry] ? a.c.m_page0[a.c.member0[w.entry] + r * 32 + lane] : kNowhere;
+        }
         auto page_id = [&](int j) {
           const int p = lane & (kPagesPerTile - 1);
-          int id = 0;
+          int id = 0, member = 0;
+          if constexpr (FORM == kPrefix) {
+            if (a.c.members[w.entry] && w.jb + j >= w.ns) {
+              const int v0 = (cache_tile(w, j) - w.ns) * kPagesPerTile;
+#pragma unroll 1
+              for (int q = 0; q < kPagesPerTile; ++q) {
+                int n = -1;
+#pragma unroll
+                for (int r = 0; r < kMaxChunks / 32; ++r) n += __popc(__ballot_sync(0xffffffffu, begins[r] <= v0 + q));
+                if (q == p) member = n;
+              }
+            }
+          }
           if (p >= pages.first(j) && p < pages.last(j)) {
-            id = w.pt[cache_tile(w, j) * kPagesPerTile + p];
+            if constexpr (FORM == kPrefix) id = page_of(a.c, w, j, p, member);
+            else id = w.pt[cache_tile(w, j) * kPagesPerTile + p];
             if (id < 0 || id >= a.c.num_pages) {
               if (d.status) atomicOr(d.status, kStatusBounds);
               id = 0;
@@ -706,10 +875,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       for (int n = 0; ok; ++n) {
         ok = mbar_wait_warp(&sh.seg_full[n % kSegRing], (n / kSegRing) & 1, &sh.abort_flag, d.status);
         if (!ok) break;
-        const SegmentOf<WIDER>& w = sh.seg[n % kSegRing];
+        const SegmentOf<FORM>& w = sh.seg[n % kSegRing];
         if (w.end) break;
         const bool narrow = w.narrow;
-        const PageSpan<WIDER> pages(w);
+        const PageSpan<FORM> pages(w);
         const int J = w.J, n0 = w.n0, n1 = w.n1;
         auto issue_s = [&](int t, int slot) {
           const uint64_t q = qd + static_cast<uint32_t>((narrow ? 0 : t) * (Q_BYTES >> 4));
@@ -794,7 +963,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       mbar_arrive(&sh.seg_full[0]);
       for (int n = 1;; ++n) {
         if (!mbar_wait(&sh.seg_empty[n % kSegRing], ((n / kSegRing) & 1) ^ 1, &sh.abort_flag, d.status)) break;
-        SegmentOf<WIDER> w;
+        SegmentOf<FORM> w;
         walk.next(a, blockIdx.x, w);
         sh.seg[n % kSegRing] = w;
         mbar_arrive(&sh.seg_full[n % kSegRing]);
@@ -810,7 +979,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       for (int n = 0; ok; ++n) {
         ok = mbar_wait_warp(&sh.seg_full[n % kSegRing], (n / kSegRing) & 1, &sh.abort_flag, d.status);
         if (!ok) break;
-        const SegmentOf<WIDER>& w = sh.seg[n % kSegRing];
+        const SegmentOf<FORM>& w = sh.seg[n % kSegRing];
         if (w.end) break;
         const int items = 2 * w.J;
         for (int i = 0; i < items; ++i) {
@@ -847,10 +1016,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sh.seg_full[n % kSegRing], (n / kSegRing) & 1, &sh.abort_flag, d.status));
       ok = softmax_groups_and(ok);
       if (!ok) break;
-      const SegmentOf<WIDER>& w = sh.seg[n % kSegRing];
+      const SegmentOf<FORM>& w = sh.seg[n % kSegRing];
       if (w.end) break;
       const bool narrow = w.narrow;
-      const PageSpan<WIDER> pages(w);
+      const PageSpan<FORM> pages(w);
       const int J = w.J, n0 = w.n0, n1 = w.n1, last_row = w.rows - 1, row0 = w.row0;
       const int steps = t ? n1 : n0, quarters = t ? w.quarters1 : w.quarters0;
       if (J > 0) {
@@ -892,11 +1061,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
       }
       const int R = w.q0 + (narrow ? 0 : t * kM) + r;  // packed row
       const int row = min(R, last_row) / grp;
-      KeyRange mine = keys_of_rows(w.pos + row, w.pos + row, w.n_keys, d.causal, d.window);
-      if constexpr (WIDER) {
-        if (mine.lo < w.all_lo) mine.lo = w.all_lo;  // a member's keys begin behind the shared ones
-        if (a.c.sinks > 0 && w.sinks == 0) mine.lo = 0;
-      }
+      const KeyRange mine = row_keys(a.c, w, row, d.causal, d.window);
       float m_run = -INFINITY, l_run = 0.f;  // maximum in raw score units
       auto totals = [&]() { return a.total + static_cast<size_t>(2 * blockIdx.x + t) * (kTotals<D> * kM) + r; };
       const KeyRange full = t ? w.full1 : w.full0;  // keys that all rows of the chain see, and of the CTA
@@ -941,8 +1106,13 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
             bool here = static_cast<int>(ld_acquire_shared(&sh.landed) - static_cast<uint32_t>(need)) >= 0;
             __syncwarp();
             const KeyRange f = range_in(w, j, full), m = range_in(w, j, mine);
-            if (k0 < f.lo || k0 + kN > f.hi) mask_tile(tS, m.lo - k0, m.hi - k0);
-            softmax_tile<D>(tS, tO, s == s0, sl2, m_run, l_run);
+            bool some = true;  // of the warp's rows see some key of the tile
+            if (k0 < f.lo || k0 + kN > f.hi) {
+              if constexpr (FORM == kPrefix) some = __any_sync(0xffffffffu, max(m.lo, k0) < min(m.hi, k0 + kN));
+              if (some) mask_tile(tS, m.lo - k0, m.hi - k0);
+            }
+            if (some) softmax_tile<D>(tS, tO, s == s0, sl2, m_run, l_run);
+            else no_weights(tS);
             const KeyRange cta = range_in(w, j, KeyRange{cta_lo, cta_hi});
             if (k0 < cta.lo || k0 + kN > cta.hi) {
               ok = wait_landed(sh, vi + 1, d.status);
@@ -951,8 +1121,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
               const int a0 = pages.first(j) * kPage, a1 = min(pages.last(j) * kPage, max(a0, cta.lo - k0));
               const int b1 = pages.last(j) * kPage, b0 = min(b1, max(a1, cta.hi - k0));
               const KeyRange seen = range_in(w, j, KeyRange{w.all_lo, w.all_hi});
-              clean_v<D>(sKV + vs * KV_BYTES, a0, a1, b0, b1, seen.lo - k0, seen.hi - k0, quarter * 32 + lane,
-                         32 * quarters, &sh.dirty);
+              if constexpr (FORM == kPrefix)
+                clean_tile<D>(sKV + vs * KV_BYTES, a0, b1, seen.lo - k0, seen.hi - k0, quarter * 32 + lane, 32 * quarters, &sh.dirty);
+              else
+                clean_v<D>(sKV + vs * KV_BYTES, a0, a1, b0, b1, seen.lo - k0, seen.hi - k0, quarter * 32 + lane,
+                           32 * quarters, &sh.dirty);
               fence_proxy_async_smem();
             }
             if (quarter == 0 && !__all_sync(0xffffffffu, here)) {
@@ -1000,10 +1173,18 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
             tmem_ld_wait();
 #pragma unroll 1
             for (int key = max(k0, m.lo); key < min(k0 + kN, m.hi); ++key) {
-              const int page = w.pt[key / kPage];
+              int at = key;  // in the row's own table
+              const int32_t* pt = w.pt;
+              if constexpr (FORM == kPrefix)
+                if (a.c.members[w.entry] && w.jb + j >= w.ns) {
+                  const int member = member_of(a.c.m_row0, a.c.member0[w.entry], a.c.members[w.entry], row);
+                  at -= member_base(a.c, w.entry, member);
+                  pt = a.c.m_pt[member];
+                }
+              const int page = pt[at / kPage];
               if (page < 0 || page >= a.c.num_pages) continue;
               const __nv_bfloat16* src =
-                  d.vpages + ((static_cast<size_t>(page) * d.n_kv_heads + w.g) * kPage + key % kPage) * D + c * 32;
+                  d.vpages + ((static_cast<size_t>(page) * d.n_kv_heads + w.g) * kPage + at % kPage) * D + c * 32;
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
                 const float e = __bfloat162float(src[i]);
@@ -1070,7 +1251,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
         size_t part_at = static_cast<size_t>(max(w.slot, 0)) * (D / 32) * a.part_rows + item_row;
         size_t ml_at = static_cast<size_t>(max(w.slot, 0)) * a.part_rows + item_row;
         int part_rows = a.part_rows;
-        if constexpr (WIDER) {
+        if constexpr (FORM == kPrefix) {
           if (a.prefix.on) {
             part_rows = w.item_rows;
             ml_at = static_cast<size_t>(w.part_row) + item_row;
@@ -1251,18 +1432,26 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_attn_merge(const __grid_c
 }
 
 // ---------------------------------------------------------------- plan (host)
-// What runs are dealt by, in units of a wide step's time. A narrow step reads two tiles; a segment costs something beside
-// its steps (q, the masks, the end): 8192 rows from nothing took 427 us with 4 units, 369 with 6, 370 with 8, 377 with 10;
+// What runs are dealt by: units of time of a step, of what a segment costs beside its steps (q, the masks, the end), of the merge's
+// launch and run.
+struct Costs {
+  int step_wide, step_narrow, segment_wide, segment_narrow, merge;
+  int masked;  // of a step over a folded group's own keys, more than of another (its masks, the cleaning of v)
+  bool every_run;  // the first budget counts a segment for every CTA: with few long items there are as many, and tries cost 1 us
+  int step(bool narrow) const { return narrow ? step_narrow : step_wide; }
+  int segment(bool narrow) const { return narrow ? segment_narrow : segment_wide; }
+};
+// A narrow step reads two tiles. 8192 rows from nothing took 427 us with 4 units a segment, 369 with 6, 370 with 8, 377 with 10;
 // 64 single rows over 2000 keys 60 us with 2 or 4, 55 with 6.
-constexpr int kSegment = 6;
-inline int step_units(bool narrow) { return narrow ? 2 : 1; }
-// The merge's launch and run.
-constexpr int kMerge = 2;
+constexpr Costs kCosts = {1, 2, 6, 6, 2, 0, false}, kSinksCosts = {1, 2, 6, 6, 2, 0, true};
+// Where long wide items (a group's rows over a prefix) and many narrow ones (its requests' own few keys) share the CTAs, their
+// ratios matter: a wide step takes 1.6 us, a narrow one 1.4; a segment beside them 6.3 us, a narrow one 4.6. In units of 0.4 us.
+constexpr Costs kPrefixCosts = {4, 4, 16, 12, 8, 2, true};
 
 // Deals the items' steps to at most `ctas` runs of at most `budget` units each; false if they do not fit. `whole`:
 // an item a run.
 template <typename Table>
-bool deal(const Table& c, int n_q_heads, int n_kv_heads, bool causal, int window, int ctas, int64_t budget, bool whole,
+bool deal(const Table& c, const Costs& k, int n_q_heads, int n_kv_heads, bool causal, int window, int ctas, int64_t budget, bool whole,
           ChunkPlan* p, int64_t* run_rows) {
   const int grp = n_q_heads / n_kv_heads;
   p->ctas = 0;
@@ -1279,28 +1468,38 @@ bool deal(const Table& c, int n_q_heads, int n_kv_heads, bool causal, int window
     const int rows = rows_of(c, i) * grp;
     if (rows == 0) continue;
     const bool narrow = narrow_form(rows);
-    const int unit = step_units(narrow), tile = narrow ? kM : 2 * kM, tiles = (rows + tile - 1) / tile;
+    const int unit = k.step(narrow), segment = k.segment(narrow), tile = narrow ? kM : 2 * kM, tiles = (rows + tile - 1) / tile;
     for (int qt = tiles - 1; qt >= 0; --qt) {
       const int q0 = qt * tile, q1 = std::min(q0 + tile, rows) - 1;
       const int steps = steps_of(c, i, q0, q1, grp, causal, window, narrow);
+      const int cheap = shared_steps(c, i, narrow, steps);
       for (int g = 0; g < n_kv_heads; ++g) {
         int step = 0, first_cta = -1, first_slot = 0, parts = 0;
         do {
           // a segment of at least one step (or the whole of an empty item) starts only where it fits the budget
-          if (p->ctas == 0 || whole || left < kSegment + std::min(steps - step, 1) * unit) {
+          if (p->ctas == 0 || whole || left < segment + std::min(steps - step, 1) * unit) {
             if (p->ctas == ctas) return false;
             open(i, qt, g, step);
           }
-          left -= kSegment;
+          left -= segment;
           if (run_rows) run_rows[p->ctas - 1] += q1 - q0 + 1;
-          const int take = whole ? steps : static_cast<int>(std::min<int64_t>(steps - step, left / unit));
+          int take = whole ? steps : static_cast<int>(std::min<int64_t>(std::max(cheap - step, 0), left / unit));
+          left -= take * unit;
+          if (!whole && step + take >= cheap) {
+            const int more = static_cast<int>(std::min<int64_t>(steps - step - take, left / (unit + k.masked)));
+            take += more;
+            left -= more * (unit + k.masked);
+          }
+          if (take == 0 && step < steps) {  // a segment of one step at least
+            take = 1;
+            left -= unit;
+          }
           p->longest = std::max(p->longest, take);
           if (parts++ == 0) {
             first_cta = p->ctas - 1;
             first_slot = 2 * first_cta + (here > 0 ? 1 : 0);
           }
           ++here;
-          left -= take * unit;
           step += take;
         } while (step < steps);
         if (parts > 1) {
@@ -1320,51 +1519,54 @@ bool deal(const Table& c, int n_q_heads, int n_kv_heads, bool causal, int window
 
 // `run_rows`: null, or every segment is a part (so nothing is gained by whole items), and receives the rows of each run's.
 template <typename Table>
-void plan_runs(const Table& c, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms, int64_t* run_rows, ChunkPlan* p) {
+void plan_runs(const Table& c, const Costs& k, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms, int64_t* run_rows, ChunkPlan* p) {
   const int grp = n_q_heads / n_kv_heads, ctas = std::min(num_sms, kMaxCtas);
   int64_t total = 0, items = 0;
   int longest = 0, least = 1;  // units of the longest item's steps, of a segment of one step
+  bool all_narrow = true;
   for (int i = 0; i < c.n; ++i) {
     const int rows = rows_of(c, i) * grp;
     if (rows == 0) continue;
     const bool narrow = narrow_form(rows);
-    const int unit = step_units(narrow), tile = narrow ? kM : 2 * kM;
-    least = std::max(least, kSegment + unit);
+    const int unit = k.step(narrow), segment = k.segment(narrow), tile = narrow ? kM : 2 * kM;
+    least = std::max(least, segment + unit);
+    all_narrow = all_narrow && narrow;
     for (int q0 = 0; q0 < rows; q0 += tile) {
       const int q1 = std::min(q0 + tile, rows) - 1;
       const int steps = steps_of(c, i, q0, q1, grp, causal, window, narrow);
-      total += static_cast<int64_t>(n_kv_heads) * (steps * unit + kSegment);
+      total += static_cast<int64_t>(n_kv_heads) * (steps * unit + (steps - shared_steps(c, i, narrow, steps)) * k.masked + segment);
       items += n_kv_heads;
       longest = std::max(longest, steps * unit);
     }
   }
   // An even share at first; runs that end early for want of a whole step, and the segments that they continue, need some
   // more. Few short items stay whole: the merge costs more than the steps that it saves.
+  if (k.every_run) total += std::max<int64_t>(0, ctas - items) * k.segment(all_narrow);
   int64_t budget = std::max<int64_t>(least, (total + ctas - 1) / ctas);
-  const bool whole = !run_rows && items <= ctas && longest <= budget - kSegment + kMerge;
-  if (items > 2 * ctas) budget += kSegment;  // nearly every run continues a segment: fewer tries
+  const bool whole = !run_rows && items <= ctas && longest <= budget - k.segment_wide + k.merge;
+  if (items > 2 * ctas) budget += k.segment_wide;  // nearly every run continues a segment: fewer tries
   for (int tries = 0;; ++tries) {
-    if (deal(c, n_q_heads, n_kv_heads, causal, window, ctas, budget, whole, p, run_rows)) return;
+    if (deal(c, k, n_q_heads, n_kv_heads, causal, window, ctas, budget, whole, p, run_rows)) return;
     budget += tries < 12 ? 1 : budget / 8 + 1;
   }
 }
 
-template <int D, bool LEAN, bool WIDER>
-cudaError_t launch_kernel_tc(const ChunkArgs<WIDER>& a, int ctas, cudaStream_t stream) {
+template <int D, bool LEAN, int FORM>
+cudaError_t launch_kernel_tc(const ChunkArgs<FORM>& a, int ctas, cudaStream_t stream) {
   static PerDevice once;
   int dev = 0;
   if (once.pending(&dev)) {
-    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<D, LEAN, WIDER>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tile<D, LEAN>::kSmem);
+    cudaError_t e = cudaFuncSetAttribute(chunk_attn_kernel<D, LEAN, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, Tile<D, LEAN>::kSmem);
     if (e != cudaSuccess) return e;
     // setmaxnreg.inc waits until the CTA's register pool can serve it: refuse to launch a build whose launch
     // count leaves the split short
     cudaFuncAttributes fa;
-    e = cudaFuncGetAttributes(&fa, chunk_attn_kernel<D, LEAN, WIDER>);
+    e = cudaFuncGetAttributes(&fa, chunk_attn_kernel<D, LEAN, FORM>);
     if (e != cudaSuccess) return e;
     if (fa.numRegs * kThreads < kRegsNeeded) return cudaErrorInvalidConfiguration;
     once.done(dev);
   }
-  return launch_kernel(chunk_attn_kernel<D, LEAN, WIDER>, dim3(ctas), dim3(kThreads), Tile<D, LEAN>::kSmem, stream, a);
+  return launch_kernel(chunk_attn_kernel<D, LEAN, FORM>, dim3(ctas), dim3(kThreads), Tile<D, LEAN>::kSmem, stream, a);
 }
 // The merge of cut items.
 template <int D>
@@ -1394,6 +1596,32 @@ inline size_t part_floats(const ChunkPlan& p, int head_dim, bool ml) {
 }
 inline size_t total_floats(const ChunkPlan& p, int head_dim) {
   return p.longest > kChain ? static_cast<size_t>(2 * p.ctas) * (head_dim + 2) * kM : 0;
+}
+
+// The arguments that the forms without a prefix share, and both launches.
+template <int FORM, typename Table>
+cudaError_t launch_rows(const ChunkAttnDesc& d, const Table& c, const ChunkPlan& p, void* workspace, int num_sms, cudaStream_t stream) {
+  if (p.ctas == 0) return cudaSuccess;
+  ChunkArgs<FORM> a;
+  const long pool_rows = static_cast<long>(c.num_pages) * d.n_kv_heads * kPage;
+  if (!tensor_map_pool(&a.tmK, d.kpages, pool_rows, d.head_dim) || !tensor_map_pool(&a.tmV, d.vpages, pool_rows, d.head_dim))
+    return cudaErrorInvalidValue;
+  a.d = d;
+  a.c = c;
+  std::memcpy(a.run, p.run, (p.ctas + 1) * sizeof(RunStart));
+  a.part = static_cast<float*>(workspace);
+  a.part_ml = a.part + part_floats(p, d.head_dim, false);
+  a.part_rows = p.part_rows;
+  a.total = a.part_ml + part_floats(p, d.head_dim, true);
+  bool lean = true;
+  for (int i = 0; i < c.n; ++i) lean = lean && static_cast<int64_t>(rows_of(c, i)) * (d.n_q_heads / d.n_kv_heads) <= kLeanRows;
+  PdlScope pdl;
+  if (d.head_dim == 128) {
+    const cudaError_t e = lean ? launch_kernel_tc<128, true, FORM>(a, p.ctas, stream) : launch_kernel_tc<128, false, FORM>(a, p.ctas, stream);
+    return e != cudaSuccess ? e : launch_merge<128>(d, p, a.part, a.part_ml, num_sms, stream);
+  }
+  const cudaError_t e = lean ? launch_kernel_tc<64, true, FORM>(a, p.ctas, stream) : launch_kernel_tc<64, false, FORM>(a, p.ctas, stream);
+  return e != cudaSuccess ? e : launch_merge<64>(d, p, a.part, a.part_ml, num_sms, stream);
 }
 
 }  // namespace

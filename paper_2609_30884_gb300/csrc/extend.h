@@ -109,18 +109,32 @@ struct ChunkAttnDesc {
   int window;                  // 0: none
   int* status;
 };
-// The entries of a call whose rows see sinks, or whose requests share prefixes: entry i's rows [row0[i], row0[i] + rows[i]) over the keys
-// from key0[i] on. With prefixes, groups of requests over the keys that they share come first (at positions behind all of them).
+// The requests of a call whose rows see the first `sinks` keys whatever their window.
+struct SinksTable : ChunkTable {
+  int sinks;
+};
+// The entries of a call whose requests share prefixes: entry i's rows [row0[i], row0[i] + rows[i]) over the keys from key0[i] on. A split group's shared keys are an entry (at a position behind
+// all of them), before the entries of requests. A folded group is one entry for all: its sinks are the shared keys, behind which, from the
+// next tile on, the pages of its members' own keys are laid end to end; member m's rows begin m_row0[m] behind the entry's, its pages at
+// m_page0[m], the first of them being page m_first[m] of its table.
 constexpr int kMaxEntries = kMaxChunks + kMaxChunks / 2;
 struct AttnTable {
   int n, num_pages;
-  int sinks;
   int row0[kMaxEntries];
   int rows[kMaxEntries];
   int pos[kMaxEntries];
   int key0[kMaxEntries];
   int n_keys[kMaxEntries];
+  int sinks[kMaxEntries];
+  int member0[kMaxEntries];  // folded: members [member0, member0 + members)
+  int members[kMaxEntries];  // 0: not folded
   const int32_t* pt[kMaxEntries];
+  int m_row0[kMaxChunks];
+  int m_page0[kMaxChunks];
+  int m_first[kMaxChunks];
+  int m_pos[kMaxChunks];
+  int m_keys[kMaxChunks];
+  const int32_t* m_pt[kMaxChunks];
 };
 constexpr int kMaxCtas = 256;
 // Where a CTA's run begins: step `step` of item (request, query tile or pair qt, kv head g); request = c.n: the end.
@@ -147,29 +161,33 @@ size_t chunk_attention_workspace(const ChunkPlan& p, int head_dim);
 cudaError_t launch_chunk_attention(const ChunkAttnDesc& d, const ChunkTable& c, const ChunkPlan& p, void* workspace,
                                    int num_sms, cudaStream_t stream);
 
-// Attention with sinks, and of requests that share prefixes.
+void plan_sinks_attention(const SinksTable& c, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms, ChunkPlan* p);
+cudaError_t launch_sinks_attention(const ChunkAttnDesc& d, const SinksTable& c, const ChunkPlan& p, void* workspace,
+                                   int num_sms, cudaStream_t stream);
+
+// Attention of requests that share prefixes.
 struct AttnPlan {
   ChunkPlan runs;
-  bool shared;                      // the table's first entries are groups; every segment is a part
+  bool shared;                      // the table has split groups; every segment is a part
   int items;
   int64_t part_rows;                // of all parts
   int64_t run_rows[kMaxCtas];
   int item0[kMaxEntries];           // items of the entries before
 };
-// Which requests share: group[i] of request i is an entry of `a`, or -1.
+// The split groups' entries are the table's first; of[i] is that of entry groups + i, or -1.
 struct PrefixGroups {
   int groups;
+  bool any;                  // some group is split or folded
   int16_t of[kMaxChunks];
 };
-void plan_attention(const AttnTable& a, bool shared, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms,
-                    AttnPlan* p);
-// The table of requests in runs of count[i] that share their first keys[i] keys; groups that gain nothing by it are none.
-void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int n, int n_q_heads, int n_kv_heads,
+void plan_prefix_attention(const AttnTable& a, bool shared, int n_q_heads, int n_kv_heads, bool causal, int num_sms, AttnPlan* p);
+// The table of requests in runs of count[i] that share their first keys[i] keys. A group is folded, split, or its requests stand apart,
+// whichever takes the fewest units of work.
+void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int n, int n_q_heads, int n_kv_heads, bool causal,
                     AttnTable* a, PrefixGroups* g);
-size_t attention_workspace(const AttnPlan& p, int head_dim);
-int attention_launches(const AttnPlan& p);
-cudaError_t launch_attention(const ChunkAttnDesc& d, const AttnTable& a, const PrefixGroups* g, const AttnPlan& p,
-                             void* workspace, int num_sms, cudaStream_t stream);
+size_t prefix_attention_workspace(const AttnPlan& p, int head_dim);
+cudaError_t launch_prefix_attention(const ChunkAttnDesc& d, const AttnTable& a, const PrefixGroups& g, const AttnPlan& p,
+                                    void* workspace, int num_sms, cudaStream_t stream);
 
 // ---------------------------------------------------------------- pages
 // Entries [first[i], first[i + 1]) of a call are table i's.

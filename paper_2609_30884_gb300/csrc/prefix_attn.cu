@@ -1,18 +1,16 @@
-// Attention of new rows over cached keys (chunk_attn.cu) in two more forms, both instances of its kernel.
+// Attention of requests that share prefixes, a form of the kernel of chunk_attn.cu.
 //
-// Sinks: row r of a request at position p sees the window p - window < j <= p and, whatever the window, the keys j < sinks. An item's
-// tiles are those of the sinks, then those of its rows' windows; nothing between is read.
-//
-// Shared prefixes: requests whose first n keys are the same (pages_fork makes such tables) are attended in two parts, joined by their
-// maxima and sums:
-//   o = (e^(m1 - m) o1 + e^(m2 - m) o2) / (e^(m1 - m) l1 + e^(m2 - m) l2),  m = max(m1, m2)
-// with (m, l, o) the maximum, the sum of exponentials and their unnormalised product with v. The rows of all requests of a group
-// are packed into one axis for the shared keys, as rows and heads are within a request, so that the keys and values of the prefix
-// are read, and multiplied, once for the group and not once a request. Each request's own keys are items like any other. Every
-// segment writes its part; one merge joins an output row's parts of the group's item and of its request's, in order.
-//
-// Where the rows of each request fill tiles of their own, sharing saves no products: the parts would cost more than they save,
-// and such groups are attended request by request (share_prefixes).
+// The rows of all requests of a group are packed into one axis for the keys that they share, as rows and heads are
+// within a request, so that keys and values of the prefix are read, and multiplied, once for the group and not once a request.
+// Their own keys are attended in one of two ways, whichever takes fewer units of work (share_prefixes):
+//   folded   the pages of the requests' own keys are laid end to end behind the shared tiles; a row sees the shared keys and its
+//            request's run of those behind them, two ranges as with sinks. The products of rows with the others' own keys are wasted; there is
+//            one item a kv head instead of one more for every request, which each cost 4.6 us beside their steps
+//   split    each request's own keys are items like any other, and the two parts of an output row are joined by their maxima and sums:
+//              o = (e^(m1 - m) o1 + e^(m2 - m) o2) / (e^(m1 - m) l1 + e^(m2 - m) l2),  m = max(m1, m2)
+//            with (m, l, o) the maximum, the sum of exponentials and their unnormalised product with v. Every segment then writes its part;
+//            one merge joins an output row's parts of the group's item and of its request's, in order
+// Where the rows of each request fill tiles of their own, sharing saves no products, and the requests are attended one by one.
 #include "chunk_attn.cuh"
 
 namespace crf {
@@ -60,7 +58,7 @@ __global__ void __launch_bounds__(kMergeThreads) chunk_attn_join(const __grid_co
   const int c = threadIdx.x % kLanes, q = threadIdx.x / kLanes % GROUPS, rr = threadIdx.x / (kLanes * GROUPS);
   const int b = min(static_cast<int>(blockIdx.x) * kRows + rr, a.rows - 1);  // a last block's spare rows repeat the last
   const int row = b / d.n_q_heads, h = b - row * d.n_q_heads;
-  int lo = a.g.groups, hi = a.c.n - 1;  // the row's request
+  int lo = a.g.groups, hi = a.c.n - 1;  // the row's request, or its folded group
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (a.c.row0[mid] <= row) lo = mid; else hi = mid - 1;
@@ -152,23 +150,23 @@ Pieces pieces_of(const AttnPlan& p, int head_dim) {
 }
 
 template <int D, bool LEAN>
-cudaError_t launch_wider(const ChunkArgs<true>& a, const PrefixGroups* g, const AttnPlan& p, int num_sms, cudaStream_t stream) {
+cudaError_t launch_prefix(const ChunkArgs<kPrefix>& a, const PrefixGroups& g, const AttnPlan& p, int num_sms, cudaStream_t stream) {
   PdlScope pdl;
-  const cudaError_t e = launch_kernel_tc<D, LEAN, true>(a, p.runs.ctas, stream);
+  const cudaError_t e = launch_kernel_tc<D, LEAN, kPrefix>(a, p.runs.ctas, stream);
   if (e != cudaSuccess) return e;
   if (!p.shared) return launch_merge<D>(a.d, p.runs, a.part, a.part_ml, num_sms, stream);
   JoinArgs j;
   std::memset(&j, 0, sizeof(j));
   j.d = a.d;
   j.c = a.c;
-  j.g = *g;
+  j.g = g;
   std::memcpy(j.item0, p.item0, sizeof(j.item0));
   j.first = a.prefix.first;
   j.last = a.prefix.last;
   j.part = a.part;
   j.part_ml = a.part_ml;
   int rows = 0;
-  for (int i = g->groups; i < a.c.n; ++i) rows += a.c.rows[i];
+  for (int i = g.groups; i < a.c.n; ++i) rows += a.c.rows[i];
   j.rows = rows * a.d.n_q_heads;
   constexpr int kRow = kMergeThreads / (D / 4);  // rows a block with one group each
   if (j.rows < 4 * kRow * num_sms) {
@@ -180,8 +178,7 @@ cudaError_t launch_wider(const ChunkArgs<true>& a, const PrefixGroups* g, const 
 
 }  // namespace
 
-void plan_attention(const AttnTable& a, bool shared, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms,
-                    AttnPlan* p) {
+void plan_prefix_attention(const AttnTable& a, bool shared, int n_q_heads, int n_kv_heads, bool causal, int num_sms, AttnPlan* p) {
   std::memset(p->run_rows, 0, sizeof(p->run_rows));
   p->shared = shared;
   p->items = 0;
@@ -192,67 +189,128 @@ void plan_attention(const AttnTable& a, bool shared, int n_q_heads, int n_kv_hea
     p->item0[i] = p->items;
     p->items += (rows + tile - 1) / tile * n_kv_heads;
   }
-  plan_runs(a, n_q_heads, n_kv_heads, causal, window, num_sms, shared ? p->run_rows : nullptr, &p->runs);
+  plan_runs(a, kPrefixCosts, n_q_heads, n_kv_heads, causal, 0, num_sms, shared ? p->run_rows : nullptr, &p->runs);
   if (shared)
     for (int b = 0; b < p->runs.ctas; ++b) p->part_rows += p->run_rows[b];
 }
 
-void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int n, int n_q_heads, int n_kv_heads,
+void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int n, int n_q_heads, int n_kv_heads, bool causal,
                     AttnTable* a, PrefixGroups* g) {
   std::memset(a, 0, sizeof(*a));
   std::memset(g, 0, sizeof(*g));
   const int grp = n_q_heads / n_kv_heads;
-  // units of one kv head's items of `rows` rows over keys [0, n)
-  auto units = [&](int rows, int n) {
-    const int packed = rows * grp, tile = narrow_form(packed) ? kM : 2 * kM;
-    const int64_t steps = tiles_of(KeyRange{0, n}, narrow_form(packed)).steps;
-    return static_cast<int64_t>((packed + tile - 1) / tile) * steps * step_units(narrow_form(packed));
+  // Units of one kv head's items of rows [r0, r0 + rows) of an entry of `t`.
+  auto units = [&](const AttnTable& t, int i) {
+    const int packed = t.rows[i] * grp;
+    const bool narrow = narrow_form(packed);
+    const int tile = narrow ? kM : 2 * kM;
+    int64_t sum = 0;
+    for (int q0 = 0; q0 < packed; q0 += tile) {
+      const int steps = steps_of(t, i, q0, std::min(q0 + tile, packed) - 1, grp, causal, 0, narrow);
+      sum += kPrefixCosts.segment(narrow) + static_cast<int64_t>(steps) * kPrefixCosts.step(narrow) +
+             static_cast<int64_t>(steps - shared_steps(t, i, narrow, steps)) * kPrefixCosts.masked;
+    }
+    return sum;
   };
+  // Entry i of `t`: request j, over its keys from key0 on.
+  auto put_request = [&](AttnTable* t, int i, int j, int key0) {
+    t->row0[i] = c.row0[j];
+    t->rows[i] = rows_of(c, j);
+    t->pos[i] = c.pos[j];
+    t->key0[i] = key0;
+    t->n_keys[i] = c.n_keys[j];
+    t->sinks[i] = t->member0[i] = t->members[i] = 0;
+    t->pt[i] = c.pt[j];
+  };
+  // The group of requests [r0, r1) over its shared keys alone.
+  auto put_shared = [&](AttnTable* t, int i, int r0, int r1, int n_shared, const int32_t* pt) {
+    t->row0[i] = c.row0[r0];
+    t->rows[i] = c.row0[r1] - c.row0[r0];
+    t->pos[i] = kMaxKeys;  // behind every key
+    t->key0[i] = 0;
+    t->n_keys[i] = n_shared;
+    t->sinks[i] = t->member0[i] = t->members[i] = 0;
+    t->pt[i] = pt;
+  };
+  // The same with its requests' own keys behind them. Members' numbers are those of the requests.
+  auto put_folded = [&](AttnTable* t, int i, int r0, int r1, int n_shared, const int32_t* pt) {
+    put_shared(t, i, r0, r1, n_shared, pt);
+    t->sinks[i] = n_shared;
+    t->member0[i] = r0;
+    t->members[i] = r1 - r0;
+    int page = 0;
+    for (int j = r0; j < r1; ++j) {
+      const int rows = rows_of(c, j);
+      t->m_row0[j] = c.row0[j] - c.row0[r0];
+      t->m_page0[j] = page;
+      t->m_first[j] = n_shared / kPage;
+      t->m_pos[j] = c.pos[j];
+      t->m_keys[j] = c.n_keys[j];
+      t->m_pt[j] = c.pt[j];
+      if (rows == 0) continue;
+      const int seen = causal && c.pos[j] + rows < c.n_keys[j] ? c.pos[j] + rows : c.n_keys[j];
+      if (seen > n_shared) page += (seen + kPage - 1) / kPage - n_shared / kPage;
+    }
+  };
+  static_assert(kMaxChunks <= kMaxEntries, "members are numbered as requests");
   a->num_pages = c.num_pages;
+  enum Way : uint8_t { kApart, kSplit, kFolded } way[kMaxChunks];
+  const int32_t* lead[kMaxChunks];
+  AttnTable t;
+  std::memset(&t, 0, sizeof(t));
   for (int i = 0, r = 0; i < n; r += count[i++]) {
-    const int rows = c.row0[r + count[i]] - c.row0[r], packed = rows * grp, tile = narrow_form(packed) ? kM : 2 * kM;
-    int64_t apart = 0;
-    int first = -1;
+    way[i] = kApart;
+    lead[i] = nullptr;
+    int64_t apart = 0, own = 0, pages = 0;
     for (int j = r; j < r + count[i]; ++j) {
-      g->of[j] = -1;
       if (rows_of(c, j) == 0) continue;
-      if (first < 0) first = j;
-      apart += units(rows_of(c, j), keys[i]);
+      if (!lead[i]) lead[i] = c.pt[j];
+      put_request(&t, 0, j, 0);
+      apart += units(t, 0);
+      put_request(&t, 0, j, keys[i]);
+      own += units(t, 0);
+      pages += std::max(0, c.n_keys[j] - keys[i]) / kPage + 2;
     }
-    // the shared items' own ends have to be earned, beside their steps
-    if (first < 0 || keys[i] == 0 || apart - units(rows, keys[i]) <= kSegment * ((packed + tile - 1) / tile)) continue;
-    const int e = g->groups++;
-    a->row0[e] = c.row0[r];
-    a->rows[e] = rows;
-    a->pos[e] = kMaxKeys;  // behind every key
-    a->n_keys[e] = keys[i];
-    a->pt[e] = c.pt[first];
-    for (int j = r; j < r + count[i]; ++j) g->of[j] = static_cast<int16_t>(e);
+    if (!lead[i] || keys[i] == 0) continue;
+    put_shared(&t, 0, r, r + count[i], keys[i], lead[i]);
+    const int64_t split = own + units(t, 0);
+    int64_t folded = INT64_MAX;
+    if (pages * kPage + keys[i] + kN <= kMaxKeys) {
+      put_folded(&t, 0, r, r + count[i], keys[i], lead[i]);
+      folded = units(t, 0);
+    }
+    if (folded < apart && folded <= split) way[i] = kFolded;
+    else if (split < apart) way[i] = kSplit;
   }
-  a->n = g->groups + c.n;
-  for (int i = 0, r = 0; i < n; r += count[i++])
-    for (int j = r; j < r + count[i]; ++j) {
-      const int e = g->groups + j;
-      a->row0[e] = c.row0[j];
-      a->rows[e] = rows_of(c, j);
-      a->pos[e] = c.pos[j];
-      a->key0[e] = g->of[j] >= 0 ? keys[i] : 0;
-      a->n_keys[e] = c.n_keys[j];
-      a->pt[e] = c.pt[j];
+  for (int i = 0, r = 0; i < n; r += count[i++]) {
+    g->any = g->any || way[i] != kApart;
+    if (way[i] == kSplit) put_shared(a, g->groups++, r, r + count[i], keys[i], lead[i]);
+  }
+  a->n = g->groups;
+  int16_t group = 0;
+  for (int i = 0, r = 0; i < n; r += count[i++]) {
+    if (way[i] == kFolded) {
+      g->of[a->n - g->groups] = -1;
+      put_folded(a, a->n++, r, r + count[i], keys[i], lead[i]);
+      continue;
     }
+    for (int j = r; j < r + count[i]; ++j) {
+      g->of[a->n - g->groups] = way[i] == kSplit ? group : int16_t{-1};
+      put_request(a, a->n++, j, way[i] == kSplit ? keys[i] : 0);
+    }
+    if (way[i] == kSplit) ++group;
+  }
 }
 
-size_t attention_workspace(const AttnPlan& p, int head_dim) {
+size_t prefix_attention_workspace(const AttnPlan& p, int head_dim) {
   const Pieces x = pieces_of(p, head_dim);
   return (x.part + x.ml + x.items + x.total) * sizeof(float);
 }
 
-int attention_launches(const AttnPlan& p) { return p.shared || p.runs.cuts ? 2 : 1; }
-
-cudaError_t launch_attention(const ChunkAttnDesc& d, const AttnTable& c, const PrefixGroups* g, const AttnPlan& p,
-                             void* workspace, int num_sms, cudaStream_t stream) {
+cudaError_t launch_prefix_attention(const ChunkAttnDesc& d, const AttnTable& c, const PrefixGroups& g, const AttnPlan& p,
+                                    void* workspace, int num_sms, cudaStream_t stream) {
   if (p.runs.ctas == 0) return cudaSuccess;
-  ChunkArgs<true> a;
+  ChunkArgs<kPrefix> a;
   std::memset(&a, 0, sizeof(a));
   const long pool_rows = static_cast<long>(c.num_pages) * d.n_kv_heads * kPage;
   if (!tensor_map_pool(&a.tmK, d.kpages, pool_rows, d.head_dim) || !tensor_map_pool(&a.tmV, d.vpages, pool_rows, d.head_dim))
@@ -279,8 +337,8 @@ cudaError_t launch_attention(const ChunkAttnDesc& d, const AttnTable& c, const P
   bool lean = true;
   for (int i = 0; i < c.n; ++i) lean = lean && static_cast<int64_t>(c.rows[i]) * (d.n_q_heads / d.n_kv_heads) <= kLeanRows;
   if (d.head_dim == 128)
-    return lean ? launch_wider<128, true>(a, g, p, num_sms, stream) : launch_wider<128, false>(a, g, p, num_sms, stream);
-  return lean ? launch_wider<64, true>(a, g, p, num_sms, stream) : launch_wider<64, false>(a, g, p, num_sms, stream);
+    return lean ? launch_prefix<128, true>(a, g, p, num_sms, stream) : launch_prefix<128, false>(a, g, p, num_sms, stream);
+  return lean ? launch_prefix<64, true>(a, g, p, num_sms, stream) : launch_prefix<64, false>(a, g, p, num_sms, stream);
 }
 
 }  // namespace crf

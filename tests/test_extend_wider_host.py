@@ -18,88 +18,99 @@ EINVAL, ESHAPE, EUNSUPPORTED, ENOMEM = abi.EINVAL, abi.ESHAPE, abi.EUNSUPPORTED,
 TILE, KEYS = 128, 128
 
 SHIM = r"""
-#include "chunk_attn_wider.cu"
+#include "prefix_attn.cu"
 namespace crf {  // what the launches need and the plan does not
 PdlScope::PdlScope() : prev_(false) {}
 PdlScope::~PdlScope() {}
 bool pdl_active() { return false; }
 }  // namespace crf
 using namespace crf;
-static ChunkArgs<true> args;
+static ChunkArgs<kPrefix> args;
+static ChunkArgs<kSinks> with_sinks;
 static AttnPlan plan;
 static PrefixGroups groups;
-static ChunkTable requests(int n, const int* n_new, const int* pos, const int* n_keys) {
+static bool prefixes;
+// The plan of requests whose page tables are rows of `tables`. info: shared, entries, split groups, items, part rows, cuts, whether any group shares;
+// returns the number of CTAs.
+extern "C" int make(int n, const int* n_new, const int* pos, const int* n_keys, const int* tables, int stride, int n_groups, const int* count,
+                    const int* keys, int hq, int hkv, int causal, int window, int sinks, int sms, int* info, int* firsts, int* lasts) {
   ChunkTable t = {};
   t.n = n;
-  for (int i = 0; i < n; ++i) {
-    t.row0[i + 1] = t.row0[i] + n_new[i];
-    t.pos[i] = pos[i];
-    t.n_keys[i] = n_keys[i];
-    t.pt[i] = reinterpret_cast<const int32_t*>(static_cast<size_t>(16 * (i + 1)));
-  }
+  for (int i = 0; i < n; ++i) t.row0[i + 1] = t.row0[i] + n_new[i], t.pos[i] = pos[i], t.n_keys[i] = n_keys[i], t.pt[i] = tables + i * stride;
   for (int i = n; i < kMaxChunks; ++i) t.row0[i + 1] = t.row0[n];
-  return t;
-}
-// The plan; the number of CTAs. info: shared, entries, groups, items, part rows, cuts.
-extern "C" int make(int n, const int* n_new, const int* pos, const int* n_keys, int n_groups, const int* count, const int* keys,
-                    int hq, int hkv, int causal, int window, int sinks, int sms, int* info, int* of, int* firsts, int* lasts) {
-  ChunkTable t = requests(n, n_new, pos, n_keys);
-  memset(&args, 0, sizeof(args));
-  AttnTable& a = args.c;
-  if (n_groups) {
-    share_prefixes(t, count, keys, n_groups, hq, hkv, &a, &groups);
-  } else {
-    groups.groups = 0;
-    a.n = n;
-    a.sinks = sinks;
-    for (int i = 0; i < n; ++i) {
-      a.row0[i] = t.row0[i], a.rows[i] = n_new[i], a.pos[i] = pos[i], a.n_keys[i] = n_keys[i], a.pt[i] = t.pt[i];
-      groups.of[i] = -1;
-    }
+  prefixes = n_groups > 0;
+  if (!prefixes) {
+    memset(&with_sinks, 0, sizeof(with_sinks));
+    with_sinks.c = SinksTable{t, sinks};
+    plan_runs(with_sinks.c, kSinksCosts, hq, hkv, causal != 0, window, sms, nullptr, &plan.runs);
+    memcpy(with_sinks.run, plan.runs.run, sizeof(with_sinks.run));
+    with_sinks.d.n_q_heads = hq, with_sinks.d.n_kv_heads = hkv, with_sinks.d.causal = causal != 0, with_sinks.d.window = window;
+    const int v[7] = {0, n, 0, 0, 0, plan.runs.cuts, 0};
+    memcpy(info, v, sizeof(v));
+    return plan.runs.ctas;
   }
-  const bool shared = n_groups && groups.groups > 0;
-  plan_attention(a, shared, hq, hkv, causal != 0, window, sms, &plan);
+  memset(&args, 0, sizeof(args));
+  memset(&groups, 0, sizeof(groups));
+  AttnTable& a = args.c;
+  share_prefixes(t, count, keys, n_groups, hq, hkv, causal != 0, &a, &groups);
+  plan_prefix_attention(a, groups.groups > 0, hq, hkv, causal != 0, sms, &plan);
   memcpy(args.run, plan.runs.run, sizeof(args.run));
-  args.d.n_q_heads = hq, args.d.n_kv_heads = hkv, args.d.causal = causal != 0, args.d.window = window;
-  args.prefix.on = shared;
+  args.d.n_q_heads = hq, args.d.n_kv_heads = hkv, args.d.causal = causal != 0, args.d.window = 0;
+  args.prefix.on = plan.shared;
   args.prefix.first = firsts, args.prefix.last = lasts;
   memcpy(args.prefix.item0, plan.item0, sizeof(plan.item0));
   int row = 0;
   for (int b = 0; b < plan.runs.ctas; ++b) args.prefix.row0[b] = row, row += static_cast<int>(plan.run_rows[b]);
-  const int v[6] = {shared, a.n, groups.groups, plan.items, static_cast<int>(plan.part_rows), plan.runs.cuts};
+  const int v[7] = {plan.shared, a.n, groups.groups, plan.items, static_cast<int>(plan.part_rows), plan.runs.cuts, groups.any};
   memcpy(info, v, sizeof(v));
-  for (int i = 0; i < n; ++i) of[i] = groups.of[i];
   return plan.runs.ctas;
 }
-extern "C" void table(int* row0, int* rows, int* pos, int* key0, int* n_keys, int* item0, int* pt) {
-  for (int i = 0; i < args.c.n; ++i) {
-    row0[i] = args.c.row0[i], rows[i] = args.c.rows[i], pos[i] = args.c.pos[i], key0[i] = args.c.key0[i];
-    n_keys[i] = args.c.n_keys[i], item0[i] = plan.item0[i], pt[i] = static_cast<int>(reinterpret_cast<size_t>(args.c.pt[i]) / 16) - 1;
-  }
+extern "C" void table(int* row0, int* rows, int* item0, int* of) {
+  if (!prefixes)
+    for (int i = 0; i < with_sinks.c.n; ++i) row0[i] = with_sinks.c.row0[i], rows[i] = rows_of(with_sinks.c, i), item0[i] = 0, of[i] = -1;
+  else
+    for (int i = 0; i < args.c.n; ++i) row0[i] = args.c.row0[i], rows[i] = args.c.rows[i], item0[i] = plan.item0[i], of[i] = i < groups.groups ? -2 : groups.of[i - groups.groups];
 }
-// A CTA's segments, 26 numbers each; tiles: 11 each: cache tile, first and last page, and the ranges of what some row sees, what all rows
-// of the two chains see. Returns the segments.
-extern "C" int walk(int cta, int* seg, int* tiles, int max_tiles) {
-  Walk<true> w;
-  w.at = args.run[cta];
-  w.part_row = args.prefix.row0[cta];
-  int n = 0, m = 0;
+static int page_at(const ChunkArgs<kSinks>&, const SegmentOf<kSinks>& s, int j, int p) { return s.pt[cache_tile(s, j) * kPagesPerTile + p]; }
+static int page_at(const ChunkArgs<kPrefix>& a, const SegmentOf<kPrefix>& s, int j, int p) {
+  int member = -1;
+  for (int i = 0; i < a.c.members[s.entry]; ++i) member += a.c.m_page0[a.c.member0[s.entry] + i] <= (cache_tile(s, j) - s.ns) * 8 + p;
+  return page_of(a.c, s, j, p, member);
+}
+// A CTA's segments, 12 numbers each; their tiles, 16 each: the range of what all rows of the two chains see, first and last page, the pages; and what
+// each row sees of each tile, 2 each. Returns the segments.
+template <int FORM>
+static int walk_form(const ChunkArgs<FORM>& a, int part_row, int cta, int* seg, int* tiles, int max_tiles, int* ranges, int max_ranges) {
+  Walk<FORM> w;
+  w.at = a.run[cta];
+  w.part_row = part_row;
+  int n = 0, m = 0, r = 0;
+  const int grp = a.d.n_q_heads / a.d.n_kv_heads;
   for (;; ++n) {
-    SegmentOf<true> s;
-    w.next(args, cta, s);
+    SegmentOf<FORM> s;
+    w.next(a, cta, s);
     if (s.end) return n;
-    const int v[26] = {s.g, s.q0, s.rows, s.pos, s.n_keys, s.row0, s.narrow, s.slot, s.all_lo, s.all_hi, s.jb, s.J, s.n0, s.n1, s.quarters0,
-                       s.quarters1, s.sinks, s.win_lo, s.ns, s.gap, s.part_row, s.item_rows, m,
-                       static_cast<int>(reinterpret_cast<size_t>(s.pt) / 16) - 1, 0, 0};
-    memcpy(seg + 26 * n, v, sizeof(v));
-    const PageSpan<true> pages(s);
+    const int v[12] = {s.g, s.q0, s.rows, s.entry, s.narrow, s.slot, s.J, s.n0, s.n1, s.part_row, s.item_rows, m};
+    memcpy(seg + 12 * n, v, sizeof(v));
+    const PageSpan<FORM> pages(s);
     for (int j = 0; j < s.J; ++j, ++m) {
       if (m >= max_tiles) return -1;
-      const KeyRange all = range_in(s, j, KeyRange{s.all_lo, s.all_hi}), f0 = range_in(s, j, s.full0), f1 = range_in(s, j, s.full1);
-      const int t[11] = {cache_tile(s, j), pages.first(j), pages.last(j), all.lo, all.hi, f0.lo, f0.hi, f1.lo, f1.hi, s.jb + j < s.ns, 0};
-      memcpy(tiles + 11 * m, t, sizeof(t));
+      const int k0 = cache_tile(s, j) * kN;
+      const KeyRange f0 = range_in(s, j, s.full0), f1 = range_in(s, j, s.full1), all = range_in(s, j, KeyRange{s.all_lo, s.all_hi});
+      int* t = tiles + 16 * m;
+      t[0] = f0.lo - k0, t[1] = f0.hi - k0, t[2] = f1.lo - k0, t[3] = f1.hi - k0, t[4] = pages.first(j), t[5] = pages.last(j), t[6] = all.lo - k0, t[7] = all.hi - k0;
+      for (int p = 0; p < 8; ++p) t[8 + p] = p >= t[4] && p < t[5] ? page_at(a, s, j, p) : -1;
+      for (int q = s.q0; q < s.q0 + s.item_rows; ++q, ++r) {
+        if (r >= max_ranges) return -2;
+        const KeyRange k = range_in(s, j, row_keys(a.c, s, q / grp, a.d.causal, a.d.window));
+        ranges[2 * r] = k.lo - k0, ranges[2 * r + 1] = k.hi - k0;
+      }
     }
   }
+}
+extern "C" int walk(int cta, int* seg, int* tiles, int max_tiles, int* ranges, int max_ranges) {
+  return prefixes ? walk_form(args, args.prefix.row0[cta], cta, seg, tiles, max_tiles, ranges, max_ranges)
+                  : walk_form(with_sinks, 0, cta, seg, tiles, max_tiles, ranges, max_ranges);
 }
 """
 
@@ -122,33 +133,37 @@ def ints(v):
 
 
 def verify(so, reqs, hq, hkv, causal=True, window=0, sinks=0, groups=(), sms=152):
-    """reqs: (rows, position, keys); groups: (requests, shared keys). Whether the call shares anything."""
+    """reqs: (rows, position, keys); groups: (requests, shared keys). Whether the call shares anything, and how many of its groups are split."""
     n, grp = len(reqs), hq // hkv
-    info, of = (ctypes.c_int * 6)(), (ctypes.c_int * max(1, n))()
-    firsts, lasts = (ctypes.c_int * 100000)(*[-1] * 100000), (ctypes.c_int * 100000)(*[-1] * 100000)
-    ctas = so.make(n, ints([r[0] for r in reqs]), ints([r[1] for r in reqs]), ints([r[2] for r in reqs]), len(groups),
-                   ints([g[0] for g in groups]), ints([g[1] for g in groups]), hq, hkv, int(causal), window, sinks, sms, info, of, firsts, lasts)
-    shared, entries, n_groups, items, part_rows, cuts = info
-    assert 0 < ctas <= sms and cuts <= 256
-    tab = [(ctypes.c_int * entries)() for _ in range(7)]
-    so.table(*tab)
-    row0, rows, pos, key0, n_keys, item0, tables = ([int(x) for x in t] for t in tab)
-    first_row = np.cumsum([0] + [r[0] for r in reqs])
-    total = int(first_row[-1]) * hq
     longest = max(r[2] for r in reqs)
-    met = np.zeros((total, longest), dtype=np.int32)  # (output row, head) x key, all entries' keys in the request's own numbering
+    pages = (longest + 15) // 16
+    tables = np.arange(n * max(1, pages), dtype=np.int32).reshape(n, -1)  # page p of request i: i pages + p
+    shared_of = [k for c, k in groups for _ in range(c)] or [0] * n
+    group_of = [g for g, (c, _) in enumerate(groups) for _ in range(c)] or list(range(n))
+    info = (ctypes.c_int * 7)()
+    firsts, lasts = (ctypes.c_int * 100000)(*[-1] * 100000), (ctypes.c_int * 100000)(*[-1] * 100000)
+    ctas = so.make(n, ints([r[0] for r in reqs]), ints([r[1] for r in reqs]), ints([r[2] for r in reqs]), tables.ctypes.data_as(ctypes.c_void_p),
+                   tables.shape[1], len(groups), ints([g[0] for g in groups]), ints([g[1] for g in groups]), hq, hkv, int(causal), window, sinks, sms,
+                   info, firsts, lasts)
+    shared, entries, split, items, part_rows, cuts, any_shares = info
+    assert 0 < ctas <= sms and cuts <= 256 and bool(shared) == (split > 0)
+    tab = [(ctypes.c_int * entries)() for _ in range(4)]
+    so.table(*tab)
+    row0, rows, item0, of = ([int(x) for x in t] for t in tab)
+    request = np.repeat(np.arange(n), [r[0] for r in reqs])  # of each row
+    first_row = np.cumsum([0] + [r[0] for r in reqs])
+    met = np.zeros((len(request) * hq, longest), dtype=np.int32)
     part_of = {}  # item -> [(part row, rows)], in order of runs
-    seg, tiles = (ctypes.c_int * (26 * 4000))(), (ctypes.c_int * (11 * 60000))()
+    seg, tiles, ranges = (ctypes.c_int * (12 * 4000))(), np.zeros((60000, 16), dtype=np.int32), np.zeros((3000000, 2), dtype=np.int32)
     slots, next_part = set(), 0
     for c in range(ctas):
-        count = so.walk(c, seg, tiles, 60000)
+        count = so.walk(c, seg, tiles.ctypes.data_as(ctypes.c_void_p), len(tiles), ranges.ctypes.data_as(ctypes.c_void_p), len(ranges))
         assert 0 <= count < 4000
+        at = 0
         for k in range(count):
-            (g, q0, packed, p, nk, r0, narrow, slot, all_lo, all_hi, jb, J, n0, n1, quarters0, quarters1, sk, win_lo, ns, gap, part_row, item_rows,
-             m, table, _, _) = seg[26 * k:26 * k + 26]
-            (e,) = [i for i in range(entries) if rows[i] and row0[i] == r0 and pos[i] == p and n_keys[i] == nk and tables[i] == table and rows[i] * grp == packed]
+            g, q0, packed, e, narrow, slot, J, n0, n1, part_row, item_rows, m = seg[12 * k:12 * k + 12]
             tile = TILE if packed <= TILE else 2 * TILE
-            assert bool(narrow) == (packed <= TILE) and q0 % tile == 0 and item_rows == min(tile, packed - q0)
+            assert packed == rows[e] * grp and bool(narrow) == (packed <= TILE) and q0 % tile == 0 and item_rows == min(tile, packed - q0)
             item = item0[e] + ((packed + tile - 1) // tile - 1 - q0 // tile) * hkv + g
             if shared:
                 assert slot == 0 and part_row == next_part
@@ -157,44 +172,51 @@ def verify(so, reqs, hq, hkv, causal=True, window=0, sinks=0, groups=(), sms=152
             elif slot >= 0:
                 assert slot not in slots and slot // 2 == c
                 slots.add(slot)
-            assert n0 == ((J + 1) // 2 if narrow else n0) and n1 == (J // 2 if narrow else n1) and 0 <= n0 <= J and 0 <= n1 <= J
-            assert max(n0, n1) == J if not narrow else n0 + n1 == J
+            assert 0 <= n0 <= J and 0 <= n1 <= J and (n0 + n1 == J and 0 <= n0 - n1 <= 1 if narrow else max(n0, n1) == J)
+            # a chain gives back the K/V tiles that it does not go through at the segment's end: more than two of them are
+            # more than the ring's five slots, which the other chain would wait for without end
+            assert narrow or min(n0, n1) == 0 or J - min(n0, n1) <= 2
             for j in range(J):
-                at, pg0, pg1, lo, hi, f0l, f0h, f1l, f1h, is_sink = tiles[11 * (m + j):11 * (m + j) + 10]
-                base = at * KEYS
-                assert 0 <= pg0 < pg1 <= 8 and base + 16 * pg1 <= (nk + 15) // 16 * 16
-                # a page is fetched for a key that some row sees, at either end
-                assert max(lo, base) < min(hi, base + KEYS) and pg0 == (max(lo, base) - base) // 16 and pg1 == (min(hi, base + KEYS) - base + 15) // 16
-                for t in range(2):
-                    if narrow and t != j % 2 or not narrow and j >= (n1 if t else n0):
+                t, mine = tiles[m + j], ranges[at:at + item_rows]
+                at += item_rows
+                pg0, pg1 = t[4:6]
+                assert 0 <= pg0 < pg1 <= 8
+                lo, hi = max(0, t[6]), min(KEYS, t[7])
+                assert lo < hi and pg0 == lo // 16 and pg1 == (hi + 15) // 16  # a page is fetched for what some row sees, at either end
+                a, b = np.clip(mine[:, 0], 0, KEYS), np.clip(mine[:, 1], 0, KEYS)
+                x = np.arange(KEYS)
+                sees = (x >= a[:, None]) & (x < b[:, None])
+                assert (~sees.any(1) | ((a >= lo) & (b <= hi))).all()
+                for ch in range(2):
+                    part = sees if narrow else sees[ch * TILE:(ch + 1) * TILE]
+                    if not len(part) or narrow and ch != j % 2:
                         continue
-                    r_first = q0 + (0 if narrow else t * TILE)
-                    some = np.zeros(KEYS, dtype=bool)
-                    full = np.ones(KEYS, dtype=bool)
-                    for r in range(r_first, min(r_first + TILE, packed)):
-                        x = p + r // grp
-                        # the row's own range in this tile, as the kernel forms it
-                        mine_lo = max(max(0, x + 1 - window) if window else 0, all_lo)
-                        if sinks and sk == 0:
-                            mine_lo = 0
-                        mine_hi = min(nk, x + 1) if causal else nk
-                        a, b = (0, min(sk, mine_hi)) if is_sink else (max(mine_lo, sk), mine_hi)
-                        a, b = max(a, base), min(b, base + KEYS)
-                        keys = np.zeros(KEYS, dtype=bool)
-                        if b > a:
-                            keys[a - base:b - base] = True
-                            met[(r0 + r // grp) * hq + g * grp + r % grp, a:b] += 1
-                            assert lo <= a and b <= hi
-                        some |= keys
-                        full &= keys
-                    fl, fh = (f1l, f1h) if t else (f0l, f0h)
-                    if not narrow or t == 0:
-                        says = np.zeros(KEYS, dtype=bool)
-                        says[max(0, min(KEYS, fl - base)):max(0, min(KEYS, fh - base))] = True
-                        assert (says == full).all(), "keys that all rows see"
+                    if not narrow and j >= (n1 if ch else n0):
+                        assert not part.any()  # the chain does not go through this tile
+                        continue
+                    says = np.zeros(KEYS, dtype=bool)
+                    says[max(0, min(KEYS, t[2 * ch])):max(0, min(KEYS, t[2 * ch + 1]))] = True
+                    exact = part.all(0)
+                    # of requests side by side the bound may leave out what all see by chance
+                    assert (says <= exact).all() and (says.all() or of[e] == -1 and groups or (says == exact).all()), "keys that all rows see"
+                if not sees.any():
+                    continue
+                ids = np.where(np.arange(8) >= 0, t[8:16], -1)
+                req_of_page, page = ids // tables.shape[1], ids % tables.shape[1]
+                q, y = np.nonzero(sees)
+                p = y // 16
+                assert (p >= pg0).all() and (p < pg1).all()
+                row = row0[e] + (q0 + q) // grp
+                key = page[p] * 16 + y % 16
+                i, whose = request[row], req_of_page[p]
+                # a page of the row's own request, or a shared key of another of its group's
+                assert ((whose == i) | (np.array(group_of)[whose] == np.array(group_of)[i]) & (key < np.array(shared_of)[i])).all()
+                assert (key < np.array([r[2] for r in reqs])[i]).all()
+                np.add.at(met, (row * hq + g * grp + (q0 + q) % grp, key), 1)
+    j = np.arange(longest)
     for i, (m_rows, p, nk) in enumerate(reqs):
         for r in range(m_rows):
-            x, j = p + r, np.arange(longest)
+            x = p + r
             want = j < nk
             if causal:
                 want &= j <= x
@@ -208,9 +230,10 @@ def verify(so, reqs, hq, hkv, causal=True, window=0, sinks=0, groups=(), sms=152
             assert firsts[item] == parts[0][0] and lasts[item] == parts[-1][0]
             for (a, m), (b, _) in zip(parts, parts[1:]):
                 assert b == a + m
-        for i in range(n):
-            assert of[i] < n_groups
-    return bool(shared)
+    # every row is one entry's, beside a split group's
+    own = sorted((row0[e], rows[e]) for e in range(entries) if of[e] != -2 and rows[e])
+    assert sum(r for _, r in own) == len(request) and all(a + r == b for (a, r), (b, _) in zip(own, own[1:]))
+    return bool(any_shares), split
 
 
 SINKS = [
@@ -242,45 +265,52 @@ def test_walk_with_sinks_of_random_calls(planner):
                sinks=rng.choice((1, 4, 128, 129, rng.randint(1, 400))), sms=rng.choice((152, 13, 2)))
 
 
-PREFIXES = [
-    ([(1, 900 + i, 901 + i) for i in range(8)], 4, 2, [(8, 900)], True),
-    ([(1, 900 + i, 901 + i) for i in range(40)], 28, 4, [(40, 897)], True),
-    ([(5, 400, 405)] * 6 + [(3, 700, 703)] * 4, 12, 2, [(6, 400), (4, 555)], True),
-    ([(1, 300, 301)] * 5 + [(2, 10, 12)], 4, 2, [(5, 256), (1, 0)], True),
-    ([(1, 300, 301), (0, 0, 0), (1, 350, 351), (4, 300, 304)], 4, 2, [(4, 300)], True),
-    ([(0, 0, 0), (1, 1600, 1601), (1, 1700, 1701)], 7, 1, [(3, 1512)], True),
-    ([(1, 600, 601), (1, 700, 701)], 7, 1, [(2, 512)], False),        # too little to earn a merge
-    ([(1, 600, 601)], 7, 1, [(1, 512)], False),                       # a group of one
-    ([(256, 300, 556)] * 2, 1, 1, [(2, 300)], False),                 # whole tiles of their own
-    ([(1, 20, 21)] * 3, 4, 2, [(3, 0)], False),                       # nothing shared
-    ([(64, 900, 964)] * 3 + [(1, 900, 901)] * 9, 4, 2, [(3, 900), (9, 900)], True),
-    ([(1, 500, 500)] * 4, 4, 2, [(4, 500)], True),                    # rows without keys of their own
+PREFIXES = [  # requests, heads, groups, how many groups are split; None: nothing is shared
+    ([(1, 900 + i, 901 + i) for i in range(8)], 4, 2, [(8, 900)], 0),
+    ([(1, 900 + i, 901 + i) for i in range(40)], 28, 4, [(40, 897)], 0),
+    ([(5, 400, 405)] * 6 + [(3, 700, 703)] * 4, 12, 2, [(6, 400), (4, 555)], 0),
+    ([(1, 300, 301)] * 5 + [(2, 10, 12)], 4, 2, [(5, 256), (1, 0)], 0),
+    ([(1, 300, 301), (0, 0, 0), (1, 350, 351), (4, 300, 304)], 4, 2, [(4, 300)], 0),
+    ([(0, 0, 0), (1, 1600, 1601), (1, 1700, 1701)], 7, 1, [(3, 1512)], 0),
+    ([(1, 600, 601)], 7, 1, [(1, 512)], None),                       # a group of one
+    ([(256, 300, 556)] * 2, 1, 1, [(2, 300)], None),                 # whole tiles of their own
+    ([(1, 20, 21)] * 3, 4, 2, [(3, 0)], None),                       # nothing shared
+    ([(64, 900, 964)] * 3 + [(1, 900, 901)] * 9, 4, 2, [(3, 900), (9, 900)], 0),
+    ([(1, 500, 500)] * 4, 4, 2, [(4, 500)], 0),                      # rows without keys of their own
+    ([(1, 900 + 500 * i, 901 + 500 * i) for i in range(5)], 4, 2, [(5, 900)], 0),
+    ([(1, 6000 + 30 * i, 6001 + 30 * i) for i in range(24)], 28, 4, [(24, 4000)], 1),   # long keys of their own: split
+    ([(1, 5000, 5001)] * 24 + [(1, 3000, 3001)] * 6, 28, 4, [(24, 3000), (6, 3000)], 1),
+    ([(1, 3000, 3001)] * 6 + [(1, 5000, 5001)] * 24 + [(1, 60, 61)], 28, 4, [(6, 3000), (24, 3000), (1, 0)], 1),
+    ([(13, 1900, 1913)] * 12 + [(13, 1900, 1940)], 28, 4, [(13, 1900)], 0),                 # several tiles of rows
+    ([(3, 1900, 5000)] * 4 + [(3, 1900, 8000)] * 3, 28, 4, [(7, 1900)], 0),                 # keys behind the rows
 ]
 
 
 @pytest.mark.parametrize("case", range(len(PREFIXES)))
 def test_walk_over_shared_prefixes(planner, case):
-    reqs, hq, hkv, groups, shares = PREFIXES[case]
+    reqs, hq, hkv, groups, split = PREFIXES[case]
     for sms in (152, 11, 1):
-        assert verify(planner, reqs, hq, hkv, groups=groups, sms=sms) == shares
+        got = verify(planner, reqs, hq, hkv, groups=groups, sms=sms)
+        assert got == (split is not None, split or 0)
     verify(planner, reqs, hq, hkv, groups=groups, causal=False)
 
 
 def test_walk_over_shared_prefixes_of_random_calls(planner):
-    rng, some = random.Random(6), 0
+    rng, some, splits = random.Random(6), 0, 0
     for _ in range(40):
         hq, hkv = rng.choice(((4, 2), (7, 1), (3, 3), (16, 1)))
         reqs, groups = [], []
         for _ in range(rng.randint(1, 4)):
-            count, shared = rng.randint(1, 7), rng.choice((0, 16, 1024, rng.randint(1, 2500)))
+            count, shared, far = rng.randint(1, 7), rng.choice((0, 16, 1024, rng.randint(1, 2500))), rng.choice((200, 4000))
             groups.append((count, shared))
             for _ in range(count):
-                m, extra = rng.choice((0, 1, 1, rng.randint(1, 30))), rng.choice((0, rng.randint(0, 200)))
+                m, extra = rng.choice((0, 1, 1, rng.randint(1, 30))), rng.choice((0, rng.randint(0, far)))
                 reqs.append((m, shared + extra, shared + extra + rng.choice((m, m, 0, rng.randint(0, m + 20)))))
         if not any(r[0] for r in reqs):
             continue
-        some += verify(planner, reqs, hq, hkv, groups=groups, causal=rng.random() < 0.8, sms=rng.choice((152, 13, 2)))
-    assert some > 15
+        got = verify(planner, reqs, hq, hkv, groups=groups, causal=rng.random() < 0.8, sms=rng.choice((152, 13, 2)))
+        some, splits = some + got[0], splits + (got[1] > 0)
+    assert some > 15 and splits > 0
 
 
 # ---------------------------------------------------------------------------------------------- refusals

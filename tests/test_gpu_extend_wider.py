@@ -159,6 +159,9 @@ GROUPS = {
     "no keys of their own": [(900, [(1, 0, -1)] * 5 + [(2, 3, -5)])],
     "keys behind the rows": [(900, [(1, 0, 30)] * 5 + [(2, 3, 200)])],
     "short": [(17, [(1, 0, 0)] * 3), (3, [(1, 1, 0)])],
+    # requests whose own keys are long: split from the shared ones where heads are many, beside a folded group and one alone
+    "long keys of their own": [(1000, [(1, 1500 + 16 * i, 0) for i in range(24)]), (900, [(2, 3, 0)] * 4), (0, [(1, 40, 0)])],
+    "rows of several tiles": [(1000, [(13, 7 * i, 0) for i in range(9)])],
 }
 
 
