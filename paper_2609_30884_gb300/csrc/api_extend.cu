@@ -407,7 +407,7 @@ crf_status run_chunk_attention(crf_ctx* ctx, const ChunkAttnDesc& d, const Chunk
 }
 
 // The requests' groups, checked, and the table of those that share.
-crf_status prefix_groups(const ChunkTable& t, const crf_prefix* prefixes, int n, int n_q_heads, int n_kv_heads, bool causal,
+crf_status prefix_groups(const ChunkTable& t, const crf_prefix* prefixes, int n, int n_q_heads, int n_kv_heads, bool causal, int num_sms,
                          AttnTable* a, PrefixGroups* g) {
   if (!prefixes) return fail(CRF_EINVAL, "prefixes is null");
   if (n < 1 || n > t.n) return fail(CRF_EINVAL, "n_prefixes %d out of range (1..%d)", n, t.n);
@@ -424,7 +424,7 @@ crf_status prefix_groups(const ChunkTable& t, const crf_prefix* prefixes, int n,
     at += count[i];
   }
   if (at != t.n) return fail(CRF_EINVAL, "the prefixes have %d requests, the call %d", at, t.n);
-  share_prefixes(t, count, keys, n, n_q_heads, n_kv_heads, causal, a, g);
+  share_prefixes(t, count, keys, n, n_q_heads, n_kv_heads, causal, num_sms, a, g);
   return CRF_OK;
 }
 
@@ -778,7 +778,7 @@ crf_status crf_prefix_attention_workspace_size(crf_ctx* ctx, int n_q_heads, int 
     if (s != CRF_OK) return s;
     AttnTable a;
     PrefixGroups g;
-    s = prefix_groups(t, prefixes, n_prefixes, n_q_heads, n_kv_heads, causal != 0, &a, &g);
+    s = prefix_groups(t, prefixes, n_prefixes, n_q_heads, n_kv_heads, causal != 0, ctx->num_sms, &a, &g);
     if (s != CRF_OK) return s;
     size_t need;
     if (g.any) {
@@ -808,7 +808,7 @@ crf_status crf_prefix_attention(crf_ctx* ctx, const crf_kv_pool* pool, int layer
     if (s != CRF_OK) return s;
     AttnTable a;
     PrefixGroups g;
-    s = prefix_groups(t, prefixes, n_prefixes, q->heads, n_kv_heads, causal != 0, &a, &g);
+    s = prefix_groups(t, prefixes, n_prefixes, q->heads, n_kv_heads, causal != 0, ctx->num_sms, &a, &g);
     if (s != CRF_OK || t.row0[t.n] == 0) return s;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (!g.any) return run_chunk_attention(ctx, d, t, workspace, ws_bytes, st);

@@ -184,7 +184,7 @@ void plan_prefix_attention(const AttnTable& a, bool shared, int n_q_heads, int n
 // The table of requests in runs of count[i] that share their first keys[i] keys. A group is folded, split, or its requests stand apart,
 // whichever takes the fewest units of work.
 void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int n, int n_q_heads, int n_kv_heads, bool causal,
-                    AttnTable* a, PrefixGroups* g);
+                    int num_sms, AttnTable* a, PrefixGroups* g);
 size_t prefix_attention_workspace(const AttnPlan& p, int head_dim);
 cudaError_t launch_prefix_attention(const ChunkAttnDesc& d, const AttnTable& a, const PrefixGroups& g, const AttnPlan& p,
                                     void* workspace, int num_sms, cudaStream_t stream);

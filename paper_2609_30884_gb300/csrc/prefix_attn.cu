@@ -10,7 +10,8 @@
 //              o = (e^(m1 - m) o1 + e^(m2 - m) o2) / (e^(m1 - m) l1 + e^(m2 - m) l2),  m = max(m1, m2)
 //            with (m, l, o) the maximum, the sum of exponentials and their unnormalised product with v. Every segment then writes its part;
 //            one merge joins an output row's parts of the group's item and of its request's, in order
-// Where the rows of each request fill tiles of their own, sharing saves no products, and the requests are attended one by one.
+// Where the rows of each request fill tiles of their own, sharing saves no products, and where there is little work in all it costs more
+// latency than it saves: the requests are then attended one by one.
 #include "chunk_attn.cuh"
 
 namespace crf {
@@ -195,7 +196,7 @@ void plan_prefix_attention(const AttnTable& a, bool shared, int n_q_heads, int n
 }
 
 void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int n, int n_q_heads, int n_kv_heads, bool causal,
-                    AttnTable* a, PrefixGroups* g) {
+                    int num_sms, AttnTable* a, PrefixGroups* g) {
   std::memset(a, 0, sizeof(*a));
   std::memset(g, 0, sizeof(*g));
   const int grp = n_q_heads / n_kv_heads;
@@ -258,6 +259,8 @@ void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int 
   const int32_t* lead[kMaxChunks];
   AttnTable t;
   std::memset(&t, 0, sizeof(t));
+  int64_t saved = 0;
+  bool any_split = false;
   for (int i = 0, r = 0; i < n; r += count[i++]) {
     way[i] = kApart;
     lead[i] = nullptr;
@@ -279,9 +282,16 @@ void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int 
       put_folded(&t, 0, r, r + count[i], keys[i], lead[i]);
       folded = units(t, 0);
     }
-    if (folded < apart && folded <= split) way[i] = kFolded;
+    if (folded < apart && folded <= split + split / 4) way[i] = kFolded;  // (a split group's parts cost every row of the call a join)
     else if (split < apart) way[i] = kSplit;
+    if (way[i] != kApart) saved += apart - (way[i] == kSplit ? split : folded);
+    any_split = any_split || way[i] == kSplit;
   }
+  // Few long items cut over all SMs begin and end later than many short ones: wide rows' q and o, masks, more parts to merge. 32 rows over
+  // 1000 shared keys (22 units an SM saved) take 20.1 us folded and 17.5 apart, drafts in two groups (11 units) 29 split and 21 apart;
+  // 8 rows over 15000 (45 units) 20.5 folded and 41.6 apart.
+  if (saved * n_kv_heads < static_cast<int64_t>(any_split ? 40 : 24) * num_sms)
+    for (int i = 0; i < n; ++i) way[i] = kApart;
   for (int i = 0, r = 0; i < n; r += count[i++]) {
     g->any = g->any || way[i] != kApart;
     if (way[i] == kSplit) put_shared(a, g->groups++, r, r + count[i], keys[i], lead[i]);

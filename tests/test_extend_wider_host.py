@@ -31,9 +31,9 @@ static AttnPlan plan;
 static PrefixGroups groups;
 static bool prefixes;
 // The plan of requests whose page tables are rows of `tables`. info: shared, entries, split groups, items, part rows, cuts, whether any group shares;
-// returns the number of CTAs.
+// returns the number of CTAs. Whether a group is worth sharing is decided for `sharers` SMs.
 extern "C" int make(int n, const int* n_new, const int* pos, const int* n_keys, const int* tables, int stride, int n_groups, const int* count,
-                    const int* keys, int hq, int hkv, int causal, int window, int sinks, int sms, int* info, int* firsts, int* lasts) {
+                    const int* keys, int hq, int hkv, int causal, int window, int sinks, int sms, int sharers, int* info, int* firsts, int* lasts) {
   ChunkTable t = {};
   t.n = n;
   for (int i = 0; i < n; ++i) t.row0[i + 1] = t.row0[i] + n_new[i], t.pos[i] = pos[i], t.n_keys[i] = n_keys[i], t.pt[i] = tables + i * stride;
@@ -52,7 +52,7 @@ extern "C" int make(int n, const int* n_new, const int* pos, const int* n_keys, 
   memset(&args, 0, sizeof(args));
   memset(&groups, 0, sizeof(groups));
   AttnTable& a = args.c;
-  share_prefixes(t, count, keys, n_groups, hq, hkv, causal != 0, &a, &groups);
+  share_prefixes(t, count, keys, n_groups, hq, hkv, causal != 0, sharers, &a, &groups);
   plan_prefix_attention(a, groups.groups > 0, hq, hkv, causal != 0, sms, &plan);
   memcpy(args.run, plan.runs.run, sizeof(args.run));
   args.d.n_q_heads = hq, args.d.n_kv_heads = hkv, args.d.causal = causal != 0, args.d.window = 0;
@@ -132,7 +132,7 @@ def ints(v):
     return (ctypes.c_int * max(1, len(v)))(*v)
 
 
-def verify(so, reqs, hq, hkv, causal=True, window=0, sinks=0, groups=(), sms=152):
+def verify(so, reqs, hq, hkv, causal=True, window=0, sinks=0, groups=(), sms=152, sharers=0):
     """reqs: (rows, position, keys); groups: (requests, shared keys). Whether the call shares anything, and how many of its groups are split."""
     n, grp = len(reqs), hq // hkv
     longest = max(r[2] for r in reqs)
@@ -144,7 +144,7 @@ def verify(so, reqs, hq, hkv, causal=True, window=0, sinks=0, groups=(), sms=152
     firsts, lasts = (ctypes.c_int * 100000)(*[-1] * 100000), (ctypes.c_int * 100000)(*[-1] * 100000)
     ctas = so.make(n, ints([r[0] for r in reqs]), ints([r[1] for r in reqs]), ints([r[2] for r in reqs]), tables.ctypes.data_as(ctypes.c_void_p),
                    tables.shape[1], len(groups), ints([g[0] for g in groups]), ints([g[1] for g in groups]), hq, hkv, int(causal), window, sinks, sms,
-                   info, firsts, lasts)
+                   sharers, info, firsts, lasts)
     shared, entries, split, items, part_rows, cuts, any_shares = info
     assert 0 < ctas <= sms and cuts <= 256 and bool(shared) == (split > 0)
     tab = [(ctypes.c_int * entries)() for _ in range(4)]
@@ -293,6 +293,13 @@ def test_walk_over_shared_prefixes(planner, case):
         got = verify(planner, reqs, hq, hkv, groups=groups, sms=sms)
         assert got == (split is not None, split or 0)
     verify(planner, reqs, hq, hkv, groups=groups, causal=False)
+
+
+def test_little_work_is_not_shared(planner):
+    # 24 units an SM have to be saved, 40 where a group is split
+    for requests, keys, shares in ((32, 1000, False), (8, 15000, True), (32, 15000, True), (2, 15000, False)):
+        reqs = [(1, keys + 5, keys + 6)] * requests
+        assert verify(planner, reqs, 28, 4, groups=[(requests, keys)], sharers=152)[0] == shares
 
 
 def test_walk_over_shared_prefixes_of_random_calls(planner):

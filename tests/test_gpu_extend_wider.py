@@ -148,25 +148,47 @@ class Shared(Setup):
         return out, lse
 
 
+# Groups are shared where that saves enough: all but those of the last three.
 GROUPS = {
-    "samples": [(900, [(1, i, 0) for i in range(8)])],
-    "many samples": [(2048, [(1, 3 * i, 0) for i in range(60)])],
-    "drafts": [(1001, [(5, 0, 0)] * 7 + [(3, 40, 0)])],
-    "two groups and one alone": [(700, [(2, 9, 0)] * 5), (0, [(3, 20, 0)]), (1607, [(1, 0, 0), (4, 130, 0), (1, 500, 0)])],
-    "ends of pages and tiles": [(1024, [(1, 0, 0)] * 6), (1023, [(1, 0, 0)] * 6), (1025, [(1, 0, 0)] * 6), (1008, [(1, 16, 0)] * 6)],
-    "long rows": [(1100, [(40, 0, 0), (1, 5, 0), (70, 20, 0), (9, 0, 0)])],
-    "requests without rows": [(800, [(0, 0, 0), (1, 4, 0), (0, 5, 0), (1, 7, 0), (3, 0, 0), (1, 0, 0), (0, 9, 0)])],
-    "no keys of their own": [(900, [(1, 0, -1)] * 5 + [(2, 3, -5)])],
-    "keys behind the rows": [(900, [(1, 0, 30)] * 5 + [(2, 3, 200)])],
-    "short": [(17, [(1, 0, 0)] * 3), (3, [(1, 1, 0)])],
+    "samples": [(9000, [(1, i, 0) for i in range(30)])],
+    "many samples": [(4096, [(1, 3 * i, 0) for i in range(100)])],
+    "drafts": [(7001, [(5, 0, 0)] * 40 + [(3, 40, 0)])],
+    "groups and one alone": [(3700, [(2, 9, 0)] * 50), (0, [(3, 20, 0)]), (4607, [(1, 0, 0), (4, 130, 0), (1, 500, 0)] * 10)],
+    "ends of pages and tiles": [(4096, [(1, 0, 0)] * 30), (4095, [(1, 0, 0)] * 30), (4097, [(1, 0, 0)] * 30), (4080, [(1, 16, 0)] * 30)],
+    "long rows": [(5100, [(40, 0, 0), (1, 5, 0), (70, 20, 0), (9, 0, 0)] * 12)],
+    "requests without rows": [(8000, [(0, 0, 0), (1, 4, 0), (0, 5, 0), (1, 7, 0), (3, 0, 0), (1, 0, 0), (0, 9, 0)] * 9)],
+    "no keys of their own": [(6000, [(1, 0, -1)] * 50 + [(2, 3, -5)] * 3)],
+    "keys behind the rows": [(6000, [(1, 0, 30)] * 50 + [(2, 3, 200)] * 3)],
     # requests whose own keys are long: split from the shared ones where heads are many, beside a folded group and one alone
-    "long keys of their own": [(1000, [(1, 1500 + 16 * i, 0) for i in range(24)]), (900, [(2, 3, 0)] * 4), (0, [(1, 40, 0)])],
-    "rows of several tiles": [(1000, [(13, 7 * i, 0) for i in range(9)])],
+    "long keys of their own": [(6000, [(1, 1500 + 16 * i, 0) for i in range(24)]), (5000, [(2, 3, 0)] * 30), (0, [(1, 40, 0)])],
+    "rows of several tiles": [(6000, [(13, 7 * i, 0) for i in range(70)])],
+    "few samples": [(900, [(1, i, 0) for i in range(8)])],
+    "two groups": [(700, [(2, 9, 0)] * 5), (0, [(3, 20, 0)]), (1607, [(1, 0, 0), (4, 130, 0), (1, 500, 0)])],
+    "short": [(17, [(1, 0, 0)] * 3), (3, [(1, 1, 0)])],
 }
 
 
+def shared_kernel(ctx, call):
+    """Whether the call ran the kernel of shared prefixes."""
+    ctx.profile_enable(True)
+    try:
+        call()
+        torch.cuda.synchronize()
+        return "prefix_attention" in ctx.profile_read()
+    finally:
+        ctx.profile_enable(False)
+
+
+def test_which_groups_are_shared(ctx):
+    unshared = {"few samples", "two groups", "short"}
+    for hq, hkv, dim in HEADS[:3]:
+        for name in sorted(GROUPS):
+            s = Shared(30, hq, hkv, dim, GROUPS[name], poison=False)
+            assert shared_kernel(ctx, lambda: s.run(ctx)) == (name not in unshared), (name, hq)  # noqa: B023
+
+
 @pytest.mark.parametrize("name", sorted(GROUPS))
-@pytest.mark.parametrize("hq,hkv,dim", HEADS)
+@pytest.mark.parametrize("hq,hkv,dim", [(4, 2, 64), (28, 4, 128), (16, 1, 128)])
 def test_shared_prefixes(ctx, hq, hkv, dim, name):
     s = Shared(31, hq, hkv, dim, GROUPS[name])
     s.verify(*s.run(ctx))
@@ -175,21 +197,21 @@ def test_shared_prefixes(ctx, hq, hkv, dim, name):
 
 @pytest.mark.parametrize("hq,hkv,dim", [(4, 2, 64), (28, 4, 128)])
 def test_shared_prefixes_without_causality(ctx, hq, hkv, dim):
-    s = Shared(32, hq, hkv, dim, [(1200, [(3, 0, 40), (1, 0, 0), (2, 7, 1), (1, 100, 0)]), (40, [(90, 0, 0)])], causal=False)
+    s = Shared(32, hq, hkv, dim, [(4200, [(3, 0, 40), (1, 0, 0), (2, 7, 1), (1, 100, 0)] * 12), (40, [(90, 0, 0)])], causal=False)
     s.verify(*s.run(ctx))
     ctx.check()
 
 
 @pytest.mark.parametrize("scale_q", [0.0, 8.0, 60.0])
 def test_shared_prefixes_of_sharp_and_flat_scores(ctx, scale_q):
-    s = Shared(33, 12, 2, 128, [(1500, [(2, 10, 0)] * 6)], scale_q=scale_q)
+    s = Shared(33, 12, 2, 128, [(8500, [(2, 10, 0)] * 30)], scale_q=scale_q)
     s.verify(*s.run(ctx))
 
 
 def test_shared_prefix_of_most_requests(ctx):
-    s = Shared(34, 4, 2, 64, [(600, [(1, i, 0) for i in range(crf.abi.MAX_CHUNKS)])])
+    s = Shared(34, 4, 2, 64, [(4600, [(1, i, 0) for i in range(crf.abi.MAX_CHUNKS)])])
     s.verify(*s.run(ctx))
-    s = Shared(35, 4, 2, 64, [(700, [(1, 5, 0), (2, 9, 0)])] * 64)
+    s = Shared(35, 4, 2, 64, [(7000, [(1, 5, 0), (2, 9, 0)])] * 64)
     s.verify(*s.run(ctx))
     ctx.check()
 
@@ -197,13 +219,13 @@ def test_shared_prefix_of_most_requests(ctx):
 def test_long_shared_prefix(ctx):
     s = Shared(36, 28, 4, 128, [(20000, [(1, i, 0) for i in range(32)])])
     s.verify(*s.run(ctx))
-    s = Shared(37, 2, 1, 64, [(200000, [(1, 5, 0), (3, 50, 0)])])
+    s = Shared(37, 2, 1, 64, [(200000, [(1, 5, 0), (3, 50, 0)] * 6)])
     s.verify(*s.run(ctx))
     ctx.check()
 
 
 def test_shared_prefix_strides_and_outputs(ctx):
-    s = Shared(38, 12, 2, 128, [(900, [(2, 5, 0)] * 5)])
+    s = Shared(38, 12, 2, 128, [(9000, [(2, 5, 0)] * 25)])
     want, lse = s.run(ctx)
     wide = torch.full((s.rows + 2, 14, 136), 3.0, dtype=BF16, device=DEV)
     q = torch.zeros(12, s.rows, 128, dtype=BF16, device=DEV).copy_(s.q.transpose(0, 1)).transpose(0, 1)
@@ -216,8 +238,8 @@ def test_shared_prefix_strides_and_outputs(ctx):
 
 
 def test_shared_prefix_of_bad_pages(ctx):
-    s = Shared(39, 4, 2, 64, [(1000, [(1, 5, 0)] * 6)], poison=False)
-    s.tables[0][3], s.tables[4][62] = len(s.k), -1
+    s = Shared(39, 4, 2, 64, [(9000, [(1, 5, 0)] * 60)], poison=False)
+    s.tables[0][3], s.tables[4][562] = len(s.k), -1
     s.run(ctx)
     with pytest.raises(CrfError, match="EINVAL"):
         ctx.check()
@@ -225,11 +247,11 @@ def test_shared_prefix_of_bad_pages(ctx):
 
 
 def test_shared_prefix_sees_what_is_not_finite(ctx):
-    s = Shared(40, 4, 2, 64, [(1000, [(1, 5, 0)] * 6)], poison=False)
+    s = Shared(40, 4, 2, 64, [(9000, [(1, 5, 0)] * 60)], poison=False)
     s.v[s.tables[0][10].long(), 0, 4, 7] = math.inf     # shared: all rows
-    s.v[s.tables[2][1003 // PAGE].long(), 1, 1003 % PAGE, 9] = math.nan  # request 2's own
+    s.v[s.tables[2][9003 // PAGE].long(), 1, 9003 % PAGE, 9] = math.nan  # request 2's own
     out, _ = s.run(ctx)
-    o = out.view(6, 2, 2, 64)
+    o = out.view(60, 2, 2, 64)
     assert bool(o[:, 0, :, 7].isposinf().all()) and bool(o[2, 1, :, 9].isnan().all())
     o[:, 0, :, 7], o[2, 1, :, 9] = 0, 0
     assert bool(o.isfinite().all())
@@ -243,7 +265,7 @@ def test_calls_repeat_their_bits_on_streams_and_in_graphs(ctx, kind):
         ws = lambda: ctx.chunk_attention_workspace(s.pool, b, 28, window=700, sinks=9)  # noqa: E731
         call = lambda o, l, w, **kw: ctx.chunk_attention(s.pool, 0, b, s.q, o, w, lse=l, window=700, sinks=9, **kw)  # noqa: E731
     else:
-        s = Shared(42, 28, 4, 128, [(3000, [(1, 7 * i, 0) for i in range(12)])])
+        s = Shared(42, 28, 4, 128, [(9000, [(1, 7 * i, 0) for i in range(16)])])
         b, p = s.batch(), s.prefixes()
         ws = lambda: ctx.prefix_attention_workspace(s.pool, b, p, 28)  # noqa: E731
         call = lambda o, l, w, **kw: ctx.prefix_attention(s.pool, 0, b, p, s.q, o, w, lse=l, **kw)  # noqa: E731
@@ -270,7 +292,7 @@ def test_a_fork_is_continued_and_scored(ctx):
     """What the calls are for, in a row: a cached prefix forks, every fork's next rows are normed, turned and appended, attended over the
     shared prefix, attended again through a window with sinks, and the logits of an output head scored."""
     g = gen(43)
-    hq, hkv, dim, n, forks, m = 12, 2, 128, 901, 6, 3
+    hq, hkv, dim, n, forks, m = 12, 2, 128, 6005, 30, 3
     (lead,), total = tables_of(g, [pages_for(n + m)], spare=60)
     kp, vp = normal(g, total, hkv, PAGE, dim), normal(g, total, hkv, PAGE, dim)
     pool = crf.KVPool([kp], [vp])
