@@ -304,7 +304,7 @@ def _put_heads(buf, at: int, device: int, name: str, x: torch.Tensor, out: Optio
 
 def _put_norm(buf, at: int, device: int, name: str, gain: torch.Tensor, kind: torch.dtype, dim: int, eps: float) -> None:
     """crf_norm of ``gain`` [dim] at ``buf[at:]``."""
-    if gain.shape != (dim,) or gain.dtype != kind or gain.get_device() != device or (dim > 1 and gain.stride(0) != 1):
+    if gain.numel() != dim or gain.dtype is not kind or gain.get_device() != device or not gain.is_contiguous():
         raise ValueError(f"{name} must be a contiguous [{dim}] of the heads' type on cuda:{device}")
     _pack_norm(buf, at, gain.data_ptr(), eps)
 
@@ -449,22 +449,23 @@ class Context:
 
     def _norm_parts(self, rope: Rope, positions: torch.Tensor, x, gain, out, k, k_gain, k_out, eps: float) -> Tuple[int, int, int]:
         """Rows, type and parts of a call on normed heads, its descriptors packed."""
-        device, buf, dim = self.device, self._parts, rope.head_dim
-        n, kind = x.shape[0], _TYPES.get(x.dtype)
+        device, buf, dim, dtype = self.device, self._parts, rope.head_dim, x.dtype
+        n, kind = len(x), _TYPES.get(dtype)
         if kind is None:
             raise ValueError("x must be bfloat16, float16 or float32")
-        self._here(positions)
+        if positions.get_device() != device:
+            raise ValueError(f"every tensor of the call must be on cuda:{device}")
         _int32_on_device("positions", positions, n)
         _put_heads(buf, 0, device, "x", x, x if out is None else out, dim)
-        _put_norm(self._norms, 0, device, "gain", gain, x.dtype, dim, eps)
+        _put_norm(self._norms, 0, device, "gain", gain, dtype, dim, eps)
         if k is None:
             return n, kind, 1
-        if k.dtype != x.dtype or k.shape[0] != n:
+        if k.dtype is not dtype or len(k) != n:
             raise ValueError("k must have x's type and rows")
         if k_gain is None:
             raise ValueError("k needs k_gain")
         _put_heads(buf, _HEADS, device, "k", k, k if k_out is None else k_out, dim)
-        _put_norm(self._norms, _NORM, device, "k_gain", k_gain, x.dtype, dim, eps)
+        _put_norm(self._norms, _NORM, device, "k_gain", k_gain, dtype, dim, eps)
         return n, kind, 2
 
     def norm_rotary(self, rope: Rope, positions: torch.Tensor, x: torch.Tensor, gain: torch.Tensor,
@@ -501,7 +502,7 @@ class Context:
             if g.shape != like.shape or g.dtype != like.dtype:
                 raise ValueError(f"{name} must have the heads' shape and type")
             _put_heads(buf, (2 + i) * _HEADS, device, name, g, None, dim)
-            if dg.shape != (dim,) or dg.dtype != torch.float32 or dg.get_device() != device or not dg.is_contiguous():
+            if dg.numel() != dim or dg.dtype is not torch.float32 or dg.get_device() != device or not dg.is_contiguous():
                 raise ValueError(f"the gain's gradient must be a contiguous float32 [{dim}] on cuda:{device}")
             self._dgains[i] = dg.data_ptr()
         status = self.lib.crf_norm_rotary_grad(self.h, rope.address, buf, self._norms, ctypes.addressof(buf) + 2 * _HEADS,
@@ -513,16 +514,14 @@ class Context:
     # -------------------------------------------------------------- log probabilities
     def _logits(self, name: str, z: torch.Tensor) -> int:
         kind = _TYPES.get(z.dtype)
-        if kind is None or z.dim() != 2 or z.get_device() != self.device or (z.shape[1] > 1 and z.stride(1) != 1):
+        if kind is None or z.dim() != 2 or z.get_device() != self.device or (z.stride(1) != 1 and z.shape[1] > 1):
             raise ValueError(f"{name} must be [rows, vocab] bfloat16, float16 or float32 on cuda:{self.device}, a row's entries adjacent")
-        if z.shape[0] >= _INT32 or z.shape[1] >= _INT32:
-            raise ValueError(f"{name}: a size does not fit 32 bits")
         return kind
 
     def _a_row(self, name: str, t: Optional[torch.Tensor], n: int, dtype: torch.dtype) -> Optional[int]:
         if t is None:
             return None
-        if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous() or t.get_device() != self.device:
+        if t.numel() != n or t.dtype is not dtype or t.get_device() != self.device or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} [{n}] on cuda:{self.device}")
         return t.data_ptr()
 
@@ -534,20 +533,21 @@ class Context:
         [rows, n], n at most 32, the lower id first among equals) and their log probabilities (fp32 [rows, n]). See crf_logprobs."""
         kind = self._logits("logits", logits)
         n, vocab = logits.shape
+        if n >= _INT32 or vocab >= _INT32:
+            raise ValueError("logits: a size does not fit 32 bits")
+        fp32 = torch.float32
         t = self._a_row("targets", targets, n, torch.int32)
-        a = self._a_row("logprob", logprob, n, torch.float32)
-        b = self._a_row("entropy", entropy, n, torch.float32)
-        c = self._a_row("lse", lse, n, torch.float32)
-        k = 0
-        for name, x, dtype in (("top_ids", top_ids, torch.int32), ("top_logprobs", top_logprobs, torch.float32)):
-            if x is not None:
-                if x.dim() != 2 or x.shape[0] != n or x.dtype != dtype or not x.is_contiguous() or x.get_device() != self.device:
-                    raise ValueError(f"{name} must be a contiguous {dtype} [{n}, alternatives] on cuda:{self.device}")
-                k = x.shape[1]
-        if top_ids is not None and top_logprobs is not None and top_ids.shape != top_logprobs.shape:
-            raise ValueError("top_ids and top_logprobs must have one shape")
-        status = self.lib.crf_logprobs(self.h, logits.data_ptr(), kind, n, vocab, logits.stride(0), t, a, b, c, k,
-                                       _ptr(top_ids), _ptr(top_logprobs),
+        a = self._a_row("logprob", logprob, n, fp32)
+        b = self._a_row("entropy", entropy, n, fp32)
+        c = self._a_row("lse", lse, n, fp32)
+        k, wanted = 0, top_ids if top_ids is not None else top_logprobs
+        if wanted is not None:
+            if wanted.dim() != 2 or len(wanted) != n:
+                raise ValueError(f"the alternatives must be [{n}, their number]")
+            k = wanted.shape[1]
+        ids = self._a_row("top_ids", top_ids, n * k, torch.int32)
+        tops = self._a_row("top_logprobs", top_logprobs, n * k, fp32)
+        status = self.lib.crf_logprobs(self.h, logits.data_ptr(), kind, n, vocab, logits.stride(0), t, a, b, c, k, ids, tops,
                                        _raw_stream(self.device) if stream is None else _stream(stream))
         if status:
             abi.check(status)
@@ -561,6 +561,8 @@ class Context:
         if self._logits("d_logits", d_logits) != kind or d_logits.shape != logits.shape:
             raise ValueError("d_logits must have the logits' shape and type")
         n, vocab = logits.shape
+        if n >= _INT32 or vocab >= _INT32:
+            raise ValueError("logits: a size does not fit 32 bits")
         if lse is None:
             raise ValueError("lse is needed")
         t = self._a_row("targets", targets, n, torch.int32)

@@ -10,8 +10,8 @@
 // The alternatives take no pass of their own over the row. A lane's maximum is known when its sums are, and the lanes of a row are
 // groups of its elements (with a cluster, the same lane of every CTA): at least k elements reach the k-th greatest of the
 // groups' maxima, and those that reach it lie in groups that do. Sixteen rounds of counting over the block find that bound, to its
-// 16 leading bits; the few lanes that reach it have their elements read again (from L2), and the elements that do, some 1.1 k of
-// a long row, are ranked by counting. Keys (value, then lower index) order them, so the order in which threads
+// 16 leading bits; the pieces of the few lanes that reach it (a maximum is kept of each) are read again (from L2), and the elements
+// that do, some 1.1 k of a long row, are ranked by counting. Keys (value, then lower index) order them, so the order in which threads
 // list them does not matter. Rows of many equal logits, and rows that rise along the vocabulary, are gone through again as a whole:
 // those equal to an exact bound are taken in order of index, or the k-th greatest key is found digit by digit.
 //
@@ -26,10 +26,11 @@ namespace crf {
 
 namespace {
 
-constexpr int kLogThreads = 512;   // at most
+constexpr int kLogThreads = 256;   // at most; four blocks an SM: 1021 fp32 rows of 152064 take 91 us so, 96 with 512 threads and two
 constexpr int kStrip = 1024;       // elements of a warp's step
 constexpr int kList = 512;         // elements that are ranked by counting
-constexpr int kChosen = 64;        // groups that are read again
+constexpr int kChosen = 64;        // lanes that are read again, at most
+constexpr int kPieces = 128;       // pieces of their elements, at most
 constexpr int kAhead = 4;          // units of them that a lane asks for at once
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFloor = -200.f;   // 2^x is 0 from here down; keeps an infinite x out of products
@@ -82,7 +83,7 @@ struct LogShared {
   Sums part[kLogThreads / 32];
   Sums cta;                         // read by the cluster's first CTA, as is
   uint32_t lane[kLogThreads];       // the order of each lane's maximum, 0 without elements
-  int chosen[kChosen];              // lanes
+  int chosen[kPieces];              // lane + kLogThreads piece
   int n_chosen, n_list, n_equal[kLogThreads / 32];
   unsigned long long list[kList];
   int digits[256];
@@ -106,7 +107,7 @@ __device__ __forceinline__ float load_logit(const T* p) {
 
 // C: CTAs of a row, a cluster.
 template <typename T, int C>
-__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logprobs_kernel(const __grid_constant__ LogprobsDesc d) {
+__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logprobs_kernel(const __grid_constant__ LogprobsDesc d) {
   using U = Unit<T, 16 / sizeof(T)>;
   constexpr int VEC = 16 / sizeof(T), kLoads = kStrip / (32 * VEC);
   __shared__ LogShared sh;
@@ -118,10 +119,23 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
   const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
   const int end = d.vocab + skew, strips = (end + kStrip - 1) / kStrip;
   const T* base = z - skew;  // never read before z
+  // a lane's elements in pieces: its every fourth strip, or those of each CTA of the cluster, a maximum each
+  constexpr int kParts = C > 1 ? C : 4;
   Sums acc{-INFINITY, 0.f, 0.f};
+  float piece[C > 1 ? 1 : kParts];
+#pragma unroll
+  for (float& p : piece) p = -INFINITY;
   bool any = false;
+  int turn = 0;
+  auto note = [&](float mx) {
+    if (C == 1 && d.n_top > 0) {
+#pragma unroll
+      for (int i = 0; i < kParts; ++i)
+        if ((turn & (kParts - 1)) == i) piece[i % (C > 1 ? 1 : kParts)] = fmaxf(piece[i % (C > 1 ? 1 : kParts)], mx);
+    }
+  };
   griddep_wait();
-  for (int st = rank * warps + warp; st < strips; st += C * warps) {
+  for (int st = rank * warps + warp; st < strips; st += C * warps, ++turn) {
     // lane l has units l, l + 32 ... of the strip
     const int v0 = st * kStrip;
     if (v0 >= skew && v0 + kStrip <= end) {
@@ -138,6 +152,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
       }
       if (mx > acc.m) acc.raise(mx);
       any = true;
+      note(mx);
       const float neg = acc.m == -INFINITY ? 0.f : -acc.m;
       const uint64_t neg2 = f32x2(neg, neg), l2e = f32x2(kLog2e, kLog2e), one = f32x2(1.f, 1.f);
       uint64_t s2 = f32x2(0.f, 0.f), d2 = f32x2(0.f, 0.f);
@@ -182,6 +197,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
 #pragma unroll
       for (int i = 0; i < kLoads * VEC; ++i) mx = fmaxf(mx, x[i]);
       if (mx > acc.m) acc.raise(mx);
+      note(mx);
       const float m = acc.m == -INFINITY ? 0.f : acc.m;
 #pragma unroll
       for (int i = 0; i < kLoads * VEC; ++i) {
@@ -209,7 +225,9 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
     sh.cta = acc;
     sh.n_chosen = sh.n_list = 0;
   }
-  uint32_t mine = sh.lane[threadIdx.x];
+  uint32_t part[kParts];
+  part[0] = sh.lane[threadIdx.x];
+  uint32_t mine = part[0];
   if (C > 1) {
     cluster_sync();
     if (rank != 0) {
@@ -217,7 +235,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
       return;
     }
 #pragma unroll
-    for (int r = 1; r < C; ++r) mine = max(mine, ld_cluster_u32(&sh.lane[threadIdx.x], r));
+    for (int r = 1; r < C; ++r) mine = max(mine, part[r % kParts] = ld_cluster_u32(&sh.lane[threadIdx.x], r));
     if (threadIdx.x == 0) {
       for (int r = 1; r < C; ++r) {
         Sums o;
@@ -230,6 +248,8 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
     }
     cluster_sync();
   } else {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) part[i] = order_of(piece[i % (C > 1 ? 1 : kParts)]);
     __syncthreads();
   }
   const float s = sh.cta.s, log_s = logf(s), lse = s == 0.f ? -INFINITY : sh.cta.m + log_s;
@@ -278,13 +298,20 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
   };
   bool again = reached > kChosen;
   if (!again) {
-    if (mine >= least) sh.chosen[atomicAdd(&sh.n_chosen, 1)] = threadIdx.x;
+    if (mine >= least) {
+#pragma unroll
+      for (int i = 0; i < kParts; ++i)
+        if (part[i] >= least) {
+          const int at = atomicAdd(&sh.n_chosen, 1);
+          if (at < kPieces) sh.chosen[at] = i * kLogThreads + threadIdx.x;
+        }
+    }
     __syncthreads();
-    // warp w has the strips w, w + warps ... of the row, over the cluster's CTAs
-    const int turns = (strips + warps - 1) / warps, units = sh.n_chosen * turns * kLoads;
+    // piece i of warp w has the strips i warps + w, (i + kParts) warps + w ... of the row
+    const int turns = (strips + kParts * warps - 1) / (kParts * warps), units = min(sh.n_chosen, kPieces) * turns * kLoads;
     auto unit_at = [&](int e) {
-      const int pair = e / kLoads, at = sh.chosen[pair / turns];
-      return (at / 32 + pair % turns * warps) * kStrip + (e % kLoads * 32 + at % 32) * VEC;
+      const int pair = e / kLoads, at = sh.chosen[pair / turns], thread = at % kLogThreads;
+      return ((at / kLogThreads + pair % turns * kParts) * warps + thread / 32) * kStrip + (e % kLoads * 32 + thread % 32) * VEC;
     };
     for (int e0 = warp * 32; e0 < units; e0 += kAhead * blockDim.x) {
       U u[kAhead];  // all in flight
@@ -313,7 +340,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
       }
     }
     __syncthreads();
-    again = sh.n_list > kList || sh.n_list < k;  // (fewer: where NaN hides behind a maximum of -inf)
+    again = sh.n_list > kList || sh.n_list < k || sh.n_chosen > kPieces;  // (fewer than k: where NaN hides behind a maximum of -inf)
     if (sh.n_list < k) least = 1u;
   }
   if (again) {
@@ -399,15 +426,15 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 2) logp
     __syncthreads();
   }
   // ---------------------------------------------------------------- ranks: a key's lanes count those above it
-  const int listed = sh.n_list, share = listed * 8 <= static_cast<int>(blockDim.x) ? 8 : 1, part = threadIdx.x % share;
+  const int listed = sh.n_list, share = listed * 8 <= static_cast<int>(blockDim.x) ? 8 : 1, own = threadIdx.x % share;
   for (int i0 = 0; i0 < listed; i0 += blockDim.x / share) {
     const int i = i0 + static_cast<int>(threadIdx.x) / share;
     const unsigned long long it = i < listed ? sh.list[i] : 0ull;
     int before = 0;
 #pragma unroll 4
-    for (int j = part; j < listed; j += share) before += sh.list[j] > it;
+    for (int j = own; j < listed; j += share) before += sh.list[j] > it;
     for (int o = share / 2; o > 0; o /= 2) before += __shfl_xor_sync(0xffffffffu, before, o);
-    if (i < listed && before < k && part == 0) {
+    if (i < listed && before < k && own == 0) {
       if (d.top_ids) d.top_ids[static_cast<int64_t>(row) * k + before] = static_cast<int32_t>(~static_cast<uint32_t>(it));
       if (d.top_logprobs) {
         const float v = value_of(static_cast<uint32_t>(it >> 32));
@@ -487,9 +514,10 @@ __global__ void __launch_bounds__(kGradThreads) logprobs_grad_kernel(const __gri
 template <typename T>
 cudaError_t launch_type(const LogprobsDesc& d, int num_sms, cudaStream_t stream) {
   const int strips = (d.vocab + 15 + kStrip - 1) / kStrip;
-  // a row's CTAs: enough that few rows fill the SMs, each with a strip a warp at least
+  // a row's CTAs: enough that few rows fill the SMs twice (100 and 200 fp32 rows of 152064 take 14 and 23 us so, 16
+  // and 26 with once, 19 and 26 with three times), each with a strip a warp at least
   int c = 1;
-  while (c < 8 && static_cast<int64_t>(d.n_rows) * c < num_sms && strips >= 2 * c) c *= 2;
+  while (c < 8 && static_cast<int64_t>(d.n_rows) * c < 2 * num_sms && strips >= 2 * c) c *= 2;
   const dim3 grid(static_cast<unsigned>(d.n_rows) * c), block(32 * std::min(kLogThreads / 32, (strips + c - 1) / c));
   PdlScope pdl;
   switch (c) {
