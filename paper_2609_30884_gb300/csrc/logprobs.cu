@@ -15,6 +15,9 @@
 // list them does not matter. Rows of many equal logits, and rows that rise along the vocabulary, are gone through again as a whole:
 // those equal to an exact bound are taken in order of index, or the k-th greatest key is found digit by digit.
 //
+// Short rows are a warp's each, which does the same within itself: the groups are halves of the lanes' elements, their bound is
+// found with ballots, and where the list does not hold what reaches it, the greatest key below the last is looked for k times.
+//
 // Rows start at any element: a row is cut at 16-byte addresses, its first and last pieces element by element.
 #include "../../include/crf.h"
 #include "rotary.cuh"
@@ -31,6 +34,8 @@ constexpr int kStrip = 1024;       // elements of a warp's step
 constexpr int kList = 512;         // elements that are ranked by counting
 constexpr int kChosen = 64;        // lanes that are read again, at most
 constexpr int kPieces = 128;       // pieces of their elements, at most
+constexpr int kRowWarps = 8;        // rows of a block where a row is a warp's
+constexpr int kRowList = 256;       // elements that one of them ranks
 constexpr int kAhead = 4;          // units of them that a lane asks for at once
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFloor = -200.f;   // 2^x is 0 from here down; keeps an infinite x out of products
@@ -105,6 +110,108 @@ __device__ __forceinline__ float load_logit(const T* p) {
   return f[0];
 }
 
+// Adds a strip to a lane's sums, and says the maximum of the lane's elements of it, by halves (its even and odd units).
+// Lane l has units l, l + 32 ... of the strip.
+template <typename T>
+__device__ __forceinline__ float2 add_strip(const T* base, int v0, int skew, int end, int lane, Sums& acc, bool& any) {
+  using U = Unit<T, 16 / sizeof(T)>;
+  constexpr int VEC = 16 / sizeof(T), kLoads = kStrip / (32 * VEC);
+  float half[2] = {NAN, NAN}, mx;
+  if (v0 >= skew && v0 + kStrip <= end) {
+    U u[kLoads];
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) u[j] = *reinterpret_cast<const U*>(base + v0 + (j * 32 + lane) * VEC);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      float x[VEC];
+      unpack(u[j], x);
+#pragma unroll
+      for (int i = 0; i < VEC; i += 2) half[j & 1] = fmax3(half[j & 1], x[i], x[i + 1]);
+    }
+    mx = fmaxf(half[0], half[1]);
+    if (mx > acc.m) acc.raise(mx);
+    any = true;
+    const float neg = acc.m == -INFINITY ? 0.f : -acc.m;
+    const uint64_t neg2 = f32x2(neg, neg), l2e = f32x2(kLog2e, kLog2e), one = f32x2(1.f, 1.f);
+    uint64_t s2 = f32x2(0.f, 0.f), d2 = f32x2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      float x[VEC];
+      unpack(u[j], x);
+#pragma unroll
+      for (int i = 0; i < VEC; i += 2) {
+        float t0, t1;
+        f32x2_split(fma_f32x2(add_f32x2(f32x2(x[i], x[i + 1]), neg2), l2e, f32x2(0.f, 0.f)), t0, t1);
+        t0 = max_nan(t0, kFloor);
+        t1 = max_nan(t1, kFloor);
+        const uint64_t e = f32x2(ex2_approx(t0), ex2_approx(t1));
+        s2 = fma_f32x2(e, one, s2);
+        d2 = fma_f32x2(e, f32x2(t0, t1), d2);
+      }
+    }
+    float s0, s1;
+    f32x2_split(s2, s0, s1);
+    acc.s += s0 + s1;
+    f32x2_split(d2, s0, s1);
+    acc.d += s0 + s1;
+  } else {
+    // a first or last strip: units that lie inside the row as they are, the others element by element; what is outside is
+    // NaN to the maxima and no part of the sums
+    float x[kLoads * VEC];
+    auto inside = [&](int j, int i) { const int v = v0 + (j * 32 + lane) * VEC + i; return v >= skew && v < end; };
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      float y[VEC];
+      if (inside(j, 0) && inside(j, VEC - 1)) {
+        unpack(*reinterpret_cast<const U*>(base + v0 + (j * 32 + lane) * VEC), y);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) y[i] = inside(j, i) ? load_logit(base + v0 + (j * 32 + lane) * VEC + i) : NAN;
+      }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[j * VEC + i] = y[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads * VEC; ++i) half[i / VEC & 1] = fmaxf(half[i / VEC & 1], x[i]);
+    mx = fmaxf(half[0], half[1]);
+    if (mx > acc.m) acc.raise(mx);
+    const float m = acc.m == -INFINITY ? 0.f : acc.m;
+#pragma unroll
+    for (int i = 0; i < kLoads * VEC; ++i) {
+      if (!inside(i / VEC, i % VEC)) continue;
+      any = true;
+      const float t = max_nan((x[i] - m) * kLog2e, kFloor), e = ex2_approx(t);
+      acc.s += e;
+      acc.d += e * t;
+    }
+  }
+  return make_float2(half[0], half[1]);
+}
+
+__device__ __forceinline__ float lse_of(const Sums& t) { return t.s == 0.f ? -INFINITY : t.m + logf(t.s); }
+
+// A row's outputs but the alternatives, by one thread.
+template <typename T>
+__device__ __forceinline__ void put_row(const LogprobsDesc& d, int row, const T* z, const Sums& t) {
+  const float lse = lse_of(t);
+  if (d.lse) d.lse[row] = lse;
+  if (d.entropy) d.entropy[row] = t.s == 0.f ? 0.f : logf(t.s) - t.d * kLn2 / t.s;
+  if (d.logprob) {
+    int token = d.targets[row];
+    float lp = 0.f;
+    if (token != -1) {
+      token = checked_token(token, d.vocab, d.status);
+      lp = t.s == 0.f ? -INFINITY : load_logit(z + token) - lse;
+    }
+    d.logprob[row] = lp;
+  }
+}
+__device__ __forceinline__ void put_top(const LogprobsDesc& d, int row, int at, unsigned long long key, float s, float lse) {
+  const int64_t to = static_cast<int64_t>(row) * d.n_top + at;
+  if (d.top_ids) d.top_ids[to] = static_cast<int32_t>(~static_cast<uint32_t>(key));
+  if (d.top_logprobs) d.top_logprobs[to] = s == 0.f ? -INFINITY : value_of(static_cast<uint32_t>(key >> 32)) - lse;
+}
+
 // C: CTAs of a row, a cluster.
 template <typename T, int C>
 __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logprobs_kernel(const __grid_constant__ LogprobsDesc d) {
@@ -127,7 +234,8 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
   for (float& p : piece) p = -INFINITY;
   bool any = false;
   int turn = 0;
-  auto note = [&](float mx) {
+  auto note = [&](float2 half) {
+    const float mx = fmaxf(half.x, half.y);
     if (C == 1 && d.n_top > 0) {
 #pragma unroll
       for (int i = 0; i < kParts; ++i)
@@ -138,76 +246,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
   for (int st = rank * warps + warp; st < strips; st += C * warps, ++turn) {
     // lane l has units l, l + 32 ... of the strip
     const int v0 = st * kStrip;
-    if (v0 >= skew && v0 + kStrip <= end) {
-      U u[kLoads];
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) u[j] = *reinterpret_cast<const U*>(base + v0 + (j * 32 + lane) * VEC);
-      float mx = NAN;
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        float x[VEC];
-        unpack(u[j], x);
-#pragma unroll
-        for (int i = 0; i < VEC; i += 2) mx = fmax3(mx, x[i], x[i + 1]);
-      }
-      if (mx > acc.m) acc.raise(mx);
-      any = true;
-      note(mx);
-      const float neg = acc.m == -INFINITY ? 0.f : -acc.m;
-      const uint64_t neg2 = f32x2(neg, neg), l2e = f32x2(kLog2e, kLog2e), one = f32x2(1.f, 1.f);
-      uint64_t s2 = f32x2(0.f, 0.f), d2 = f32x2(0.f, 0.f);
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        float x[VEC];
-        unpack(u[j], x);
-#pragma unroll
-        for (int i = 0; i < VEC; i += 2) {
-          float t0, t1;
-          f32x2_split(fma_f32x2(add_f32x2(f32x2(x[i], x[i + 1]), neg2), l2e, f32x2(0.f, 0.f)), t0, t1);
-          t0 = max_nan(t0, kFloor);
-          t1 = max_nan(t1, kFloor);
-          const uint64_t e = f32x2(ex2_approx(t0), ex2_approx(t1));
-          s2 = fma_f32x2(e, one, s2);
-          d2 = fma_f32x2(e, f32x2(t0, t1), d2);
-        }
-      }
-      float s0, s1;
-      f32x2_split(s2, s0, s1);
-      acc.s += s0 + s1;
-      f32x2_split(d2, s0, s1);
-      acc.d += s0 + s1;
-    } else {
-      // a first or last strip: units that lie inside the row as they are, the others element by element; what is outside is
-      // NaN to the maxima and no part of the sums
-      float x[kLoads * VEC];
-      auto inside = [&](int j, int i) { const int v = v0 + (j * 32 + lane) * VEC + i; return v >= skew && v < end; };
-#pragma unroll
-      for (int j = 0; j < kLoads; ++j) {
-        float y[VEC];
-        if (inside(j, 0) && inside(j, VEC - 1)) {
-          unpack(*reinterpret_cast<const U*>(base + v0 + (j * 32 + lane) * VEC), y);
-        } else {
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) y[i] = inside(j, i) ? load_logit(base + v0 + (j * 32 + lane) * VEC + i) : NAN;
-        }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) x[j * VEC + i] = y[i];
-      }
-      float mx = NAN;
-#pragma unroll
-      for (int i = 0; i < kLoads * VEC; ++i) mx = fmaxf(mx, x[i]);
-      if (mx > acc.m) acc.raise(mx);
-      note(mx);
-      const float m = acc.m == -INFINITY ? 0.f : acc.m;
-#pragma unroll
-      for (int i = 0; i < kLoads * VEC; ++i) {
-        if (!inside(i / VEC, i % VEC)) continue;
-        any = true;
-        const float t = max_nan((x[i] - m) * kLog2e, kFloor), e = ex2_approx(t);
-        acc.s += e;
-        acc.d += e * t;
-      }
-    }
+    note(add_strip(base, v0, skew, end, lane, acc, any));
   }
   sh.lane[threadIdx.x] = any ? order_of(acc.m) : 0u;
 #pragma unroll
@@ -252,21 +291,8 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
     for (int i = 0; i < kParts; ++i) part[i] = order_of(piece[i % (C > 1 ? 1 : kParts)]);
     __syncthreads();
   }
-  const float s = sh.cta.s, log_s = logf(s), lse = s == 0.f ? -INFINITY : sh.cta.m + log_s;
-  if (threadIdx.x == 0) {
-    if (d.lse) d.lse[row] = lse;
-    if (d.entropy) d.entropy[row] = s == 0.f ? 0.f : log_s - sh.cta.d * kLn2 / s;
-    if (d.logprob) {
-      int t = d.targets[row];
-      float lp = 0.f;
-      if (t != -1) {
-        t = checked_token(t, d.vocab, d.status);
-        const float v = load_logit(z + t);
-        lp = s == 0.f ? -INFINITY : v - lse;
-      }
-      d.logprob[row] = lp;
-    }
-  }
+  const float s = sh.cta.s, lse = lse_of(sh.cta);
+  if (threadIdx.x == 0) put_row(d, row, z, sh.cta);
   const int k = d.n_top;
   if (k == 0) return;
 
@@ -363,7 +389,12 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
       if (lane == 0) sh.n_equal[warp] = equal;
       __syncthreads();
       above = sh.n_list;
+      for (int w = equal = 0; w < warps; ++w) equal += sh.n_equal[w];
       __syncthreads();
+      if (above + equal < k) {  // NaN behind a bound of -inf
+        above = kList + 1;
+        least = 1u;
+      }
     }
     if (above <= kList - kMaxTop) {
       // all above the bound, and the first of those equal to it
@@ -434,13 +465,122 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
 #pragma unroll 4
     for (int j = own; j < listed; j += share) before += sh.list[j] > it;
     for (int o = share / 2; o > 0; o /= 2) before += __shfl_xor_sync(0xffffffffu, before, o);
-    if (i < listed && before < k && own == 0) {
-      if (d.top_ids) d.top_ids[static_cast<int64_t>(row) * k + before] = static_cast<int32_t>(~static_cast<uint32_t>(it));
-      if (d.top_logprobs) {
-        const float v = value_of(static_cast<uint32_t>(it >> 32));
-        d.top_logprobs[static_cast<int64_t>(row) * k + before] = s == 0.f ? -INFINITY : v - lse;
+    if (i < listed && before < k && own == 0) put_top(d, row, before, it, s, lse);
+  }
+}
+
+// ---------------------------------------------------------------- a warp a row
+template <typename T>
+__global__ void __launch_bounds__(32 * kRowWarps) logprobs_rows_kernel(const __grid_constant__ LogprobsDesc d) {
+  using U = Unit<T, 16 / sizeof(T)>;
+  constexpr int VEC = 16 / sizeof(T), kLoads = kStrip / (32 * VEC);
+  static_assert(kLoads * VEC == 32, "a lane's elements of a strip are the bits of a word");
+  __shared__ unsigned long long lists[kRowWarps][kRowList];
+  griddep_launch_dependents();
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = blockIdx.x * (blockDim.x / 32) + warp;
+  if (row >= d.n_rows) return;
+  const T* z = static_cast<const T*>(d.z) + row * d.z_row;
+  const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
+  const int end = d.vocab + skew, strips = (end + kStrip - 1) / kStrip;
+  const T* base = z - skew;  // never read before z
+  Sums acc{-INFINITY, 0.f, 0.f};
+  bool any = false;
+  griddep_wait();
+  // the maxima of a lane's elements by halves: 64 groups of the row's elements
+  float even = -INFINITY, odd = -INFINITY;
+  for (int st = 0; st < strips; ++st) {
+    const float2 half = add_strip(base, st * kStrip, skew, end, lane, acc, any);
+    even = fmaxf(even, half.x);
+    odd = fmaxf(odd, half.y);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) {
+    Sums other;
+    other.m = __shfl_xor_sync(0xffffffffu, acc.m, o);
+    other.s = __shfl_xor_sync(0xffffffffu, acc.s, o);
+    other.d = __shfl_xor_sync(0xffffffffu, acc.d, o);
+    acc.add(other);
+  }
+  if (lane == 0) put_row(d, row, z, acc);
+  const int k = d.n_top;
+  if (k == 0) return;
+  const float s = acc.s, lse = lse_of(acc);
+  const uint32_t mine[2] = {any ? order_of(even) : 0u, any ? order_of(odd) : 0u};
+  auto groups_from = [&](uint32_t order) { return __popc(__ballot_sync(0xffffffffu, mine[0] >= order)) + __popc(__ballot_sync(0xffffffffu, mine[1] >= order)); };
+  uint32_t least = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit)
+    if (groups_from(least | (1u << bit)) >= k) least |= 1u << bit;
+  least = max(least, 1u);
+  auto key = [&](uint32_t order, int v) { return static_cast<unsigned long long>(order) << 32 | ~static_cast<uint32_t>(v - skew); };
+  auto place = [&](int st, int bit) { return st * kStrip + (bit / VEC * 32 + lane) * VEC + bit % VEC; };
+  // what is above -inf compares as floats do (at -inf and below, groups without elements count: the whole row is listed then)
+  const bool above = least > order_of(-INFINITY);
+  if (!above) least = 1u;
+  const float bound = value_of(least);
+  unsigned long long* list = lists[warp];
+  int n = 0;
+  for (int st = 0; st < strips && n <= kRowList; ++st) {
+    uint32_t hits = 0;
+    U u[kLoads];  // all in flight
+    auto whole = [&](int j) { return above && mine[j & 1] >= least && place(st, j * VEC) >= skew && place(st, j * VEC) + VEC <= end; };
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      if (whole(j)) u[j] = *reinterpret_cast<const U*>(base + place(st, j * VEC));
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) {
+      if (whole(j)) {
+        float x[VEC];
+        unpack(u[j], x);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) hits |= static_cast<uint32_t>(x[i] >= bound) << (j * VEC + i);
+      } else if (!above || mine[j & 1] >= least) {
+        const int v = place(st, j * VEC);
+#pragma unroll 1
+        for (int i = 0; i < VEC; ++i)
+          if (v + i >= skew && v + i < end && order_of(load_logit(base + v + i)) >= least) hits |= 1u << (j * VEC + i);
       }
     }
+    const int count = __popc(hits);
+    int to = count;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+      const int up = __shfl_up_sync(0xffffffffu, to, o);
+      if (lane >= o) to += up;
+    }
+    int at = n + to - count;
+    n += __shfl_sync(0xffffffffu, to, 31);
+    if (n > kRowList) break;
+    for (; hits; hits &= hits - 1) {
+      const int v = place(st, __ffs(hits) - 1);
+      list[at++] = key(order_of(load_logit(base + v)), v);
+    }
+  }
+  __syncwarp();
+  if (n >= k && n <= kRowList) {
+    for (int i = lane; i < n; i += 32) {
+      const unsigned long long it = list[i];
+      int before = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) before += list[j] > it;
+      if (before < k) put_top(d, row, before, it, s, lse);
+    }
+    return;
+  }
+  // many equal logits, or few that are no NaN: the greatest key below the last, k times
+  unsigned long long last = ~0ull;
+#pragma unroll 1
+  for (int r = 0; r < k; ++r) {
+    unsigned long long best = 0;
+#pragma unroll 4
+    for (int v = skew + lane; v < end; v += 32) {
+      const unsigned long long it = key(order_of(load_logit(base + v)), v);
+      if (it < last && it > best) best = it;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
+    if (lane == 0) put_top(d, row, r, best, s, lse);
+    last = best;
   }
 }
 
@@ -514,10 +654,17 @@ __global__ void __launch_bounds__(kGradThreads) logprobs_grad_kernel(const __gri
 template <typename T>
 cudaError_t launch_type(const LogprobsDesc& d, int num_sms, cudaStream_t stream) {
   const int strips = (d.vocab + 15 + kStrip - 1) / kStrip;
+  // Short rows are a warp's each, many of up to eight strips too: 16384 bf16 rows of 512 take 14 us so with no alternatives and 35
+  // with 32, 36 and 304 as blocks; of 8000, 55 and 105, 130 and 267 as blocks. 1500 of 8000 take the same either way, 100 take 15, 12 as blocks.
+  if (strips <= 2 || (strips <= 8 && d.n_rows >= 16 * num_sms)) {
+    const int w = std::max(1, std::min(kRowWarps, d.n_rows / num_sms));
+    PdlScope pdl;
+    return launch_kernel(logprobs_rows_kernel<T>, dim3((d.n_rows + w - 1) / w), dim3(32 * w), 0, stream, d);
+  }
   // a row's CTAs: enough that few rows fill the SMs twice (100 and 200 fp32 rows of 152064 take 14 and 23 us so, 16
-  // and 26 with once, 19 and 26 with three times), each with a strip a warp at least
+  // and 26 with once, 19 and 26 with three times), each with four strips at least
   int c = 1;
-  while (c < 8 && static_cast<int64_t>(d.n_rows) * c < 2 * num_sms && strips >= 2 * c) c *= 2;
+  while (c < 8 && static_cast<int64_t>(d.n_rows) * c < 2 * num_sms && strips >= 4 * c) c *= 2;
   const dim3 grid(static_cast<unsigned>(d.n_rows) * c), block(32 * std::min(kLogThreads / 32, (strips + c - 1) / c));
   PdlScope pdl;
   switch (c) {

@@ -158,6 +158,21 @@ def test_nan_and_infinity(ctx):
     assert ids[4].tolist() == last + [0, 1]
 
 
+@pytest.mark.parametrize("rows,vocab", [(1, 40), (1, 300), (1, 5000), (400, 1030), (400, 5000), (400, 20000), (1, 152064), (310, 100000)])
+def test_numbers_among_nan(ctx, rows, vocab):
+    g = gen(13)
+    for dtype in (torch.bfloat16, torch.float32):
+        z = torch.full((rows, vocab), math.nan, device=DEV, dtype=dtype)
+        ids = torch.randperm(vocab, device=DEV, generator=g)[:10]
+        # of the ten, seven values in order and three -inf, which stand before NaN
+        z[:, ids] = torch.tensor([7, 6, 5, 4, 3, 2, 1] + 3 * [-math.inf], device=DEV, dtype=dtype)
+        want = ids[:7].tolist() + sorted(ids[7:].tolist())
+        want += [i for i in range(vocab) if i not in want][:22]
+        for k in (1, 9, 32):
+            out = score(ctx, z, None, k)
+            assert out["top_ids"].tolist() == [want[:k]] * rows and bool(out["lse"].isnan().all())
+
+
 def test_targets_outside_the_vocabulary(ctx):
     g = gen(6)
     z = logits(g, 5, 700, torch.bfloat16)
