@@ -9,10 +9,10 @@
 // Bound by memory: every element is read once and written once. As in rotary.cu a thread owns one 16-byte unit of a head (for
 // the half layout two, the pair's halves), in four neighbouring heads, two in a gradient; here the lanes of a head, a power of
 // two, are neighbours in a warp and join the sum of squares by shuffles. What it takes to stay near memory is few instructions: 512
-// elements of a warp's step took 283 of them at first (16384 bf16 rows of 32 heads 58 us, the gradient 155). So places are
-// found by shifts, arithmetic is on two elements an instruction, gains and angles are multiplied once for a thread's heads, and all
-// of its heads' shuffles go level by level. Heads whose units are no such thing (odd sizes, strides or alignments) take a warp
-// each, an element or a pair a lane.
+// elements of a warp's step took 283 of them at first (16384 bf16 rows of 32 heads 58 us, the gradient 155; now 45, 89% of the
+// copy rate, and 86, 69%, still bound by instructions). So places are found by shifts, arithmetic is on two elements an
+// instruction, gains and angles are multiplied once for a thread's heads, and all of its heads' shuffles go level by level. Heads
+// whose units are no such thing (odd sizes, strides or alignments) take a warp each, an element or a pair a lane.
 //
 // The gains' gradient: a thread keeps the same elements of its heads' part over all the rows that its block walks, so
 // their sums stay in its registers; a block's sums meet in shared memory, the blocks' in a second small kernel, both in a
@@ -368,8 +368,8 @@ template <bool INTER>
 constexpr int kGradBatch = INTER ? 2 : 1;
 constexpr int kGradUnits = 4;
 // A thread's units of the next two tiles are on their way into places of its own in shared memory: in registers one tile took 128
-// of them and two blocks an SM had too few bytes in flight. Positions go three tiles ahead, because the next tile's angles are
-// formed before the barrier that follows their landing.
+// of them and two blocks an SM had too few bytes in flight. Positions go four tiles ahead, because all threads read what a few of
+// them copied: the next tile's have landed, and a barrier has followed, one tile before its angles are formed.
 constexpr int kStages = 3, kPositions = 4;
 struct NormGradShared {
   Angles angle[2];
@@ -436,11 +436,12 @@ __global__ void __launch_bounds__(kRotThreads, 2) head_norm_grad_kernel(const __
     g_at += g_jump;
   };
   fetch_pos(0);
-  copy_async_commit();
   fetch_pos(1);
-  fetch(0);
   copy_async_commit();
   fetch_pos(2);
+  fetch(0);
+  copy_async_commit();
+  fetch_pos(3);
   fetch(1);
   copy_async_commit();
   if (heads > 0) {
@@ -450,7 +451,7 @@ __global__ void __launch_bounds__(kRotThreads, 2) head_norm_grad_kernel(const __
       if (two) unpack_pairs<T, VEC>(*reinterpret_cast<const uint4*>(gain + p.e1), wy);
   }
   copy_async_wait<1>();
-  __syncthreads();  // the first two tiles' positions
+  __syncthreads();  // the first three tiles' positions
   int64_t row = first_row;
   auto angles = [&](int64_t at, int slot, Angles& to) {
     const int64_t row0 = at - p.rb;
@@ -460,11 +461,11 @@ __global__ void __launch_bounds__(kRotThreads, 2) head_norm_grad_kernel(const __
   __syncthreads();
   int stage = 0, ahead = 2, pos = 0, buffer = 0;
   for (int64_t tile = blockIdx.x; tile < tiles; tile += a.row_blocks) {
-    // (the stage and the positions of the tile before are free: all have passed the barrier behind them)
-    fetch_pos((pos + 3) & (kPositions - 1));
+    // (the stage of the tile before and this one's positions are free: all have passed the barrier behind them)
+    fetch_pos(pos);
     fetch(ahead);
     copy_async_commit();
-    copy_async_wait<2>();
+    copy_async_wait<2>();  // this tile's units, and the positions of the one after the next
     const float* c = sh.angle[buffer].cos + p.rb * (d.rot_dim / 2) + p.pair;
     const float* n = sh.angle[buffer].sin + p.rb * (d.rot_dim / 2) + p.pair;
     const uint4* from = s_unit + stage * kGradUnits * threads + threadIdx.x;
