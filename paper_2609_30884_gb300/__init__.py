@@ -450,7 +450,7 @@ class Context:
     def _norm_parts(self, rope: Rope, positions: torch.Tensor, x, gain, out, k, k_gain, k_out, eps: float) -> Tuple[int, int, int]:
         """Rows, type and parts of a call on normed heads, its descriptors packed."""
         device, buf, dim, dtype = self.device, self._parts, rope.head_dim, x.dtype
-        n, kind = len(x), _TYPES.get(dtype)
+        n, kind = x.shape[0], _TYPES.get(dtype)
         if kind is None:
             raise ValueError("x must be bfloat16, float16 or float32")
         if positions.get_device() != device:
@@ -460,7 +460,7 @@ class Context:
         _put_norm(self._norms, 0, device, "gain", gain, dtype, dim, eps)
         if k is None:
             return n, kind, 1
-        if k.dtype is not dtype or len(k) != n:
+        if k.dtype is not dtype or k.shape[0] != n:
             raise ValueError("k must have x's type and rows")
         if k_gain is None:
             raise ValueError("k needs k_gain")
@@ -542,9 +542,10 @@ class Context:
         c = self._a_row("lse", lse, n, fp32)
         k, wanted = 0, top_ids if top_ids is not None else top_logprobs
         if wanted is not None:
-            if wanted.dim() != 2 or len(wanted) != n:
+            shape = wanted.shape
+            if len(shape) != 2 or shape[0] != n:
                 raise ValueError(f"the alternatives must be [{n}, their number]")
-            k = wanted.shape[1]
+            k = shape[1]
         ids = self._a_row("top_ids", top_ids, n * k, torch.int32)
         tops = self._a_row("top_logprobs", top_logprobs, n * k, fp32)
         status = self.lib.crf_logprobs(self.h, logits.data_ptr(), kind, n, vocab, logits.stride(0), t, a, b, c, k, ids, tops,
@@ -649,38 +650,37 @@ class Context:
         return self._attention_workspace(self.lib.crf_prefix_attention_workspace_size, pool, chunks, n_q_heads, prefixes.address,
                                          prefixes.n, int(causal))
 
-    def _put_attention(self, pool: KVPool, layer: int, chunks: Chunks, q, out, workspace, lse, scale: float) -> Tuple[int, int]:
-        """Checks of an attention call's tensors; its heads are packed. KV heads and head_dim."""
-        hkv, dim = self._pool_layer(pool, layer)
-        device, n = self.device, chunks.rows
-        if chunks.device != device:
-            raise ValueError(f"the page tables must be on cuda:{device}")
-        if not chunks.attend_ok:
-            raise ValueError(f"page tables need {chunks.attend_entries} entries to attend")
-        if q.dtype != torch.bfloat16 or q.shape[0] != n:
-            raise ValueError(f"q must be bfloat16 with {n} rows")
-        heads = _put_heads(self._parts, 0, device, "q", q, out, dim)
-        self._here(workspace, lse)
-        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (n, heads)):
-            raise ValueError("lse must be a contiguous float32 [rows, heads]")
-        if 0 < scale < 2.0**-149:
-            raise ValueError("scale would be 0 in float32, which stands for 1 / sqrt(head_dim)")
-        return hkv, dim
-
     def chunk_attention(self, pool: KVPool, layer: int, chunks: Chunks, q: torch.Tensor, out: torch.Tensor,
                         workspace: torch.Tensor, lse: Optional[torch.Tensor] = None, scale: float = 0.0,
                         causal: bool = True, window: int = 0, stream=None, sinks: int = 0) -> None:
         """out = attention of the rows q [rows, heads, head_dim] (bf16) over their requests' cached keys of
         ``layer`` (see crf_chunk_attention); ``lse`` fp32 [rows, heads]; ``scale`` 0: 1 / sqrt(head_dim). With a
         ``window``, the first ``sinks`` keys stay in sight (see crf_chunk_attention_sinks)."""
-        hkv, dim = self._put_attention(pool, layer, chunks, q, out, workspace, lse, scale)
-        if window or sinks:
+        hkv, dim = self._pool_layer(pool, layer)
+        device, buf, n = self.device, self._parts, chunks.rows
+        if chunks.device != device:
+            raise ValueError(f"the page tables must be on cuda:{device}")
+        if not chunks.attend_ok:
+            raise ValueError(f"page tables need {chunks.attend_entries} entries to attend")
+        if q.dtype != torch.bfloat16 or q.shape[0] != n:
+            raise ValueError(f"q must be bfloat16 with {n} rows")
+        heads = _put_heads(buf, 0, device, "q", q, out, dim)
+        if workspace.get_device() != device or (lse is not None and lse.get_device() != device):
+            raise ValueError(f"every tensor of the call must be on cuda:{device}")
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (n, heads)):
+            raise ValueError("lse must be a contiguous float32 [rows, heads]")
+        if 0 < scale < 2.0**-149:
+            raise ValueError("scale would be 0 in float32, which stands for 1 / sqrt(head_dim)")
+        if window:
             _fits("window", window)
-            _fits("sinks", sinks)
-        status = self.lib.crf_chunk_attention_sinks(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, self._parts,
-                                                    None if lse is None else lse.data_ptr(), scale, causal, window, sinks,
-                                                    workspace.data_ptr(), workspace.numel(),
-                                                    _raw_stream(self.device) if stream is None else _stream(stream))
+        to, st = None if lse is None else lse.data_ptr(), _raw_stream(device) if stream is None else _stream(stream)
+        if sinks:
+            status = self.lib.crf_chunk_attention_sinks(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, buf, to,
+                                                        scale, causal, window, _fits("sinks", sinks), workspace.data_ptr(),
+                                                        workspace.numel(), st)
+        else:
+            status = self.lib.crf_chunk_attention(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, buf, to,
+                                                  scale, causal, window, workspace.data_ptr(), workspace.numel(), st)
         if status:
             abi.check(status)
 
@@ -689,7 +689,21 @@ class Context:
                          stream=None) -> None:
         """chunk_attention of requests that share prefixes: the keys and values that the requests of a group share are read once
         for all of them (see crf_prefix_attention)."""
-        hkv, dim = self._put_attention(pool, layer, chunks, q, out, workspace, lse, scale)
+        hkv, dim = self._pool_layer(pool, layer)
+        device, buf, n = self.device, self._parts, chunks.rows
+        if chunks.device != device:
+            raise ValueError(f"the page tables must be on cuda:{device}")
+        if not chunks.attend_ok:
+            raise ValueError(f"page tables need {chunks.attend_entries} entries to attend")
+        if q.dtype != torch.bfloat16 or q.shape[0] != n:
+            raise ValueError(f"q must be bfloat16 with {n} rows")
+        heads = _put_heads(buf, 0, device, "q", q, out, dim)
+        if workspace.get_device() != device or (lse is not None and lse.get_device() != device):
+            raise ValueError(f"every tensor of the call must be on cuda:{device}")
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (n, heads)):
+            raise ValueError("lse must be a contiguous float32 [rows, heads]")
+        if 0 < scale < 2.0**-149:
+            raise ValueError("scale would be 0 in float32, which stands for 1 / sqrt(head_dim)")
         status = self.lib.crf_prefix_attention(self.h, pool.address, layer, hkv, dim, chunks.address, chunks.n, prefixes.address,
                                                prefixes.n, self._parts, None if lse is None else lse.data_ptr(), scale, causal,
                                                workspace.data_ptr(), workspace.numel(),

@@ -1,4 +1,36 @@
-// The kernel of attention of new rows over cached keys, and the plan of its runs (chunk_attn.cu says what it computes and why it is built so).
+// Attention of a chunk of new rows over their requests' cached keys, on tcgen05. Row r of a request at position
+// p sees the keys lo <= j < hi with hi = min(n_keys, p + 1) (causal; n_keys otherwise) and lo = max(0, p - window + 1)
+// (0 without a window): o = softmax(scale q k) v, lse = log sum exp(scale q k).
+//
+// The query heads of one kv head read the same keys, so a request's rows and the group's heads are packed into
+// one axis (row r, head h of the group -> r group + h) and cut into tiles of 128 rows, the M of an MMA. Two chains
+// S -> softmax -> P V run side by side in a CTA, so that one's products fill the other's softmax:
+//   wide form    256 packed rows or a last part of them: chain t is query tile t, both read the same K/V tiles
+//   narrow form  requests of at most 128 packed rows (one token of 7 heads: 7): one query tile, chain t takes
+//                every other K/V tile, and the chains' (o, maximum, sum) meet in shared memory at the end
+// A step of the pair of chains is one K/V tile (wide) or two (narrow).
+//
+// Work: the steps of all items (request, query tile or pair, kv head) laid end to end are dealt to one CTA per SM in
+// equal runs (plan_runs). A run is a sequence of segments, whole items or parts of them; a part writes its
+// unnormalised o, maximum and sum in fp32 to the workspace and chunk_attn_merge joins an item's parts in order of
+// keys. The K/V ring runs on from segment to segment, so the copies of the next one land during this one's end.
+//
+// Warps: 0 gathers the pages of K and V tiles with TMA, 1 issues the MMAs, one thread of 2 finds the segments ahead, 3
+// sees the ring's copies land, in order, and counts them (a chain that waited for a slot's phase itself could take
+// the phase before for it: that one may be the other chain's, and copies land out of order),
+// 4-7 and 8-11 are the chains' softmax (one packed row a thread; S from TMEM, P back over it as bf16, o
+// rescaled there when the maximum grows by more than 2^8); they also bring q into shared memory (rows of any strides,
+// packed heads). Warps whose 32 rows are all padding only keep the others company. As in the prefill attention
+// (attention_tc.cu), the issuing warp waits only for each chain's P and commits only each chain's S; the softmax
+// warps check that the next K/V tiles have landed and release the ring's slots. Every wait is bounded.
+//
+// Unseen slots may hold anything: pages that no row of the CTA sees are not fetched and stay out of P V; scores of
+// unseen keys become -inf whatever they were; v of keys that no row sees is zeroed, and in tiles that only some rows
+// see an infinite or NaN element of v is zeroed and given back, at the end, to the rows that see it (0 times infinity
+// would be NaN in the others; infinities absorb whatever they are added to, so when does not matter).
+//
+// Its forms (sinks_attn.cu, prefix_attn.cu) see two ranges of keys a row, or rows of several requests at once; the loop over tiles, the ring,
+// the roles of the warps and the plan are the same.
 #pragma once
 
 #include "common.cuh"
@@ -1438,8 +1470,8 @@ struct Costs {
   int step_wide, step_narrow, segment_wide, segment_narrow, merge;
   int masked;  // of a step over a folded group's own keys, more than of another (its masks, the cleaning of v)
   bool every_run;  // the first budget counts a segment for every CTA: with few long items there are as many, and tries cost 1 us
-  int step(bool narrow) const { return narrow ? step_narrow : step_wide; }
-  int segment(bool narrow) const { return narrow ? segment_narrow : segment_wide; }
+  constexpr int step(bool narrow) const { return narrow ? step_narrow : step_wide; }
+  constexpr int segment(bool narrow) const { return narrow ? segment_narrow : segment_wide; }
 };
 // A narrow step reads two tiles. 8192 rows from nothing took 427 us with 4 units a segment, 369 with 6, 370 with 8, 377 with 10;
 // 64 single rows over 2000 keys 60 us with 2 or 4, 55 with 6.
@@ -1450,8 +1482,8 @@ constexpr Costs kPrefixCosts = {4, 4, 16, 12, 8, 2, true};
 
 // Deals the items' steps to at most `ctas` runs of at most `budget` units each; false if they do not fit. `whole`:
 // an item a run.
-template <typename Table>
-bool deal(const Table& c, const Costs& k, int n_q_heads, int n_kv_heads, bool causal, int window, int ctas, int64_t budget, bool whole,
+template <const Costs& K, typename Table>
+bool deal(const Table& c, int n_q_heads, int n_kv_heads, bool causal, int window, int ctas, int64_t budget, bool whole,
           ChunkPlan* p, int64_t* run_rows) {
   const int grp = n_q_heads / n_kv_heads;
   p->ctas = 0;
@@ -1459,7 +1491,7 @@ bool deal(const Table& c, const Costs& k, int n_q_heads, int n_kv_heads, bool ca
   int64_t left = 0;     // of the current CTA's budget
   int here = 0;         // segments of the current CTA
   auto open = [&](int req, int qt, int g, int step) {
-    if (run_rows) run_rows[p->ctas] = 0;
+    if (K.masked && run_rows) run_rows[p->ctas] = 0;
     p->run[p->ctas++] = RunStart{req, qt, g, step};
     left = budget;
     here = 0;
@@ -1468,11 +1500,11 @@ bool deal(const Table& c, const Costs& k, int n_q_heads, int n_kv_heads, bool ca
     const int rows = rows_of(c, i) * grp;
     if (rows == 0) continue;
     const bool narrow = narrow_form(rows);
-    const int unit = k.step(narrow), segment = k.segment(narrow), tile = narrow ? kM : 2 * kM, tiles = (rows + tile - 1) / tile;
+    const int unit = K.step(narrow), segment = K.segment(narrow), tile = narrow ? kM : 2 * kM, tiles = (rows + tile - 1) / tile;
     for (int qt = tiles - 1; qt >= 0; --qt) {
       const int q0 = qt * tile, q1 = std::min(q0 + tile, rows) - 1;
       const int steps = steps_of(c, i, q0, q1, grp, causal, window, narrow);
-      const int cheap = shared_steps(c, i, narrow, steps);
+      const int cheap = K.masked ? shared_steps(c, i, narrow, steps) : steps;
       for (int g = 0; g < n_kv_heads; ++g) {
         int step = 0, first_cta = -1, first_slot = 0, parts = 0;
         do {
@@ -1482,17 +1514,19 @@ bool deal(const Table& c, const Costs& k, int n_q_heads, int n_kv_heads, bool ca
             open(i, qt, g, step);
           }
           left -= segment;
-          if (run_rows) run_rows[p->ctas - 1] += q1 - q0 + 1;
-          int take = whole ? steps : static_cast<int>(std::min<int64_t>(std::max(cheap - step, 0), left / unit));
+          if (K.masked && run_rows) run_rows[p->ctas - 1] += q1 - q0 + 1;
+          int take = whole ? steps : static_cast<int>(std::min<int64_t>(std::max((K.masked ? cheap : steps) - step, 0), left / unit));
           left -= take * unit;
-          if (!whole && step + take >= cheap) {
-            const int more = static_cast<int>(std::min<int64_t>(steps - step - take, left / (unit + k.masked)));
-            take += more;
-            left -= more * (unit + k.masked);
-          }
-          if (take == 0 && step < steps) {  // a segment of one step at least
-            take = 1;
-            left -= unit;
+          if (K.masked && !whole) {
+            if (step + take >= cheap) {
+              const int more = static_cast<int>(std::min<int64_t>(steps - step - take, left / (unit + K.masked)));
+              take += more;
+              left -= more * (unit + K.masked);
+            }
+            if (take == 0 && step < steps) {  // a segment of one step at least
+              take = 1;
+              left -= unit;
+            }
           }
           p->longest = std::max(p->longest, take);
           if (parts++ == 0) {
@@ -1518,8 +1552,8 @@ bool deal(const Table& c, const Costs& k, int n_q_heads, int n_kv_heads, bool ca
 
 
 // `run_rows`: null, or every segment is a part (so nothing is gained by whole items), and receives the rows of each run's.
-template <typename Table>
-void plan_runs(const Table& c, const Costs& k, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms, int64_t* run_rows, ChunkPlan* p) {
+template <const Costs& K, typename Table>
+void plan_runs(const Table& c, int n_q_heads, int n_kv_heads, bool causal, int window, int num_sms, int64_t* run_rows, ChunkPlan* p) {
   const int grp = n_q_heads / n_kv_heads, ctas = std::min(num_sms, kMaxCtas);
   int64_t total = 0, items = 0;
   int longest = 0, least = 1;  // units of the longest item's steps, of a segment of one step
@@ -1528,25 +1562,25 @@ void plan_runs(const Table& c, const Costs& k, int n_q_heads, int n_kv_heads, bo
     const int rows = rows_of(c, i) * grp;
     if (rows == 0) continue;
     const bool narrow = narrow_form(rows);
-    const int unit = k.step(narrow), segment = k.segment(narrow), tile = narrow ? kM : 2 * kM;
+    const int unit = K.step(narrow), segment = K.segment(narrow), tile = narrow ? kM : 2 * kM;
     least = std::max(least, segment + unit);
     all_narrow = all_narrow && narrow;
     for (int q0 = 0; q0 < rows; q0 += tile) {
       const int q1 = std::min(q0 + tile, rows) - 1;
       const int steps = steps_of(c, i, q0, q1, grp, causal, window, narrow);
-      total += static_cast<int64_t>(n_kv_heads) * (steps * unit + (steps - shared_steps(c, i, narrow, steps)) * k.masked + segment);
+      total += static_cast<int64_t>(n_kv_heads) * (steps * unit + (K.masked ? (steps - shared_steps(c, i, narrow, steps)) * K.masked : 0) + segment);
       items += n_kv_heads;
       longest = std::max(longest, steps * unit);
     }
   }
   // An even share at first; runs that end early for want of a whole step, and the segments that they continue, need some
   // more. Few short items stay whole: the merge costs more than the steps that it saves.
-  if (k.every_run) total += std::max<int64_t>(0, ctas - items) * k.segment(all_narrow);
+  if (K.every_run) total += std::max<int64_t>(0, ctas - items) * K.segment(all_narrow);
   int64_t budget = std::max<int64_t>(least, (total + ctas - 1) / ctas);
-  const bool whole = !run_rows && items <= ctas && longest <= budget - k.segment_wide + k.merge;
-  if (items > 2 * ctas) budget += k.segment_wide;  // nearly every run continues a segment: fewer tries
+  const bool whole = !run_rows && items <= ctas && longest <= budget - K.segment_wide + K.merge;
+  if (items > 2 * ctas) budget += K.segment_wide;  // nearly every run continues a segment: fewer tries
   for (int tries = 0;; ++tries) {
-    if (deal(c, k, n_q_heads, n_kv_heads, causal, window, ctas, budget, whole, p, run_rows)) return;
+    if (deal<K>(c, n_q_heads, n_kv_heads, causal, window, ctas, budget, whole, p, run_rows)) return;
     budget += tries < 12 ? 1 : budget / 8 + 1;
   }
 }

@@ -42,7 +42,7 @@ extern "C" int make(int n, const int* n_new, const int* pos, const int* n_keys, 
   if (!prefixes) {
     memset(&with_sinks, 0, sizeof(with_sinks));
     with_sinks.c = SinksTable{t, sinks};
-    plan_runs(with_sinks.c, kSinksCosts, hq, hkv, causal != 0, window, sms, nullptr, &plan.runs);
+    plan_runs<kSinksCosts>(with_sinks.c, hq, hkv, causal != 0, window, sms, nullptr, &plan.runs);
     memcpy(with_sinks.run, plan.runs.run, sizeof(with_sinks.run));
     with_sinks.d.n_q_heads = hq, with_sinks.d.n_kv_heads = hkv, with_sinks.d.causal = causal != 0, with_sinks.d.window = window;
     const int v[7] = {0, n, 0, 0, 0, plan.runs.cuts, 0};
