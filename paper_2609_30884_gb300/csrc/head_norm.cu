@@ -9,15 +9,15 @@
 // Bound by memory: every element is read once and written once. As in rotary.cu a thread owns one 16-byte unit of a head (for
 // the half layout two, the pair's halves), in four neighbouring heads, two in a gradient; here the lanes of a head, a power of
 // two, are neighbours in a warp and join the sum of squares by shuffles. What it takes to stay near memory is few instructions: 512
-// elements of a warp's step took 283 of them at first (16384 bf16 rows of 32 heads 58 us, the gradient 155; now 45, 89% of the
-// copy rate, and 86, 69%, still bound by instructions). So places are found by shifts, arithmetic is on two elements an
-// instruction, gains and angles are multiplied once for a thread's heads, and all of its heads' shuffles go level by level. Heads
+// elements of a warp's step took 283 of them at first (16384 bf16 rows of 32 heads 58 us, the gradient 155; now 44, 90% of the
+// copy rate, and 73, 81%). So places are found by shifts, arithmetic is on two elements an instruction, gains and angles are
+// multiplied once for a thread's heads, and all of its heads' shuffles go level by level. Heads
 // whose units are no such thing (odd sizes, strides or alignments) take a warp each, an element or a pair a lane.
 //
 // The gains' gradient: a thread keeps the same elements of its heads' part over all the rows that its block walks, so
 // their sums stay in its registers; a block's sums meet in shared memory, the blocks' in a second small kernel, both in a
-// fixed order: the same inputs give the same bits. The next row's loads are on their way, and its angles formed, before the block's one
-// barrier a row.
+// fixed order: the same inputs give the same bits. The next rows' loads are on their way, and a batch of their angles formed, before the
+// block's one barrier a batch.
 #include "../../include/crf.h"
 #include "rotary.cuh"
 
@@ -151,6 +151,26 @@ __device__ __forceinline__ void form_angles(const RotaryDesc& d, const int* pos,
   }
 }
 
+// N neighbouring angles, from where N of them are aligned to what they take (at most 16 bytes).
+template <int N>
+__device__ __forceinline__ void load_angles(const float* from, float (&to)[N]) {
+  if constexpr (N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const float4 v = *reinterpret_cast<const float4*>(from + i);
+      to[i] = v.x;
+      to[i + 1] = v.y;
+      to[i + 2] = v.z;
+      to[i + 3] = v.w;
+    }
+  } else {
+    static_assert(N == 2, "an angle a pair of 8 or 4 elements");
+    const float2 v = *reinterpret_cast<const float2*>(from);
+    to[0] = v.x;
+    to[1] = v.y;
+  }
+}
+
 // ---------------------------------------------------------------- forward, 16-byte units
 template <typename T, int VEC, bool INTER, int BATCH>
 __global__ void __launch_bounds__(kRotThreads, BATCH == 1 ? 1 : 3) head_norm_kernel(const __grid_constant__ NormArgs a) {
@@ -231,8 +251,9 @@ __global__ void __launch_bounds__(kRotThreads, BATCH == 1 ? 1 : 3) head_norm_ker
   uint64_t k0[P], k1[P], k2[H], k3[H];
   unpack_pairs<T, VEC>(wl, k0);
   if (p.turning) {
-    const float* c = s_angle.cos + p.rb * (d.rot_dim / 2) + p.pair;
-    const float* n = s_angle.sin + p.rb * (d.rot_dim / 2) + p.pair;
+    float c[INTER ? P : VEC], n[INTER ? P : VEC];
+    load_angles(s_angle.cos + p.rb * (d.rot_dim / 2) + p.pair, c);
+    load_angles(s_angle.sin + p.rb * (d.rot_dim / 2) + p.pair, n);
     if constexpr (INTER) {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
@@ -361,6 +382,7 @@ struct NormGradArgs {
   HeadNormGradDesc d;
   Tiling t;
   int row_blocks;           // blocks along the rows: each takes every row_blocks-th tile of rows
+  int log_batch;
   float* partial;           // [part][block][head_dim]
 };
 // A thread's heads: as many as make four units of x and g.
@@ -368,9 +390,10 @@ template <bool INTER>
 constexpr int kGradBatch = INTER ? 2 : 1;
 constexpr int kGradUnits = 4;
 // A thread's units of the next two tiles are on their way into places of its own in shared memory: in registers one tile took 128
-// of them and two blocks an SM had too few bytes in flight. Positions go four tiles ahead, because all threads read what a few of
-// them copied: the next tile's have landed, and a barrier has followed, one tile before its angles are formed.
-constexpr int kStages = 3, kPositions = 4;
+// of them and two blocks an SM had too few bytes in flight. Angles are formed for a batch of 2^log_batch tiles, so that there is work for
+// all threads and a barrier a batch: 16384 bf16 rows of 32 heads take 94 us with a barrier a tile, 82, 77 and 73 with batches of 2, 4 and 8. Positions go four batches ahead, because all threads read what a few of them copied: the next batch's
+// have landed, and a barrier has followed, one batch before its angles are formed.
+constexpr int kStages = 3, kPositions = 4, kLogBatch = 3;
 struct NormGradShared {
   Angles angle[2];
   int pos[kPositions][kRotMaxRows];
@@ -412,12 +435,14 @@ __global__ void __launch_bounds__(kRotThreads, 2) head_norm_grad_kernel(const __
   const T* g_at = static_cast<const T*>(q == 0 ? a.d.grad[0] : a.d.grad[1]) + first_row * g_row + p.head * g_head + p.e0;
   T* o_at = static_cast<T*>(t.out) + first_row * t.out_row + p.head * t.out_head + p.e0;
   const int64_t x_jump = jump * t.x_row, g_jump = jump * g_row, o_jump = jump * t.out_row;
-  int64_t f_row = first_row, pos_row = (static_cast<int64_t>(blockIdx.x) << log_rows) + threadIdx.x;
+  const int log_all = log_rows + a.log_batch;  // rows of a batch
+  int64_t f_row = first_row;
+  int64_t pos_row = ((blockIdx.x + static_cast<int64_t>(threadIdx.x >> log_rows) * a.row_blocks) << log_rows) + (threadIdx.x & ((1 << log_rows) - 1));
   const int heads = p.heads;
   griddep_wait();
   auto fetch_pos = [&](int slot) {
-    if (threadIdx.x < 1 << log_rows && pos_row < d.n_rows) copy_async4(&sh.pos[slot][threadIdx.x], d.positions + pos_row);
-    pos_row += jump;
+    if (threadIdx.x < 1 << log_all && pos_row < d.n_rows) copy_async4(&sh.pos[slot][threadIdx.x], d.positions + pos_row);
+    pos_row += jump << a.log_batch;
   };
   auto fetch = [&](int stage) {
     if (f_row < d.n_rows) {
@@ -451,23 +476,26 @@ __global__ void __launch_bounds__(kRotThreads, 2) head_norm_grad_kernel(const __
       if (two) unpack_pairs<T, VEC>(*reinterpret_cast<const uint4*>(gain + p.e1), wy);
   }
   copy_async_wait<1>();
-  __syncthreads();  // the first three tiles' positions
+  __syncthreads();  // the first three batches' positions
   int64_t row = first_row;
+  // of the batch from the tile of row `at` on (behind the last row: of no position in particular)
   auto angles = [&](int64_t at, int slot, Angles& to) {
-    const int64_t row0 = at - p.rb;
-    if (row0 < d.n_rows) form_angles(d, sh.pos[slot], log_rows, static_cast<int>(min(static_cast<int64_t>(1) << log_rows, d.n_rows - row0)), to);
+    if (at - p.rb < d.n_rows) form_angles(d, sh.pos[slot], log_all, 1 << log_all, to);
   };
   angles(row, 0, sh.angle[0]);
   __syncthreads();
-  int stage = 0, ahead = 2, pos = 0, buffer = 0;
+  int stage = 0, ahead = 2, pos = 0, buffer = 0, in = 0;  // in: the tile of the batch
   for (int64_t tile = blockIdx.x; tile < tiles; tile += a.row_blocks) {
-    // (the stage of the tile before and this one's positions are free: all have passed the barrier behind them)
-    fetch_pos(pos);
+    if (in == 0) fetch_pos(pos);  // (this batch's are free: all have passed the barrier behind them)
     fetch(ahead);
     copy_async_commit();
-    copy_async_wait<2>();  // this tile's units, and the positions of the one after the next
-    const float* c = sh.angle[buffer].cos + p.rb * (d.rot_dim / 2) + p.pair;
-    const float* n = sh.angle[buffer].sin + p.rb * (d.rot_dim / 2) + p.pair;
+    copy_async_wait<2>();  // this tile's units; positions of a batch or more ahead
+    const int angle = ((in << log_rows) + p.rb) * (d.rot_dim / 2) + p.pair;
+    float c[INTER ? P : VEC], n[INTER ? P : VEC];
+    if (p.turning) {
+      load_angles(sh.angle[buffer].cos + angle, c);
+      load_angles(sh.angle[buffer].sin + angle, n);
+    }
     const uint4* from = s_unit + stage * kGradUnits * threads + threadIdx.x;
     const int now = row < d.n_rows ? heads : 0;
     // u: the gradient, turned back
@@ -536,12 +564,15 @@ __global__ void __launch_bounds__(kRotThreads, 2) head_norm_grad_kernel(const __
     }
     o_at += o_jump;
     row += jump;
-    buffer ^= 1;
-    pos = (pos + 1) & (kPositions - 1);
     stage = stage == kStages - 1 ? 0 : stage + 1;
     ahead = ahead == kStages - 1 ? 0 : ahead + 1;
-    angles(row, pos, sh.angle[buffer]);
-    __syncthreads();
+    if (++in == 1 << a.log_batch) {
+      in = 0;
+      buffer ^= 1;
+      pos = (pos + 1) & (kPositions - 1);
+      angles(row, pos, sh.angle[buffer]);
+      __syncthreads();
+    }
   }
   copy_async_wait<0>();
   __syncthreads();
@@ -791,6 +822,9 @@ cudaError_t launch_grad(const HeadNormGradDesc& g, float* partial, int num_sms, 
     const int64_t tiles = (static_cast<int64_t>(d.n_rows) + (1 << a.t.log_rows) - 1) >> a.t.log_rows;
     a.row_blocks = static_cast<int>(std::min<int64_t>(tiles, std::max(1, resident * num_sms / columns)));
     sums.blocks = a.row_blocks * columns;
+    while (a.log_batch < kLogBatch && tiles >> a.log_batch > a.row_blocks && (1 << (a.t.log_rows + a.log_batch + 1)) <= kRotMaxRows &&
+           (d.rot_dim / 2) << (a.t.log_rows + a.log_batch + 1) <= kRotMaxAngles)
+      ++a.log_batch;
     e = d.interleaved ? launch_grad_units<T, true>(a, threads, columns, stream) : launch_grad_units<T, false>(a, threads, columns, stream);
   } else {
     sums.blocks = std::min(d.n_rows, 4 * num_sms);
