@@ -24,13 +24,15 @@
 
 #include <algorithm>
 #include <cstring>
+#include <type_traits>
 
 namespace crf {
 
 namespace {
 
 constexpr int kLogThreads = 256;   // at most; four blocks an SM: 1021 fp32 rows of 152064 take 91 us so, 96 with 512 threads and two
-constexpr int kStrip = 1024;       // elements of a warp's step
+constexpr int kStrip = 1024;       // elements of a warp's step, of a short row or at a row's ends
+constexpr int kWide = 8;           // 16-byte units of a lane in a step within a long row: 2001 bf16 rows of 151936 103 us, 109 with 4
 constexpr int kList = 512;         // elements that are ranked by counting
 constexpr int kChosen = 64;        // lanes that are read again, at most
 constexpr int kPieces = 128;       // pieces of their elements, at most
@@ -56,6 +58,29 @@ __device__ __forceinline__ float value_of(uint32_t order) {
   if (order <= 1u) return NAN;
   return __uint_as_float(order >> 31 ? order & 0x7fffffffu : ~order);
 }
+
+// The maximum of units, NaN only while there is nothing else; of 16-bit types two elements an instruction, in the type.
+template <typename T>
+struct UnitMax {
+  uint32_t m = 0x7fff7fffu;  // two NaN, of both types
+  __device__ __forceinline__ void add(const Unit<T, 8>& u) {
+    const uint4 w = *reinterpret_cast<const uint4*>(&u);
+    for (const uint32_t x : {w.x, w.y, w.z, w.w}) {
+      if constexpr (std::is_same_v<T, __half>) asm("max.f16x2 %0, %0, %1;" : "+r"(m) : "r"(x));
+      else asm("max.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(x));
+    }
+  }
+  __device__ __forceinline__ float value() const {
+    const float2 f = unpack2(T(), m);
+    return fmaxf(f.x, f.y);
+  }
+};
+template <>
+struct UnitMax<float> {
+  float m = NAN;
+  __device__ __forceinline__ void add(const Unit<float, 4>& u) { m = fmax3(fmax3(m, u.e[0], u.e[1]), u.e[2], u.e[3]); }
+  __device__ __forceinline__ float value() const { return m; }
+};
 
 // A running maximum, sum of 2^x and sum of 2^x x.
 struct Sums {
@@ -112,22 +137,23 @@ __device__ __forceinline__ float load_logit(const T* p) {
 
 // Adds a strip to a lane's sums, and says the maximum of the lane's elements of it, by halves (its even and odd units).
 // Lane l has units l, l + 32 ... of the strip.
-template <typename T>
+template <typename T, int kLoads>
 __device__ __forceinline__ float2 add_strip(const T* base, int v0, int skew, int end, int lane, Sums& acc, bool& any) {
   using U = Unit<T, 16 / sizeof(T)>;
-  constexpr int VEC = 16 / sizeof(T), kLoads = kStrip / (32 * VEC);
+  constexpr int VEC = 16 / sizeof(T), kStep = 32 * VEC * kLoads;
   float half[2] = {NAN, NAN}, mx;
-  if (v0 >= skew && v0 + kStrip <= end) {
+  if (v0 >= skew && v0 + kStep <= end) {
     U u[kLoads];
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) u[j] = *reinterpret_cast<const U*>(base + v0 + (j * 32 + lane) * VEC);
+    UnitMax<T> even, odd;
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      float x[VEC];
-      unpack(u[j], x);
-#pragma unroll
-      for (int i = 0; i < VEC; i += 2) half[j & 1] = fmax3(half[j & 1], x[i], x[i + 1]);
+    for (int j = 0; j < kLoads; j += 2) {
+      even.add(u[j]);
+      odd.add(u[j + 1]);
     }
+    half[0] = even.value();
+    half[1] = odd.value();
     mx = fmaxf(half[0], half[1]);
     if (mx > acc.m) acc.raise(mx);
     any = true;
@@ -216,7 +242,8 @@ __device__ __forceinline__ void put_top(const LogprobsDesc& d, int row, int at, 
 template <typename T, int C>
 __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logprobs_kernel(const __grid_constant__ LogprobsDesc d) {
   using U = Unit<T, 16 / sizeof(T)>;
-  constexpr int VEC = 16 / sizeof(T), kLoads = kStrip / (32 * VEC);
+  constexpr int VEC = 16 / sizeof(T), kLoads = kWide, kNarrow = kStrip / (32 * VEC), kStep = 32 * VEC * kLoads;
+  static_assert(kStep % kStrip == 0, "a step at a row's ends is gone through in strips");
   __shared__ LogShared sh;
   griddep_launch_dependents();
   const int row = blockIdx.x / C, rank = C > 1 ? static_cast<int>(cluster_ctarank()) : 0;
@@ -224,7 +251,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
   const T* z = static_cast<const T*>(d.z) + row * d.z_row;
   // virtual index v = element + skew: 16-byte aligned where v is a multiple of VEC
   const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
-  const int end = d.vocab + skew, strips = (end + kStrip - 1) / kStrip;
+  const int end = d.vocab + skew, strips = (end + kStep - 1) / kStep;
   const T* base = z - skew;  // never read before z
   // a lane's elements in pieces: its every fourth strip, or those of each CTA of the cluster, a maximum each
   constexpr int kParts = C > 1 ? C : 4;
@@ -245,8 +272,13 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
   griddep_wait();
   for (int st = rank * warps + warp; st < strips; st += C * warps, ++turn) {
     // lane l has units l, l + 32 ... of the strip
-    const int v0 = st * kStrip;
-    note(add_strip(base, v0, skew, end, lane, acc, any));
+    const int v0 = st * kStep;
+    if (v0 >= skew && v0 + kStep <= end) {
+      note(add_strip<T, kLoads>(base, v0, skew, end, lane, acc, any));
+    } else {
+#pragma unroll 1
+      for (int v = v0; v < min(v0 + kStep, end); v += kStrip) note(add_strip<T, kNarrow>(base, v, skew, end, lane, acc, any));
+    }
   }
   sh.lane[threadIdx.x] = any ? order_of(acc.m) : 0u;
 #pragma unroll
@@ -337,7 +369,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
     const int turns = (strips + kParts * warps - 1) / (kParts * warps), units = min(sh.n_chosen, kPieces) * turns * kLoads;
     auto unit_at = [&](int e) {
       const int pair = e / kLoads, at = sh.chosen[pair / turns], thread = at % kLogThreads;
-      return ((at / kLogThreads + pair % turns * kParts) * warps + thread / 32) * kStrip + (e % kLoads * 32 + thread % 32) * VEC;
+      return ((at / kLogThreads + pair % turns * kParts) * warps + thread / 32) * kStep + (e % kLoads * 32 + thread % 32) * VEC;
     };
     for (int e0 = warp * 32; e0 < units; e0 += kAhead * blockDim.x) {
       U u[kAhead];  // all in flight
@@ -489,7 +521,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) logprobs_rows_kernel(const __g
   // the maxima of a lane's elements by halves: 64 groups of the row's elements
   float even = -INFINITY, odd = -INFINITY;
   for (int st = 0; st < strips; ++st) {
-    const float2 half = add_strip(base, st * kStrip, skew, end, lane, acc, any);
+    const float2 half = add_strip<T, kLoads>(base, st * kStrip, skew, end, lane, acc, any);
     even = fmaxf(even, half.x);
     odd = fmaxf(odd, half.y);
   }
@@ -665,7 +697,10 @@ cudaError_t launch_type(const LogprobsDesc& d, int num_sms, cudaStream_t stream)
   // and 26 with once, 19 and 26 with three times), each with four strips at least
   int c = 1;
   while (c < 8 && static_cast<int64_t>(d.n_rows) * c < 2 * num_sms && strips >= 4 * c) c *= 2;
-  const dim3 grid(static_cast<unsigned>(d.n_rows) * c), block(32 * std::min(kLogThreads / 32, (strips + c - 1) / c));
+  constexpr int kStep = 32 * 16 / static_cast<int>(sizeof(T)) * kWide;
+  // as few warps as take no more turns: 700 bf16 rows of 20011 ten steps a row by five warps, all resident at once
+  const int steps = ((d.vocab + 15 + kStep - 1) / kStep + c - 1) / c, most = kLogThreads / 32, turns = (steps + most - 1) / most;
+  const dim3 grid(static_cast<unsigned>(d.n_rows) * c), block(32 * ((steps + turns - 1) / turns));
   PdlScope pdl;
   switch (c) {
     case 1: return launch_kernel(logprobs_kernel<T, 1>, grid, block, 0, stream, d);
