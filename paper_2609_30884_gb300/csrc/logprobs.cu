@@ -30,9 +30,9 @@ namespace crf {
 
 namespace {
 
-constexpr int kLogThreads = 256;   // at most; four blocks an SM: 1021 fp32 rows of 152064 take 91 us so, 96 with 512 threads and two
+constexpr int kLogThreads = 256;   // at most; four blocks an SM: 1021 fp32 rows of 152064 take 89 us so, 96 with 512 threads and two
 constexpr int kStrip = 1024;       // elements of a warp's step, of a short row or at a row's ends
-constexpr int kWide = 8;           // 16-byte units of a lane in a step within a long row: 2001 bf16 rows of 151936 103 us, 109 with 4
+constexpr int kWide = 8;           // 16-byte units of a lane in a step within a long row: 2001 bf16 rows of 151936 98 us, some 5 more with 4
 constexpr int kList = 512;         // elements that are ranked by counting
 constexpr int kChosen = 64;        // lanes that are read again, at most
 constexpr int kPieces = 128;       // pieces of their elements, at most
@@ -253,20 +253,21 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
   const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
   const int end = d.vocab + skew, strips = (end + kStep - 1) / kStep;
   const T* base = z - skew;  // never read before z
-  // a lane's elements in pieces: its every fourth strip, or those of each CTA of the cluster, a maximum each
-  constexpr int kParts = C > 1 ? C : 4;
+  // a lane's elements in pieces, a maximum each: those of each CTA of the cluster, or halves of every other step
+  constexpr int kSplit = C > 1 ? C : 2, kHalves = C > 1 ? 1 : 2, kParts = kSplit * kHalves;
   Sums acc{-INFINITY, 0.f, 0.f};
-  float piece[C > 1 ? 1 : kParts];
-#pragma unroll
-  for (float& p : piece) p = -INFINITY;
+  float piece[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // without a cluster
   bool any = false;
   int turn = 0;
   auto note = [&](float2 half) {
-    const float mx = fmaxf(half.x, half.y);
-    if (C == 1 && d.n_top > 0) {
+    if constexpr (C == 1) {
+      if (d.n_top == 0) return;
 #pragma unroll
-      for (int i = 0; i < kParts; ++i)
-        if ((turn & (kParts - 1)) == i) piece[i % (C > 1 ? 1 : kParts)] = fmaxf(piece[i % (C > 1 ? 1 : kParts)], mx);
+      for (int i = 0; i < 4; i += 2)
+        if ((turn & 1) == i / 2) {
+          piece[i] = fmaxf(piece[i], half.x);
+          piece[i + 1] = fmaxf(piece[i + 1], half.y);
+        }
     }
   };
   griddep_wait();
@@ -320,7 +321,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
     cluster_sync();
   } else {
 #pragma unroll
-    for (int i = 0; i < kParts; ++i) part[i] = order_of(piece[i % (C > 1 ? 1 : kParts)]);
+    for (int i = 0; i < kParts; ++i) part[i] = order_of(piece[i & 3]);
     __syncthreads();
   }
   const float s = sh.cta.s, lse = lse_of(sh.cta);
@@ -365,11 +366,12 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
         }
     }
     __syncthreads();
-    // piece i of warp w has the strips i warps + w, (i + kParts) warps + w ... of the row
-    const int turns = (strips + kParts * warps - 1) / (kParts * warps), units = min(sh.n_chosen, kPieces) * turns * kLoads;
+    // piece i of warp w has the steps (i / kHalves) warps + w, (i / kHalves + kSplit) warps + w ... of the row, or a half of their units
+    constexpr int kUnits = kLoads / kHalves;
+    const int turns = (strips + kSplit * warps - 1) / (kSplit * warps), units = min(sh.n_chosen, kPieces) * turns * kUnits;
     auto unit_at = [&](int e) {
-      const int pair = e / kLoads, at = sh.chosen[pair / turns], thread = at % kLogThreads;
-      return ((at / kLogThreads + pair % turns * kParts) * warps + thread / 32) * kStep + (e % kLoads * 32 + thread % 32) * VEC;
+      const int pair = e / kUnits, at = sh.chosen[pair / turns], thread = at % kLogThreads, i = at / kLogThreads;
+      return ((i / kHalves + pair % turns * kSplit) * warps + thread / 32) * kStep + ((e % kUnits * kHalves + i % kHalves) * 32 + thread % 32) * VEC;
     };
     for (int e0 = warp * 32; e0 < units; e0 += kAhead * blockDim.x) {
       U u[kAhead];  // all in flight
@@ -686,18 +688,19 @@ __global__ void __launch_bounds__(kGradThreads) logprobs_grad_kernel(const __gri
 template <typename T>
 cudaError_t launch_type(const LogprobsDesc& d, int num_sms, cudaStream_t stream) {
   const int strips = (d.vocab + 15 + kStrip - 1) / kStrip;
-  // Short rows are a warp's each, many of up to eight strips too: 16384 bf16 rows of 512 take 14 us so with no alternatives and 35
-  // with 32, 36 and 304 as blocks; of 8000, 55 and 105, 130 and 267 as blocks. 1500 of 8000 take the same either way, 100 take 15, 12 as blocks.
+  // Short rows are a warp's each, many of up to eight strips too: 16384 bf16 rows of 4000 take 34 us so without alternatives and 68
+  // with 32, 70 and 168 as blocks; of 8000, 54 and 104, 81 and 182 as blocks; 2500 of 8000, 16 and 31, 18 and 34 as blocks. Fewer rows, or
+  // longer ones, are faster as blocks (100 of 8000 with 32: 9, 15 a warp each).
   if (strips <= 2 || (strips <= 8 && d.n_rows >= 16 * num_sms)) {
     const int w = std::max(1, std::min(kRowWarps, d.n_rows / num_sms));
     PdlScope pdl;
     return launch_kernel(logprobs_rows_kernel<T>, dim3((d.n_rows + w - 1) / w), dim3(32 * w), 0, stream, d);
   }
   // a row's CTAs: enough that few rows fill the SMs twice (100 and 200 fp32 rows of 152064 take 14 and 23 us so, 16
-  // and 26 with once, 19 and 26 with three times), each with four strips at least
-  int c = 1;
-  while (c < 8 && static_cast<int64_t>(d.n_rows) * c < 2 * num_sms && strips >= 4 * c) c *= 2;
+  // and 26 with once, 19 and 26 with three times), each with two steps at least, so that 32 alternatives find groups enough
   constexpr int kStep = 32 * 16 / static_cast<int>(sizeof(T)) * kWide;
+  int c = 1;
+  while (c < 8 && static_cast<int64_t>(d.n_rows) * c < 2 * num_sms && d.vocab >= 4 * c * kStep) c *= 2;
   // as few warps as take no more turns: 700 bf16 rows of 20011 ten steps a row by five warps, all resident at once
   const int steps = ((d.vocab + 15 + kStep - 1) / kStep + c - 1) / c, most = kLogThreads / 32, turns = (steps + most - 1) / most;
   const dim3 grid(static_cast<unsigned>(d.n_rows) * c), block(32 * ((steps + turns - 1) / turns));
