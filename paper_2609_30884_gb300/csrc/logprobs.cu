@@ -30,9 +30,9 @@ namespace crf {
 
 namespace {
 
-constexpr int kLogThreads = 256;   // at most; four blocks an SM: 1021 fp32 rows of 152064 take 89 us so, 96 with 512 threads and two
+constexpr int kLogThreads = 256;   // at most; four blocks an SM: 1021 fp32 rows of 152064 take 88 us so, 96 with 512 threads and two
 constexpr int kStrip = 1024;       // elements of a warp's step, of a short row or at a row's ends
-constexpr int kWide = 8;           // 16-byte units of a lane in a step within a long row: 2001 bf16 rows of 151936 98 us, some 5 more with 4
+constexpr int kWide = 8;           // 16-byte units of a lane in a step within a long row: 2001 bf16 rows of 151936 96 us, some 5 more with 4
 constexpr int kList = 512;         // elements that are ranked by counting
 constexpr int kChosen = 64;        // lanes that are read again, at most
 constexpr int kPieces = 128;       // pieces of their elements, at most

@@ -14,7 +14,8 @@
 // latency than it saves: the requests are then attended one by one.
 //
 // Bound by latency at the usual sizes: 32 single rows (28 heads over 4) of 15000 shared keys and up to 600 of their own take 29 us (129 one by one),
-// 64 of them 39 (241), 128 over 4000 keys 38 (137): some 18 steps a run of 1.6 us, q, and the merge of 7 us, where the bytes take 6.
+// 64 of them 39 (241), 128 over 4000 keys 38 (137). A start of 4.5 us, some six steps a run of 1.6 to 2.4, q and the end of a part 5.5, the
+// merge 7, where the bytes take 6.
 #include "chunk_attn.cuh"
 
 namespace crf {
