@@ -72,20 +72,17 @@ __device__ __forceinline__ Place place_of(const Tiling& a, const RotaryDesc& d) 
   return t;
 }
 
-// Positions, and the pages of rows that go into a cache (-1: no page of the pool).
-__device__ __forceinline__ void find_row(const RotaryDesc& d, const ChunkTable& c, int r, int* pos, int* page) {
-  *page = 0;
-  if (d.positions) {
-    *pos = d.positions[r];
-    return;
-  }
+// Position of row r of a cache's requests, and its page as the table has it.
+__device__ __forceinline__ void find_row(const ChunkTable& c, int r, int* pos, int* page) {
   const int i = chunk_of_row(c, r);
   *pos = c.pos[i] + (r - c.row0[i]);
   *page = c.pt[i][*pos / kPage];
-  if (*page < 0 || *page >= c.num_pages) {
-    if (d.status) atomicOr(d.status, kStatusBounds);
-    *page = -1;  // its writes are left out
-  }
+}
+// The page, or -1 where the pool has none such: writes to it are left out.
+__device__ __forceinline__ int checked_row_page(const RotaryDesc& d, const ChunkTable& c, int page) {
+  if (page >= 0 && page < c.num_pages) return page;
+  if (d.status) atomicOr(d.status, kStatusBounds);
+  return -1;
 }
 // Where a part's row goes, and the step from head to head.
 __device__ __forceinline__ int64_t out_at(const RotaryDesc& d, const RotPart& t, int64_t row, int pos, int page) {
@@ -207,11 +204,14 @@ __global__ void __launch_bounds__(kRotThreads, BATCH == 1 ? 1 : 3) head_norm_ker
     wl = *reinterpret_cast<const uint4*>(gain + p.e0);
     if (two) wh = *reinterpret_cast<const uint4*>(gain + p.e1);
   }
+  [[maybe_unused]] int looked_up = 0;
   if constexpr (PAGED) {
-    if (threadIdx.x < here) find_row(d, a.c, static_cast<int>(row0) + threadIdx.x, &s_pos[threadIdx.x], &s_page[threadIdx.x]);
+    if (threadIdx.x < here) find_row(a.c, static_cast<int>(row0) + threadIdx.x, &s_pos[threadIdx.x], &looked_up);
     __syncthreads();
   }
   form_angles(d, PAGED ? s_pos : d.positions + row0, a.t.log_rows, here, s_angle);
+  if constexpr (PAGED)  // (the page is on its way while angles are formed)
+    if (threadIdx.x < here) s_page[threadIdx.x] = checked_row_page(d, a.c, looked_up);
   __syncthreads();
   if (__all_sync(0xffffffffu, heads == 0)) return;
   const int page = PAGED ? s_page[p.rb] : 0;
@@ -337,11 +337,19 @@ __global__ void __launch_bounds__(kRotThreads) head_norm_loose_kernel(const __gr
   const int row = blockIdx.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int pairs = d.rot_dim / 2;
   griddep_wait();
-  if (threadIdx.x == 0) find_row(d, a.c, row, s_pos, s_page);
+  if (threadIdx.x == 0) {
+    if (d.positions) {
+      s_pos[0] = d.positions[row];
+    } else {
+      int looked_up;
+      find_row(a.c, row, s_pos, &looked_up);
+      s_page[0] = checked_row_page(d, a.c, looked_up);
+    }
+  }
   __syncthreads();
   form_angles(d, s_pos, 0, 1, s_angle);
   __syncthreads();
-  const int page = s_page[0];
+  const int page = d.positions ? 0 : s_page[0];
   for (int s = warp; s < a.t.slots; s += blockDim.x / 32) {
     const int p = s >= a.t.slot0[2] ? 2 : s >= a.t.slot0[1] ? 1 : 0;
     const RotPart t = p == 0 ? d.part[0] : p == 1 ? d.part[1] : d.part[2];
