@@ -38,6 +38,7 @@ constexpr int kChosen = 64;        // lanes that are read again, at most
 constexpr int kPieces = 128;       // pieces of their elements, at most
 constexpr int kRowWarps = 8;        // rows of a block where a row is a warp's
 constexpr int kRowList = 256;       // elements that one of them ranks
+constexpr int kAheadBytes = 32768;  // of a next row: 2001 bf16 rows of 151936 with 8 alternatives 112 us, 116 without, 119 with 128 KB
 constexpr int kAhead = 4;          // units of them that a lane asks for at once
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFloor = -200.f;   // 2^x is 0 from here down; keeps an infinite x out of products
@@ -238,9 +239,9 @@ __device__ __forceinline__ void put_top(const LogprobsDesc& d, int row, int at, 
   if (d.top_logprobs) d.top_logprobs[to] = s == 0.f ? -INFINITY : value_of(static_cast<uint32_t>(key >> 32)) - lse;
 }
 
-// C: CTAs of a row, a cluster.
+// C: CTAs of a row, a cluster. next: as many rows as have blocks on the SMs at a time.
 template <typename T, int C>
-__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logprobs_kernel(const __grid_constant__ LogprobsDesc d) {
+__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logprobs_kernel(const __grid_constant__ LogprobsDesc d, int next) {
   using U = Unit<T, 16 / sizeof(T)>;
   constexpr int VEC = 16 / sizeof(T), kLoads = kWide, kNarrow = kStrip / (32 * VEC), kStep = 32 * VEC * kLoads;
   static_assert(kStep % kStrip == 0, "a step at a row's ends is gone through in strips");
@@ -280,6 +281,13 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
 #pragma unroll 1
       for (int v = v0; v < min(v0 + kStep, end); v += kStrip) note(add_strip<T, kNarrow>(base, v, skew, end, lane, acc, any));
     }
+  }
+  // While a block looks for alternatives it loads nothing: the beginning of the row that its place on the SM is likely to have next
+  // is brought to L2 meanwhile (4000 fp32 rows of 20011 with 8 alternatives 72 us, 78 without).
+  if (C == 1 && threadIdx.x == 0 && d.n_top > 0 && row + next < d.n_rows) {
+    const uintptr_t from = (reinterpret_cast<uintptr_t>(z + next * d.z_row) + 15) & ~uintptr_t{15};
+    const int bytes = min(kAheadBytes, (d.vocab - VEC) * static_cast<int>(sizeof(T))) & ~15;
+    if (bytes > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"(bytes) : "memory");
   }
   sh.lane[threadIdx.x] = any ? order_of(acc.m) : 0u;
 #pragma unroll
@@ -704,13 +712,14 @@ cudaError_t launch_type(const LogprobsDesc& d, int num_sms, cudaStream_t stream)
   // as few warps as take no more turns: 700 bf16 rows of 20011 ten steps a row by five warps, all resident at once
   const int steps = ((d.vocab + 15 + kStep - 1) / kStep + c - 1) / c, most = kLogThreads / 32, turns = (steps + most - 1) / most;
   const dim3 grid(static_cast<unsigned>(d.n_rows) * c), block(32 * ((steps + turns - 1) / turns));
+  const int next = num_sms * (4 * kLogThreads / static_cast<int>(block.x));
   PdlScope pdl;
   switch (c) {
-    case 1: return launch_kernel(logprobs_kernel<T, 1>, grid, block, 0, stream, d);
-    case 2: return launch_kernel(logprobs_kernel<T, 2>, grid, block, 0, stream, d);
-    case 4: return launch_kernel(logprobs_kernel<T, 4>, grid, block, 0, stream, d);
+    case 1: return launch_kernel(logprobs_kernel<T, 1>, grid, block, 0, stream, d, next);
+    case 2: return launch_kernel(logprobs_kernel<T, 2>, grid, block, 0, stream, d, next);
+    case 4: return launch_kernel(logprobs_kernel<T, 4>, grid, block, 0, stream, d, next);
   }
-  return launch_kernel(logprobs_kernel<T, 8>, grid, block, 0, stream, d);
+  return launch_kernel(logprobs_kernel<T, 8>, grid, block, 0, stream, d, next);
 }
 
 template <typename T>
