@@ -16,7 +16,7 @@
 // those equal to an exact bound are taken in order of index, or the k-th greatest key is found digit by digit.
 //
 // Short rows are a warp's each, which does the same within itself: the groups are halves of the lanes' elements, their bound is
-// found with ballots, and where the list does not hold what reaches it, the greatest key below the last is looked for k times.
+// found with ballots, halves of a strip that reach it are read again, and where the list does not hold what reaches it, the greatest key below the last is looked for k times.
 //
 // Rows start at any element: a row is cut at 16-byte addresses, its first and last pieces element by element.
 #include "../../include/crf.h"
@@ -38,6 +38,7 @@ constexpr int kChosen = 64;        // lanes that are read again, at most
 constexpr int kPieces = 128;       // pieces of their elements, at most
 constexpr int kRowWarps = 8;        // rows of a block where a row is a warp's
 constexpr int kRowList = 256;       // elements that one of them ranks
+constexpr int kRowStrips = 8;       // of such a row, at most
 constexpr int kAheadBytes = 32768;  // of a next row: 2001 bf16 rows of 151936 with 8 alternatives 112 us, 116 without, 119 with 128 KB
 constexpr int kAhead = 4;          // units of them that a lane asks for at once
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -513,11 +514,12 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
 
 // ---------------------------------------------------------------- a warp a row
 template <typename T>
-__global__ void __launch_bounds__(32 * kRowWarps) logprobs_rows_kernel(const __grid_constant__ LogprobsDesc d) {
+__global__ void __launch_bounds__(32 * kRowWarps, 4) logprobs_rows_kernel(const __grid_constant__ LogprobsDesc d) {
   using U = Unit<T, 16 / sizeof(T)>;
   constexpr int VEC = 16 / sizeof(T), kLoads = kStrip / (32 * VEC);
-  static_assert(kLoads * VEC == 32, "a lane's elements of a strip are the bits of a word");
   __shared__ unsigned long long lists[kRowWarps][kRowList];
+  __shared__ uint32_t maxima[kRowWarps][2 * kRowStrips][32];    // of the halves of a lane's elements of each strip
+  __shared__ uint16_t pieces[kRowWarps][2 * kRowStrips * 32];   // 32 (2 strip + half) + lane: those that are read again
   griddep_launch_dependents();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, row = blockIdx.x * (blockDim.x / 32) + warp;
   if (row >= d.n_rows) return;
@@ -534,6 +536,10 @@ __global__ void __launch_bounds__(32 * kRowWarps) logprobs_rows_kernel(const __g
     const float2 half = add_strip<T, kLoads>(base, st * kStrip, skew, end, lane, acc, any);
     even = fmaxf(even, half.x);
     odd = fmaxf(odd, half.y);
+    if (d.n_top > 0) {
+      maxima[warp][2 * st][lane] = order_of(half.x);
+      maxima[warp][2 * st + 1][lane] = order_of(half.y);
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) {
@@ -553,50 +559,67 @@ __global__ void __launch_bounds__(32 * kRowWarps) logprobs_rows_kernel(const __g
 #pragma unroll
   for (int bit = 31; bit >= 16; --bit)
     if (groups_from(least | (1u << bit)) >= k) least |= 1u << bit;
-  least = max(least, 1u);
   auto key = [&](uint32_t order, int v) { return static_cast<unsigned long long>(order) << 32 | ~static_cast<uint32_t>(v - skew); };
-  auto place = [&](int st, int bit) { return st * kStrip + (bit / VEC * 32 + lane) * VEC + bit % VEC; };
-  // what is above -inf compares as floats do (at -inf and below, groups without elements count: the whole row is listed then)
-  const bool above = least > order_of(-INFINITY);
-  if (!above) least = 1u;
-  const float bound = value_of(least);
   unsigned long long* list = lists[warp];
   int n = 0;
-  for (int st = 0; st < strips && n <= kRowList; ++st) {
-    uint32_t hits = 0;
-    U u[kLoads];  // all in flight
-    auto whole = [&](int j) { return above && mine[j & 1] >= least && place(st, j * VEC) >= skew && place(st, j * VEC) + VEC <= end; };
+  if (least > order_of(-INFINITY)) {
+    int found = 0;
+#pragma unroll 2
+    for (int h = 0; h < 2 * strips; ++h) {
+      const bool in = maxima[warp][h][lane] >= least;
+      const uint32_t ins = __ballot_sync(0xffffffffu, in);
+      if (in) pieces[warp][found + __popc(ins & ((1u << lane) - 1))] = static_cast<uint16_t>(h * 32 + lane);
+      found += __popc(ins);
+    }
+    __syncwarp();
+    constexpr int kUnits = kLoads / 2, kMany = VEC == 8 ? 4 : 6;  // what 64 registers hold; a lane's elements are the bits of a word
+    const int units = found * kUnits;
+    const float bound = value_of(least);  // above -inf, where floats compare as their orders do
+    auto unit_at = [&](int e) {
+      const int piece = pieces[warp][e / kUnits];
+      return piece / 64 * kStrip + ((e % kUnits * 2 + piece / 32 % 2) * 32 + piece % 32) * VEC;
+    };
+    for (int e0 = 0; e0 < units && n <= kRowList; e0 += 32 * kMany) {
+      U u[kMany];  // all in flight
+      int v[kMany];
+      uint32_t hits = 0;
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      if (whole(j)) u[j] = *reinterpret_cast<const U*>(base + place(st, j * VEC));
+      for (int q = 0; q < kMany; ++q) {
+        const int e = e0 + q * 32 + lane;
+        v[q] = e < units ? unit_at(e) : end;
+        if (v[q] >= skew && v[q] + VEC <= end) u[q] = *reinterpret_cast<const U*>(base + v[q]);
+      }
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      if (whole(j)) {
-        float x[VEC];
-        unpack(u[j], x);
+      for (int q = 0; q < kMany; ++q) {
+        if (v[q] >= skew && v[q] + VEC <= end) {
+          float x[VEC];
+          unpack(u[q], x);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) hits |= static_cast<uint32_t>(x[i] >= bound) << (j * VEC + i);
-      } else if (!above || mine[j & 1] >= least) {
-        const int v = place(st, j * VEC);
+          for (int i = 0; i < VEC; ++i) hits |= static_cast<uint32_t>(x[i] >= bound) << (q * VEC + i);
+        } else if (v[q] < end) {
 #pragma unroll 1
-        for (int i = 0; i < VEC; ++i)
-          if (v + i >= skew && v + i < end && order_of(load_logit(base + v + i)) >= least) hits |= 1u << (j * VEC + i);
+          for (int i = 0; i < VEC; ++i)
+            if (v[q] + i >= skew && v[q] + i < end && load_logit(base + v[q] + i) >= bound) hits |= 1u << (q * VEC + i);
+        }
+      }
+      const int count = __popc(hits);
+      int to = count;
+#pragma unroll
+      for (int o = 1; o < 32; o *= 2) {
+        const int up = __shfl_up_sync(0xffffffffu, to, o);
+        if (lane >= o) to += up;
+      }
+      int at = n + to - count;
+      n += __shfl_sync(0xffffffffu, to, 31);
+      if (n > kRowList) break;
+      for (; hits; hits &= hits - 1) {
+        const int bit = __ffs(hits) - 1, at_v = unit_at(e0 + bit / VEC * 32 + lane) + bit % VEC;
+        list[at++] = key(order_of(load_logit(base + at_v)), at_v);
       }
     }
-    const int count = __popc(hits);
-    int to = count;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-      const int up = __shfl_up_sync(0xffffffffu, to, o);
-      if (lane >= o) to += up;
-    }
-    int at = n + to - count;
-    n += __shfl_sync(0xffffffffu, to, 31);
-    if (n > kRowList) break;
-    for (; hits; hits &= hits - 1) {
-      const int v = place(st, __ffs(hits) - 1);
-      list[at++] = key(order_of(load_logit(base + v)), v);
-    }
+  } else if (d.vocab <= kRowList) {  // (groups without elements count, at -inf and below)
+    for (int v = skew + lane; v < end; v += 32) list[v - skew] = key(order_of(load_logit(base + v)), v);
+    n = d.vocab;
   }
   __syncwarp();
   if (n >= k && n <= kRowList) {
@@ -696,10 +719,10 @@ __global__ void __launch_bounds__(kGradThreads) logprobs_grad_kernel(const __gri
 template <typename T>
 cudaError_t launch_type(const LogprobsDesc& d, int num_sms, cudaStream_t stream) {
   const int strips = (d.vocab + 15 + kStrip - 1) / kStrip;
-  // Short rows are a warp's each, many of up to eight strips too: 16384 bf16 rows of 4000 take 34 us so without alternatives and 68
-  // with 32, 70 and 168 as blocks; of 8000, 54 and 104, 81 and 182 as blocks; 2500 of 8000, 16 and 31, 18 and 34 as blocks. Fewer rows, or
+  // Short rows are a warp's each, many of up to eight strips too: 16384 bf16 rows of 4000 take 34 us so without alternatives and 58
+  // with 32, 70 and 168 as blocks; of 8000, 55 and 81, 81 and 182 as blocks; 2500 of 8000, 16 and 24, 18 and 34 as blocks. Fewer rows, or
   // longer ones, are faster as blocks (100 of 8000 with 32: 9, 15 a warp each).
-  if (strips <= 2 || (strips <= 8 && d.n_rows >= 16 * num_sms)) {
+  if (strips <= 2 || (strips <= kRowStrips && d.n_rows >= 16 * num_sms)) {
     const int w = std::max(1, std::min(kRowWarps, d.n_rows / num_sms));
     PdlScope pdl;
     return launch_kernel(logprobs_rows_kernel<T>, dim3((d.n_rows + w - 1) / w), dim3(32 * w), 0, stream, d);
