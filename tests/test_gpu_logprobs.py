@@ -95,6 +95,28 @@ def test_many_rows(ctx, rows, vocab):
     assert_scored(score(ctx, z, t, 8), z, t)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("vocab", [1009, 2049, 4097, 8170, 8177])
+def test_many_short_rows(ctx, vocab, dtype):
+    g = gen(14)
+    big = logits(g, 2600, vocab + 5, dtype)
+    for first in (0, 3):
+        z = big[:, first:first + vocab]
+        t = torch.randint(-1, vocab, (2600,), device=DEV, generator=g, dtype=torch.int32)
+        for k in (0, 8, 32):
+            assert_scored(score(ctx, z, t, k), z, t)
+    ctx.check()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_short_rows_of_ties_and_extremes(ctx, dtype):
+    for vocab in (200, 700, 5000):
+        z = torch.cat([make_row(name, vocab, dtype) for name in ROWS]).repeat(210, 1)
+        for k in (1, 17, 32):
+            assert_scored(score(ctx, z, None, k), z)
+    ctx.check()
+
+
 def test_largest_vocabulary(ctx):
     g = gen(3)
     for dtype in (torch.float32, torch.bfloat16):
