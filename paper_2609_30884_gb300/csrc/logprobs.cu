@@ -16,7 +16,8 @@
 // those equal to an exact bound are taken in order of index, or the k-th greatest key is found digit by digit.
 //
 // Short rows are a warp's each, which does the same within itself: the groups are halves of the lanes' elements, their bound is
-// found with ballots, halves of a strip that reach it are read again, and where the list does not hold what reaches it, the greatest key below the last is looked for k times.
+// found with ballots, halves of a strip that reach it are read again, and where the list does not hold what reaches it, the greatest
+// key below the last is looked for k times.
 //
 // Rows start at any element: a row is cut at 16-byte addresses, its first and last pieces element by element.
 #include "../../include/crf.h"
