@@ -494,7 +494,8 @@ CRF_API crf_status crf_pages_workspace_size(crf_ctx* ctx, int num_pages, const c
  * row_stride >= vocab; that of one row is not read) gives, each output NULL if it is not wanted,
  *   lse[r]      log sum exp z
  *   logprob[r]  z_t - lse of the token t = targets[r] (device int32); 0 where t is -1, a padded row. Any other id
- *               outside [0, vocab) is read as token 0 and reported by crf_check
+ *               outside [0, vocab) is read as token 0 and reported by crf_check. Formed from the row's maximum and the log of
+ *               the sum beside it, so that the rounding of lse, which large logits make coarse, is not in it
  *   entropy[r]  lse - sum p z, p = exp(z - lse)
  *   top_ids, top_logprobs [n_rows][n_top]: the n_top (0..CRF_MAX_TOP, at most vocab) most probable tokens, descending, the lower
  *               id first among equal logits, and their log probabilities
@@ -507,7 +508,8 @@ CRF_API crf_status crf_logprobs(crf_ctx* ctx, const void* logits, int type, int 
 
 /* Its gradient with respect to the logits, from the forward call's lse and entropy:
  *   d_logits = g_logprob (1[v = t] - p) - g_entropy p (log p + entropy),
- * fp32 rounded once to `type`. g_logprob (with targets) or g_entropy (with entropy), device fp32 [n_rows], may be
+ * p = exp(z - lse) with the lse that is given (its rounding, up to 2^-24 |lse|, is a relative error of p); fp32 rounded once
+ * to `type`. g_logprob (with targets) or g_entropy (with entropy), device fp32 [n_rows], may be
  * NULL: no such term. Rows whose target is -1 have no first term; a row of lse -inf has gradient 0. d_logits has rows of
  * d_row_stride >= vocab and may be the logits themselves with the same stride; otherwise it does not overlap them. */
 CRF_API crf_status crf_logprobs_grad(crf_ctx* ctx, const void* logits, int type, int n_rows, int vocab, int64_t row_stride,

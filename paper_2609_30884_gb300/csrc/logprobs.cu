@@ -217,28 +217,30 @@ __device__ __forceinline__ float2 add_strip(const T* base, int v0, int skew, int
   return make_float2(half[0], half[1]);
 }
 
-__device__ __forceinline__ float lse_of(const Sums& t) { return t.s == 0.f ? -INFINITY : t.m + logf(t.s); }
+// Log probability of a logit from the row's maximum and the log of its sum (-inf: the row holds nothing). The maximum goes first:
+// their sum, rounded at the size of the logits, would leave that rounding in (2e-3 at logits of 60000).
+__device__ __forceinline__ float logprob_of(float z, float m, float log_s) { return log_s == -INFINITY ? -INFINITY : (z - m) - log_s; }
 
 // A row's outputs but the alternatives, by one thread.
 template <typename T>
 __device__ __forceinline__ void put_row(const LogprobsDesc& d, int row, const T* z, const Sums& t) {
-  const float lse = lse_of(t);
-  if (d.lse) d.lse[row] = lse;
-  if (d.entropy) d.entropy[row] = t.s == 0.f ? 0.f : logf(t.s) - t.d * kLn2 / t.s;
+  const float log_s = logf(t.s);
+  if (d.lse) d.lse[row] = t.s == 0.f ? -INFINITY : t.m + log_s;
+  if (d.entropy) d.entropy[row] = t.s == 0.f ? 0.f : log_s - t.d * kLn2 / t.s;
   if (d.logprob) {
     int token = d.targets[row];
     float lp = 0.f;
     if (token != -1) {
       token = checked_token(token, d.vocab, d.status);
-      lp = t.s == 0.f ? -INFINITY : load_logit(z + token) - lse;
+      lp = logprob_of(load_logit(z + token), t.m, log_s);
     }
     d.logprob[row] = lp;
   }
 }
-__device__ __forceinline__ void put_top(const LogprobsDesc& d, int row, int at, unsigned long long key, float s, float lse) {
+__device__ __forceinline__ void put_top(const LogprobsDesc& d, int row, int at, unsigned long long key, float m, float log_s) {
   const int64_t to = static_cast<int64_t>(row) * d.n_top + at;
   if (d.top_ids) d.top_ids[to] = static_cast<int32_t>(~static_cast<uint32_t>(key));
-  if (d.top_logprobs) d.top_logprobs[to] = s == 0.f ? -INFINITY : value_of(static_cast<uint32_t>(key >> 32)) - lse;
+  if (d.top_logprobs) d.top_logprobs[to] = logprob_of(value_of(static_cast<uint32_t>(key >> 32)), m, log_s);
 }
 
 // C: CTAs of a row, a cluster. next: as many rows as have blocks on the SMs at a time.
@@ -334,7 +336,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
     for (int i = 0; i < kParts; ++i) part[i] = order_of(piece[i & 3]);
     __syncthreads();
   }
-  const float s = sh.cta.s, lse = lse_of(sh.cta);
+  const float m = sh.cta.m, log_s = logf(sh.cta.s);
   if (threadIdx.x == 0) put_row(d, row, z, sh.cta);
   const int k = d.n_top;
   if (k == 0) return;
@@ -509,7 +511,7 @@ __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(kLogThreads, 4) logp
 #pragma unroll 4
     for (int j = own; j < listed; j += share) before += sh.list[j] > it;
     for (int o = share / 2; o > 0; o /= 2) before += __shfl_xor_sync(0xffffffffu, before, o);
-    if (i < listed && before < k && own == 0) put_top(d, row, before, it, s, lse);
+    if (i < listed && before < k && own == 0) put_top(d, row, before, it, m, log_s);
   }
 }
 
@@ -553,7 +555,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) logprobs_rows_kernel(const 
   if (lane == 0) put_row(d, row, z, acc);
   const int k = d.n_top;
   if (k == 0) return;
-  const float s = acc.s, lse = lse_of(acc);
+  const float m = acc.m, log_s = logf(acc.s);
   const uint32_t mine[2] = {any ? order_of(even) : 0u, any ? order_of(odd) : 0u};
   auto groups_from = [&](uint32_t order) { return __popc(__ballot_sync(0xffffffffu, mine[0] >= order)) + __popc(__ballot_sync(0xffffffffu, mine[1] >= order)); };
   uint32_t least = 0;
@@ -629,7 +631,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) logprobs_rows_kernel(const 
       int before = 0;
 #pragma unroll 4
       for (int j = 0; j < n; ++j) before += list[j] > it;
-      if (before < k) put_top(d, row, before, it, s, lse);
+      if (before < k) put_top(d, row, before, it, m, log_s);
     }
     return;
   }
@@ -645,7 +647,7 @@ __global__ void __launch_bounds__(32 * kRowWarps, 4) logprobs_rows_kernel(const 
     }
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-    if (lane == 0) put_top(d, row, r, best, s, lse);
+    if (lane == 0) put_top(d, row, r, best, m, log_s);
     last = best;
   }
 }
