@@ -157,6 +157,14 @@ __host__ __device__ inline KeyRange folded_row(const AttnTable& c, int i, int r,
   const int m = member_of(c.m_row0, c.member0[i], c.members[i], r), base = member_base(c, i, m);
   return KeyRange{base + c.sinks[i], base + member_keys(c, i, m, r, causal)};
 }
+// Whether some row of a folded entry sees slot `slot` of page `page` of its own keys. A member's first page may begin with shared keys, and
+// its last end with slots that hold no key of its.
+__host__ __device__ inline bool own_slot_seen(const AttnTable& c, int i, int page, int slot, bool causal) {
+  const int m = member_of(c.m_page0, c.member0[i], c.members[i], page);
+  const int rows_to = m + 1 < c.member0[i] + c.members[i] ? c.m_row0[m + 1] : c.rows[i];
+  const int key = (c.m_first[m] + page - c.m_page0[m]) * kPage + slot;
+  return key >= c.sinks[i] && key < member_keys(c, i, m, rows_to - 1, causal);
+}
 __host__ __device__ inline KeyRange some_keys(const AttnTable& c, int i, int ra, int rb, bool causal, int window) {
   if (c.members[i]) {
     // whole pages: from the first member's on, up to the last that the last row needs
@@ -451,12 +459,40 @@ __device__ __forceinline__ void clean_v(uint8_t* slot, int a0, int a1, int b0, i
   }
 }
 
+// Bits 15 and 31 of the sum: an exponent of ones in the word's elements (of a unit's, any). The word without such elements.
+__device__ __forceinline__ uint32_t carries(const uint4& v) {
+  return ((v.x & 0x7F807F80u) + 0x00800080u) | ((v.y & 0x7F807F80u) + 0x00800080u) | ((v.z & 0x7F807F80u) + 0x00800080u) |
+         ((v.w & 0x7F807F80u) + 0x00800080u);
+}
+__device__ __forceinline__ uint32_t finite_bf16x2(uint32_t e) {
+  return e & ~((not_finite_bf16(e) ? 0x0000FFFFu : 0u) | (not_finite_bf16(e >> 16) ? 0xFFFF0000u : 0u));
+}
+
+// What is not finite in the units `at` of the keys key, key + 8 ... of [lo, hi) becomes zero; *dirty is set where some row sees such a key.
+// (Where slots without a key set it, rows were gone through again for nothing: 32 rows over 15000 shared keys and up to 600 of their own, NaN
+// in the slots behind their last keys, took 1330 us. Now 34, and 30 where those slots are finite.) Seldom called, and not inlined: the loop
+// over tiles waits for instructions as it is, and took 30.5 us with the search in it.
+template <int D>
+__device__ __noinline__ void clean_keys(uint8_t* at, int key, int keys, int lo, int hi, const AttnTable& c, int entry, int page, bool causal,
+                                        volatile int* dirty) {
+#pragma unroll 1
+  for (int k = 0; k < keys; ++k, key += 8, at += Tile<D, false>::GROUP_BYTES) {
+    if (key < lo || key >= hi) continue;
+    const uint4 was = *reinterpret_cast<const uint4*>(at);
+    if ((carries(was) & 0x80008000u) == 0) continue;
+    *reinterpret_cast<uint4*>(at) = make_uint4(finite_bf16x2(was.x), finite_bf16x2(was.y), finite_bf16x2(was.z), finite_bf16x2(was.w));
+    if (page < 0 || own_slot_seen(c, entry, page + key / kPage, key % kPage, causal)) *dirty = 1;
+  }
+}
+
 // The same for the form in which whole tiles are cleaned (a folded group's own keys): all keys of the tile, a thread the same
 // 16-byte unit of every eighth key, so that its places are a constant stride apart, eight loads in flight, no branch between them; one
 // test for the two elements of a word, an exponent of ones plus one carrying into the sign's place. What no copy has
-// brought, behind the fetched pages' keys [k0, k1), is read as well and decides nothing.
+// brought, behind the fetched pages' keys [k0, k1), is read as well and decides nothing. `page`: the tile's first page among a folded entry's
+// own, or -1; such pages have slots that hold no key, and what is not finite there is zeroed and left at that.
 template <int D>
-__device__ __forceinline__ void clean_tile(uint8_t* slot, int k0, int k1, int lo, int hi, int thread, int threads, volatile int* dirty) {
+__device__ __forceinline__ void clean_tile(uint8_t* slot, int k0, int k1, int lo, int hi, int thread, int threads, volatile int* dirty,
+                                           const AttnTable& c, int entry, int page, bool causal) {
   constexpr int kUnits = D / 8, kAhead = 8;
   const int unit = thread % kUnits;
   if (k0 < lo || hi < k1) {
@@ -472,24 +508,9 @@ __device__ __forceinline__ void clean_tile(uint8_t* slot, int k0, int k1, int lo
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) v[k] = *reinterpret_cast<const uint4*>(at + (g + k) * Tile<D, false>::GROUP_BYTES);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        bad |= ((v[k].x & 0x7F807F80u) + 0x00800080u) | ((v[k].y & 0x7F807F80u) + 0x00800080u) |
-               ((v[k].z & 0x7F807F80u) + 0x00800080u) | ((v[k].w & 0x7F807F80u) + 0x00800080u);
+      for (int k = 0; k < kAhead; ++k) bad |= carries(v[k]);
       if ((bad & 0x80008000u) == 0) continue;
-#pragma unroll 1
-      for (int k = 0; k < kAhead; ++k) {
-        const int key = (g + k) * 8 + r;
-        if (key < lo || key >= hi) continue;
-        uint32_t* e = reinterpret_cast<uint32_t*>(at + (g + k) * Tile<D, false>::GROUP_BYTES);
-#pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t out = (not_finite_bf16(e[q]) ? 0x0000FFFFu : 0u) | (not_finite_bf16(e[q] >> 16) ? 0xFFFF0000u : 0u);
-          if (out) {
-            e[q] &= ~out;
-            *dirty = 1;
-          }
-        }
-      }
+      clean_keys<D>(at + g * Tile<D, false>::GROUP_BYTES, g * 8 + r, kAhead, lo, hi, c, entry, page, causal, dirty);
     }
   }
 }
@@ -1154,7 +1175,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_attn_kernel(const __grid_co
               const int b1 = pages.last(j) * kPage, b0 = min(b1, max(a1, cta.hi - k0));
               const KeyRange seen = range_in(w, j, KeyRange{w.all_lo, w.all_hi});
               if constexpr (FORM == kPrefix)
-                clean_tile<D>(sKV + vs * KV_BYTES, a0, b1, seen.lo - k0, seen.hi - k0, quarter * 32 + lane, 32 * quarters, &sh.dirty);
+                clean_tile<D>(sKV + vs * KV_BYTES, a0, b1, seen.lo - k0, seen.hi - k0, quarter * 32 + lane, 32 * quarters, &sh.dirty, a.c, w.entry,
+                              a.c.members[w.entry] == 0 || w.jb + j < w.ns ? -1 : (cache_tile(w, j) - w.ns) * kPagesPerTile, d.causal);
               else
                 clean_v<D>(sKV + vs * KV_BYTES, a0, a1, b0, b1, seen.lo - k0, seen.hi - k0, quarter * 32 + lane,
                            32 * quarters, &sh.dirty);
