@@ -1537,7 +1537,9 @@ bool deal(const Table& c, int n_q_heads, int n_kv_heads, bool causal, int window
           }
           left -= segment;
           if (K.masked && run_rows) run_rows[p->ctas - 1] += q1 - q0 + 1;
-          int take = whole ? steps : static_cast<int>(std::min<int64_t>(std::max((K.masked ? cheap : steps) - step, 0), left / unit));
+          // (only masked steps can lie behind `step`; the test in every form cost 32 single rows' plan 0.4 of 7 us)
+          const int ahead = K.masked ? std::max(cheap - step, 0) : steps - step;
+          int take = whole ? steps : static_cast<int>(std::min<int64_t>(ahead, left / unit));
           left -= take * unit;
           if (K.masked && !whole) {
             if (step + take >= cheap) {
