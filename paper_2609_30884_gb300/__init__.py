@@ -543,8 +543,8 @@ class Context:
         k, wanted = 0, top_ids if top_ids is not None else top_logprobs
         if wanted is not None:
             shape = wanted.shape
-            if len(shape) != 2 or shape[0] != n:
-                raise ValueError(f"the alternatives must be [{n}, their number]")
+            if len(shape) != 2 or shape[0] != n or (top_logprobs is not None and top_logprobs.shape != shape):
+                raise ValueError(f"the alternatives must be [{n}, their number], ids and log probabilities alike")
             k = shape[1]
         ids = self._a_row("top_ids", top_ids, n * k, torch.int32)
         tops = self._a_row("top_logprobs", top_logprobs, n * k, fp32)
