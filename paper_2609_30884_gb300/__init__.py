@@ -435,6 +435,8 @@ class Context:
         n, kind = x.shape[0], _TYPES.get(x.dtype)
         if kind is None:
             raise ValueError("x must be bfloat16, float16 or float32")
+        if n >= _INT32:
+            raise ValueError("x: its rows do not fit 32 bits")
         self._here(positions)
         _int32_on_device("positions", positions, n)
         _put_heads(buf, 0, device, "x", x, x if out is None else out, dim)
@@ -453,6 +455,8 @@ class Context:
         n, kind = x.shape[0], _TYPES.get(dtype)
         if kind is None:
             raise ValueError("x must be bfloat16, float16 or float32")
+        if n >= _INT32:
+            raise ValueError("x: its rows do not fit 32 bits")
         if positions.get_device() != device:
             raise ValueError(f"every tensor of the call must be on cuda:{device}")
         _int32_on_device("positions", positions, n)
