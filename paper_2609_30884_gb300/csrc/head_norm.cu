@@ -54,22 +54,28 @@ struct Place {
   int pair;    // its first pair
 };
 template <int VEC, bool INTER, int BATCH>
-__device__ __forceinline__ Place place_of(const Tiling& a, const RotaryDesc& d) {
+__host__ __device__ __forceinline__ Place place_of(const Tiling& a, const RotaryDesc& d, int thread, int column) {
   Place t;
-  const int u = threadIdx.x & ((1 << a.log_lanes) - 1), rest = threadIdx.x >> a.log_lanes;
+  const int u = thread & ((1 << a.log_lanes) - 1), rest = thread >> a.log_lanes;
   t.rb = rest & ((1 << a.log_rows) - 1);
-  const int at = rest >> a.log_rows, slot = at + blockIdx.y * a.block_slots;
+  const int at = rest >> a.log_rows, slot = at + column * a.block_slots;
   const bool there = at < a.block_slots && slot < a.slots && u < a.units;
   t.part = slot >= a.slot0[2] ? 2 : slot >= a.slot0[1] ? 1 : 0;
   const int first = t.part == 0 ? 0 : t.part == 1 ? a.slot0[1] : a.slot0[2];
   const int all = t.part == 0 ? d.part[0].heads : t.part == 1 ? d.part[1].heads : d.part[2].heads;
   t.head = (slot - first) * BATCH;
-  t.heads = there ? min(BATCH, all - t.head) : 0;
+  t.heads = !there ? 0 : all - t.head < BATCH ? all - t.head : BATCH;
   t.turning = u < a.rot_units;
   t.e0 = t.turning ? u * VEC : d.rot_dim + (u - a.rot_units) * VEC;
   t.e1 = t.turning && !INTER ? t.e0 + d.rot_dim / 2 : t.e0;
   t.pair = u * (INTER ? VEC / 2 : VEC);
   return t;
+}
+// Whether a thread of the gradient has a second unit: the other half of its pairs, or its next head. Threads behind the last head have none,
+// wherever their place would be.
+template <bool INTER>
+__host__ __device__ __forceinline__ bool second_unit(const Place& p) {
+  return INTER ? p.heads > 1 : p.heads > 0 && p.turning;
 }
 
 // Position of row r of a cache's requests, and its page as the table has it.
@@ -180,7 +186,7 @@ __global__ void __launch_bounds__(kRotThreads, BATCH == 1 ? 1 : 3) head_norm_ker
   __shared__ __align__(16) Angles s_angle;
   griddep_launch_dependents();
   const RotaryDesc& d = a.d.r;
-  const Place p = place_of<VEC, INTER, BATCH>(a.t, d);
+  const Place p = place_of<VEC, INTER, BATCH>(a.t, d, threadIdx.x, blockIdx.y);
   const int64_t row0 = static_cast<int64_t>(blockIdx.x) << a.t.log_rows, row = row0 + p.rb;
   const int heads = row < d.n_rows ? p.heads : 0, here = static_cast<int>(min(static_cast<int64_t>(1) << a.t.log_rows, d.n_rows - row0));
   const RotPart t = p.part == 0 ? d.part[0] : p.part == 1 ? d.part[1] : d.part[2];
@@ -430,11 +436,11 @@ __global__ void __launch_bounds__(kRotThreads, 2) head_norm_grad_kernel(const __
   extern __shared__ __align__(16) uint4 s_unit[];  // [stage][x, its second or next, g likewise][thread]; then sums [head's lanes][head_dim]
   griddep_launch_dependents();
   const RotaryDesc& d = a.d.r;
-  const Place p = place_of<VEC, INTER, B>(a.t, d);
+  const Place p = place_of<VEC, INTER, B>(a.t, d, threadIdx.x, blockIdx.y);
   const int q = p.part & 1, threads = blockDim.x;
   const RotPart t = q == 0 ? d.part[0] : d.part[1];
   const int64_t g_row = q == 0 ? a.d.g_row[0] : a.d.g_row[1], g_head = q == 0 ? a.d.g_head[0] : a.d.g_head[1];
-  const bool two = kTwo && p.turning;
+  const bool second = second_unit<INTER>(p), two = kTwo && second;
   const int e1 = p.e1 - p.e0, log_rows = a.t.log_rows;
   const int64_t tiles = (static_cast<int64_t>(d.n_rows) + (1 << log_rows) - 1) >> log_rows;
   uint64_t acc_x[P], acc_y[H], wx[P], wy[H];
@@ -464,7 +470,7 @@ __global__ void __launch_bounds__(kRotThreads, 2) head_norm_grad_kernel(const __
         copy_async16(to, x_at);
         copy_async16(to + 2 * threads, g_at);
       }
-      if (kTwo ? two : heads > 1) {
+      if (second) {
         copy_async16(to + threads, x_at + (kTwo ? e1 : t.x_head));
         copy_async16(to + 3 * threads, g_at + (kTwo ? e1 : g_head));
       }
