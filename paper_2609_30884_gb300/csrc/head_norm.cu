@@ -10,9 +10,12 @@
 // the half layout two, the pair's halves), in four neighbouring heads, two in a gradient; here the lanes of a head, a power of
 // two, are neighbours in a warp and join the sum of squares by shuffles. What it takes to stay near memory is few instructions: 512
 // elements of a warp's step took 283 of them at first (16384 bf16 rows of 32 heads 58 us, the gradient 155; now 44, 90% of the
-// copy rate, and 73, 81%). So places are found by shifts, arithmetic is on two elements an instruction, gains and angles are
-// multiplied once for a thread's heads, and all of its heads' shuffles go level by level. Heads
-// whose units are no such thing (odd sizes, strides or alignments) take a warp each, an element or a pair a lane.
+// copy rate, and 72, 83%). So places are found by shifts, arithmetic is on two elements an instruction, gains and angles are
+// multiplied once for a thread's heads, and all of its heads' shuffles go level by level. (In the half layout of 16-bit heads that is more than
+// the 80 registers that three blocks an SM leave: 32 to 52 bytes a thread are spilled.) Heads whose units are no such thing (odd
+// sizes, strides or alignments, a half of the turning part that is no whole unit, more than 32 units) take a warp each, an element or
+// a pair a lane, and are slow: 16384 bf16 rows of 32 heads of 128 that turn 8 elements 254 us, the gradient 866;
+// of 80 that turn 40 199 and 732; 8192 fp32 rows of 16 heads of 256 63 and 192 interleaved, 107 and 136 where 64 elements turn.
 //
 // The gains' gradient: a thread keeps the same elements of its heads' part over all the rows that its block walks, so
 // their sums stay in its registers; a block's sums meet in shared memory, the blocks' in a second small kernel, both in a
@@ -410,7 +413,7 @@ constexpr int kGradBatch = INTER ? 2 : 1;
 constexpr int kGradUnits = 4;
 // A thread's units of the next two tiles are on their way into places of its own in shared memory: in registers one tile took 128
 // of them and two blocks an SM had too few bytes in flight. Angles are formed for a batch of 2^log_batch tiles, so that there is work for
-// all threads and a barrier a batch: 16384 bf16 rows of 32 heads take 94 us with a barrier a tile, 82, 77 and 73 with batches of 2, 4 and 8. Positions go four batches ahead, because all threads read what a few of them copied: the next batch's
+// all threads and a barrier a batch: 16384 bf16 rows of 32 heads took 94 us with a barrier a tile, 82, 77 and 73 with batches of 2, 4 and 8. Positions go four batches ahead, because all threads read what a few of them copied: the next batch's
 // have landed, and a barrier has followed, one batch before its angles are formed.
 constexpr int kStages = 3, kPositions = 4, kLogBatch = 3;
 struct NormGradShared {

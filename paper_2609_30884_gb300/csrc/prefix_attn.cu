@@ -293,7 +293,10 @@ void share_prefixes(const ChunkTable& c, const int* count, const int* keys, int 
   }
   // Few long items cut over all SMs begin and end later than many short ones: wide rows' q and o, masks, more parts to merge. 32 rows over
   // 1000 shared keys (22 units an SM saved) take 20.1 us folded and 17.5 apart, drafts in two groups (11 units) 29 split and 21 apart;
-  // 8 rows over 15000 (45 units) 20.5 folded and 41.6 apart.
+  // 8 rows over 15000 (45 units) 20.5 folded and 41.6 apart. All of these are 28 heads over 4, and the units know nothing of a shared call's
+  // fixed cost: timed both ways over 72 calls (8 to 32 rows or drafts, 1000 to 15000 keys, 28 heads over 4, 12 and 4 over 2), none was
+  // shared to its loss, but 19 stood apart that sharing would have made 1 to 9 us faster, 8 rows of 12 heads over 2 and 15000 keys most
+  // (25 apart, 16 folded).
   if (saved * n_kv_heads < static_cast<int64_t>(any_split ? 40 : 24) * num_sms)
     for (int i = 0; i < n; ++i) way[i] = kApart;
   for (int i = 0, r = 0; i < n; r += count[i++]) {

@@ -3,8 +3,9 @@
 // has one range of keys a row, and one mask. A tile that holds keys of both ranges is gone through twice. Nothing between the ranges is read,
 // not even its entries of the page table.
 //
-// Bound as the plain form: single rows by memory (16 rows, window 4096 of 4K-16K keys: 35 us, 134 MB), long chunks by the tensor cores (4096
-// rows over a window of 4096: 200 us, 1210 TFLOP/s of what the windows need; their masked ends are computed beside it).
+// Single rows: 16 with a window of 4096 of 4K-16K keys take 35 us; their 134 MB take 20 at the copy rate and 21 here, the rest are the start, whole
+// steps of a run, one more masked tile an item, and the merge (128 runs, each item cut in two). Long chunks are bound by the chains of
+// products and softmax: 4096 rows over a window of 4096 200 us, 1210 TFLOP/s of what the windows need; their masked ends are computed beside it.
 #include "chunk_attn.cuh"
 
 namespace crf {
