@@ -356,9 +356,9 @@ CRF_API crf_status crf_norm_rotary(crf_ctx* ctx, const crf_rope* rope, const crf
 
 /* Its gradient: parts[i].x is the forward call's x, grads[i].x the gradient of y (its `out` members are not read), parts[i].out
  * receives that of x and dgains[i] (host array of device fp32 [head_dim]) that of the gain, summed over rows and heads in
- * a fixed order. parts[i].out may be parts[i].x or grads[i].x, with the same strides; otherwise nothing overlaps. Where x has a
- * stride of 0, every row or head still gets a gradient of its own. With n_rows == 0 the gains' gradients are
- * zeros. `workspace` >= crf_norm_rotary_workspace_size bytes, 256-byte aligned. */
+ * a fixed order (parts that share a gain have one dgain each, too). parts[i].out may be parts[i].x or grads[i].x, with the same
+ * strides; otherwise nothing overlaps. Where x has a stride of 0, every row or head still gets a gradient of its own. With
+ * n_rows == 0 the gains' gradients are zeros. `workspace` >= crf_norm_rotary_workspace_size bytes, 256-byte aligned. */
 CRF_API crf_status crf_norm_rotary_workspace_size(crf_ctx* ctx, int head_dim, int n_rows, size_t* bytes);
 CRF_API crf_status crf_norm_rotary_grad(crf_ctx* ctx, const crf_rope* rope, const crf_heads* parts, const crf_norm* norms,
                                         const crf_heads* grads, float* const* dgains, int n_parts, int type, int n_rows,

@@ -573,6 +573,10 @@ crf_status crf_norm_rotary_grad(crf_ctx* ctx, const crf_rope* rope, const crf_he
       d.g_row[p] = g.x_row;
       d.g_head[p] = g.x_head;
     }
+    if (n_parts == 2) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(dgains[0]), b = reinterpret_cast<uintptr_t>(dgains[1]);
+      if ((a < b ? b - a : a - b) < rope->head_dim * sizeof(float)) return fail(CRF_EINVAL, "dgains overlap: each part writes its own");
+    }
     s = check_workspace(workspace, ws_bytes, head_norm_grad_workspace(rope->head_dim, ctx->num_sms));
     if (s != CRF_OK) return s;
     DeviceScope dev(ctx->device);
